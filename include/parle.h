@@ -347,6 +347,84 @@ int parle_debug_buffer(const parle_ctx *ctx, int kind, int layer, size_t *byte_o
 int parle_softmax_ce_static(const float *logits, const int32_t *labels, int n, int B, int C,
                             float *dlogits, float *loss, int32_t *flags, void *cuda_stream);
 
+/* Token operators (the paper has no counterpart: its networks take real vectors).  The two ends of a model over tokens and
+ * its regulariser, for callers that form the gradient themselves (parle_inner_update with a flat vector, n_layers == 0) or
+ * prepare minibatches for parle_inner_step; all of them enqueue on cuda_stream (a cudaStream_t as void*, NULL = default
+ * stream) of the current device, keep nothing between calls, call no allocator, may be captured in a CUDA graph, and may run
+ * at the same time on several streams.  Elements are of one of three types; sums, exponentials and products are
+ * fp32, a result is rounded once (to nearest, ties to even).  Pitches ("ld", "gs") are in elements; pointers need the
+ * alignment of their elements only (16-byte aligned rows are faster).  Outputs may not overlap inputs unless said.
+ * Token numbers are int32 in [0, vocab); PARLE_NO_TOKEN marks a place without a token (padding).  Any other number counts
+ * as PARLE_NO_TOKEN too and sets the bit PARLE_FLAG_BAD_LABEL in *flags (dev [1] int32 or NULL; a call only sets the
+ * bit, the caller clears it).
+ * EINVAL: NULL, a size, pitch, type or scalar out of range, outputs whose rows overlap.  EALIGN: a pointer not on a boundary of
+ * its element.  ETOOBIG: more than PARLE_TOKEN_MAX_ROWS rows or PARLE_TOKEN_MAX_ELEMENTS elements.  ECUDA: a launch failed. */
+#define PARLE_F32 0
+#define PARLE_BF16 1
+#define PARLE_F16 2
+#define PARLE_NO_TOKEN -1
+#define PARLE_TOP_MAX 32
+#define PARLE_TOKEN_MAX_ROWS (1LL << 30)
+#define PARLE_TOKEN_MAX_ELEMENTS (1LL << 40)
+
+/* Row-wise log probabilities of logits x dev [rows, vocab], row pitch ld:
+ *   log p_j = scale (x_j - m) - log sum_i exp(scale (x_i - m)),  m = max x          (scale = 1 / temperature > 0)
+ *   logprob     dev [rows] fp32 or NULL      log p of tokens[row]; 0 for a row without a token (tokens NULL: logprob NULL)
+ *   entropy     dev [rows] fp32 or NULL      -sum_j p_j log p_j
+ *   top_token   dev [rows, k] int32 or NULL  the k most probable tokens, best first, of equal logits the lower token first
+ *   top_logprob dev [rows, k] fp32 or NULL   their log probabilities
+ * k in [0, PARLE_TOP_MAX].  Logits of -inf have probability 0 and are no alternatives: where a row has fewer than k
+ * others, the rest is PARLE_NO_TOKEN with -inf.  A row of -inf alone: log probability -inf, entropy 0, no alternatives.
+ * A row with NaN or +inf: NaN, and PARLE_NO_TOKEN for the alternatives. */
+int parle_token_logprobs(const void *logits, int dtype, long long rows, int vocab, long long ld, const int32_t *tokens,
+                         double scale, int k, float *logprob, float *entropy, int32_t *top_token, float *top_logprob,
+                         int32_t *flags, void *cuda_stream);
+
+/* Gradient of sum_rows (d_logprob[row] logprob[row] + d_entropy[row] entropy[row]) with respect to the logits:
+ *   dlogits_j = scale ( d_logprob (1[j = token] - p_j) - d_entropy p_j (log p_j + entropy) )
+ * d_logprob, d_entropy dev [rows] fp32; one of them may be NULL (= 0).  dlogits dev [rows, vocab] of the logits' type, row
+ * pitch ld_d >= vocab; it may be the logits' own memory (same pointer and pitch).  logprob and entropy, dev [rows] fp32
+ * or NULL, are formed as above in the same pass.  d_logprob is not read as anything but 0 in a row without a token.  A row
+ * whose incoming gradients are both 0, and a row of -inf alone, gets zeros; another row with NaN or +inf gets NaN. */
+int parle_token_logprobs_grad(const void *logits, int dtype, long long rows, int vocab, long long ld, const int32_t *tokens,
+                              double scale, const float *d_logprob, const float *d_entropy, float *logprob, float *entropy,
+                              void *dlogits, long long ld_d, int32_t *flags, void *cuda_stream);
+
+/* Rows of n tables (n in [1, PARLE_MAX_REPLICAS], one per replica), scaled:
+ *   out[g, t, :] = scale * table[g, tokens[g, t], :]
+ * table dev [n, vocab, dim]: table g starts at element g * table_gs, rows ld_table apart; tokens dev [n, length];
+ * out dev [n, length, dim] likewise with out_gs, ld_out, of a type of its own.  A place without a token gets zeros.
+ * A table inside a parameter vector [n, stride] has table_gs = stride. */
+int parle_embedding(const void *table, int table_dtype, long long table_gs, long long ld_table, int n, int vocab, int dim,
+                    const int32_t *tokens, long long length, double scale, void *out, int out_dtype,
+                    long long out_gs, long long ld_out, int32_t *flags, void *cuda_stream);
+
+/* Its gradient with respect to the tables, fp32 as every gradient of this library:
+ *   dtable[g, v, :] = scale * sum over t with tokens[g, t] = v of dout[g, t, :]
+ * summed in fp32 in an order that the tokens alone decide (positions sorted by token; the same inputs give the same bits).
+ * accumulate == 0: all vocab rows are written (zeros for tokens that do not occur); else the sums are added to dtable and rows
+ * of tokens that do not occur are left untouched.  Elements between rows (ld_dtable > dim) are never touched.
+ * dtable_gs = stride puts the gradient into the grad vector that parle_inner_update reads.
+ * workspace dev, 128-byte aligned, >= parle_embedding_grad_workspace_bytes() (0 for invalid sizes): scratch of this call alone
+ * until its work has finished.  EWORKSPACE if too small. */
+size_t parle_embedding_grad_workspace_bytes(int n, long long length, int vocab, int dim);
+int parle_embedding_grad(const void *dout, int dout_dtype, long long dout_gs, long long ld_dout, const int32_t *tokens,
+                         int n, long long length, int vocab, int dim, double scale, float *dtable, long long dtable_gs,
+                         long long ld_dtable, int accumulate, void *workspace, size_t workspace_bytes, int32_t *flags,
+                         void *cuda_stream);
+
+/* Dropout of x dev [rows, cols] with an optional residual, y = residual + dropout(x), all of one type, row pitches ld_*.
+ * The mask is a function of (seed, offset, element number e = row * cols + col) and is stored nowhere: Philox 4x32-10 with
+ * counter (e / 8, offset) and key seed gives four words, each word two 16-bit fields (low half first), one per element of the
+ * group of eight.  x is kept when its field is >= t = round(65536 p) and multiplied by 65536 / (65536 - t); else it
+ * counts as 0, whatever its value.  p in [0, 1].  The backward pass is the same call on the output's gradient (without
+ * residual, whose gradient is the output's).  offset_dev (dev [1] uint64, 8-byte aligned, or NULL) is added to offset when
+ * the kernel runs: a captured call that is replayed draws new masks when the caller advances it.
+ * y may be the memory of x, of residual, or (same pointer and pitch) of both. */
+int parle_dropout(const void *x, long long ld_x, const void *residual, long long ld_r, void *y, long long ld_y,
+                  int dtype, long long rows, long long cols, double p, uint64_t seed, uint64_t offset,
+                  const uint64_t *offset_dev, void *cuda_stream);
+
 /* Kernels launched by this context since creation (for accounting). */
 long long parle_launch_count(const parle_ctx *ctx);
 

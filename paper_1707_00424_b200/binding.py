@@ -49,7 +49,7 @@ def lib() -> C.CDLL:
         from .build import build
         build()
     L = C.CDLL(path)
-    vp, ci, cd, sz = C.c_void_p, C.c_int, C.c_double, C.c_size_t
+    vp, ci, cd, sz, ll = C.c_void_p, C.c_int, C.c_double, C.c_size_t, C.c_longlong
     sig = {
         "parle_init": (ci, [C.POINTER(vp), ci, C.POINTER(_Model), cd, cd, cd, cd, cd]),
         "parle_destroy": (None, [vp]),
@@ -90,6 +90,12 @@ def lib() -> C.CDLL:
         "parle_profile_class_name": (C.c_char_p, [ci]),
         "parle_debug_buffer": (ci, [vp, ci, ci, C.POINTER(sz), C.POINTER(sz)]),
         "parle_softmax_ce_static": (ci, [vp, vp, ci, ci, ci, vp, vp, vp, vp]),
+        "parle_token_logprobs": (ci, [vp, ci, ll, ci, ll, vp, cd, ci, vp, vp, vp, vp, vp, vp]),
+        "parle_token_logprobs_grad": (ci, [vp, ci, ll, ci, ll, vp, cd, vp, vp, vp, vp, vp, ll, vp, vp]),
+        "parle_embedding": (ci, [vp, ci, ll, ll, ci, ci, ci, vp, ll, cd, vp, ci, ll, ll, vp, vp]),
+        "parle_embedding_grad_workspace_bytes": (sz, [ci, ll, ci, ci]),
+        "parle_embedding_grad": (ci, [vp, ci, ll, ll, vp, ci, ll, ci, ci, cd, vp, ll, ll, ci, vp, sz, vp, vp]),
+        "parle_dropout": (ci, [vp, ll, vp, ll, vp, ll, ci, ll, ll, cd, C.c_uint64, C.c_uint64, vp, vp]),
         "parle_launch_count": (C.c_longlong, [vp]),
         "parle_last_cuda_error": (ci, [vp]),
         "parle_strerror": (C.c_char_p, [ci]),

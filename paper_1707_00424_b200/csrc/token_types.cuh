@@ -1,0 +1,102 @@
+// Element types of the token operators (embedding, dropout, token log probabilities): loads to and stores from fp32.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace parle {
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+
+// One rounding, to nearest with ties to even, of a value computed in fp32.
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+
+// Eight consecutive elements as fp32; p is aligned to 16 bytes.  (16 bytes of a 16-bit type, 2 x 16 bytes of fp32.)
+__device__ __forceinline__ void unpack8(const float4 &a, const float4 &b, float (&v)[8]) {
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+template <typename T> struct Pack8;                      // the raw form of eight elements, so that loads can be issued early
+template <> struct Pack8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float *p) {
+        a = reinterpret_cast<const float4 *>(p)[0];
+        b = reinterpret_cast<const float4 *>(p)[1];
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const { unpack8(a, b, v); }
+    __device__ __forceinline__ void set(const float (&v)[8]) {
+        a = make_float4(v[0], v[1], v[2], v[3]);
+        b = make_float4(v[4], v[5], v[6], v[7]);
+    }
+    __device__ __forceinline__ void store(float *p) const {
+        reinterpret_cast<float4 *>(p)[0] = a;
+        reinterpret_cast<float4 *>(p)[1] = b;
+    }
+};
+template <> struct Pack8<__nv_bfloat16> {
+    uint4 a;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { a = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                    // a bf16 is the upper half of the fp32 word
+            v[2 * i] = __uint_as_float(w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    __device__ __forceinline__ void set(const float (&v)[8]) {
+        __nv_bfloat162 h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        a = *reinterpret_cast<const uint4 *>(h);
+    }
+    __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = a; }
+};
+template <> struct Pack8<__half> {
+    uint4 a;
+    __device__ __forceinline__ void load(const __half *p) { a = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
+        }
+    }
+    __device__ __forceinline__ void set(const float (&v)[8]) {
+        __half2 h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+        a = *reinterpret_cast<const uint4 *>(h);
+    }
+    __device__ __forceinline__ void store(__half *p) const { *reinterpret_cast<uint4 *>(p) = a; }
+};
+
+inline bool valid_dtype(int dtype) { return dtype == PARLE_F32 || dtype == PARLE_BF16 || dtype == PARLE_F16; }
+inline int dtype_bytes(int dtype) { return dtype == PARLE_F32 ? 4 : 2; }
+// Whether p lies on a boundary of its element type.
+inline bool element_aligned(const void *p, int dtype) { return reinterpret_cast<uintptr_t>(p) % dtype_bytes(dtype) == 0; }
+// Whether rows of this pitch, starting at p, all start on 16-byte boundaries.
+inline bool rows_aligned16(const void *p, long long ld, int dtype) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * dtype_bytes(dtype)) % 16 == 0;
+}
+
+// Calls f with a null pointer of the element type as a tag.
+template <typename F> int with_dtype(int dtype, F f) {
+    switch (dtype) {
+        case PARLE_F32: return f((float *)nullptr);
+        case PARLE_BF16: return f((__nv_bfloat16 *)nullptr);
+        case PARLE_F16: return f((__half *)nullptr);
+    }
+    return PARLE_EINVAL;
+}
+
+inline int launch_status() { return cudaGetLastError() == cudaSuccess ? PARLE_OK : PARLE_ECUDA; }
+
+}  // namespace parle
