@@ -368,7 +368,7 @@ int parle_softmax_ce_static(const float *logits, const int32_t *labels, int n, i
 #define PARLE_TOKEN_MAX_ELEMENTS (1LL << 40)
 
 /* Row-wise log probabilities of logits x dev [rows, vocab], row pitch ld:
- *   log p_j = scale (x_j - m) - log sum_i exp(scale (x_i - m)),  m = max x          (scale = 1 / temperature > 0)
+ *   log p_j = scale (x_j - m) - log sum_i exp(scale (x_i - m)),  m = max x    (scale = 1 / temperature, in [1e-6, 1e6])
  *   logprob     dev [rows] fp32 or NULL      log p of tokens[row]; 0 for a row without a token (tokens NULL: logprob NULL)
  *   entropy     dev [rows] fp32 or NULL      -sum_j p_j log p_j
  *   top_token   dev [rows, k] int32 or NULL  the k most probable tokens, best first, of equal logits the lower token first

@@ -8,7 +8,9 @@
 // A row is read once by one block (or, when there are few rows, by the blocks of one cluster), in 16-byte granules cut at
 // 16-byte boundaries of memory, so rows of any pitch are read with wide loads; only a row's first and last granule may be
 // partial and are read by element.  Maximum, sum and sum of e d are carried together ("online": when a thread meets a larger
-// maximum it rescales its two sums), all in fp32; exponentials are base 2 on s log2(e) (x - m).
+// maximum it rescales its two sums), all in fp32.  Exponentials are base 2: e_j = 2^(x_j c - R) with c = s log2(e), one fused
+// multiply-add per argument, where the reference R is the rounded product of c and the largest logit so far.  R's rounding is
+// common to every term of the row and to log S, so it cancels.
 #include <math.h>
 
 #include <initializer_list>
@@ -20,9 +22,8 @@ using namespace parle;
 
 namespace {
 
-constexpr int kGroups = 64;             // thread groups whose maxima bound the k-th largest logit from below
 constexpr int kTopMost = PARLE_TOP_MAX;
-constexpr int kCandidates = 768;        // logits at least as large as the bound that are ranked at once
+constexpr int kCandidates = 512;        // logits at least as large as the bound that are ranked at once
 constexpr int kClusterMost = 8;
 
 struct RowsArgs {
@@ -30,7 +31,7 @@ struct RowsArgs {
     const int32_t *tokens;
     long long ld, rows;
     int vocab, k;
-    float scale, scale_log2e;
+    float scale, scale_log2e;                              // s, s log2(e)
     float *logprob, *entropy, *top_logprob;
     int32_t *top_token, *flags;
     const float *d_logprob, *d_entropy;
@@ -43,14 +44,38 @@ __device__ __forceinline__ float exp2_approx(float v) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-// max that hands a NaN on
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+// Two fp32 numbers in one register pair: one instruction for two products, sums or multiply-adds.
+typedef unsigned long long float_pair;
+__device__ __forceinline__ float_pair pair(float lo, float hi) {
+    float_pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
     return r;
 }
-// 2^-200 is zero in fp32: below it e d counts as 0 (and 0 * -inf does not arise)
-constexpr float kFar = -200.f;
+__device__ __forceinline__ void split(float_pair v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ float_pair fma2(float_pair a, float_pair b, float_pair c) {
+    float_pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float_pair add2(float_pair a, float_pair b) {
+    float_pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float_pair mul2(float_pair a, float_pair b) {
+    float_pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// Scaled logits x c below -kFar count as -kFar (their probability is 0 either way, and 0 * -inf does not arise in the sum of
+// e d); references below -kNear as -kNear.  Rows whose largest scaled logit is not between -kNear and kNear -- all masked with
+// -inf or large negative numbers, or with very large logits -- are summed again with (x - max) c ("far"): there the reference's
+// rounding, 2^-24 of it, would shift the exponents by more than 2^-4.
+constexpr float kFar = 2097152.f, kNear = 1048576.f;      // 2^21, 2^20
+
+template <typename T> struct Granule;
+template <typename T, int U> __device__ __forceinline__ float largest_of(const Granule<T> (&g)[U]);
 
 // 16 bytes of logits.
 template <typename T> struct Granule {
@@ -69,55 +94,123 @@ template <typename T> struct Granule {
             p.get(v);
         }
     }
+    // As pairs, not below `low` (low_bound()); NaN stays.
+    __device__ __forceinline__ void pairs(uint32_t low, float_pair (&v)[N / 2]) const {
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+        if constexpr (sizeof(T) == 4) {
+            v[0] = pair(clamped(__uint_as_float(w[0]), low), clamped(__uint_as_float(w[1]), low));
+            v[1] = pair(clamped(__uint_as_float(w[2]), low), clamped(__uint_as_float(w[3]), low));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (std::is_same<T, __half>::value) {      // fp16 has no number below the references: clamped as fp32
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+                    v[i] = pair(clamped(f.x, low), clamped(f.y, low));
+                } else {
+                    uint32_t u;
+                    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(u) : "r"(w[i]), "r"(low));
+                    v[i] = pair(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ static float clamped(float v, uint32_t low) {
+        float r;
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(v), "f"(__uint_as_float(low)));
+        return r;
+    }
+    __device__ __forceinline__ float largest() const { return largest_of<T, 1>({*this}); }
 };
 
-// A row as granules: granule q holds elements q N - head .. q N - head + N - 1.
+// Largest element of some granules; NaN is passed over (the sums carry it).
+template <typename T, int U> __device__ __forceinline__ float largest_of(const Granule<T> (&g)[U]) {
+    if constexpr (sizeof(T) == 4) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(g[u].raw.x), __uint_as_float(g[u].raw.y)),
+                               fmaxf(__uint_as_float(g[u].raw.z), __uint_as_float(g[u].raw.w))));
+        return m;
+    } else {
+        using T2 = std::conditional_t<std::is_same<T, __half>::value, __half2, __nv_bfloat162>;
+        T2 m;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const T2 *h = reinterpret_cast<const T2 *>(&g[u].raw);
+            const T2 v = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+            m = u ? __hmax2(m, v) : v;
+        }
+        return fmaxf(to_float(m.x), to_float(m.y));
+    }
+}
+
+// The bound -kFar / c, as Granule::pairs() takes it: an fp32 number, or two bf16 ones.
+template <typename T> __device__ __forceinline__ uint32_t low_bound(float c) {
+    const uint32_t w = __float_as_uint(-kFar / c);
+    if constexpr (!std::is_same<T, __nv_bfloat16>::value) return w;
+    return (w >> 16) | (w & 0xffff0000u);                 // towards zero
+}
+
+// A row as granules: granule q is base[q] and holds elements q N - head .. q N - head + N - 1.
 template <typename T> struct Row {
     static constexpr int N = Granule<T>::N;
-    const T *x;
+    const uint4 *base;
     int vocab, head, granules;
+    int first_whole, wholes;                              // granules that lie in the row altogether: consecutive
     __device__ __forceinline__ Row(const void *logits, long long ld, long long row, int vocab_) {
-        x = static_cast<const T *>(logits) + row * ld;
+        const uintptr_t at = reinterpret_cast<uintptr_t>(static_cast<const T *>(logits) + row * ld);
+        base = reinterpret_cast<const uint4 *>(at & ~(uintptr_t)15);
         vocab = vocab_;
-        head = (int)((reinterpret_cast<uintptr_t>(x) / sizeof(T)) % N);
+        head = (int)((at & 15) / sizeof(T));
         granules = (head + vocab + N - 1) / N;
+        first_whole = head ? 1 : 0;
+        wholes = (head + vocab) / N - first_whole;        // (-1 for a row inside one granule)
     }
+    __device__ __forceinline__ const T *x() const { return reinterpret_cast<const T *>(base) + head; }
     __device__ __forceinline__ int first_element(int q) const { return q * N - head; }
-    __device__ __forceinline__ bool whole(int q) const { return q * N >= head && (q + 1) * N - head <= vocab; }
+    __device__ __forceinline__ bool whole(int q) const { return q >= first_whole && q - first_whole < wholes; }
+    __device__ __forceinline__ bool all_whole(int first, int last, int end) const {
+        return first >= first_whole && last - first_whole < wholes && last < end;
+    }
+    // The granule that holds an element.
+    __device__ __forceinline__ int granule_of(int element) const { return (element + head) / N; }
     __device__ __forceinline__ Granule<T> load(int q, int end) const {
         Granule<T> g;
         if (q >= end) { g.fill_none(); return g; }
-        const int e0 = first_element(q);
         if (whole(q)) {
-            g.raw = *reinterpret_cast<const uint4 *>(x + e0);
+            g.raw = base[q];
         } else {
             g.fill_none();
             T *v = reinterpret_cast<T *>(&g.raw);
+            const int e0 = first_element(q);
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                if (e0 + i >= 0 && e0 + i < vocab) v[i] = x[e0 + i];
+                if (e0 + i >= 0 && e0 + i < vocab) v[i] = x()[e0 + i];
         }
         return g;
     }
+    // U granules, `step` apart, that belong to one thread; granules from `end` on are -inf.
+    template <int U> __device__ __forceinline__ void load_all(int q0, int step, int end, Granule<T> (&raw)[U]) const {
+        if (all_whole(q0, q0 + (U - 1) * step, end)) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u].raw = base[q0 + u * step];
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u] = load(q0 + u * step, end);
+        }
+    }
 };
 
-// Maximum, sum of 2^((x - m) c) and sum of 2^((x - m) c) (x - m) c over some logits.
+// Reference R, sum of e = 2^(x c - R) and sum of e (x c - R) over some logits.
 struct Sums {
-    float m, s, a;
-    __device__ __forceinline__ void clear() { m = -INFINITY; s = 0.f; a = 0.f; }
-    // The same sums relative to a maximum `to` >= m.
-    __device__ __forceinline__ void rebase(float to, float c) {
-        const float shift = m == to ? 0.f : (m - to) * c, f = m == to ? 1.f : exp2_approx(shift);
-        a = f == 0.f ? 0.f : f * (a + shift * s);        // f > 0: shift is finite
+    float r, s, a;
+    __device__ __forceinline__ void clear() { r = -kNear; s = 0.f; a = 0.f; }
+    // The same sums relative to a reference `to` >= r.
+    __device__ __forceinline__ void rebase(float to) {
+        const float shift = r - to, f = exp2_approx(shift);
+        a = f == 0.f ? 0.f : f * fmaf(shift, s, a);
         s *= f;                                           // (a NaN stays)
-        m = to;
-    }
-    __device__ __forceinline__ void add(Sums o, float c) {
-        const float to = fmaxf(m, o.m);
-        rebase(to, c);
-        o.rebase(to, c);
-        s += o.s;
-        a += o.a;
+        r = to;
     }
 };
 
@@ -141,6 +234,10 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
 }
+// In two halves: says that this thread is done with the other blocks' shared memory / waits until all are.  (Relaxed: it orders no
+// memory, so nobody's stores in flight are waited for.)
+__device__ __forceinline__ void cluster_done() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
+__device__ __forceinline__ void cluster_await_done() { asm volatile("barrier.cluster.wait;" ::: "memory"); }
 // Address of another block's copy of a shared variable.
 template <typename V> __device__ __forceinline__ const V *at_rank(const V *p, uint32_t rank) {
     uint64_t r;
@@ -148,101 +245,120 @@ template <typename V> __device__ __forceinline__ const V *at_rank(const V *p, ui
     return reinterpret_cast<const V *>(r);
 }
 
-template <int BLOCK> struct Shared {
-    float m[BLOCK / 32], s[BLOCK / 32], a[BLOCK / 32];
-    float bm, bs, ba;                                     // the block's sums, read by the other blocks of its cluster
+template <int BLOCK> struct SharedSums {
+    Sums warp[BLOCK / 32];
+    Sums block;                                           // read by the other blocks of its cluster
+};
+
+template <int BLOCK> struct Shared : SharedSums<BLOCK> {
+    static constexpr int kGroups = BLOCK < 64 ? BLOCK : 64;      // thread groups whose maxima bound the k-th largest logit from below
     unsigned long long group[BLOCK];                      // the threads' best (logit, granule)
     unsigned long long bound;
-    int found;
+    int found, owners;
+    int owner[BLOCK];
     unsigned long long candidate[kCandidates];
     unsigned long long top[kTopMost];
 };
 
-// Sums over a block, the same in every thread.
-template <int BLOCK> __device__ __forceinline__ Sums block_sums(Sums t, Shared<BLOCK> &sh, float c) {
+// The sums of all 32 lanes, in every lane: one rescaling to the largest reference, then plain sums.
+__device__ __forceinline__ Sums warp_sums(Sums t) {
+    float to = t.r;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, o));
+    t.rebase(to);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-        Sums u;
-        u.m = __shfl_xor_sync(0xffffffffu, t.m, o);
-        u.s = __shfl_xor_sync(0xffffffffu, t.s, o);
-        u.a = __shfl_xor_sync(0xffffffffu, t.a, o);
-        t.add(u, c);
+        t.s += __shfl_xor_sync(0xffffffffu, t.s, o);
+        t.a += __shfl_xor_sync(0xffffffffu, t.a, o);
     }
-    if (threadIdx.x % 32 == 0) { sh.m[threadIdx.x / 32] = t.m; sh.s[threadIdx.x / 32] = t.s; sh.a[threadIdx.x / 32] = t.a; }
-    __syncthreads();
-    Sums r;
-    r.m = sh.m[0]; r.s = sh.s[0]; r.a = sh.a[0];
-#pragma unroll
-    for (int w = 1; w < BLOCK / 32; ++w) {
-        Sums u;
-        u.m = sh.m[w]; u.s = sh.s[w]; u.a = sh.a[w];
-        r.add(u, c);
-    }
-    return r;
+    return t;
 }
 
-// The k largest of the block's logits (granules begin .. end), best first, into sh.top; fewer than k finite or -inf logits leave
-// keys of 0.  `best` is this thread's largest (logit, granule).
-//
-// The k-th largest of 64 groups' maxima is a lower bound of the k-th largest logit, and only threads whose own maximum reaches
-// it can hold one of the k: they hand their logits above the bound on (typically k to 2 k of them), which are ranked by
-// counting.  Equal maxima are ordered by granule, so a row of equal logits hands on 8 k, not V, of them.
-template <typename T, int BLOCK>
-__device__ void block_top(const Row<T> &row, int begin, int end, int k, unsigned long long best, Shared<BLOCK> &sh) {
-    constexpr int N = Granule<T>::N;
-    const int lane = threadIdx.x % 32;
-    sh.group[threadIdx.x] = best;
-    if (threadIdx.x < k) sh.top[threadIdx.x] = 0;
-    if (threadIdx.x == 0) { sh.found = 0; sh.bound = 0; }
-    __syncthreads();
-    if (threadIdx.x < kGroups) {
-        unsigned long long g = sh.group[threadIdx.x];
-#pragma unroll
-        for (int t = threadIdx.x + kGroups; t < BLOCK; t += kGroups) g = max(g, sh.group[t]);
-        sh.group[threadIdx.x] = g;
-    }
-    __syncthreads();
-    if (threadIdx.x < kGroups) {
-        const unsigned long long g = sh.group[threadIdx.x];
-        int above = 0;
-#pragma unroll 8
-        for (int t = 0; t < kGroups; ++t) above += sh.group[t] > g || (sh.group[t] == g && t < (int)threadIdx.x);
-        if (above == k - 1) sh.bound = g;
-    }
-    __syncthreads();
-    const unsigned long long bound = sh.bound;            // (logit, granule) of the k-th group; 0 if fewer groups have any logits
-    // threads that reach the bound, one after the other; the warp reads such a thread's granules together
-    unsigned reach = __ballot_sync(0xffffffffu, best >= bound && best != 0);
-    while (reach) {
-        const int owner = __ffs(reach) - 1;
-        reach &= reach - 1;
-        const int own0 = begin + (int)(threadIdx.x - lane) + owner;
-        for (int q0 = own0; q0 < end; q0 += BLOCK * 32) {
-            const int q = q0 + lane * BLOCK;
-            if (q >= end) continue;
-            float v[N];
-            row.load(q, end).get(v);
-            const int e0 = row.first_element(q);
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if (e0 + i < 0 || e0 + i >= row.vocab || !(v[i] == v[i]) || order_key(v[i], q) < bound) continue;
-                const int at = atomicAdd(&sh.found, 1);
-                if (at < kCandidates) sh.candidate[at] = order_key(v[i], (uint32_t)(e0 + i));
-            }
-        }
+// Sums over a block, the same in every thread.  (What a thread wrote to shared memory before is visible to all after.)
+template <int BLOCK> __device__ __forceinline__ Sums block_sums(Sums t, SharedSums<BLOCK> &sh) {
+    t = warp_sums(t);
+    if constexpr (BLOCK == 32) {
         __syncwarp();
+        return t;
     }
+    if (threadIdx.x % 32 == 0) sh.warp[threadIdx.x / 32] = t;
     __syncthreads();
+    t.clear();
+    if (threadIdx.x % 32 < BLOCK / 32) t = sh.warp[threadIdx.x % 32];
+    return warp_sums(t);
+}
+
+// The k largest of a block's logits.
+//
+// The k-th largest of 64 thread groups' maxima is a lower bound of the k-th largest logit, and only threads whose own maximum
+// reaches it can hold one of the k: they hand their logits above the bound on (typically k to 2 k of them), which are ranked by
+// counting.  Equal maxima are ordered by granule, so a row of equal logits hands on k granules, not all.
+
+// Before block_sums(): every thread's largest (logit, granule), 0 if it has none above -inf.
+template <int BLOCK> __device__ __forceinline__ void offer_best(unsigned long long best, Shared<BLOCK> &sh) {
+    sh.group[threadIdx.x] = best;
+    if (threadIdx.x < kTopMost) sh.top[threadIdx.x] = 0;
+    if (threadIdx.x == 0) { sh.found = 0; sh.owners = 0; sh.bound = 0; }
+}
+
+// After it: the bound, as (logit, granule); 0 where fewer than k groups have a logit.
+template <int BLOCK> __device__ __forceinline__ unsigned long long top_bound(int k, Shared<BLOCK> &sh) {
+    constexpr int G = Shared<BLOCK>::kGroups, PARTS = BLOCK / G;
+    if constexpr (PARTS > 1) {
+        if (threadIdx.x < G) {
+            unsigned long long g = sh.group[threadIdx.x];
+#pragma unroll
+            for (int t = threadIdx.x + G; t < BLOCK; t += G) g = max(g, sh.group[t]);
+            sh.group[threadIdx.x] = g;
+        }
+        __syncthreads();
+    }
+    const int i = threadIdx.x / PARTS, part = threadIdx.x % PARTS;
+    const unsigned long long g = sh.group[i];
+    int above = 0;
+#pragma unroll
+    for (int t = part; t < G; t += PARTS) above += sh.group[t] > g || (sh.group[t] == g && t < i);
+#pragma unroll
+    for (int o = PARTS / 2; o > 0; o >>= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
+    if (above == k - 1 && part == 0) sh.bound = g;
+    __syncthreads();
+    return sh.bound;
+}
+
+// Hands on a granule's logits that reach the bound.
+template <typename T, int BLOCK>
+__device__ __forceinline__ void hand_on(const Row<T> &row, const Granule<T> &raw, int q, unsigned long long bound, Shared<BLOCK> &sh) {
+    constexpr int N = Granule<T>::N;
+    if (order_key(raw.largest(), (uint32_t)q) < bound) return;       // (a granule of NaN alone compares either way)
+    float v[N];
+    raw.get(v);
+    const int e0 = row.first_element(q);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (!(v[i] > -INFINITY) || order_key(v[i], (uint32_t)q) < bound) continue;      // (beside the row lies -inf)
+        const int at = atomicAdd(&sh.found, 1);
+        if (at < kCandidates) sh.candidate[at] = order_key(v[i], (uint32_t)(e0 + i));
+    }
+}
+
+// Ranks what was handed on (after a barrier): the k largest, best first, into sh.top; 0 where there are fewer.
+template <typename T, int BLOCK>
+__device__ __forceinline__ void rank_candidates(const Row<T> &row, int begin, int end, int k, Shared<BLOCK> &sh) {
+    constexpr int PARTS = 4;
     const int found = sh.found;
     if (found <= kCandidates) {
-        for (int i = threadIdx.x; i < found; i += BLOCK) {
-            const unsigned long long key = sh.candidate[i];
+        for (int i0 = 0; i0 < found; i0 += BLOCK / PARTS) {
+            const int i = i0 + (int)threadIdx.x / PARTS;
+            const unsigned long long key = i < found ? sh.candidate[i] : 0;
             int above = 0;
-            for (int j = 0; j < found; ++j) above += sh.candidate[j] > key;
-            if (above < k) sh.top[above] = key;
+            for (int j = threadIdx.x % PARTS; j < found; j += PARTS) above += sh.candidate[j] > key;
+#pragma unroll
+            for (int o = PARTS / 2; o > 0; o >>= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
+            if (i < found && above < k) sh.top[above] = key;
         }
     } else {
         // too many logits above the bound (large ones gathered in few groups): one pass over the block's logits per rank
+        constexpr int N = Granule<T>::N;
         unsigned long long last = ~0ull;
         for (int r = 0; r < k; ++r) {
             unsigned long long mine = 0;
@@ -252,14 +368,13 @@ __device__ void block_top(const Row<T> &row, int begin, int end, int k, unsigned
                 const int e0 = row.first_element(q);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    if (e0 + i < 0 || e0 + i >= row.vocab || !(v[i] == v[i])) continue;
                     const unsigned long long key = order_key(v[i], (uint32_t)(e0 + i));
-                    if (key < last && key > mine) mine = key;
+                    if (v[i] > -INFINITY && key < last && key > mine) mine = key;
                 }
             }
             for (int o = 16; o > 0; o >>= 1) mine = max(mine, __shfl_xor_sync(0xffffffffu, mine, o));
             __syncthreads();
-            if (lane == 0) sh.group[threadIdx.x / 32] = mine;
+            if (threadIdx.x % 32 == 0) sh.group[threadIdx.x / 32] = mine;
             __syncthreads();
             for (int w = 0; w < BLOCK / 32; ++w) mine = max(mine, sh.group[w]);
             if (threadIdx.x == 0) sh.top[r] = mine;
@@ -269,82 +384,151 @@ __device__ void block_top(const Row<T> &row, int begin, int end, int k, unsigned
     __syncthreads();
 }
 
-// Maximum of a granule's logits (NaN is passed over; the sums carry it).
-template <typename T> __device__ __forceinline__ float granule_max(const float (&v)[Granule<T>::N]) {
-    float g = v[0];
-#pragma unroll
-    for (int i = 1; i < Granule<T>::N; ++i) g = fmaxf(g, v[i]);
-    return g;
-}
-
-// First pass over a block's share of a row.  best: largest (logit, granule) of this thread.
-template <typename T, int BLOCK, bool ENT>
-__device__ __forceinline__ Sums pass_sums(const Row<T> &row, int begin, int end, float c, int &best_granule) {
-    constexpr int N = Granule<T>::N, U = 4;
+// A thread's sums while it goes over granules, U at a time.
+template <typename T> struct Online {
+    static constexpr int P = Granule<T>::N / 2;
     Sums t;
-    t.clear();
-    best_granule = -1;
-    for (int q0 = begin + threadIdx.x; q0 < end; q0 += BLOCK * U) {
-        Granule<T> raw[U];
+    float top;                                            // largest logit so far, and the first granule that holds it
+    int best;
+    float c;
+    uint32_t low;
+    float_pair s2, a2;
+    __device__ __forceinline__ explicit Online(float c_) : top(-INFINITY), best(-1), c(c_), low(low_bound<T>(c_)) {
+        t.clear();
+        s2 = a2 = pair(0.f, 0.f);
+    }
+    template <int U> __device__ __forceinline__ void add(const Granule<T> (&raw)[U], int q0, int step) {
+        const float most = largest_of(raw);
+        if (most > top) {                                 // rare after the first granules
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = row.load(q0 + u * BLOCK, end);
-        float top = t.m;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float v[N];
-            raw[u].get(v);
-            const float g = granule_max<T>(v);
-            if (g > top) { top = g; best_granule = q0 + u * BLOCK; }
+            for (int u = U - 1; u >= 0; --u)
+                if (raw[u].largest() == most) best = q0 + u * step;
+            top = most;
+            const float to = fmaxf(top * c, -kNear);
+            if (to > t.r) {
+                collect();
+                t.rebase(to);
+                s2 = pair(t.s, 0.f);
+                a2 = pair(t.a, 0.f);
+            }
         }
-        if (top > t.m) t.rebase(top, c);
-        const float m = t.m == -INFINITY ? 0.f : t.m;
+        const float_pair c2 = pair(c, c), r2 = pair(-t.r, -t.r);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            float v[N];
-            raw[u].get(v);
+            float_pair x[P];
+            raw[u].pairs(low, x);
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float d = (v[i] - m) * c, e = exp2_approx(d);
-                t.s += e;
-                if (ENT) t.a = fmaf(e, max_nan(d, kFar), t.a);
+            for (int i = 0; i < P; ++i) {
+                const float_pair d = fma2(x[i], c2, r2);
+                float lo, hi;
+                split(d, lo, hi);
+                const float_pair e = pair(exp2_approx(lo), exp2_approx(hi));
+                s2 = add2(s2, e);
+                a2 = fma2(e, d, a2);
             }
         }
     }
+    __device__ __forceinline__ const Sums &collect() {
+        float lo, hi;
+        split(s2, lo, hi); t.s = lo + hi;
+        split(a2, lo, hi); t.a = lo + hi;
+        return t;
+    }
+};
+
+// First pass over a row or a share of it: the next U granules are on their way while U are summed.
+template <typename T, int BLOCK, int U> __device__ __forceinline__ void pass_sums(const Row<T> &row, int begin, int end, Online<T> &sums) {
+    Granule<T> next[U];
+    row.load_all(begin + (int)threadIdx.x, BLOCK, end, next);
+    for (int q0 = begin + threadIdx.x; q0 < end; q0 += BLOCK * U) {
+        Granule<T> raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = next[u];
+        if (q0 + BLOCK * U < end) row.load_all(q0 + BLOCK * U, BLOCK, end, next);
+        sums.add(raw, q0, BLOCK);
+    }
+}
+
+template <int BLOCK> __device__ __forceinline__ float block_max(float v, SharedSums<BLOCK> &sh) {
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    __syncthreads();                                      // (others may still read sh.warp)
+    if (threadIdx.x % 32 == 0) sh.warp[threadIdx.x / 32].r = v;
+    __syncthreads();
+    for (int w = 0; w < BLOCK / 32; ++w) v = fmaxf(v, sh.warp[w].r);
+    __syncthreads();
+    return v;
+}
+
+// The sums of a far row, relative to its largest logit (in Sums::r, unscaled): every block of a cluster goes over the whole row (such rows are few).
+template <typename T, int BLOCK> __device__ __noinline__ Sums far_sums(const Row<T> row, float c, SharedSums<BLOCK> &sh) {
+    constexpr int N = Granule<T>::N;
+    float most = -INFINITY;
+    for (int q = threadIdx.x; q < row.granules; q += BLOCK) most = fmaxf(most, row.load(q, row.granules).largest());
+    const float m = block_max(most, sh);
+    Sums t;
+    t.r = 0.f; t.s = 0.f; t.a = 0.f;
+    for (int q = threadIdx.x; q < row.granules; q += BLOCK) {
+        float v[N];
+        row.load(q, row.granules).get(v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (v[i] == -INFINITY) continue;              // (also what lies beside the row)
+            const float d = (v[i] - m) * c, e = exp2_approx(d);
+            t.s += e;
+            if (e != 0.f) t.a = fmaf(e, d, t.a);
+        }
+    }
+    t = block_sums<BLOCK>(t, sh);
+    t.r = m;
     return t;
 }
 
-// Sums of the whole row: the block's, joined with those of the other blocks of its cluster.
-template <int BLOCK> __device__ __forceinline__ Sums row_sums(Sums t, Shared<BLOCK> &sh, float c, int blocks) {
-    Sums r = block_sums<BLOCK>(t, sh, c);
-    if (blocks > 1) {
-        if (threadIdx.x == 0) { sh.bm = r.m; sh.bs = r.s; sh.ba = r.a; }
-        cluster_sync_all();
-        r.clear();
-        for (int b = 0; b < blocks; ++b) {                // the same order in every block
-            Sums u;
-            u.m = *at_rank(&sh.bm, b); u.s = *at_rank(&sh.bs, b); u.a = *at_rank(&sh.ba, b);
-            r.add(u, c);
-        }
-    }
-    return r;
+// Sums of the whole row from the blocks' sums; also what a block has put into its shared memory before is visible to the others after.
+template <int BLOCK> __device__ __forceinline__ Sums cluster_sums(Sums t, SharedSums<BLOCK> &sh, int blocks) {
+    if (blocks == 1) return t;
+    if (threadIdx.x == 0) sh.block = t;
+    cluster_sync_all();
+    t.clear();
+    if ((int)threadIdx.x % 32 < blocks) t = *at_rank(&sh.block, threadIdx.x % 32);
+    return warp_sums(t);                                  // the same in every block
 }
 
 // What a row's outputs are made of.  A row without a logit above -inf ("empty") has S = 0; NaN or +inf among the logits make S NaN.
 struct RowResult {
-    float m, log_s, entropy, inv_s;
-    bool empty;
-    __device__ __forceinline__ RowResult(const Sums &r) {
-        empty = r.s == 0.f;
-        m = empty ? 0.f : r.m;
-        log_s = empty ? 0.f : logf(r.s);
-        inv_s = empty ? 0.f : 1.f / r.s;
-        entropy = empty ? 0.f : log_s - 0.6931471805599453f * r.a * inv_s;
+    float scale, c, r, log2_s, entropy, inv_s;             // far: r is the largest logit itself
+    bool empty, far;
+    __device__ __forceinline__ RowResult() : scale(0.f), c(0.f), r(0.f), log2_s(0.f), entropy(0.f), inv_s(0.f), empty(true), far(false) {}
+    __device__ __forceinline__ void set(const Sums &t) {
+        empty = t.s == 0.f;
+        r = t.r;
+        log2_s = empty ? 0.f : log2f(t.s);
+        inv_s = empty ? 0.f : 1.f / t.s;
+        entropy = empty ? 0.f : kLn2 * (log2_s - t.a * inv_s);
     }
-    __device__ __forceinline__ float logprob(float x, float scale) const {
+    __device__ __forceinline__ float logprob(float x) const {
         if (empty) return -INFINITY;
-        return (x - m) * scale - log_s;
+        if (far) return (x - r) * scale - kLn2 * log2_s;
+        const float d = fmaf(x, c, -r);
+        if (d == -INFINITY) return x * scale + 0.f * inv_s;       // x c overflows and x s may not; the rest is less than its rounding
+        return kLn2 * (d - log2_s);
     }
+    static constexpr float kLn2 = 0.6931471805599453f;
 };
+
+// The row's result from its sums, with the far rows' second way.
+template <typename T, int BLOCK>
+__device__ __forceinline__ RowResult row_result(const Row<T> &row, const Sums &t, float scale, float c, SharedSums<BLOCK> &sh) {
+    RowResult r;
+    r.scale = scale;
+    r.c = c;
+    if (fabsf(t.r) < kNear) {
+        r.set(t);
+    } else {                                              // the same decision in every block of the cluster
+        r.far = true;
+        r.set(far_sums<T, BLOCK>(row, c, sh));
+    }
+    return r;
+}
 
 // A row's given token.  Its logit is read before the row's sums are joined: after that an in-place gradient may overwrite it.
 struct Given {
@@ -354,11 +538,11 @@ struct Given {
     template <typename T> __device__ __forceinline__ Given(const RowsArgs &p, const Row<T> &row, long long at) {
         token = p.tokens ? p.tokens[at] : PARLE_NO_TOKEN;
         real = token >= 0 && token < p.vocab;
-        x = p.logprob && real && threadIdx.x == 0 ? to_float(row.x[token]) : 0.f;
+        x = p.logprob && real && threadIdx.x == 0 ? to_float(row.x()[token]) : 0.f;
     }
     // by one thread
     __device__ __forceinline__ void write(const RowsArgs &p, long long at, const RowResult &r) const {
-        if (p.logprob) p.logprob[at] = real ? r.logprob(x, p.scale) : 0.f;
+        if (p.logprob) p.logprob[at] = real ? r.logprob(x) : 0.f;
         if (p.entropy) p.entropy[at] = r.entropy;
     }
     __device__ __forceinline__ void note_bad(const RowsArgs &p) const {
@@ -366,158 +550,421 @@ struct Given {
     }
 };
 
-// One row per block, or per cluster of `blocks` blocks that take a slice of its granules each.
-template <typename T, int BLOCK, bool ENT>
-__global__ void __launch_bounds__(BLOCK) token_logprobs_kernel(const RowsArgs p, int blocks) {
+// The k largest of a cluster's sh.top lists, in its first block (after a cluster barrier), into sh.top.  No key below the largest of
+// the lists' k-th keys can be among them, which leaves little more than k to rank.
+template <int BLOCK> __device__ __forceinline__ void merge_top(int k, int blocks, Shared<BLOCK> &sh) {
+    unsigned long long bound = 0;
+    for (int b = 0; b < blocks; ++b) bound = max(bound, at_rank(sh.top, b)[k - 1]);
+    __syncthreads();                                      // (sh.candidate and sh.found were in use)
+    if (threadIdx.x == 0) sh.found = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < blocks * k; i += BLOCK) {
+        const unsigned long long key = at_rank(sh.top, i / k)[i % k];
+        if (key && key >= bound) sh.candidate[atomicAdd(&sh.found, 1)] = key;
+    }
+    __syncthreads();
+    const int found = sh.found;
+    if (threadIdx.x < kTopMost) sh.top[threadIdx.x] = 0;  // (every block but this one is done with its own list)
+    __syncthreads();
+    for (int i = threadIdx.x; i < found; i += BLOCK) {
+        const unsigned long long key = sh.candidate[i];
+        int above = 0;
+#pragma unroll 8
+        for (int j = 0; j < found; ++j) above += sh.candidate[j] > key;
+        if (above < k) sh.top[above] = key;
+    }
+    __syncthreads();
+}
+
+// The alternatives of a row.
+template <int BLOCK>
+__device__ __forceinline__ void write_top(const RowsArgs &p, long long at, const RowResult &r, Shared<BLOCK> &sh) {
+    if (threadIdx.x >= p.k) return;
+    const unsigned long long key = sh.top[threadIdx.x];
+    const bool undefined = !(r.inv_s == r.inv_s), real = !undefined && key;
+    if (p.top_token) p.top_token[at * p.k + threadIdx.x] = real ? key_token(key) : PARLE_NO_TOKEN;
+    if (p.top_logprob) p.top_logprob[at * p.k + threadIdx.x] = undefined ? r.inv_s : real ? r.logprob(key_value(key)) : -INFINITY;
+}
+
+// Rows of any length, streamed: one block per row.
+template <typename T, int BLOCK, int U>
+__global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_kernel(const RowsArgs p) {
     __shared__ Shared<BLOCK> sh;
-    const long long at = blockIdx.x / blocks;
-    const int rank = blocks > 1 ? (int)cluster_rank() : 0;
+    const long long at = blockIdx.x;
     const Row<T> row(p.logits, p.ld, at, p.vocab);
-    const int per_block = (row.granules + blocks - 1) / blocks;
-    const int begin = min(row.granules, rank * per_block), end = min(row.granules, begin + per_block);
     const Given given(p, row, at);
-    int best_granule;
-    const Sums t = pass_sums<T, BLOCK, ENT>(row, begin, end, p.scale_log2e, best_granule);
-    const unsigned long long best = best_granule >= 0 ? order_key(t.m, (uint32_t)best_granule) : 0;
-    const RowResult r(row_sums<BLOCK>(t, sh, p.scale_log2e, blocks));
-    if (threadIdx.x == 0 && rank == 0) {
+    Online<T> sums(p.scale_log2e);
+    pass_sums<T, BLOCK, U>(row, 0, row.granules, sums);
+    const unsigned long long best = sums.best >= 0 ? order_key(sums.top, (uint32_t)sums.best) : 0;
+    if (p.k > 0) offer_best(best, sh);
+    const RowResult r = row_result<T, BLOCK>(row, block_sums<BLOCK>(sums.collect(), sh), p.scale, p.scale_log2e, sh);
+    if (threadIdx.x == 0) {
         given.write(p, at, r);
         given.note_bad(p);
     }
-    if (p.k > 0) {
-        block_top<T, BLOCK>(row, begin, end, p.k, best, sh);
-        if (blocks > 1) {                                 // rank the cluster's k-lists in its first block
-            cluster_sync_all();
-            if (rank == 0) {
-                const int all = blocks * p.k;
-                for (int i = threadIdx.x; i < all; i += BLOCK) sh.candidate[i] = at_rank(sh.top, i / p.k)[i % p.k];
-                __syncthreads();
-                if (threadIdx.x < p.k) sh.group[threadIdx.x] = 0;
-                __syncthreads();
-                for (int i = threadIdx.x; i < all; i += BLOCK) {
-                    const unsigned long long key = sh.candidate[i];
-                    int above = 0;
-                    for (int j = 0; j < all; ++j) above += sh.candidate[j] > key;
-                    if (key && above < p.k) sh.group[above] = key;
-                }
-                __syncthreads();
-            }
+    if (p.k == 0) return;
+    const unsigned long long bound = top_bound(p.k, sh);
+    if (best && best >= bound) sh.owner[atomicAdd(&sh.owners, 1)] = threadIdx.x;
+    __syncthreads();
+    // the granules of the threads that reach the bound, read by all threads, four in flight
+    const int per_owner = (row.granules + BLOCK - 1) / BLOCK, items = sh.owners * per_owner;
+    for (int i0 = threadIdx.x; i0 < items; i0 += BLOCK * 4) {
+        Granule<T> raw[4];
+        int q[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + u * BLOCK;
+            q[u] = i < items ? sh.owner[i / per_owner] + (i % per_owner) * BLOCK : row.granules;
+            raw[u] = row.load(q[u], row.granules);
         }
-        if (rank == 0 && threadIdx.x < p.k) {
-            const unsigned long long key = blocks > 1 ? sh.group[threadIdx.x] : sh.top[threadIdx.x];
-            const float x = key ? key_value(key) : -INFINITY;
-            const bool undefined = !(r.inv_s == r.inv_s), real = !undefined && x > -INFINITY;
-            if (p.top_token) p.top_token[at * p.k + threadIdx.x] = real ? key_token(key) : PARLE_NO_TOKEN;
-            if (p.top_logprob) p.top_logprob[at * p.k + threadIdx.x] = undefined ? r.inv_s : real ? r.logprob(x, p.scale) : -INFINITY;
-        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) hand_on(row, raw[u], q[u], bound, sh);
     }
-    if (blocks > 1) cluster_sync_all();                   // no block leaves while another may read its shared memory
+    __syncthreads();
+    rank_candidates(row, 0, row.granules, p.k, sh);
+    write_top(p, at, r, sh);
 }
 
-// The gradient, in a second pass over the row (which is then in L2).
-template <typename T, int BLOCK, bool ENT>
-__global__ void __launch_bounds__(BLOCK) token_logprobs_grad_kernel(const RowsArgs p, int blocks) {
-    __shared__ Shared<BLOCK> sh;
-    constexpr int N = Granule<T>::N, U = 4;
+// dlogits but for the given token's 1: e ( a + b d ), with a and b over S.
+template <typename T, bool ENT> struct Slope {
+    static constexpr int N = Granule<T>::N, P = N / 2;
+    float_pair c2, r2, a2, b2;
+    uint32_t low;
+    __device__ __forceinline__ Slope(const RowResult &t, float a, float b)
+        : c2(pair(t.c, t.c)), r2(pair(-t.r, -t.r)), a2(pair(a, a)), b2(pair(b, b)), low(low_bound<T>(t.c)) {}
+    __device__ __forceinline__ float_pair value(float_pair x) const {
+        const float_pair d = fma2(x, c2, r2);
+        float lo, hi;
+        split(d, lo, hi);
+        return mul2(pair(exp2_approx(lo), exp2_approx(hi)), ENT ? fma2(b2, d, a2) : a2);
+    }
+    __device__ __forceinline__ void values(const Granule<T> &raw, float (&v)[N]) const {
+        float_pair x[P];
+        raw.pairs(low, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) split(value(x[i]), v[2 * i], v[2 * i + 1]);
+    }
+    // of one logit, by the same steps
+    __device__ __forceinline__ float value(T x) const {
+        Granule<T> g;
+        g.fill_none();
+        *reinterpret_cast<T *>(&g.raw) = x;
+        float_pair f[P];
+        g.pairs(low, f);
+        float lo, hi;
+        split(value(f[0]), lo, hi);
+        return lo;
+    }
+};
+
+template <typename T> __device__ __forceinline__ uint4 packed(const float (&v)[Granule<T>::N]) {
+    if constexpr (sizeof(T) == 4) {
+        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    } else {
+        Pack8<T> o;
+        o.set(v);
+        return o.a;
+    }
+}
+
+// Where a row of dlogits goes: by granule where it begins at the same place of 16 bytes as the logits, else by element.
+template <typename T> struct OutRow {
+    static constexpr int N = Granule<T>::N;
+    T *out;
+    uint4 *base;                                          // NULL: by element
+    __device__ __forceinline__ OutRow(const RowsArgs &p, const Row<T> &row, long long at) {
+        out = static_cast<T *>(p.dlogits) + at * p.ld_d;
+        const uintptr_t a = reinterpret_cast<uintptr_t>(out);
+        base = (a - reinterpret_cast<uintptr_t>(row.x())) % 16 == 0 ? reinterpret_cast<uint4 *>(a & ~(uintptr_t)15) : nullptr;
+    }
+    __device__ __noinline__ static void store_elements(T *out, int e0, int vocab, uint4 packed) {
+        const T *v = reinterpret_cast<const T *>(&packed);
+        for (int j = max(0, -e0); j < N && e0 + j < vocab; ++j) out[e0 + j] = v[j];
+    }
+    __device__ __forceinline__ void store(const Row<T> &row, int q, bool whole, const float (&v)[N]) const {
+        if (base && whole) base[q] = packed<T>(v);
+        else store_elements(out, row.first_element(q), row.vocab, packed<T>(v));
+    }
+};
+
+// The given token's share g of a row of dlogits, added after the rest by the thread that wrote its granule.
+template <typename T> struct TokenShare {
+    bool mine;
+    T x;                                                  // the token's logit (read before an in-place gradient may overwrite it)
+    __device__ __forceinline__ TokenShare(const Row<T> &row, const Given &given, int first, int step, int end) {
+        const int q = given.real ? row.granule_of(given.token) : -1;
+        mine = given.real && q >= first && q < end && (q - first) % step == 0;
+        if (mine) x = row.x()[given.token];
+    }
+};
+
+// The gradient of granules first, first + step, .. < end of a far row.
+template <typename T>
+__device__ __noinline__ void far_gradient(const Row<T> row, int first, int step, int end, const RowResult r, float a, float b, float g, int token, const OutRow<T> out) {
+    constexpr int N = Granule<T>::N;
+    for (int q = first; q < end; q += step) {
+        float v[N];
+        row.load(q, end).get(v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float d = (v[i] - r.r) * r.c, e = exp2_approx(d);
+            v[i] = e == 0.f ? 0.f * a : e * fmaf(b, d, a);          // (an undefined row's a is NaN)
+            if (row.first_element(q) + i == token) v[i] += g;
+        }
+        out.store(row, q, false, v);
+    }
+}
+
+// What a row of the gradient needs besides its sums.
+struct Incoming {
+    float g, h;
+    bool none;                                            // no incoming gradient: zeros, whatever the logits
+    __device__ __forceinline__ Incoming(const RowsArgs &p, const Given &given, long long at) {
+        g = given.real && p.d_logprob ? p.d_logprob[at] * p.scale : 0.f;
+        h = p.d_entropy ? p.d_entropy[at] * p.scale : 0.f;
+        none = g == 0.f && h == 0.f;
+    }
+    // e ( a + b d ) / S + g 1[j = t]: a = -(g + h (H - log S)), b = -h log 2
+    __device__ __forceinline__ float a(const RowResult &r) const { return -fmaf(h, r.entropy - RowResult::kLn2 * r.log2_s, g) * r.inv_s; }
+    __device__ __forceinline__ float b(const RowResult &r) const { return -h * RowResult::kLn2 * r.inv_s; }
+};
+
+// Zeros in the block's share of a row of dlogits.
+template <typename T, int BLOCK> __device__ __forceinline__ void zero_row(const RowsArgs &p, long long at, int rank, int blocks) {
+    constexpr int N = Granule<T>::N;
+    const Row<T> to(p.dlogits, p.ld_d, at, p.vocab);
+    T *out = static_cast<T *>(p.dlogits) + at * p.ld_d;
+    const int share = (to.granules + blocks - 1) / blocks, from = rank * share;
+    for (int q = from + threadIdx.x; q < min(to.granules, from + share); q += BLOCK) {
+        const int e0 = to.first_element(q);
+        if (to.whole(q)) const_cast<uint4 *>(to.base)[q] = make_uint4(0, 0, 0, 0);
+        else
+            for (int i = max(0, -e0); i < N && e0 + i < p.vocab; ++i) out[e0 + i] = from_float<T>(0.f);
+    }
+}
+
+// The gradient of long rows, by a block or a cluster of blocks: a second pass reads the row again, from L2.  Its reads and the
+// stores are marked as the last use of their lines, so that rows between their two passes stay.
+template <typename T, int BLOCK, int U, bool ENT>
+__global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_grad_kernel(const RowsArgs p, int blocks) {
+    __shared__ SharedSums<BLOCK> sh;
     const long long at = blockIdx.x / blocks;
     const int rank = blocks > 1 ? (int)cluster_rank() : 0;
     const Row<T> row(p.logits, p.ld, at, p.vocab);
     const int per_block = (row.granules + blocks - 1) / blocks;
     const int begin = min(row.granules, rank * per_block), end = min(row.granules, begin + per_block);
     const Given given(p, row, at);
-    float g = given.real && p.d_logprob ? p.d_logprob[at] * p.scale : 0.f;
-    const float h = p.d_entropy ? p.d_entropy[at] * p.scale : 0.f;
-    const bool none = g == 0.f && h == 0.f;               // a row without an incoming gradient: zeros, whatever its logits
-    const float c = p.scale_log2e;
-    RowResult r{Sums{-INFINITY, 0.f, 0.f}};
-    if (!none || p.logprob || p.entropy) {
-        int best_granule;
-        r = RowResult(row_sums<BLOCK>(pass_sums<T, BLOCK, ENT>(row, begin, end, c, best_granule), sh, c, blocks));
-        if (threadIdx.x == 0 && rank == 0) given.write(p, at, r);
-    }
+    const Incoming in(p, given, at);
+    const OutRow<T> out(p, row, at);
+    const TokenShare<T> share(row, given, begin + (int)threadIdx.x, BLOCK, end);
     if (threadIdx.x == 0 && rank == 0) given.note_bad(p);
-    if (r.empty) g = 0.f;
-    // p_j ( a + b d_j ) + g 1[j = t], d in units of log 2
-    const float a = none ? 0.f : -(g + h * (r.entropy - r.log_s)), b = -h * 0.6931471805599453f;
-    const float inv_s = none ? 0.f : r.inv_s, m = none ? 0.f : r.m;
-    T *out = static_cast<T *>(p.dlogits) + at * p.ld_d;
-    const bool same_phase = (reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(row.x)) % 16 == 0;
-    for (int q0 = begin + threadIdx.x; q0 < end; q0 += BLOCK * U) {
-        Granule<T> raw[U];
+    if (in.none && !p.logprob && !p.entropy) return zero_row<T, BLOCK>(p, at, rank, blocks);      // (every block of the cluster)
+    Online<T> sums(p.scale_log2e);
+    pass_sums<T, BLOCK, U>(row, begin, end, sums);
+    const RowResult r = row_result<T, BLOCK>(row, cluster_sums<BLOCK>(block_sums<BLOCK>(sums.collect(), sh), sh, blocks), p.scale, p.scale_log2e, sh);
+    if (threadIdx.x == 0 && rank == 0) given.write(p, at, r);
+    if (r.far && blocks > 1) cluster_sync_all();          // each block has read the whole row before any writes an in-place gradient
+    if (blocks > 1) cluster_done();
+    if (in.none || r.empty) {
+        zero_row<T, BLOCK>(p, at, rank, blocks);
+    } else if (r.far) {
+        far_gradient<T>(row, begin + (int)threadIdx.x, BLOCK, end, r, in.a(r), in.b(r), in.g, given.token, out);
+    } else {
+        const Slope<T, ENT> slope(r, in.a(r), in.b(r));
+        // from the end: what was read last is the likeliest to be in L1 and L2 still
+        const int stride = BLOCK * U;
+        const auto fast = [&](int q0) { return out.base && row.all_whole(q0, q0 + (U - 1) * BLOCK, end); };
+        const auto fetch = [&](int q0, Granule<T> (&raw)[U]) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (none) raw[u].fill_none();
-            else raw[u] = row.load(q0 + u * BLOCK, end);
-        }
+            for (int u = 0; u < U; ++u) raw[u].raw = __ldcs(row.base + q0 + u * BLOCK);
+        };
+        int q0 = begin + (int)threadIdx.x + (end - begin - 1) / stride * stride;
+        Granule<T> next[U];
+        if (fast(q0)) fetch(q0, next);
+        for (; q0 >= begin; q0 -= stride) {
+            if (fast(q0)) {
+                Granule<T> raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int q = q0 + u * BLOCK;
-            if (q >= end) break;
-            float v[N];
-            raw[u].get(v);
-            const int e0 = row.first_element(q);
+                for (int u = 0; u < U; ++u) raw[u] = next[u];
+                if (q0 - stride >= begin && fast(q0 - stride)) fetch(q0 - stride, next);
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float d = (v[i] - m) * c, e = exp2_approx(d) * inv_s;
-                v[i] = e * (ENT ? fmaf(b, max_nan(d, kFar), a) : a);
-                if (e0 + i == given.token) v[i] += g;
-            }
-            if (same_phase && row.whole(q)) {
-                T w[N];
-#pragma unroll
-                for (int i = 0; i < N; ++i) w[i] = from_float<T>(v[i]);
-                *reinterpret_cast<uint4 *>(out + e0) = *reinterpret_cast<const uint4 *>(w);
+                for (int u = 0; u < U; ++u) {
+                    float v[Granule<T>::N];
+                    slope.values(raw[u], v);
+                    __stcs(out.base + q0 + u * BLOCK, packed<T>(v));
+                }
             } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (e0 + i >= 0 && e0 + i < p.vocab) out[e0 + i] = from_float<T>(v[i]);
+                if (q0 - stride >= begin && fast(q0 - stride)) fetch(q0 - stride, next);
+                for (int u = 0; u < U; ++u) {
+                    const int q = q0 + u * BLOCK;
+                    if (q >= end) break;
+                    float v[Granule<T>::N];
+                    slope.values(row.load(q, end), v);
+                    out.store(row, q, row.whole(q), v);
+                }
             }
         }
+        if (share.mine) out.out[given.token] = from_float<T>(slope.value(share.x) + in.g);
     }
-    if (blocks > 1) cluster_sync_all();
+    if (blocks > 1) cluster_await_done();                 // no block leaves while another may read its shared memory
 }
 
-// How many blocks share a row: few rows of many granules are split so that the SMs have work.
-int blocks_per_row(long long rows, long long granules, int block, int sms) {
-    int blocks = 1;
-    while (blocks < kClusterMost && rows * blocks * 2 <= 2 * sms && granules >= (long long)block * blocks * 8) blocks *= 2;
-    return blocks;
+// Rows held in registers, U granules a thread, by a block or a cluster of blocks: everything is in flight at once and read once,
+// and the gradient is formed from what is held.  GRAD: the gradient (ENT: with an entropy's); else log probabilities, entropy, top.
+template <typename T, int BLOCK, int U, bool GRAD, bool ENT>
+__global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kernel(const RowsArgs p, int blocks) {
+    __shared__ Shared<BLOCK> sh;
+    constexpr int P = Granule<T>::N / 2;
+    const long long at = blockIdx.x / blocks;
+    const int rank = blocks > 1 ? (int)cluster_rank() : 0;
+    const Row<T> row(p.logits, p.ld, at, p.vocab);
+    const int per_block = (row.granules + blocks - 1) / blocks;      // at most BLOCK * U
+    const int begin = min(row.granules, rank * per_block), end = min(row.granules, begin + per_block);
+    const int q0 = begin + (int)threadIdx.x;
+    const Given given(p, row, at);
+    const Incoming in(p, given, at);
+    if (threadIdx.x == 0 && rank == 0) given.note_bad(p);
+    if (GRAD && in.none && !p.logprob && !p.entropy) return zero_row<T, BLOCK>(p, at, rank, blocks);      // (every block of the cluster)
+    const TokenShare<T> share(row, given, q0, BLOCK, GRAD ? end : 0);
+    Granule<T> raw[U];
+    row.load_all(q0, BLOCK, end, raw);
+    float top = -INFINITY;
+    int best_granule = -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const float v = raw[u].largest();
+        if (v > top) { top = v; best_granule = q0 + u * BLOCK; }
+    }
+    const float c = p.scale_log2e;
+    Sums t;
+    t.r = fmaxf(top * c, -kNear);
+    {
+        const uint32_t low = low_bound<T>(c);
+        const float_pair c2 = pair(c, c), r2 = pair(-t.r, -t.r);
+        float_pair s2 = pair(0.f, 0.f), a2 = pair(0.f, 0.f);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (q0 + u * BLOCK >= end) break;
+            float_pair x[P];
+            raw[u].pairs(low, x);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const float_pair d = fma2(x[i], c2, r2);
+                float lo, hi;
+                split(d, lo, hi);
+                const float_pair e = pair(exp2_approx(lo), exp2_approx(hi));
+                s2 = add2(s2, e);
+                if (ENT || !GRAD) a2 = fma2(e, d, a2);
+            }
+        }
+        float lo, hi;
+        split(s2, lo, hi); t.s = lo + hi;
+        split(a2, lo, hi); t.a = lo + hi;
+    }
+    const unsigned long long best = best_granule >= 0 ? order_key(top, (uint32_t)best_granule) : 0;
+    if (!GRAD && p.k > 0) offer_best(best, sh);
+    t = block_sums<BLOCK>(t, sh);
+    if (!GRAD && p.k > 0) {
+        const unsigned long long bound = top_bound(p.k, sh);
+        if (best && best >= bound) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (q0 + u * BLOCK < end) hand_on(row, raw[u], q0 + u * BLOCK, bound, sh);
+        }
+        __syncthreads();
+        rank_candidates(row, begin, end, p.k, sh);
+    }
+    const RowResult r = row_result<T, BLOCK>(row, cluster_sums<BLOCK>(t, sh, blocks), p.scale, c, sh);
+    if (threadIdx.x == 0 && rank == 0) given.write(p, at, r);
+    if constexpr (GRAD) {
+        const OutRow<T> out(p, row, at);
+        if (r.far && blocks > 1) cluster_sync_all();      // each block has read the whole row before any writes an in-place gradient
+        if (blocks > 1) cluster_done();
+        if (in.none || r.empty) {
+            zero_row<T, BLOCK>(p, at, rank, blocks);
+        } else if (r.far) {
+            far_gradient<T>(row, q0, BLOCK, end, r, in.a(r), in.b(r), in.g, given.token, out);
+        } else {
+            const Slope<T, ENT> slope(r, in.a(r), in.b(r));
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int q = q0 + u * BLOCK;
+                if (q >= end) break;
+                float v[Granule<T>::N];
+                slope.values(raw[u], v);
+                out.store(row, q, row.whole(q), v);
+            }
+            if (share.mine) out.out[given.token] = from_float<T>(slope.value(share.x) + in.g);
+        }
+    } else if (p.k > 0 && rank == 0) {
+        if (blocks > 1) merge_top(p.k, blocks, sh);
+        write_top(p, at, r, sh);
+    }
+    if (!GRAD && blocks > 1) cluster_done();
+    if (blocks > 1) cluster_await_done();                 // no block leaves while another may read its shared memory
 }
 
-template <typename T, int BLOCK> int launch_rows(const RowsArgs &p, bool grad, int blocks, cudaStream_t stream) {
+// A launch of rows * blocks blocks, `blocks` of them a cluster.
+cudaLaunchConfig_t row_config(long long rows, int blocks, int threads, cudaLaunchAttribute &attr, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(p.rows * blocks));
-    cfg.blockDim = dim3(BLOCK);
+    cfg.gridDim = dim3((unsigned)(rows * blocks));
+    cfg.blockDim = dim3(threads);
     cfg.stream = stream;
-    cudaLaunchAttribute attr = {};
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = blocks;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = blocks > 1 ? 1 : 0;
-    const bool ent = p.entropy || p.d_entropy;
-    cudaError_t e;
-    if (grad) e = ent ? cudaLaunchKernelEx(&cfg, token_logprobs_grad_kernel<T, BLOCK, true>, p, blocks)
-                      : cudaLaunchKernelEx(&cfg, token_logprobs_grad_kernel<T, BLOCK, false>, p, blocks);
-    else e = ent ? cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, BLOCK, true>, p, blocks)
-                 : cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, BLOCK, false>, p, blocks);
-    if (e != cudaSuccess) return PARLE_ECUDA;
+    return cfg;
+}
+
+template <typename T, int BLOCK, int U, bool GRAD, bool ENT> int launch_held(const RowsArgs &p, int blocks, cudaStream_t stream) {
+    cudaLaunchAttribute attr = {};
+    const cudaLaunchConfig_t cfg = row_config(p.rows, blocks, BLOCK, attr, stream);
+    if (cudaLaunchKernelEx(&cfg, token_logprobs_held_kernel<T, BLOCK, U, GRAD, ENT>, p, blocks) != cudaSuccess) return PARLE_ECUDA;
+    return launch_status();
+}
+
+template <typename T, int BLOCK, int U, bool ENT> int launch_grad(const RowsArgs &p, int blocks, cudaStream_t stream) {
+    cudaLaunchAttribute attr = {};
+    const cudaLaunchConfig_t cfg = row_config(p.rows, blocks, BLOCK, attr, stream);
+    if (cudaLaunchKernelEx(&cfg, token_logprobs_grad_kernel<T, BLOCK, U, ENT>, p, blocks) != cudaSuccess) return PARLE_ECUDA;
+    return launch_status();
+}
+
+template <typename T, bool GRAD, bool ENT> int launch_rows(const RowsArgs &p, int sms, cudaStream_t stream) {
+    // granules of a row, one more where rows do not all begin on 16-byte boundaries
+    const long long granules = ((long long)p.vocab * sizeof(T) + 15) / 16 + (reinterpret_cast<uintptr_t>(p.logits) % 16 || p.ld * sizeof(T) % 16 ? 1 : 0);
+    constexpr int U = 8;
+    if (granules <= 32 * 4) return launch_held<T, 32, 4, GRAD, ENT>(p, 1, stream);
+    if (granules <= 32 * U) return launch_held<T, 32, U, GRAD, ENT>(p, 1, stream);
+    if (granules <= 128 * U) return launch_held<T, 128, U, GRAD, ENT>(p, 1, stream);
+    // Few long rows: a cluster of up to 8 blocks each (a cluster costs some microseconds of its own).  Measured, 131072 bf16 logits,
+    // cluster against one block: 1 row 6.5 / 10.8 us (gradient 8.4 / 16.7), 32 rows 8.6 / 11.8 (10.5 / 16.7), 64 rows 10.6 / 12.4
+    // (12.6 / 16.7), 128 rows 16.9 / 12.6 (20.9 / 16.6); 20000 bf16 logits, 1 row: 6.5 / 5.9 (8.0 / 7.5).
+    const long long blocks = (granules + 256 * U - 1) / (256 * U);
+    if (granules > 4096 && blocks <= kClusterMost && p.rows * blocks <= (GRAD ? 4 : 2) * sms)
+        return launch_held<T, 256, U, GRAD, ENT>(p, (int)blocks, stream);
+    // One block a row; 512 threads where fewer rows between their two passes keep them in L2.  Measured, gradient of 131072 bf16 logits,
+    // 512 against 256 threads: 2048 rows 204 / 231 us; of 65536, 1024 rows 59 / 60; of 32768, 1024 rows 37 / 32.
+    if constexpr (GRAD) {
+        return granules > 8192 ? launch_grad<T, 512, 4, ENT>(p, 1, stream) : launch_grad<T, 256, 4, ENT>(p, 1, stream);
+    } else {
+        token_logprobs_kernel<T, 256, 4><<<(unsigned)p.rows, 256, 0, stream>>>(p);
+    }
     return launch_status();
 }
 
 template <typename T> int launch_logprobs(const RowsArgs &p, bool grad, cudaStream_t stream) {
-    const long long granules = ((long long)p.vocab * sizeof(T) + 15) / 16;
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return PARLE_ECUDA;
-    if (granules <= 256) return launch_rows<T, 64>(p, grad, 1, stream);
-    if (granules <= 1024) return launch_rows<T, 128>(p, grad, 1, stream);
-    if (granules <= 4096) return launch_rows<T, 256>(p, grad, blocks_per_row(p.rows, granules, 256, sms), stream);
-    return launch_rows<T, 512>(p, grad, blocks_per_row(p.rows, granules, 512, sms), stream);
+    if (!grad) return launch_rows<T, false, true>(p, sms, stream);
+    return p.entropy || p.d_entropy ? launch_rows<T, true, true>(p, sms, stream) : launch_rows<T, true, false>(p, sms, stream);
 }
 
 int check_rows(const void *logits, int dtype, long long rows, int vocab, long long ld, const int32_t *tokens, double scale) {
     if (!valid_dtype(dtype) || rows < 0 || vocab < 1 || ld < 0) return PARLE_EINVAL;
-    if (!(scale > 0.0) || !isfinite((float)(scale * 1.4426950408889634)) || (float)scale == 0.f) return PARLE_EINVAL;
+    if (!(scale >= 1e-6 && scale <= 1e6)) return PARLE_EINVAL;      // (keeps scaled logits and bounds on them in fp32's range)
     if (rows > 0 && !logits) return PARLE_EINVAL;
     if (rows > PARLE_TOKEN_MAX_ROWS / kClusterMost || vocab > PARLE_TOKEN_MAX_ROWS) return PARLE_ETOOBIG;
     if (!element_aligned(logits, dtype) || !element_aligned(tokens, PARLE_F32)) return PARLE_EALIGN;

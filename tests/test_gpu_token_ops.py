@@ -168,6 +168,14 @@ def test_logprobs_shapes_and_optional_outputs():
     assert rc == 0 and torch.equal(out.view(3, 4, 2).long(), want.topk(2).indices)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [5, 1031, 9001])
+@pytest.mark.parametrize("scale", [1e-6, 1e6])
+def test_logprobs_at_the_smallest_and_largest_scale(dtype, vocab, scale):
+    x = special_rows(vocab, dtype)
+    check_logprobs(x, np.array([(7 * r + 1) % vocab for r in range(x.shape[0])]), scale, 9)
+
+
 def check_grad(x, tokens, g, h, scale, inplace=False, pad=0, shift=0, outputs=False):
     rows, vocab = x.shape
     tok = torch.from_numpy(np.asarray(tokens, np.int32)).to(DEV)

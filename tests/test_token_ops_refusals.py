@@ -43,7 +43,7 @@ def dropout(x=P, ld_x=8, residual=None, ld_r=0, y=2 * P, ld_y=8, dtype=F32, rows
     (logprobs, dict(logits=None), EINVAL), (logprobs, dict(dtype=3), EINVAL), (logprobs, dict(rows=-1), EINVAL),
     (logprobs, dict(vocab=0), EINVAL), (logprobs, dict(ld=-1), EINVAL), (logprobs, dict(scale=0.0), EINVAL),
     (logprobs, dict(scale=-1.0), EINVAL), (logprobs, dict(scale=math.nan), EINVAL), (logprobs, dict(scale=math.inf), EINVAL),
-    (logprobs, dict(scale=3e38), EINVAL), (logprobs, dict(scale=1e-60), EINVAL), (logprobs, dict(tokens=None), EINVAL),
+    (logprobs, dict(scale=3e38), EINVAL), (logprobs, dict(scale=1e-60), EINVAL), (logprobs, dict(scale=9e-7), EINVAL), (logprobs, dict(scale=1.1e6), EINVAL), (logprobs, dict(tokens=None), EINVAL),
     (logprobs, dict(k=33, top_token=P), EINVAL), (logprobs, dict(k=-1), EINVAL), (logprobs, dict(k=0, top_token=P), EINVAL),
     (logprobs, dict(logprob=None), EINVAL), (logprobs, dict(rows=1 << 31), ETOOBIG), (logprobs, dict(vocab=(1 << 30) + 1), ETOOBIG),
     (logprobs, dict(logits=P + 2), EALIGN), (logprobs, dict(logits=P + 1, dtype=BF16), EALIGN), (logprobs, dict(tokens=P + 2), EALIGN),
