@@ -405,8 +405,9 @@ int parle_embedding(const void *table, int table_dtype, long long table_gs, long
  * accumulate == 0: all vocab rows are written (zeros for tokens that do not occur); else the sums are added to dtable and rows
  * of tokens that do not occur are left untouched.  Elements between rows (ld_dtable > dim) are never touched.
  * dtable_gs = stride puts the gradient into the grad vector that parle_inner_update reads.
- * workspace dev, 128-byte aligned, >= parle_embedding_grad_workspace_bytes() (0 for invalid sizes): scratch of this call alone
- * until its work has finished.  EWORKSPACE if too small. */
+ * workspace dev, 128-byte aligned, >= parle_embedding_grad_workspace_bytes(): scratch of this call alone until its work has
+ * finished.  Up to 1024 positions no workspace is needed: 0 bytes, and NULL is taken (0 for invalid sizes too).
+ * EWORKSPACE if too small. */
 size_t parle_embedding_grad_workspace_bytes(int n, long long length, int vocab, int dim);
 int parle_embedding_grad(const void *dout, int dout_dtype, long long dout_gs, long long ld_dout, const int32_t *tokens,
                          int n, long long length, int vocab, int dim, double scale, float *dtable, long long dtable_gs,

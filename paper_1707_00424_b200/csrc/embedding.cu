@@ -3,13 +3,20 @@
 //   out[g, t, :] = scale * table[g, token[g, t], :]
 //   dtable[g, v, :] = scale * sum over t with token[g, t] = v of dout[g, t, :]      (t in ascending order, fp32)
 //
-// The gradient is formed by sorted tokens: positions are sorted by (token, position), the sorted sequence is cut into chunks of
-// kChunk positions, a block sums the runs of equal tokens in its chunk and writes the rows of those that begin and end there;
-// a run that crosses a chunk's border leaves one partial row per chunk, which a second kernel joins.  No floating-point
-// atomics: the same inputs give the same bits.
+// No floating-point atomics: the same inputs give the same bits.  Two ways to the gradient:
+//
+// Up to kDirectMost positions ("direct", one launch, no workspace): a block takes a set of table rows, looks through all the
+// tokens, notes for each of its rows the positions that hold its token, puts them in order and sums.
+//
+// More positions ("sorted"): one kernel sorts the positions by (token, position) in the shared memory of a cluster.  The sorted
+// sequence is then cut into chunks of kChunk positions; a block sums the runs of equal tokens in its chunk and writes the rows of
+// those that begin and end there, while other blocks write zeros to the rows of tokens that do not occur.  A run that crosses a
+// chunk's border leaves one partial row per chunk, which a last kernel joins.  Work is shared out by position, so it does not
+// matter how often which token occurs.
 #include <limits.h>
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "token_types.cuh"
@@ -83,59 +90,409 @@ int threads_per_row(int steps) {
     return t;
 }
 
-// ---- gradient: sorting ---------------------------------------------------------------------------------------------------------
+// ---- gradient --------------------------------------------------------------------------------------------------------------------
 
-constexpr int kChunk = 32;              // sorted positions a block of the reduction sums
-constexpr int kRankedMost = 8192;       // longest sequence ranked by counting
-constexpr int kDigits = 256;            // of a radix pass (8 bits)
-constexpr int kTile = 4096;             // positions a block of a radix pass moves
-constexpr int kSplit = 8;               // threads that share the counting for one position
-
-// A position without a token sorts behind all others: key = vocab.
-__device__ __forceinline__ int sort_key(int token, int vocab) { return token >= 0 && token < vocab ? token : vocab; }
+struct GradArgs {
+    const void *dout;
+    float *dtable;
+    const int32_t *tokens;
+    int32_t *flags;
+    const int *keys, *places;                             // sorted
+    float *partial;                                       // [n][chunks][2][dim]: a chunk's first run (if it began before), last run (if it goes on)
+    uint32_t *occurs;                                     // [n][words]: bit v of a table: token v occurs
+    int words;
+    int *crossings;                                       // how many runs cross a border, then (table, chunk in which it begins, token, -) of each
+    long long dout_gs, ld_dout, dtable_gs, ld_dtable;
+    int length, vocab, dim, chunks;
+    float scale;
+    int accumulate;
+};
 
 __device__ __forceinline__ void note_bad_token(int token, int vocab, int32_t *flags) {
     if (flags && token != PARLE_NO_TOKEN && (token < 0 || token >= vocab)) atomicOr(flags, PARLE_FLAG_BAD_LABEL);
 }
 
-// Short sequences: the place of position t in the sorted order is the number of positions s with key(s) < key(t), or equal and
-// s < t.  length^2 comparisons, no passes; kSplit threads share one t.
-__global__ void __launch_bounds__(kThreads)
-rank_tokens_kernel(const int32_t *tokens, int length, int vocab, int *keys, int *places, int32_t *flags) {
-    __shared__ int tile[kThreads * 4];
-    const int g = blockIdx.y;
-    tokens += (long long)g * length;
-    const int t = blockIdx.x * (kThreads / kSplit) + threadIdx.x / kSplit, part = threadIdx.x % kSplit;
-    const int token = t < length ? tokens[t] : PARLE_NO_TOKEN;
-    const int key = sort_key(token, vocab);
-    int before = 0;
-    for (int s0 = 0; s0 < length; s0 += kThreads * 4) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < kThreads * 4; i += kThreads) tile[i] = s0 + i < length ? sort_key(tokens[s0 + i], vocab) : INT_MAX;
-        __syncthreads();
-#pragma unroll 8
-        for (int i = part; i < kThreads * 4; i += kSplit) before += tile[i] < key + (s0 + i < t ? 1 : 0);
+// ---- direct gradient -------------------------------------------------------------------------------------------------------------
+
+constexpr int kDirectMost = 1024;       // longest sequence
+constexpr int kNoted = 32;              // positions of a row that are noted
+constexpr int kRowsMost = 64;           // table rows of a block
+constexpr int kColumns = 512;           // columns of a block
+constexpr int kWarps = kThreads / 32;
+
+// Eight columns of a lane out of 256 from `first` on: eight neighbours by wide loads (E = 8), or every 32nd (E = 1).
+template <typename T, int E> struct Lane8 {
+    Pack8<T> raw;
+    T one[E == 1 ? 8 : 1];
+    __device__ __forceinline__ static int column(int first, int k) { return E == 8 ? first + ((int)threadIdx.x % 32) * 8 + k : first + k * 32 + (int)threadIdx.x % 32; }
+    __device__ __forceinline__ void load(const T *row, int first, int dim) {
+        if constexpr (E == 8) {
+            if (column(first, 0) < dim) raw.load(row + column(first, 0));
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (column(first, k) < dim) one[k] = row[column(first, k)];
+        }
     }
-    for (int o = kSplit / 2; o > 0; o >>= 1) before += __shfl_down_sync(0xffffffffu, before, o, kSplit);
-    if (t < length && part == 0) {
-        keys[(long long)g * length + before] = key;
-        places[(long long)g * length + before] = t;
-        note_bad_token(token, vocab, flags);
+    __device__ __forceinline__ void add_to(float (&acc)[8]) const {
+        float v[8];
+        if constexpr (E == 8) {
+            raw.get(v);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = to_float(one[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) acc[k] += v[k];
+    }
+};
+
+template <int E> __device__ __forceinline__ void store_row(const GradArgs &p, float *row, int first, float (&acc)[8]) {
+    if constexpr (E == 8) {
+        const int c = Lane8<float, 8>::column(first, 0);
+        if (c >= p.dim) return;
+        if (p.accumulate) {
+            Pack8<float> old;
+            float v[8];
+            old.load(row + c);
+            old.get(v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) acc[k] = fmaf(p.scale, acc[k], v[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) acc[k] *= p.scale;
+        }
+        Pack8<float> out;
+        out.set(acc);
+        out.store(row + c);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int c = Lane8<float, 1>::column(first, k);
+            if (c < p.dim) row[c] = p.accumulate ? fmaf(p.scale, acc[k], row[c]) : p.scale * acc[k];
+        }
     }
 }
 
-// One pass of a stable radix sort, least significant digit first.  First: how often each digit occurs in a tile.
+// grid (G, column parts, n); block b has the table rows v with v mod G = b, so that neighbouring tokens, which are often frequent
+// together, fall to different blocks.
+template <typename T, int E>
+__global__ void __launch_bounds__(kThreads, 4) embedding_grad_direct_kernel(const GradArgs p, int log_groups) {
+    __shared__ int count[kRowsMost], frequent[kRowsMost], frequents;
+    __shared__ int noted[kRowsMost][kNoted];
+    __shared__ float parts[kWarps / 2][kColumns];         // of a frequent token's row
+    const int g = blockIdx.z, b = blockIdx.x, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int col0 = blockIdx.y * kColumns, groups = 1 << log_groups;
+    const int rows = (p.vocab - b + groups - 1) >> log_groups;
+    const int32_t *tokens = p.tokens + (long long)g * p.length;
+    const T *dout = static_cast<const T *>(p.dout) + (long long)g * p.dout_gs;
+    float *dtable = p.dtable + (long long)g * p.dtable_gs;
+    if (threadIdx.x < kRowsMost) count[threadIdx.x] = 0;
+    if (threadIdx.x == 0) frequents = 0;
+    int token[kDirectMost / kThreads];
+#pragma unroll
+    for (int u = 0; u < kDirectMost / kThreads; ++u) {
+        const int t = threadIdx.x + u * kThreads;
+        token[u] = t < p.length ? tokens[t] : PARLE_NO_TOKEN;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kDirectMost / kThreads; ++u) {
+        if (b == 0 && blockIdx.y == 0) note_bad_token(token[u], p.vocab, p.flags);
+        if ((token[u] & (groups - 1)) != b || (unsigned)token[u] >= (unsigned)p.vocab) continue;
+        const int row = token[u] >> log_groups, at = atomicAdd(&count[row], 1);
+        if (at < kNoted) noted[row][at] = threadIdx.x + u * kThreads;
+    }
+    __syncthreads();
+    for (int i = warp; i < rows; i += kWarps) {
+        const int m = count[i];
+        float *row = dtable + (long long)((i << log_groups) + b) * p.ld_dtable;
+        if (m == 0) {
+            if (p.accumulate) continue;
+            const int end = min(p.dim, col0 + kColumns);
+            if constexpr (E == 8) {
+                for (int c = col0 + lane * 4; c < end; c += 128) *reinterpret_cast<float4 *>(row + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+            } else {
+                for (int c = col0 + lane; c < end; c += 32) row[c] = 0.f;
+            }
+            continue;
+        }
+        if (m > kNoted) {
+            if (lane == 0) frequent[atomicAdd(&frequents, 1)] = i;
+            continue;
+        }
+        // the noted positions in ascending order: one per lane, moved to the number of smaller ones
+        int place = lane < m ? noted[i][lane] : INT_MAX;
+        if (m > 1) {
+            int smaller = 0;
+            for (int j = 0; j < m; ++j) smaller += __shfl_sync(0xffffffffu, place, j) < place;
+            __syncwarp();
+            if (lane < m) noted[i][smaller] = place;
+            __syncwarp();
+            place = noted[i][min(lane, m - 1)];
+        }
+        float acc[2][8] = {};
+        for (int j = 0; j < m; j += 2) {
+            Lane8<T, E> v[2][2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const T *from = dout + (long long)__shfl_sync(0xffffffffu, place, min(j + u, m - 1)) * p.ld_dout;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (j + u < m) v[u][h].load(from, col0 + h * 256, p.dim);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (j + u < m) v[u][h].add_to(acc[h]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) store_row<E>(p, row, col0 + h * 256, acc[h]);
+    }
+    // rows of frequent tokens: two warps side by side, four along the positions; their parts are added in order
+    __syncthreads();
+    const int half = warp % 2, quarter = warp / 2;
+    const int per_part = (p.length + kWarps / 2 - 1) / (kWarps / 2);
+    const int from = min(p.length, quarter * per_part), to = min(p.length, from + per_part);
+    for (int f = 0; f < frequents; ++f) {
+        const int v = (frequent[f] << log_groups) + b;
+        float acc[8] = {};
+        for (int t0 = from; t0 < to; t0 += 32) {
+            unsigned found = __ballot_sync(0xffffffffu, t0 + lane < to && tokens[t0 + lane] == v);
+            while (found) {
+                Lane8<T, E> x[4];
+                int many = 0;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    if (!found) break;
+                    x[u].load(dout + (long long)(t0 + __ffs(found) - 1) * p.ld_dout, col0 + half * 256, p.dim);
+                    found &= found - 1;
+                    ++many;
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (u < many) x[u].add_to(acc);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) parts[quarter][Lane8<T, E>::column(half * 256, k)] = acc[k];
+        __syncthreads();
+        float *row = dtable + (long long)v * p.ld_dtable;
+        for (int c = threadIdx.x; c < kColumns && col0 + c < p.dim; c += kThreads) {
+            const float sum = ((parts[0][c] + parts[1][c]) + parts[2][c]) + parts[3][c];
+            row[col0 + c] = p.accumulate ? fmaf(p.scale, sum, row[col0 + c]) : p.scale * sum;
+        }
+        __syncthreads();
+    }
+}
+
+// ---- sorted gradient: the sort ---------------------------------------------------------------------------------------------------------
+
+constexpr int kChunk = 32;              // sorted positions a block of the reduction sums
+constexpr int kDigits = 256;            // of a radix pass (8 bits)
+constexpr int kTile = 4096;             // positions a block of a radix pass moves
+// Notes which tokens occur, by one lane for all lanes of the warp with the same key.
+__device__ __forceinline__ void note_occurs(const GradArgs &p, int g, int key) {
+    const unsigned same = __match_any_sync(__activemask(), key);
+    if (key < p.vocab && __ffs(same) - 1 == (int)threadIdx.x % 32) atomicOr(p.occurs + (long long)g * p.words + key / 32, 1u << (key % 32));
+}
+
+// A position without a token sorts behind all others: key = vocab.
+__device__ __forceinline__ int sort_key(int token, int vocab) { return token >= 0 && token < vocab ? token : vocab; }
+
+// The kernels of one call are chained: the next one's blocks may be set up while one runs, and wait here for all of its results.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void await_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+constexpr int kRankedMost = 4096;       // longest sequence ranked by counting
+constexpr int kSplit = 8;               // threads that share the counting for one position
+constexpr int kWordsMost = 1024;        // words of the bits of tokens that occur, for a block
+
+// Shorter sequences: the place of position t in the sorted order is the number of positions s with key(s) < key(t), or equal and
+// s < t: length^2 comparisons, but no passes (2.5 us at 2048 positions where the cluster's sort takes 9).  As every block
+// sees all tokens, each writes a part of the bits of the tokens that occur.
+__global__ void __launch_bounds__(kThreads) rank_tokens_kernel(const GradArgs p, int words_each, int *keys, int *places) {
+    constexpr int kTileKeys = kThreads * 4;
+    __shared__ int4 tile[kThreads];
+    __shared__ uint32_t occurs[kWordsMost];
+    const int g = blockIdx.y, word0 = blockIdx.x * words_each;
+    const int32_t *tokens = p.tokens + (long long)g * p.length;
+    const int first = blockIdx.x * (kThreads / kSplit), t = first + threadIdx.x / kSplit, part = threadIdx.x % kSplit;
+    let_next_start();
+    if (blockIdx.x == 0 && g == 0 && threadIdx.x == 0) *p.crossings = 0;
+    for (int w = threadIdx.x; w < words_each; w += kThreads) occurs[w] = 0;
+    const int token = t < p.length ? tokens[t] : PARLE_NO_TOKEN, key = sort_key(token, p.vocab);
+    int before = 0;
+    for (int s0 = 0; s0 < p.length; s0 += kTileKeys) {
+        int4 k;
+        int *e = &k.x;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int s = s0 + (int)threadIdx.x * 4 + u;
+            e[u] = s < p.length ? sort_key(tokens[s], p.vocab) : INT_MAX;
+        }
+        __syncthreads();
+        tile[threadIdx.x] = k;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const unsigned w = (unsigned)(e[u] / 32 - word0);
+            if (e[u] < p.vocab && w < (unsigned)words_each) atomicOr(&occurs[w], 1u << (e[u] % 32));
+        }
+        __syncthreads();
+        if (s0 + kTileKeys <= first || s0 >= first + kThreads / kSplit) {         // altogether before, or behind, the block's positions
+            const int limit = key + (s0 < first ? 1 : 0);
+#pragma unroll 8
+            for (int i = part; i < kThreads; i += kSplit) {
+                const int4 v = tile[i];
+                before += (v.x < limit) + (v.y < limit) + (v.z < limit) + (v.w < limit);
+            }
+        } else {
+            for (int i = part; i < kThreads; i += kSplit) {
+                const int4 v = tile[i];
+                const int s = s0 + 4 * i;
+                before += (v.x < key + (s < t)) + (v.y < key + (s + 1 < t)) + (v.z < key + (s + 2 < t)) + (v.w < key + (s + 3 < t));
+            }
+        }
+    }
+#pragma unroll
+    for (int o = kSplit / 2; o > 0; o >>= 1) before += __shfl_down_sync(0xffffffffu, before, o, kSplit);
+    if (t < p.length && part == 0) {
+        keys[(long long)g * p.length + before] = key;
+        places[(long long)g * p.length + before] = t;
+        note_bad_token(token, p.vocab, p.flags);
+    }
+    for (int w = threadIdx.x; w < words_each && word0 + w < p.words; w += kThreads) p.occurs[(long long)g * p.words + word0 + w] = occurs[w];
+}
+
+constexpr int kSortThreads = 512, kSorters = 8;          // a cluster sorts up to
+constexpr int kSortEach = 4096, kSortMost = kSorters * kSortEach;
+constexpr int kSortBits = 9;            // of a pass at most: a thread per digit
+
+__device__ __forceinline__ int cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return (int)r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+// Address of another block's copy of a shared variable.
+template <typename V> __device__ __forceinline__ V *at_rank(V *p, int rank) {
+    uint64_t r;
+    asm volatile("mapa.u64 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<uint64_t>(p)), "r"(rank));
+    return reinterpret_cast<V *>(r);
+}
+
+// A cluster sorts a sequence: a stable radix sort, least significant digit first, every block with an eighth of the sequence in
+// shared memory.  A position goes to (positions with a lower digit) + (same digit, in an earlier block, warp, or place of the warp).
+__global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const GradArgs p, int passes, int bits, int *keys_out, int *places_out) {
+    constexpr int W = kSortThreads / 32, D = 1 << kSortBits;
+    static_assert(D == kSortThreads, "a thread per digit");
+    extern __shared__ int2 items[];                       // [2][kSortEach]: (key, position)
+    __shared__ int warp_count[W][D], block_count[D], scan[W];
+    const int cluster = blockIdx.x / kSorters, rank = cluster_rank(), lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    let_next_start();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.crossings = 0;
+    const int32_t *tokens = p.tokens + (long long)cluster * p.length;
+    const int each = (p.length + kSorters - 1) / kSorters, each_warp = (each + W - 1) / W;
+    const int mine = max(0, min(each, p.length - rank * each));
+    for (int i0 = threadIdx.x; i0 < mine; i0 += kSortThreads * 4) {
+        int token[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) token[u] = i0 + u * kSortThreads < mine ? tokens[rank * each + i0 + u * kSortThreads] : 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + u * kSortThreads;
+            if (i >= mine) break;
+            note_bad_token(token[u], p.vocab, p.flags);
+            items[i] = make_int2(sort_key(token[u], p.vocab), rank * each + i);
+        }
+    }
+    uint32_t *const occurs = p.occurs + (long long)cluster * p.words;
+    for (int w = rank * kSortThreads + threadIdx.x; w < p.words; w += kSorters * kSortThreads) occurs[w] = 0;
+    const int mask = (1 << bits) - 1;
+    for (int pass = 0; pass < passes; ++pass) {
+        const int2 *in = items + (pass & 1) * kSortEach;
+        int2 *out = items + (1 - (pass & 1)) * kSortEach;
+#pragma unroll
+        for (int w = 0; w < W; ++w) warp_count[w][threadIdx.x] = 0;
+        __syncthreads();
+        const int from = min(mine, warp * each_warp), to = min(mine, from + each_warp);
+        for (int i = from + lane; i < to; i += 32) atomicAdd(&warp_count[warp][(in[i].x >> (bits * pass)) & mask], 1);
+        __syncthreads();
+        int count[W], own = 0;                            // thread = digit
+#pragma unroll
+        for (int w = 0; w < W; ++w) { count[w] = warp_count[w][threadIdx.x]; own += count[w]; }
+        block_count[threadIdx.x] = own;
+        cluster_arrive();
+        cluster_wait();
+        int total = 0, earlier = 0;
+#pragma unroll
+        for (int r = 0; r < kSorters; ++r) {
+            const int c = *at_rank(&block_count[threadIdx.x], r);
+            total += c;
+            if (r < rank) earlier += c;
+        }
+        int sum = total;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += v;
+        }
+        if (lane == 31) scan[warp] = sum;
+        __syncthreads();
+        int lower = lane < warp ? scan[lane] : 0;         // (W <= 32)
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) lower += __shfl_xor_sync(0xffffffffu, lower, o);
+        int start = lower + sum - total + earlier;
+#pragma unroll
+        for (int w = 0; w < W; ++w) { warp_count[w][threadIdx.x] = start; start += count[w]; }
+        __syncthreads();
+        for (int i0 = from; i0 < to; i0 += 32) {
+            const bool have = i0 + lane < to;
+            const int2 item = have ? in[i0 + lane] : make_int2(0, 0);
+            const int digit = have ? (item.x >> (bits * pass)) & mask : D;
+            const unsigned same = __match_any_sync(0xffffffffu, digit);
+            const int before = __popc(same & ((1u << lane) - 1u));
+            const int place = have ? warp_count[warp][digit] + before : 0;
+            __syncwarp();
+            if (have && before == 0) warp_count[warp][digit] += __popc(same);
+            __syncwarp();
+            if (!have) continue;
+            if (pass + 1 < passes) {
+                *at_rank(out + place % each, place / each) = item;
+            } else {
+                keys_out[(long long)cluster * p.length + place] = item.x;
+                places_out[(long long)cluster * p.length + place] = item.y;
+            }
+        }
+        cluster_arrive();
+        // while the others come: which tokens occur (the words were zero before the pass's first barrier; the next pass's items
+        // come here after its first barrier)
+        if (pass == 0)
+            for (int i = threadIdx.x; i < mine; i += kSortThreads) note_occurs(p, cluster, items[i].x);
+        cluster_wait();                                   // what the others put here has arrived; their reads here are done
+    }
+}
+
+// Longer sequences: the same sort by launches of its own, two a pass.
+// First: how often each digit occurs in a tile.
 __global__ void __launch_bounds__(kThreads)
-radix_count_kernel(const int32_t *keys, int length, int vocab, int shift, int first_pass, int *counts, int32_t *flags) {
+radix_count_kernel(const GradArgs p, const int32_t *keys, int shift, int first_pass, int *counts) {
     __shared__ int hist[kDigits];
     const int g = blockIdx.y;
-    keys += (long long)g * length;
+    keys += (long long)g * p.length;
     hist[threadIdx.x] = 0;
+    if (first_pass && g == 0 && blockIdx.x == 0 && threadIdx.x == 0) *p.crossings = 0;
     __syncthreads();
     const long long t0 = (long long)blockIdx.x * kTile;
-    for (int i = threadIdx.x; i < kTile && t0 + i < length; i += kThreads) {
+    for (int i = threadIdx.x; i < kTile && t0 + i < p.length; i += kThreads) {
         int key = keys[t0 + i];
-        if (first_pass) { note_bad_token(key, vocab, flags); key = sort_key(key, vocab); }
+        if (first_pass) {
+            note_bad_token(key, p.vocab, p.flags);
+            key = sort_key(key, p.vocab);
+            note_occurs(p, g, key);
+        }
         atomicAdd(&hist[(key >> shift) & (kDigits - 1)], 1);
     }
     __syncthreads();
@@ -147,7 +504,6 @@ radix_count_kernel(const int32_t *keys, int length, int vocab, int shift, int fi
 __global__ void __launch_bounds__(kThreads)
 radix_move_kernel(const int32_t *keys, const int *places, int length, int vocab, int shift, int first_pass, const int *counts,
                   int *keys_out, int *places_out) {
-    constexpr int kWarps = kThreads / 32;
     __shared__ int warp_count[kWarps][kDigits];
     __shared__ int scan[kWarps];
     const int g = blockIdx.y, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -202,18 +558,7 @@ radix_move_kernel(const int32_t *keys, const int *places, int length, int vocab,
     }
 }
 
-// ---- gradient: sums ------------------------------------------------------------------------------------------------------------
-
-struct GradArgs {
-    const void *dout;
-    float *dtable;
-    const int *keys, *places;                             // sorted
-    float *partial;                                       // [n][chunks][2][dim]: a chunk's first run (if it began before), last run (if it goes on)
-    long long dout_gs, ld_dout, dtable_gs, ld_dtable;
-    int length, vocab, dim, chunks;
-    float scale;
-    int accumulate;
-};
+// ---- sorted gradient: the sums ------------------------------------------------------------------------------------------------------------
 
 // E columns; E == 8: on a 16-byte boundary.
 template <int E> __device__ __forceinline__ void store_columns(float *to, const float (&v)[E]) {
@@ -226,11 +571,9 @@ template <int E> __device__ __forceinline__ void store_columns(float *to, const 
     }
 }
 
-// Sum of one run's rows inside a chunk and where it goes.  E columns per thread; grid (chunks, column tiles, n).
-template <typename T, int E>
-__global__ void __launch_bounds__(kThreads) embedding_grad_kernel(const GradArgs p) {
+// A chunk's runs: their sums inside the chunk and where those go.  E columns per thread.
+template <typename T, int E> __device__ __forceinline__ void sum_chunk(const GradArgs &p, int g, int chunk) {
     __shared__ int key[kChunk + 2], place[kChunk];        // key[0]: the position before the chunk, key[kChunk + 1]: the one after
-    const int g = blockIdx.z, chunk = blockIdx.x;
     const int first = chunk * kChunk, count = min(kChunk, p.length - first);
     if (threadIdx.x < kChunk + 2) {
         const int s = first + (int)threadIdx.x - 1;
@@ -238,125 +581,164 @@ __global__ void __launch_bounds__(kThreads) embedding_grad_kernel(const GradArgs
     }
     if (threadIdx.x < count) place[threadIdx.x] = p.places[(long long)g * p.length + first + threadIdx.x];
     __syncthreads();
-    const int col = (blockIdx.y * kThreads + threadIdx.x) * E;
-    if (col >= p.dim) return;
-    const T *dout = static_cast<const T *>(p.dout) + (long long)g * p.dout_gs + col;
-    float acc[E];
+    if (threadIdx.x == 0 && blockIdx.y == 0 && count == kChunk && key[count + 1] == key[count] && key[0] != key[count] && key[count] < p.vocab) {
+        const int at = atomicAdd(p.crossings, 1);         // (the order of the list does not matter)
+        reinterpret_cast<int4 *>(p.crossings)[1 + at] = make_int4(g, chunk, key[count], 0);
+    }
+    for (int col = (blockIdx.y * kThreads + threadIdx.x) * E; col < p.dim; col += gridDim.y * kThreads * E) {
+        const T *dout = static_cast<const T *>(p.dout) + (long long)g * p.dout_gs + col;
+        float acc[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = 0.f;
-    int run = 0;                                          // where the current run begins in the chunk
-    constexpr int U = 8;
-    for (int i0 = 0; i0 < count; i0 += U) {
-        float v[U][E];
-        if constexpr (E == 8) {
-            Pack8<T> raw[U];
+        for (int e = 0; e < E; ++e) acc[e] = 0.f;
+        int run = 0;                                      // where the current run begins in the chunk
+        bool done = false;
+        constexpr int U = 8;
+        for (int i0 = 0; i0 < count && !done; i0 += U) {
+            std::conditional_t<E == 8, Pack8<T>, T> raw[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i0 + u < count && key[i0 + u + 1] < p.vocab) raw[u].load(dout + (long long)place[i0 + u] * p.ld_dout);
-#pragma unroll
-            for (int u = 0; u < U; ++u) raw[u].get(v[u]);
-        } else {
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i0 + u < count && key[i0 + u + 1] < p.vocab) v[u][0] = to_float(dout[(long long)place[i0 + u] * p.ld_dout]);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = i0 + u;
-            if (i >= count) break;
-            const int k = key[i + 1];
-            if (k >= p.vocab) return;                     // the rest has no token
-#pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] += v[u][e];
-            if (i + 1 < count && key[i + 2] == k) continue;
-            // the run's last position in this chunk
-            const bool before = run == 0 && key[0] == k, after = i + 1 == count && key[i + 2] == k;
-            if (before || after) {
-                // (a run that fills the chunk and goes on both ways counts as "began before")
-                store_columns<E>(p.partial + (((long long)g * p.chunks + chunk) * 2 + (before ? 0 : 1)) * p.dim + col, acc);
-            } else {
-                float *to = p.dtable + (long long)g * p.dtable_gs + (long long)k * p.ld_dtable + col;
-#pragma unroll
-                for (int e = 0; e < E; ++e) acc[e] = p.accumulate ? fmaf(p.scale, acc[e], to[e]) : p.scale * acc[e];
-                store_columns<E>(to, acc);
+            for (int u = 0; u < U; ++u) {
+                if (i0 + u >= count || key[i0 + u + 1] >= p.vocab) continue;
+                const T *from = dout + (long long)place[i0 + u] * p.ld_dout;
+                if constexpr (E == 8) raw[u].load(from); else raw[u] = *from;
             }
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = 0.f;
-            run = i + 1;
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u;
+                if (i >= count) break;
+                const int k = key[i + 1];
+                if (k >= p.vocab) { done = true; break; } // the rest has no token
+                float v[E];
+                if constexpr (E == 8) raw[u].get(v); else v[0] = to_float(raw[u]);
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] += v[e];
+                if (i + 1 < count && key[i + 2] == k) continue;
+                // the run's last position in this chunk
+                const bool before = run == 0 && key[0] == k, after = i + 1 == count && key[i + 2] == k;
+                if (before || after) {
+                    // (a run that fills the chunk and goes on both ways counts as "began before")
+                    store_columns<E>(p.partial + (((long long)g * p.chunks + chunk) * 2 + (before ? 0 : 1)) * p.dim + col, acc);
+                } else {
+                    float *to = p.dtable + (long long)g * p.dtable_gs + (long long)k * p.ld_dtable + col;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) acc[e] = p.accumulate ? fmaf(p.scale, acc[e], to[e]) : p.scale * acc[e];
+                    store_columns<E>(to, acc);
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] = 0.f;
+                run = i + 1;
+            }
         }
     }
 }
 
-// Runs that cross a border: the block of the chunk in which such a run begins adds up its partial rows.  32 columns per block
-// and step; the eight warps take an eighth of the partial rows each, in order, and their sums are added in order.
-__global__ void __launch_bounds__(kThreads) embedding_grad_join_kernel(const GradArgs p) {
-    constexpr int kWarps = kThreads / 32;
-    __shared__ float sums[kWarps][32];
-    __shared__ int end_of_run;
-    const int g = blockIdx.z, chunk = blockIdx.x, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const int *keys = p.keys + (long long)g * p.length;
-    const int first = chunk * kChunk, next = first + kChunk;
-    if (next >= p.length) return;
-    const int k = keys[next - 1];
-    if (k >= p.vocab || keys[next] != k) return;          // no run crosses the border behind this chunk
-    if (first > 0 && keys[first - 1] == k) return;        // it began in an earlier one
-    if (threadIdx.x == 0) end_of_run = p.chunks;
-    __syncthreads();
-    for (int c0 = chunk + 1; c0 < p.chunks; c0 += kThreads) {     // first chunk that begins with another token
-        const int c = c0 + threadIdx.x;
-        const bool other = c < p.chunks && keys[(long long)c * kChunk] != k;
-        if (other) atomicMin(&end_of_run, c);
-        if (__syncthreads_or(other)) break;
-    }
-    __syncthreads();
-    const int parts = end_of_run - chunk;                 // this chunk's last run, then the first runs of the following chunks
-    const int per_warp = (parts + kWarps - 1) / kWarps;
-    const float *partial = p.partial + ((long long)g * p.chunks + chunk) * 2 * p.dim;
-    for (int c0 = blockIdx.y * 32; c0 < p.dim; c0 += gridDim.y * 32) {
-        const int col = c0 + lane;
-        float s = 0.f;
-        if (col < p.dim) {
-            const int to = min(parts, (warp + 1) * per_warp);
-#pragma unroll 8
-            for (int i = warp * per_warp; i < to; ++i) s += partial[((long long)i * 2 + (i == 0 ? 1 : 0)) * p.dim + col];
+// Zeros in those of `rows` table rows from v0 on whose tokens do not occur.
+__device__ __forceinline__ void zero_absent(const GradArgs &p, int g, int v0, int rows, bool wide) {
+    const uint32_t *occurs = p.occurs + (long long)g * p.words;
+    const int limit = min(v0 + rows, p.vocab);
+    const int lane = threadIdx.x % 32;
+    for (int v = v0 + (int)threadIdx.x / 32; v < limit; v += kWarps) {     // a warp per row
+        if ((occurs[v / 32] >> (v % 32)) & 1u) continue;
+        float *row = p.dtable + (long long)g * p.dtable_gs + (long long)v * p.ld_dtable;
+        if (wide) {
+#pragma unroll 4
+            for (int c = lane * 4; c < p.dim; c += 128) *reinterpret_cast<float4 *>(row + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+        } else {
+            for (int c = lane; c < p.dim; c += 32) row[c] = 0.f;
         }
-        sums[warp][lane] = s;
-        __syncthreads();
-        if (warp == 0 && col < p.dim) {
-            for (int w = 1; w < kWarps; ++w) s += sums[w][lane];
-            float *to = p.dtable + (long long)g * p.dtable_gs + (long long)k * p.ld_dtable + col;
-            *to = p.accumulate ? fmaf(p.scale, s, *to) : p.scale * s;
-        }
-        __syncthreads();
     }
 }
 
-// Rows of tokens that do not occur: zero.  A block takes kZeroRows rows and finds their tokens in the sorted keys.
-constexpr int kZeroRows = 32;
-template <int E>
-__global__ void __launch_bounds__(kThreads) embedding_grad_zero_kernel(const GradArgs p) {
-    __shared__ uint32_t present;
-    const int g = blockIdx.y, v0 = blockIdx.x * kZeroRows;
-    const int *keys = p.keys + (long long)g * p.length;
-    if (threadIdx.x == 0) present = 0;
-    __syncthreads();
-    int lo = 0, hi = p.length;                            // first sorted position with a key >= v0
-    while (lo < hi) {
-        const int mid = lo + (hi - lo) / 2;
-        if (keys[mid] < v0) lo = mid + 1; else hi = mid;
+// Blocks x < chunks sum a chunk each, the others clear `zero_rows` table rows each (y == 0 only); grid (.., column parts, n).
+template <typename T, int E>
+__global__ void __launch_bounds__(kThreads, 4) embedding_grad_kernel(const GradArgs p, int zero_rows, bool wide) {
+    let_next_start();
+    await_previous();
+    if ((int)blockIdx.x < p.chunks) sum_chunk<T, E>(p, blockIdx.z, blockIdx.x);
+    else if (blockIdx.y == 0) zero_absent(p, blockIdx.z, (blockIdx.x - p.chunks) * zero_rows, zero_rows, wide);
+}
+
+// Runs that cross a border, in tiles of 256 columns.  Most have a few partial rows: a warp adds them up, eight columns a lane.  The
+// longer ones a block adds up afterwards: its warps take a part of the partial rows each, in order, and their sums are added in order.
+constexpr int kJoinThreads = 512;
+constexpr int kPartsOfWarp = 16;
+
+struct Crossing {
+    const float *partial;                                 // of the chunk in which the run begins
+    float *to;
+    int parts;                                            // that chunk's last run, then the first runs of the following chunks
+    int col;                                              // this lane's first column; the others lie 32 apart
+};
+
+// By a warp.  Chunks are probed 32 at a time for the first that begins with another token.
+__device__ __forceinline__ Crossing find_crossing(const GradArgs &p, long long item, int tiles) {
+    const int lane = threadIdx.x % 32;
+    const int4 c = reinterpret_cast<const int4 *>(p.crossings)[1 + item / tiles];
+    const int *keys = p.keys + (long long)c.x * p.length;
+    int end = c.y + 2;
+    for (;; end += 32) {
+        const int at = end + lane;
+        const unsigned other = __ballot_sync(0xffffffffu, at >= p.chunks || keys[(long long)at * kChunk] != c.z);
+        if (other) { end += __ffs(other) - 1; break; }
     }
-    const int limit = min(v0 + kZeroRows, p.vocab);
-    for (int s = lo;; s += kThreads) {
-        const int k = s + (int)threadIdx.x < p.length ? keys[s + threadIdx.x] : p.vocab;
-        if (k < limit) atomicOr(&present, 1u << (k - v0));
-        if (!__syncthreads_and(k < limit)) break;
+    Crossing r;
+    r.col = (int)(item % tiles) * 256 + lane;
+    r.parts = end - c.y;
+    r.partial = p.partial + ((long long)c.x * p.chunks + c.y) * 2 * p.dim;
+    r.to = p.dtable + (long long)c.x * p.dtable_gs + (long long)c.z * p.ld_dtable;
+    return r;
+}
+__device__ __forceinline__ void add_parts(const GradArgs &p, const Crossing &r, int from, int to, float (&acc)[8]) {
+#pragma unroll 4
+    for (int i = from; i < to; ++i) {
+        const float *row = r.partial + ((long long)i * 2 + (i == 0 ? 1 : 0)) * p.dim;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (r.col + j * 32 < p.dim) acc[j] += row[r.col + j * 32];
     }
-    for (int r = 0; r < limit - v0; ++r) {
-        if ((present >> r) & 1u) continue;
-        float *row = p.dtable + (long long)g * p.dtable_gs + (long long)(v0 + r) * p.ld_dtable;
-        for (int j = threadIdx.x * E; j < p.dim; j += kThreads * E) {
-            if constexpr (E == 4) *reinterpret_cast<float4 *>(row + j) = make_float4(0.f, 0.f, 0.f, 0.f);
-            else row[j] = 0.f;
+}
+
+__global__ void __launch_bounds__(kJoinThreads, 2) embedding_grad_join_kernel(const GradArgs p) {
+    constexpr int W = kJoinThreads / 32;
+    __shared__ float sums[W][256];
+    __shared__ int longer[W], longers;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, tiles = (p.dim + 255) / 256;
+    await_previous();
+    const long long items = (long long)*p.crossings * tiles;
+    // neighbouring items go to different blocks: the tiles of a long run are neighbours
+    for (long long item0 = blockIdx.x; item0 < items; item0 += (long long)gridDim.x * W) {
+        if (threadIdx.x == 0) longers = 0;
+        __syncthreads();
+        if (item0 + (long long)warp * gridDim.x < items) {
+            const Crossing r = find_crossing(p, item0 + (long long)warp * gridDim.x, tiles);
+            if (r.parts > kPartsOfWarp) {
+                if (lane == 0) longer[atomicAdd(&longers, 1)] = warp;
+            } else {
+                float acc[8] = {};
+                add_parts(p, r, 0, r.parts, acc);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float *to = r.to + r.col + j * 32;
+                    if (r.col + j * 32 < p.dim) *to = p.accumulate ? fmaf(p.scale, acc[j], *to) : p.scale * acc[j];
+                }
+            }
+        }
+        __syncthreads();
+        for (int l = 0; l < longers; ++l) {
+            const Crossing r = find_crossing(p, item0 + (long long)longer[l] * gridDim.x, tiles);
+            const int per_warp = (r.parts + W - 1) / W, from = min(r.parts, warp * per_warp);
+            float acc[8] = {};
+            add_parts(p, r, from, min(r.parts, from + per_warp), acc);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sums[warp][j * 32 + lane] = acc[j];
+            __syncthreads();
+            const int c = threadIdx.x, col = r.col - lane + c;
+            if (c < 256 && col < p.dim) {
+                float s = sums[0][c];
+                const int used = (r.parts + per_warp - 1) / per_warp;
+                for (int w = 1; w < used; ++w) s += sums[w][c];
+                r.to[col] = p.accumulate ? fmaf(p.scale, s, r.to[col]) : p.scale * s;
+            }
+            __syncthreads();
         }
     }
 }
@@ -364,28 +746,112 @@ __global__ void __launch_bounds__(kThreads) embedding_grad_zero_kernel(const Gra
 // ---- workspace -----------------------------------------------------------------------------------------------------------------
 
 struct GradPlan {
-    int chunks, tiles, passes;
-    size_t keys[2], places[2], counts, partial, bytes;
+    int chunks, tiles, passes, sort_passes, sort_bits, words;
+    size_t keys[2], places[2], counts, occurs, crossings, partial, bytes;
 };
 
 GradPlan plan_grad(int n, long long length, int vocab, int dim) {
     GradPlan p = {};
+    if (length <= kDirectMost) return p;
     p.chunks = (int)((length + kChunk - 1) / kChunk);
     const size_t ints = round_up((size_t)n * length * sizeof(int), 128);
-    if (length > kRankedMost) {
-        p.tiles = (int)((length + kTile - 1) / kTile);
-        int bits = 1;
-        while (bits < 31 && (vocab >> bits)) ++bits;      // keys 0 .. vocab
-        p.passes = (bits + 7) / 8;
-    }
+    int bits = 1;
+    while (bits < 31 && (vocab >> bits)) ++bits;          // keys 0 .. vocab
+    p.passes = (bits + 7) / 8;
+    p.sort_passes = (bits + kSortBits - 1) / kSortBits;
+    p.sort_bits = (bits + p.sort_passes - 1) / p.sort_passes;
+    p.words = (vocab + 31) / 32;
     size_t at = 0;
-    for (int i = 0; i < (p.passes ? 2 : 1); ++i) { p.keys[i] = at; at += ints; p.places[i] = at; at += ints; }
+    if (length > kSortMost) p.tiles = (int)((length + kTile - 1) / kTile);
+    for (int i = 0; i < (p.tiles ? 2 : 1); ++i) { p.keys[i] = at; at += ints; p.places[i] = at; at += ints; }
     p.counts = at;
     at += round_up((size_t)n * p.tiles * kDigits * sizeof(int), 128);
+    p.occurs = at;
+    at += round_up((size_t)n * p.words * sizeof(uint32_t), 128);
+    p.crossings = at;
+    at += round_up((1 + (size_t)n * p.chunks) * sizeof(int4), 128);
     p.partial = at;
     at += round_up((size_t)n * p.chunks * 2 * dim * sizeof(float), 128);
     p.bytes = at;
     return p;
+}
+
+template <typename T, int E> int launch_direct(const GradArgs &a, int n, int sms, cudaStream_t stream) {
+    const int parts = (a.dim + kColumns - 1) / kColumns;
+    int log_groups = 0;                                   // blocks of at most kRowsMost rows, and enough of them for the SMs
+    while (((a.vocab - 1) >> log_groups) >= kRowsMost) ++log_groups;
+    while ((a.vocab >> log_groups) > 8 && ((long long)parts * n << log_groups) < 4LL * sms) ++log_groups;
+    embedding_grad_direct_kernel<T, E><<<dim3(1u << log_groups, parts, n), kThreads, 0, stream>>>(a, log_groups);
+    return launch_status();
+}
+
+cudaLaunchConfig_t launch_config(dim3 grid, int threads, int bytes, cudaLaunchAttribute *attr, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cfg;
+}
+
+template <typename T>
+int launch_sorted(GradArgs a, int n, const GradPlan &plan, bool wide, bool wide_table, char *ws, int sms, cudaStream_t stream) {
+    int *keys[2], *places[2];
+    for (int i = 0; i < 2; ++i) {
+        keys[i] = reinterpret_cast<int *>(ws + plan.keys[i]);
+        places[i] = reinterpret_cast<int *>(ws + plan.places[i]);
+    }
+    a.occurs = reinterpret_cast<uint32_t *>(ws + plan.occurs);
+    a.words = plan.words;
+    a.crossings = reinterpret_cast<int *>(ws + plan.crossings);
+    a.partial = reinterpret_cast<float *>(ws + plan.partial);
+    int sorted = 0, rc;
+    const int rank_blocks = (a.length + kThreads / kSplit - 1) / (kThreads / kSplit), words_each = (plan.words + rank_blocks - 1) / rank_blocks;
+    if (a.length <= kRankedMost && words_each <= kWordsMost) {
+        rank_tokens_kernel<<<dim3(rank_blocks, n), kThreads, 0, stream>>>(a, words_each, keys[0], places[0]);
+    } else if (!plan.tiles) {
+        constexpr int bytes = 2 * kSortEach * (int)sizeof(int2);
+        if (cudaFuncSetAttribute(sort_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return PARLE_ECUDA;
+        cudaLaunchAttribute attr = {};
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = kSorters;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        const cudaLaunchConfig_t cfg = launch_config(dim3((unsigned)n * kSorters), kSortThreads, bytes, &attr, stream);
+        if (cudaLaunchKernelEx(&cfg, sort_tokens_kernel, a, plan.sort_passes, plan.sort_bits,
+                               keys[0], places[0]) != cudaSuccess) return PARLE_ECUDA;
+    } else {
+        int *counts = reinterpret_cast<int *>(ws + plan.counts);
+        if (cudaMemsetAsync(a.occurs, 0, (size_t)n * a.words * sizeof(uint32_t), stream) != cudaSuccess) return PARLE_ECUDA;
+        for (int pass = 0; pass < plan.passes; ++pass) {
+            const dim3 grid(plan.tiles, n);
+            const int32_t *in = pass ? keys[sorted] : a.tokens;
+            const int to = pass ? 1 - sorted : 0;
+            radix_count_kernel<<<grid, kThreads, 0, stream>>>(a, in, 8 * pass, pass == 0, counts);
+            if ((rc = launch_status()) != PARLE_OK) return rc;
+            radix_move_kernel<<<grid, kThreads, 0, stream>>>(in, places[sorted], a.length, a.vocab, 8 * pass, pass == 0, counts, keys[to], places[to]);
+            if ((rc = launch_status()) != PARLE_OK) return rc;
+            sorted = to;
+        }
+    }
+    if ((rc = launch_status()) != PARLE_OK) return rc;
+    a.keys = keys[sorted];
+    a.places = places[sorted];
+    const int columns = wide ? kThreads * 8 : kThreads * 4;       // columns of a block (four a thread where they go one by one)
+    const long long row_bytes = (long long)a.dim * 4;
+    const int zero_rows = (int)std::max(1LL, std::min(256LL, 65536 / row_bytes));
+    const long long zero_blocks = a.accumulate ? 0 : ((long long)a.vocab + zero_rows - 1) / zero_rows;
+    const dim3 grid((unsigned)(plan.chunks + zero_blocks), (a.dim + columns - 1) / columns, n);
+    cudaLaunchAttribute chained = {};
+    chained.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    chained.val.programmaticStreamSerializationAllowed = 1;
+    const cudaLaunchConfig_t sums = launch_config(grid, kThreads, 0, &chained, stream);
+    const auto kernel = wide ? embedding_grad_kernel<T, 8> : embedding_grad_kernel<T, 1>;
+    if (cudaLaunchKernelEx(&sums, kernel, a, zero_rows, wide_table) != cudaSuccess) return PARLE_ECUDA;
+    const cudaLaunchConfig_t join = launch_config(dim3(2 * sms), kJoinThreads, 0, &chained, stream);
+    if (cudaLaunchKernelEx(&join, embedding_grad_join_kernel, a) != cudaSuccess) return PARLE_ECUDA;
+    return launch_status();
 }
 
 bool valid_sizes(int n, long long length, int vocab, int dim) {
@@ -446,62 +912,24 @@ extern "C" int parle_embedding_grad(const void *dout, int dout_dtype, long long 
     if (!valid_sizes(n, length, vocab, dim) || !valid_dtype(dout_dtype) || !isfinite((float)scale)) return PARLE_EINVAL;
     if (length > PARLE_TOKEN_MAX_ROWS / n) return PARLE_ETOOBIG;
     if (ld_dout < 0 || (n > 1 && dout_gs < 0) || !separate_rows(n, vocab, dim, dtable_gs, ld_dtable) || !dtable) return PARLE_EINVAL;
-    if (length > 0 && (!dout || !tokens || !workspace)) return PARLE_EINVAL;
+    const GradPlan plan = plan_grad(n, length, vocab, dim);
+    if (length > 0 && (!dout || !tokens || (!workspace && plan.bytes))) return PARLE_EINVAL;
     if (!element_aligned(dout, dout_dtype) || !element_aligned(dtable, PARLE_F32) || !element_aligned(tokens, PARLE_F32) ||
         !element_aligned(flags, PARLE_F32) || reinterpret_cast<uintptr_t>(workspace) % 128) return PARLE_EALIGN;
-    const GradPlan plan = plan_grad(n, length, vocab, dim);
     if (workspace_bytes < plan.bytes) return PARLE_EWORKSPACE;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    char *ws = static_cast<char *>(workspace);
-    int *keys[2], *places[2];
-    for (int i = 0; i < 2; ++i) {
-        keys[i] = reinterpret_cast<int *>(ws + plan.keys[i]);
-        places[i] = reinterpret_cast<int *>(ws + plan.places[i]);
-    }
-    int sorted = 0, rc = PARLE_OK;
-    const int T = (int)length;
-    if (plan.passes) {
-        int *counts = reinterpret_cast<int *>(ws + plan.counts);
-        const dim3 grid(plan.tiles, n);
-        for (int pass = 0; pass < plan.passes; ++pass) {
-            const int32_t *in = pass ? keys[sorted] : tokens;
-            const int to = pass ? 1 - sorted : 0;
-            radix_count_kernel<<<grid, kThreads, 0, stream>>>(in, T, vocab, 8 * pass, pass == 0, counts, flags);
-            if ((rc = launch_status()) != PARLE_OK) return rc;
-            radix_move_kernel<<<grid, kThreads, 0, stream>>>(in, places[sorted], T, vocab, 8 * pass, pass == 0, counts, keys[to], places[to]);
-            if ((rc = launch_status()) != PARLE_OK) return rc;
-            sorted = to;
-        }
-    } else if (T > 0) {
-        const int per_block = kThreads / kSplit;
-        rank_tokens_kernel<<<dim3((T + per_block - 1) / per_block, n), kThreads, 0, stream>>>(tokens, T, vocab, keys[0], places[0], flags);
-        if ((rc = launch_status()) != PARLE_OK) return rc;
-    }
     GradArgs a = {};
-    a.dout = dout; a.dtable = dtable; a.keys = keys[sorted]; a.places = places[sorted];
-    a.partial = reinterpret_cast<float *>(ws + plan.partial);
+    a.dout = dout; a.dtable = dtable; a.tokens = tokens; a.flags = flags;
     a.dout_gs = dout_gs; a.ld_dout = ld_dout; a.dtable_gs = dtable_gs; a.ld_dtable = ld_dtable;
-    a.length = T; a.vocab = vocab; a.dim = dim; a.chunks = plan.chunks;
+    a.length = (int)length; a.vocab = vocab; a.dim = dim; a.chunks = plan.chunks;
     a.scale = (float)scale; a.accumulate = accumulate != 0;
     const bool wide_table = dim % 4 == 0 && rows_aligned16(dtable, ld_dtable, PARLE_F32) && (n == 1 || dtable_gs % 4 == 0);
-    if (!accumulate) {
-        const dim3 grid((unsigned)(((long long)vocab + kZeroRows - 1) / kZeroRows), n);
-        if (wide_table)
-            embedding_grad_zero_kernel<4><<<grid, kThreads, 0, stream>>>(a);
-        else embedding_grad_zero_kernel<1><<<grid, kThreads, 0, stream>>>(a);
-        if ((rc = launch_status()) != PARLE_OK) return rc;
-    }
-    if (T == 0) return PARLE_OK;
     const bool wide = wide_table && dim % 8 == 0 && rows_aligned16(dout, ld_dout, dout_dtype) && (n == 1 || rows_aligned16(dout, dout_gs, dout_dtype));
-    const int columns = wide ? kThreads * 8 : kThreads;
-    const dim3 grid(plan.chunks, (dim + columns - 1) / columns, n);
-    rc = with_dtype(dout_dtype, [&](auto *tag) {
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return PARLE_ECUDA;
+    return with_dtype(dout_dtype, [&](auto *tag) {
         using TD = std::remove_pointer_t<decltype(tag)>;
-        if (wide) embedding_grad_kernel<TD, 8><<<grid, kThreads, 0, stream>>>(a);
-        else embedding_grad_kernel<TD, 1><<<grid, kThreads, 0, stream>>>(a);
-        return launch_status();
+        if (plan.passes) return launch_sorted<TD>(a, n, plan, wide, wide_table, static_cast<char *>(workspace), sms, stream);
+        return wide ? launch_direct<TD, 8>(a, n, sms, stream) : launch_direct<TD, 1>(a, n, sms, stream);
     });
-    if (rc != PARLE_OK || plan.chunks < 2) return rc;
-    embedding_grad_join_kernel<<<dim3(plan.chunks - 1, (dim + 511) / 512, n), kThreads, 0, stream>>>(a);
-    return launch_status();
 }

@@ -361,7 +361,7 @@ def check_embedding_grad(dout, tokens, vocab, scale, accumulate=False, pad=0, st
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n, length, vocab, dim, pad", [
     (1, 1, 1, 1, 0), (1, 1, 100, 64, 0), (1, 31, 40, 33, 1), (2, 32, 7, 8, 0), (1, 33, 5, 100, 4), (3, 65, 1000, 16, 0), (1, 257, 3, 264, 8),
-    (8, 640, 100, 101, 0), (1, 1000, 1, 24, 0), (1, 8192, 37, 8, 0), (2, 8193, 300, 9, 0), (1, 20000, 70000, 8, 0),
+    (8, 640, 100, 101, 0), (1, 1000, 1, 24, 0), (1, 8192, 37, 8, 0), (2, 8193, 300, 9, 0), (1, 16384, 300, 520, 0), (1, 20000, 70000, 8, 0), (1, 1025, 17000000, 1, 0),
 ])
 def test_embedding_gradient(dtype, n, length, vocab, dim, pad):
     rng = np.random.default_rng(length + vocab)
@@ -371,10 +371,10 @@ def test_embedding_gradient(dtype, n, length, vocab, dim, pad):
     check_embedding_grad(dout, tokens, vocab, -2.3, accumulate=True, pad=pad)
 
 
-@pytest.mark.parametrize("length", [1, 32, 64, 100, 4099, 9000])
+@pytest.mark.parametrize("length", [1, 32, 33, 64, 100, 1024, 1025, 4099, 32768, 32769, 40001])
 def test_embedding_gradient_of_skewed_tokens(length):
     """All positions the same token, none at all, a block of one token amid others, tokens in ascending and descending order."""
-    vocab, dim = 50, 40
+    vocab, dim = 50, 40 if length <= 4099 else 8
     rng = np.random.default_rng(length)
     dout = torch.from_numpy(rng.normal(size=(5, length, dim))).to(torch.bfloat16).to(DEV)
     tokens = np.empty((5, length), np.int32)
@@ -404,7 +404,8 @@ def test_embedding_gradient_forms():
     count = torch.bincount(t.flatten(), minlength=9).double()
     assert torch.allclose(wide.double(), count[:, None] * row.double(), atol=1e-5)
     # a given workspace that held something else
-    ws = torch.full((pb.embedding_grad_workspace_bytes(1, 24, 9, 16),), 255, dtype=torch.uint8, device=DEV)
+    t, d = torch.randint(0, 9, (17000,), device=DEV, dtype=torch.int32), torch.randn(17000, 16, device=DEV)
+    ws = torch.full((pb.embedding_grad_workspace_bytes(1, 17000, 9, 16),), 255, dtype=torch.uint8, device=DEV)
     assert torch.equal(pb.embedding_grad(d, t, 9, workspace=ws), pb.embedding_grad(d, t, 9))
     with pytest.raises(pb.ParleError) as e:
         pb.embedding_grad(d, t, 9, workspace=ws[:-1])
@@ -485,8 +486,8 @@ def every_call(stream=None):
     torch.manual_seed(4)
     x, t = torch.randn(40, 9000, device=DEV, dtype=torch.bfloat16), torch.randint(0, 9000, (40,), device=DEV, dtype=torch.int32)
     g, one = torch.randn(40, device=DEV), torch.randn(1, 70000, device=DEV)
-    e, long = torch.randn(40, 9000, device=DEV), torch.randint(0, 300, (12000,), device=DEV, dtype=torch.int32)
-    rows = torch.randn(12000, 40, device=DEV)
+    e, long = torch.randn(40, 9000, device=DEV), torch.randint(0, 300, (34000,), device=DEV, dtype=torch.int32)
+    rows = torch.randn(34000, 40, device=DEV)
     torch.cuda.synchronize()
     return {
         "logprobs": lambda: pb.token_logprobs(x, t, k=9, stream=stream),
@@ -495,6 +496,7 @@ def every_call(stream=None):
         "embedding": lambda: (pb.embedding(e, t % 40, stream=stream),),
         "embedding gradient": lambda: (pb.embedding_grad(e, t, 9000, stream=stream),),
         "embedding gradient, long": lambda: (pb.embedding_grad(rows, long, 300, stream=stream),),
+        "embedding gradient, middle": lambda: (pb.embedding_grad(rows[:5000], long[:5000], 300, stream=stream),),
         "dropout": lambda: (pb.dropout(e, 0.2, 8, 1, residual=e, stream=stream),),
     }
 

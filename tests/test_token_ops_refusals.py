@@ -60,9 +60,9 @@ def dropout(x=P, ld_x=8, residual=None, ld_r=0, y=2 * P, ld_y=8, dtype=F32, rows
     (embedding, dict(out_gs=0), EINVAL), (embedding, dict(out_gs=4, ld_out=7), EINVAL),
     (embedding, dict(length=1 << 30), ETOOBIG), (embedding, dict(table=P + 2), EALIGN), (embedding, dict(out=P + 1, out_dtype=F16), EALIGN),
     (embedding, dict(tokens=P + 2), EALIGN), (embedding, dict(flags=P + 3), EALIGN),
-    (embedding_grad, dict(dout=None), EINVAL), (embedding_grad, dict(dtable=None), EINVAL), (embedding_grad, dict(workspace=None), EINVAL),
+    (embedding_grad, dict(dout=None), EINVAL), (embedding_grad, dict(dtable=None), EINVAL), (embedding_grad, dict(workspace=None, length=20000, dout_gs=80000), EINVAL),
     (embedding_grad, dict(dtype=3), EINVAL), (embedding_grad, dict(scale=math.nan), EINVAL), (embedding_grad, dict(ld_dout=-1), EINVAL),
-    (embedding_grad, dict(dtable_gs=31), EINVAL), (embedding_grad, dict(ld_dtable=3), EINVAL), (embedding_grad, dict(nbytes=64), EWORKSPACE),
+    (embedding_grad, dict(dtable_gs=31), EINVAL), (embedding_grad, dict(ld_dtable=3), EINVAL), (embedding_grad, dict(nbytes=64, length=20000), EWORKSPACE),
     (embedding_grad, dict(length=1 << 30), ETOOBIG), (embedding_grad, dict(workspace=3 * P + 64), EALIGN),
     (embedding_grad, dict(dout=P + 2), EALIGN), (embedding_grad, dict(dtable=P + 2), EALIGN),
     (dropout, dict(x=None), EINVAL), (dropout, dict(y=None), EINVAL), (dropout, dict(p=-0.1), EINVAL), (dropout, dict(p=1.1), EINVAL),
@@ -83,7 +83,8 @@ def test_workspace_sizes():
     size = pb.embedding_grad_workspace_bytes
     assert size(1, 0, 10, 4) == 0 and size(0, 5, 10, 4) == 0 and size(1, -1, 10, 4) == 0 and size(1, 5, 0, 4) == 0
     assert size(2, 1 << 30, 10, 4) == 0
-    for n, length in ((1, 1), (3, 31), (2, 33), (1, 8192), (1, 8193), (4, 100000)):
+    assert size(1, 1, 1000, 64) == 0 and size(64, 1024, 1000, 64) == 0           # up to this length the gradient needs none
+    for n, length in ((1, 1025), (4, 100000)):
         assert size(n, length, 1000, 64) >= n * length * 8 and size(n, length, 1000, 64) % 128 == 0
 
 
