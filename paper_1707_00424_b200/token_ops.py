@@ -14,10 +14,19 @@ NO_TOKEN = -1
 TOP_MAX = 32
 _EINVAL = -1
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_FLOAT, _INT, _INTS, _LONGS = torch.float32, torch.int32, (torch.int32,), (torch.int64, torch.uint64)
 
 
 def _refuse(call: str, why: str):
     raise ParleError(_EINVAL, f"{call}: {why}")
+
+
+def _device_of(call: str, t) -> int:
+    """Index of the tensor's CUDA device."""
+    index = t.get_device()
+    if index < 0:
+        _refuse(call, f"a tensor is on {t.device}: a CUDA device is needed")
+    return index
 
 
 def _dtype(call: str, name: str, t) -> int:
@@ -27,80 +36,93 @@ def _dtype(call: str, name: str, t) -> int:
     return d
 
 
-def _on(call: str, device, **tensors):
-    """Every given tensor is on the CUDA device `device`."""
-    if device.type != "cuda":
-        _refuse(call, f"the tensors are on {device}: a CUDA device is needed")
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            _refuse(call, f"{name} is on {t.device}, the others on {device}")
-
-
-def _dense(call: str, name: str, t, shape, dtype):
-    """A contiguous tensor of this shape and type."""
-    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+def _dense(call: str, name: str, t, shape, dtype, index: int) -> int:
+    """Address of a contiguous tensor of this shape and type on this device."""
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
         _refuse(call, f"{name} has to be a contiguous {dtype} tensor of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+    if t.get_device() != index:
+        _refuse(call, f"{name} is on {t.device}, the other tensors on cuda:{index}")
+    return t.data_ptr()
 
 
-def _flags(call: str, flags):
-    if flags is not None and (flags.numel() != 1 or flags.dtype != torch.int32):
-        _refuse(call, "flags has to be one int32")
+def _word(call: str, name: str, t, dtypes, index: int) -> int:
+    """Address of a tensor of one element, 0 for None."""
+    if t is None:
+        return 0
+    if t.numel() != 1 or t.dtype not in dtypes or t.get_device() != index:
+        _refuse(call, f"{name} has to be one element of {' or '.join(map(str, dtypes))} on cuda:{index}")
+    return t.data_ptr()
 
 
-def _groups(call: str, name: str, t, *shape):
-    """t as [.., .., dim] of this shape, its last dimension dense, without a copy."""
-    if t.shape != shape:
+def _rows(call: str, name: str, t, index: int):
+    """t [..., cols] as (address, rows, cols, pitch); its last dimension has to be dense."""
+    if t.dim() != 2:
+        if t.dim() == 0:
+            _refuse(call, f"{name} has no dimension")
         try:
-            t = t.view(shape)
+            t = t.view(t.numel() // t.shape[-1] if t.shape[-1] else 0, t.shape[-1])
         except RuntimeError:
-            _refuse(call, f"{name} of shape {tuple(t.shape)} and strides {t.stride()} is no {shape} without a copy")
-    if shape[-1] > 1 and t.stride(-1) != 1:
+            _refuse(call, f"{name} of shape {tuple(t.shape)} and strides {t.stride()} is no array of rows without a copy")
+    if t.get_device() != index:
+        _refuse(call, f"{name} is on {t.device}, the other tensors on cuda:{index}")
+    (rows, cols), (pitch, step) = t.shape, t.stride()
+    if step != 1 and cols > 1:
         _refuse(call, f"the last dimension of {name} is not dense (strides {t.stride()})")
-    return t
+    return t.data_ptr(), rows, cols, pitch if rows > 1 else cols
 
 
-def _pitch(t, dim: int) -> int:
-    """Pitch of dimension `dim`; that of a dimension of one element has no meaning and becomes the dense one."""
-    if t.shape[dim] > 1:
-        return t.stride(dim)
-    return max(1, t.shape[-1]) * (t.shape[-2] if dim == t.dim() - 3 else 1)
+def _groups(call: str, name: str, t, n: int, rows: int, cols: int, index: int):
+    """t as [n, rows, cols], without a copy: (address, group pitch, row pitch)."""
+    if t.dim() != 3 or t.shape[1] != rows:
+        try:
+            t = t.view(n, rows, cols)
+        except RuntimeError:
+            _refuse(call, f"{name} of shape {tuple(t.shape)} and strides {t.stride()} is no {(n, rows, cols)} without a copy")
+    if t.get_device() != index:
+        _refuse(call, f"{name} is on {t.device}, the other tensors on cuda:{index}")
+    group, pitch, step = t.stride()
+    if step != 1 and cols > 1:
+        _refuse(call, f"the last dimension of {name} is not dense (strides {t.stride()})")
+    if rows <= 1:                                        # the pitch of a dimension of one element has no meaning
+        pitch = cols
+    return t.data_ptr(), group if n > 1 else max(1, rows) * cols, pitch
 
 
-def _rows(call: str, name: str, t):
-    """t [..., cols] as [rows, cols]."""
-    if t.dim() == 2:
-        return _groups(call, name, t, *t.shape)
-    if t.dim() == 0:
-        _refuse(call, f"{name} has no dimension")
-    return _groups(call, name, t, t.numel() // t.shape[-1] if t.shape[-1] else 0, t.shape[-1])
-
-
-def _call(call: str, device, stream, *args):
-    """lib().<call>(*args, stream) with `device` current."""
-    fn = getattr(lib(), call)
+def _call(call: str, index: int, stream, *args):
+    """lib().<call>(*args, stream) with device `index` current."""
+    fn = getattr(_LIB or _load(), call)
     if stream is None:
-        stream = torch.cuda.current_stream(device)
-    elif stream.device != device:
-        _refuse(call, f"the stream is on {stream.device}, the tensors on {device}")
-    if torch.cuda.current_device() == device.index:
-        rc = fn(*args, stream.cuda_stream)
+        raw = _current_raw_stream(index)
     else:
-        with torch.cuda.device(device):
-            rc = fn(*args, stream.cuda_stream)
+        if stream.device.index != index:
+            _refuse(call, f"the stream is on {stream.device}, the tensors on cuda:{index}")
+        raw = stream.cuda_stream
+    if _current_device() == index:
+        rc = fn(*args, raw)
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, raw)
     if rc != 0:
         raise ParleError(rc, call)
 
 
-def _new(device, stream, shape, dtype):
+# (torch.cuda.current_stream() and current_device() make objects on the way: 2.2 us instead of 0.2 us a call)
+_current_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+_LIB = None
+
+
+def _load():
+    global _LIB
+    _LIB = lib()
+    return _LIB
+
+
+def _new(index: int, stream, shape, dtype):
     """Memory for a result: of the stream that the call runs on."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(shape, dtype=dtype, device=index)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
-
-
-def _ptr(t) -> int:
-    return 0 if t is None else t.data_ptr()
+        return torch.empty(shape, dtype=dtype, device=index)
 
 
 def token_logprobs(logits, tokens=None, k: int = 0, scale: float = 1.0, *, logprob=None, entropy=None, top_token=None,
@@ -109,33 +131,33 @@ def token_logprobs(logits, tokens=None, k: int = 0, scale: float = 1.0, *, logpr
     (parle_token_logprobs): log probability of tokens [...] (int32, NO_TOKEN where there is none; logprob is None without
     tokens), entropy, and the k <= TOP_MAX most probable tokens with their log probabilities, [..., k]."""
     call = "parle_token_logprobs"
-    _on(call, logits.device, tokens=tokens, logprob=logprob, entropy=entropy, top_token=top_token, top_logprob=top_logprob, flags=flags)
-    dtype, x, lead, device = _dtype(call, "logits", logits), _rows(call, "logits", logits), logits.shape[:-1], logits.device
+    index, dtype = _device_of(call, logits), _dtype(call, "logits", logits)
+    x, rows, vocab, pitch = _rows(call, "logits", logits, index)
+    lead = logits.shape[:-1]
     if not 0 <= k <= TOP_MAX:
         _refuse(call, f"k = {k} is not in [0, {TOP_MAX}]")
-    if tokens is not None:
-        _dense(call, "tokens", tokens, lead, torch.int32)
+    if tokens is None:
+        if logprob is not None:
+            _refuse(call, "logprob needs tokens")
+        tokens_at = logprob_at = 0
+    else:
+        tokens_at = _dense(call, "tokens", tokens, lead, _INT, index)
         if logprob is None:
-            logprob = _new(device, stream, lead, torch.float32)
-        else:
-            _dense(call, "logprob", logprob, lead, torch.float32)
-    elif logprob is not None:
-        _refuse(call, "logprob needs tokens")
+            logprob = _new(index, stream, lead, _FLOAT)
+        logprob_at = _dense(call, "logprob", logprob, lead, _FLOAT, index)
     if entropy is None:
-        entropy = _new(device, stream, lead, torch.float32)
-    else:
-        _dense(call, "entropy", entropy, lead, torch.float32)
+        entropy = _new(index, stream, lead, _FLOAT)
+    entropy_at = _dense(call, "entropy", entropy, lead, _FLOAT, index)
+    best = (*lead, k)
     if top_token is None:
-        top_token = _new(device, stream, (*lead, k), torch.int32)
-    else:
-        _dense(call, "top_token", top_token, (*lead, k), torch.int32)
+        top_token = _new(index, stream, best, _INT)
     if top_logprob is None:
-        top_logprob = _new(device, stream, (*lead, k), torch.float32)
-    else:
-        _dense(call, "top_logprob", top_logprob, (*lead, k), torch.float32)
-    _flags(call, flags)
-    _call(call, device, stream, x.data_ptr(), dtype, x.shape[0], x.shape[1], _pitch(x, 0), _ptr(tokens), scale, k, _ptr(logprob),
-          entropy.data_ptr(), top_token.data_ptr() if k else 0, top_logprob.data_ptr() if k else 0, _ptr(flags))
+        top_logprob = _new(index, stream, best, _FLOAT)
+    top_token_at, top_logprob_at = _dense(call, "top_token", top_token, best, _INT, index), _dense(call, "top_logprob", top_logprob, best, _FLOAT, index)
+    if not k:
+        top_token_at = top_logprob_at = 0
+    _call(call, index, stream, x, dtype, rows, vocab, pitch, tokens_at, scale, k, logprob_at, entropy_at, top_token_at, top_logprob_at,
+          _word(call, "flags", flags, _INTS, index))
     return logprob, entropy, top_token, top_logprob
 
 
@@ -144,21 +166,19 @@ def token_logprobs_grad(logits, tokens=None, d_logprob=None, d_entropy=None, sca
     """dlogits of sum(d_logprob * logprob + d_entropy * entropy) (parle_token_logprobs_grad); dlogits may be logits itself.
     logprob and entropy are formed in the same pass when given."""
     call = "parle_token_logprobs_grad"
-    _on(call, logits.device, tokens=tokens, d_logprob=d_logprob, d_entropy=d_entropy, dlogits=dlogits, logprob=logprob, entropy=entropy, flags=flags)
-    dtype, x, lead, device = _dtype(call, "logits", logits), _rows(call, "logits", logits), logits.shape[:-1], logits.device
-    if tokens is not None:
-        _dense(call, "tokens", tokens, lead, torch.int32)
-    for name, t in (("d_logprob", d_logprob), ("d_entropy", d_entropy), ("logprob", logprob), ("entropy", entropy)):
-        if t is not None:
-            _dense(call, name, t, lead, torch.float32)
+    index, dtype = _device_of(call, logits), _dtype(call, "logits", logits)
+    x, rows, vocab, pitch = _rows(call, "logits", logits, index)
+    lead = logits.shape[:-1]
+    given = [0 if t is None else _dense(call, name, t, lead, kind, index)
+             for name, t, kind in (("tokens", tokens, _INT), ("d_logprob", d_logprob, _FLOAT), ("d_entropy", d_entropy, _FLOAT),
+                                   ("logprob", logprob, _FLOAT), ("entropy", entropy, _FLOAT))]
     if dlogits is None:
-        dlogits = _new(device, stream, logits.shape, logits.dtype)
-    elif dlogits.shape != logits.shape or dlogits.dtype != logits.dtype:
+        dlogits = _new(index, stream, logits.shape, logits.dtype)
+    elif dlogits.shape != logits.shape or dlogits.dtype is not logits.dtype:
         _refuse(call, f"dlogits is {dlogits.dtype} {tuple(dlogits.shape)}, logits {logits.dtype} {tuple(logits.shape)}")
-    d = _rows(call, "dlogits", dlogits)
-    _flags(call, flags)
-    _call(call, device, stream, x.data_ptr(), dtype, x.shape[0], x.shape[1], _pitch(x, 0), _ptr(tokens), scale, _ptr(d_logprob),
-          _ptr(d_entropy), _ptr(logprob), _ptr(entropy), d.data_ptr(), _pitch(d, 0), _ptr(flags))
+    d, _, _, d_pitch = _rows(call, "dlogits", dlogits, index)
+    _call(call, index, stream, x, dtype, rows, vocab, pitch, given[0], scale, given[1], given[2], given[3], given[4], d, d_pitch,
+          _word(call, "flags", flags, _INTS, index))
     return dlogits
 
 
@@ -166,24 +186,28 @@ def embedding(table, tokens, scale: float = 1.0, *, out=None, dtype=None, flags=
     """out[..., :] = scale * table[tokens[...], :] (parle_embedding): table [vocab, dim] with tokens of any shape, or one table per
     replica, [n, vocab, dim], with tokens [n, ...].  out: tokens' shape + [dim], of type `dtype` (the table's)."""
     call = "parle_embedding"
-    _on(call, table.device, tokens=tokens, out=out, flags=flags)
-    if table.dim() not in (2, 3):
+    index, table_dtype = _device_of(call, table), _dtype(call, "table", table)
+    if table.dim() == 3:
+        n, vocab, dim = table.shape
+        if tokens.dim() == 0 or tokens.shape[0] != n:
+            _refuse(call, f"{n} tables and tokens of shape {tuple(tokens.shape)}")
+        table_at, table_gs, ld_table = _groups(call, "table", table, n, vocab, dim, index)
+    elif table.dim() == 2:
+        n = 1
+        table_at, vocab, dim, ld_table = _rows(call, "table", table, index)
+        table_gs = vocab * dim
+    else:
         _refuse(call, f"table has {table.dim()} dimensions, not [vocab, dim] or [n, vocab, dim]")
-    t3 = table if table.dim() == 3 else table[None]
-    n, vocab, dim = t3.shape
-    t3 = _groups(call, "table", t3, n, vocab, dim)
-    if table.dim() == 3 and (tokens.dim() == 0 or tokens.shape[0] != n):
-        _refuse(call, f"{n} tables and tokens of shape {tuple(tokens.shape)}")
-    _dense(call, "tokens", tokens, tokens.shape, torch.int32)
+    shape = tokens.shape
+    tokens_at = _dense(call, "tokens", tokens, shape, _INT, index)
     if out is None:
-        out = _new(table.device, stream, (*tokens.shape, dim), dtype or table.dtype)
-    elif out.shape != (*tokens.shape, dim) or (dtype is not None and out.dtype != dtype):
-        _refuse(call, f"out is {out.dtype} {tuple(out.shape)}, not {dtype or out.dtype} {(*tokens.shape, dim)}")
+        out = _new(index, stream, (*shape, dim), dtype or table.dtype)
+    elif out.shape != (*shape, dim) or (dtype is not None and out.dtype is not dtype):
+        _refuse(call, f"out is {out.dtype} {tuple(out.shape)}, not {dtype or out.dtype} {(*shape, dim)}")
     length = tokens.numel() // n if n else 0
-    o = _groups(call, "out", out, n, length, dim)
-    _flags(call, flags)
-    _call(call, table.device, stream, t3.data_ptr(), _dtype(call, "table", table), _pitch(t3, 0), _pitch(t3, 1), n, vocab, dim,
-          tokens.data_ptr(), length, scale, o.data_ptr(), _dtype(call, "out", out), _pitch(o, 0), _pitch(o, 1), _ptr(flags))
+    out_at, out_gs, ld_out = _groups(call, "out", out, n, length, dim, index)
+    _call(call, index, stream, table_at, table_dtype, table_gs, ld_table, n, vocab, dim, tokens_at, length, scale, out_at,
+          _dtype(call, "out", out), out_gs, ld_out, _word(call, "flags", flags, _INTS, index))
     return out
 
 
@@ -196,36 +220,40 @@ def embedding_grad(dout, tokens, vocab: int, scale: float = 1.0, *, n=None, dtab
                    flags=None, stream=None):
     """dtable[v, :] = scale * sum of the rows of dout [..., dim] whose token is v (parle_embedding_grad): fp32 [vocab, dim], or
     [n, vocab, dim] when dtable has three dimensions or n is given (tokens and dout then begin with n).  accumulate adds to
-    dtable.  workspace: uint8 scratch of embedding_grad_workspace_bytes(), allocated when not given."""
+    dtable.  workspace: scratch of embedding_grad_workspace_bytes(), allocated when not given."""
     call = "parle_embedding_grad"
-    device = dout.device
-    _on(call, device, tokens=tokens, dtable=dtable, workspace=workspace, flags=flags)
-    _dense(call, "tokens", tokens, tokens.shape, torch.int32)
-    if dout.shape[:-1] != tokens.shape or dout.dim() == 0:
-        _refuse(call, f"dout of shape {tuple(dout.shape)} and tokens of shape {tuple(tokens.shape)}")
-    dim = dout.shape[-1]
+    index, dtype = _device_of(call, dout), _dtype(call, "dout", dout)
+    shape = tokens.shape
+    tokens_at = _dense(call, "tokens", tokens, shape, _INT, index)
+    dim = dout.shape[-1] if dout.dim() else 0
+    if dout.shape != (*shape, dim):
+        _refuse(call, f"dout of shape {tuple(dout.shape)} and tokens of shape {tuple(shape)}")
     if dtable is None:
         if accumulate:
             _refuse(call, "accumulate needs a dtable")
-        dtable = _new(device, stream, (vocab, dim) if n is None else (n, vocab, dim), torch.float32)
-    grouped = dtable.dim() == 3
-    groups = dtable.shape[0] if grouped else 1
-    if dtable.dtype != torch.float32 or dtable.shape[-2:] != (vocab, dim) or dtable.dim() not in (2, 3) or (n is not None and (not grouped or n != groups)):
-        _refuse(call, f"dtable is {dtable.dtype} {tuple(dtable.shape)}: fp32 [{vocab}, {dim}] or [n, {vocab}, {dim}] is needed")
-    if grouped and (tokens.dim() == 0 or tokens.shape[0] != groups):
-        _refuse(call, f"{groups} tables and tokens of shape {tuple(tokens.shape)}")
+        dtable = _new(index, stream, (vocab, dim) if n is None else (n, vocab, dim), _FLOAT)
+    if dtable.dim() == 3:
+        groups = dtable.shape[0]
+        fits = dtable.shape == (groups, vocab, dim) and n in (None, groups) and tokens.dim() > 0 and shape[0] == groups
+    else:
+        groups, fits = 1, dtable.shape == (vocab, dim) and n is None
+    if not fits or dtable.dtype is not _FLOAT:
+        _refuse(call, f"dtable is {dtable.dtype} {tuple(dtable.shape)}: fp32 [{vocab}, {dim}], or [n, {vocab}, {dim}] for tokens [n, ...], is needed")
     length = tokens.numel() // groups if groups else 0
-    d = _groups(call, "dout", dout, groups, length, dim)
-    t = _groups(call, "dtable", dtable if grouped else dtable[None], groups, vocab, dim)
-    need = lib().parle_embedding_grad_workspace_bytes(groups, length, vocab, dim)
+    dout_at, dout_gs, ld_dout = _groups(call, "dout", dout, groups, length, dim, index)
+    dtable_at, dtable_gs, ld_dtable = _groups(call, "dtable", dtable, groups, vocab, dim, index)
     if workspace is None:
-        workspace = _new(device, stream, need, torch.uint8)
-    elif not workspace.is_contiguous():
-        _refuse(call, "workspace is not contiguous")
-    _flags(call, flags)
-    _call(call, device, stream, d.data_ptr(), _dtype(call, "dout", dout), _pitch(d, 0), _pitch(d, 1), tokens.data_ptr(), groups, length,
-          vocab, dim, scale, t.data_ptr(), _pitch(t, 0), _pitch(t, 1), 1 if accumulate else 0, workspace.data_ptr(),
-          workspace.numel() * workspace.element_size(), _ptr(flags))
+        nbytes = (_LIB or _load()).parle_embedding_grad_workspace_bytes(groups, length, vocab, dim)
+        workspace_at = 0
+        if nbytes:
+            workspace = _new(index, stream, nbytes, torch.uint8)
+            workspace_at = workspace.data_ptr()
+    else:
+        if not workspace.is_contiguous() or workspace.get_device() != index:
+            _refuse(call, f"workspace has to be contiguous and on cuda:{index}")
+        workspace_at, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _call(call, index, stream, dout_at, dtype, dout_gs, ld_dout, tokens_at, groups, length, vocab, dim, scale, dtable_at, dtable_gs, ld_dtable,
+          1 if accumulate else 0, workspace_at, nbytes, _word(call, "flags", flags, _INTS, index))
     return dtable
 
 
@@ -233,19 +261,20 @@ def dropout(x, p: float, seed: int, offset: int = 0, *, residual=None, out=None,
     """residual + dropout(x), the mask a function of (seed, offset + *offset_dev, element number) (parle_dropout).  out may be x or
     residual.  The gradient of x is dropout(gradient of the output, p, seed, offset)."""
     call = "parle_dropout"
-    _on(call, x.device, residual=residual, out=out, offset_dev=offset_dev)
-    dtype, device = _dtype(call, "x", x), x.device
+    index, dtype = _device_of(call, x), _dtype(call, "x", x)
+    x_at, rows, cols, ld_x = _rows(call, "x", x, index)
+    residual_at = ld_r = 0
+    if residual is not None:
+        if residual.shape != x.shape or residual.dtype is not x.dtype:
+            _refuse(call, f"residual is {residual.dtype} {tuple(residual.shape)}, x {x.dtype} {tuple(x.shape)}")
+        residual_at, _, _, ld_r = _rows(call, "residual", residual, index)
     if out is None:
-        out = _new(device, stream, x.shape, x.dtype)
-    for name, t in (("residual", residual), ("out", out)):
-        if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
-            _refuse(call, f"{name} is {t.dtype} {tuple(t.shape)}, x {x.dtype} {tuple(x.shape)}")
-    if offset_dev is not None and (offset_dev.numel() != 1 or offset_dev.dtype not in (torch.int64, torch.uint64)):
-        _refuse(call, "offset_dev has to be one 64-bit integer")
+        out = _new(index, stream, x.shape, x.dtype)
+    elif out.shape != x.shape or out.dtype is not x.dtype:
+        _refuse(call, f"out is {out.dtype} {tuple(out.shape)}, x {x.dtype} {tuple(x.shape)}")
+    out_at, _, _, ld_y = _rows(call, "out", out, index)
     if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
         _refuse(call, "seed and offset are unsigned 64-bit numbers")
-    a, y = _rows(call, "x", x), _rows(call, "out", out)
-    r = None if residual is None else _rows(call, "residual", residual)
-    _call(call, device, stream, a.data_ptr(), _pitch(a, 0), _ptr(r), 0 if r is None else _pitch(r, 0), y.data_ptr(), _pitch(y, 0), dtype,
-          a.shape[0], a.shape[1], p, seed, offset, _ptr(offset_dev))
+    _call(call, index, stream, x_at, ld_x, residual_at, ld_r, out_at, ld_y, dtype, rows, cols, p, seed, offset,
+          _word(call, "offset_dev", offset_dev, _LONGS, index))
     return out
