@@ -20,7 +20,8 @@ struct DropoutArgs {
     void *y;
     long long ld_x, ld_r, ld_y;
     long long rows, cols;
-    uint32_t threshold;                                  // 0 .. 65536
+    uint32_t upper_threshold;                            // t << 16; t = 65536: all dropped, see drop_all
+    int drop_all;
     float scale;
     unsigned long long seed, offset;
     const unsigned long long *offset_dev;
@@ -42,16 +43,10 @@ __device__ __forceinline__ uint4 philox4x32_10(unsigned long long group, unsigne
     return make_uint4(c0, c1, c2, c3);
 }
 
-// Bit i: element i of the group is kept.
-__device__ __forceinline__ uint32_t keep_bits(const uint4 &w, uint32_t threshold) {
-    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-    uint32_t bits = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        bits |= (v[i] & 0xffffu) >= threshold ? 1u << (2 * i) : 0u;
-        bits |= (v[i] >> 16) >= threshold ? 2u << (2 * i) : 0u;
-    }
-    return bits;
+// Whether element i of a group is kept: its field against the threshold, both in the upper half of a word.
+__device__ __forceinline__ bool kept(const uint4 &w, int i, uint32_t upper_threshold) {
+    const uint32_t v = i < 2 ? w.x : i < 4 ? w.y : i < 6 ? w.z : w.w;
+    return (i % 2 ? v : v << 16) >= upper_threshold;
 }
 
 __device__ __forceinline__ unsigned long long call_offset(const DropoutArgs &p) {
@@ -61,103 +56,199 @@ __device__ __forceinline__ unsigned long long call_offset(const DropoutArgs &p) 
 // A dropped element is zero whatever its value was (a selection: NaN and Inf do not pass through the product).
 __device__ __forceinline__ float dropped(float x, bool keep, float scale) { return keep ? x * scale : 0.f; }
 
+// A group's fields.  (All zero, below any threshold but 0, where everything is dropped: 65536 << 16 does not fit.)
+__device__ __forceinline__ uint4 fields(const DropoutArgs &p, unsigned long long group, unsigned long long offset) {
+    return p.drop_all ? make_uint4(0, 0, 0, 0) : philox4x32_10(group, offset, p.seed);
+}
+
 constexpr int kThreads = 256;
 
-// Groups of eight elements that lie in one row and start on 16-byte boundaries in every operand: one thread per group, `U`
-// groups in flight.  `per_row` groups a row; rows == 1 stands for a wholly contiguous array.
-template <typename T, bool RES, int U>
-__global__ void __launch_bounds__(kThreads) dropout_groups_kernel(const DropoutArgs p, long long groups, long long per_row) {
-    const long long first = (long long)blockIdx.x * (kThreads * U) + threadIdx.x;
-    const unsigned long long offset = call_offset(p);
-    Pack8<T> x[U], r[U];
-    long long at_y[U];
+// One group: x and r as loaded, group number g.
+template <typename T, bool RES> __device__ __forceinline__ Pack8<T> drop_group(const DropoutArgs &p, const Pack8<T> &x, const Pack8<T> &r, unsigned long long g, unsigned long long offset) {
+    const uint4 w = fields(p, g, offset);
+    float v[8], e[8];
+    x.get(v);
+    if (RES) r.get(e);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const long long g = first + u * kThreads;
-        if (g >= groups) break;
-        long long row = 0, col = g * 8;
-        if (p.rows > 1) { row = g / per_row; col = (g - row * per_row) * 8; }
-        x[u].load(static_cast<const T *>(p.x) + row * p.ld_x + col);
-        if (RES) r[u].load(static_cast<const T *>(p.residual) + row * p.ld_r + col);
-        at_y[u] = row * p.ld_y + col;
+    for (int i = 0; i < 8; ++i) {
+        v[i] = dropped(v[i], kept(w, i, p.upper_threshold), p.scale);
+        if (RES) v[i] += e[i];
     }
+    Pack8<T> out;
+    out.set(v);
+    return out;
+}
+
+// Contiguous arrays on 16-byte boundaries: kFlight groups of eight elements of a thread in flight.  16384 x 4096 bf16: with a
+// residual 61 us, the copy rate; without 45 us, 0.91 of it: there the integer work of the generator (20 wide multiplications and as
+// many three-way xors for eight elements) takes most of the issue slots.
+constexpr int kFlight = 4;
+template <typename T, bool RES>
+__global__ void __launch_bounds__(kThreads) dropout_flat_kernel(const DropoutArgs p, long long groups) {
+    const long long first = (long long)blockIdx.x * (kThreads * kFlight) + threadIdx.x;
+    Pack8<T> x[kFlight], r[kFlight];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < kFlight; ++u) {
         const long long g = first + u * kThreads;
         if (g >= groups) break;
-        const uint32_t keep = keep_bits(philox4x32_10((unsigned long long)g, offset, p.seed), p.threshold);
-        float v[8], w[8];
-        x[u].get(v);
-        if (RES) r[u].get(w);
+        x[u].load(static_cast<const T *>(p.x) + g * 8);
+        if (RES) r[u].load(static_cast<const T *>(p.residual) + g * 8);
+    }
+    const unsigned long long offset = call_offset(p);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[i] = dropped(v[i], (keep >> i) & 1u, p.scale);
-            if (RES) v[i] += w[i];
-        }
-        Pack8<T> out;
-        out.set(v);
-        out.store(static_cast<T *>(p.y) + at_y[u]);
+    for (int u = 0; u < kFlight; ++u) {
+        const long long g = first + u * kThreads;
+        if (g >= groups) break;
+        drop_group<T, RES>(p, x[u], r[u], (unsigned long long)g, offset).store(static_cast<T *>(p.y) + g * 8);
     }
 }
 
-// Any pitch and alignment: a warp takes 32 consecutive groups (256 elements in row-major order); every lane draws one group's
-// numbers, then the warp walks over the 256 elements 32 at a time, so that its accesses are consecutive, and each lane
-// fetches its element's keep bit from the lane that drew it.
+// Rows of whole groups on 16-byte boundaries, at any pitch: 1 << log_per_row threads of a block take a row, in col_blocks blocks
+// if it is long.
+template <typename T, bool RES>
+__global__ void __launch_bounds__(kThreads) dropout_rows_kernel(const DropoutArgs p, int log_per_row, unsigned col_blocks) {
+    const int per_row = (int)(p.cols / 8);
+    const unsigned row_block = blockIdx.x / col_blocks, col_block = blockIdx.x - row_block * col_blocks;
+    const long long row = (long long)row_block * (kThreads >> log_per_row) + (threadIdx.x >> log_per_row);
+    if (row >= p.rows) return;
+    const int first = (int)(col_block * kFlight << log_per_row) + (threadIdx.x & ((1 << log_per_row) - 1));
+    const T *px = static_cast<const T *>(p.x) + row * p.ld_x, *pr = static_cast<const T *>(p.residual) + row * p.ld_r;
+    T *py = static_cast<T *>(p.y) + row * p.ld_y;
+    Pack8<T> x[kFlight], r[kFlight];
+#pragma unroll
+    for (int u = 0; u < kFlight; ++u) {
+        const int c = first + (u << log_per_row);
+        if (c >= per_row) break;
+        x[u].load(px + (long long)c * 8);
+        if (RES) r[u].load(pr + (long long)c * 8);
+    }
+    const unsigned long long offset = call_offset(p);
+#pragma unroll
+    for (int u = 0; u < kFlight; ++u) {
+        const int c = first + (u << log_per_row);
+        if (c >= per_row) break;
+        drop_group<T, RES>(p, x[u], r[u], (unsigned long long)row * per_row + c, offset).store(py + (long long)c * 8);
+    }
+}
+
+// Any pitch and alignment, rows of at least kSegment elements: a warp takes kSegment elements of a row, which lie in at most 32
+// groups; every lane draws one group's numbers, then the warp walks over the elements 32 at a time, so that its accesses are
+// consecutive, and each lane fetches its element's keep bit from the lane that drew it.  All loads come before the stores (y may
+// be x).
+constexpr int kSegment = 248;
 template <typename T>
-__global__ void __launch_bounds__(kThreads) dropout_elements_kernel(const DropoutArgs p, long long first_group, long long elements) {
+__global__ void __launch_bounds__(kThreads) dropout_segments_kernel(const DropoutArgs p, long long segments, unsigned per_row) {
     const int lane = threadIdx.x % 32;
-    const long long warp = (long long)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
-    const long long group0 = first_group + warp * 32;
-    const long long e0 = group0 * 8;
-    if (e0 >= elements) return;
-    const uint32_t keep = keep_bits(philox4x32_10((unsigned long long)(group0 + lane), call_offset(p), p.seed), p.threshold);
-    const long long row0 = e0 / p.cols, col0 = e0 - row0 * p.cols;
+    const long long s = (long long)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+    if (s >= segments) return;
+    const long long row = quotient(s, per_row), col = (s - row * per_row) * kSegment, e0 = row * p.cols + col;
+    const int count = (int)min((long long)kSegment, p.cols - col);
+    const T *px = static_cast<const T *>(p.x) + row * p.ld_x + col, *pr = static_cast<const T *>(p.residual) + row * p.ld_r + col;
+    T *py = static_cast<T *>(p.y) + row * p.ld_y + col;
+    float x[8], r[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int o = i * 32 + lane;                     // element of the warp's 256
-        const uint32_t bits = __shfl_sync(0xffffffffu, keep, o / 8);
-        if (e0 + o >= elements) continue;
+        const int o = i * 32 + lane;
+        if (o >= count) break;
+        x[i] = to_float(px[o]);
+        if (p.residual) r[i] = to_float(pr[o]);
+    }
+    const uint4 w = fields(p, (unsigned long long)(e0 / 8 + lane), call_offset(p));
+    uint32_t keep = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) keep |= kept(w, i, p.upper_threshold) ? 1u << i : 0u;
+    const int shift = (int)(e0 % 8);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int o = i * 32 + lane;
+        const uint32_t bits = __shfl_sync(0xffffffffu, keep, (o + shift) / 8);
+        if (o >= count) continue;
+        float v = dropped(x[i], (bits >> ((o + shift) % 8)) & 1u, p.scale);
+        if (p.residual) v += r[i];
+        py[o] = from_float<T>(v);
+    }
+}
+
+// Shorter rows, and the last elements of contiguous arrays: the same over 32 consecutive groups (256 elements in row-major order).
+template <typename T>
+__global__ void __launch_bounds__(kThreads) dropout_elements_kernel(const DropoutArgs p, long long group0, long long elements) {
+    const int lane = threadIdx.x % 32;
+    const long long first = group0 + ((long long)blockIdx.x * (kThreads / 32) + threadIdx.x / 32) * 32, e0 = first * 8;
+    if (e0 >= elements) return;
+    const long long row0 = quotient(e0, p.cols), col0 = e0 - row0 * p.cols;
+    float x[8], r[8];
+    long long at_y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int o = i * 32 + lane;
+        if (e0 + o >= elements) break;
         long long row = row0, col = col0 + o;
         if (col >= p.cols) {
-            const long long down = col / p.cols;
+            const int down = p.cols >= 256 ? 1 : (int)col / (int)p.cols;
             row += down;
             col -= down * p.cols;
         }
-        const float x = to_float(static_cast<const T *>(p.x)[row * p.ld_x + col]);
-        float v = dropped(x, (bits >> (o % 8)) & 1u, p.scale);
-        if (p.residual) v += to_float(static_cast<const T *>(p.residual)[row * p.ld_r + col]);
-        static_cast<T *>(p.y)[row * p.ld_y + col] = from_float<T>(v);
+        x[i] = to_float(static_cast<const T *>(p.x)[row * p.ld_x + col]);
+        if (p.residual) r[i] = to_float(static_cast<const T *>(p.residual)[row * p.ld_r + col]);
+        at_y[i] = row * p.ld_y + col;
+    }
+    const uint4 w = fields(p, (unsigned long long)(first + lane), call_offset(p));
+    uint32_t keep = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) keep |= kept(w, i, p.upper_threshold) ? 1u << i : 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int o = i * 32 + lane;
+        const uint32_t bits = __shfl_sync(0xffffffffu, keep, o / 8);
+        if (e0 + o >= elements) continue;
+        float v = dropped(x[i], (bits >> (o % 8)) & 1u, p.scale);
+        if (p.residual) v += r[i];
+        static_cast<T *>(p.y)[at_y[i]] = from_float<T>(v);
     }
 }
 
-template <typename T> int launch_dropout(const DropoutArgs &a, int dtype, cudaStream_t stream) {
-    DropoutArgs p = a;
+template <typename T> int launch_dropout(const DropoutArgs &p, int dtype, cudaStream_t stream) {
     const long long elements = p.rows * p.cols;
-    const bool contiguous = p.rows == 1 || (p.ld_x == p.cols && p.ld_y == p.cols && (!p.residual || p.ld_r == p.cols));
-    if (contiguous) { p.rows = 1; p.cols = p.ld_x = p.ld_r = p.ld_y = elements; }
-    const bool aligned = contiguous
-        ? rows_aligned16(p.x, 0, dtype) && rows_aligned16(p.y, 0, dtype) && rows_aligned16(p.residual, 0, dtype)
-        : p.cols % 8 == 0 && rows_aligned16(p.x, p.ld_x, dtype) && rows_aligned16(p.y, p.ld_y, dtype) &&
-              (!p.residual || rows_aligned16(p.residual, p.ld_r, dtype));
-    long long done = 0;                                  // elements covered by whole aligned groups
-    if (aligned) {
-        constexpr int U = 2;
-        const long long groups = elements / 8;
-        done = groups * 8;
-        if (groups) {
-            const long long blocks = (groups + kThreads * U - 1) / (kThreads * U);
-            if (p.residual) dropout_groups_kernel<T, true, U><<<(unsigned)blocks, kThreads, 0, stream>>>(p, groups, p.cols / 8);
-            else dropout_groups_kernel<T, false, U><<<(unsigned)blocks, kThreads, 0, stream>>>(p, groups, p.cols / 8);
-            const int rc = launch_status();
-            if (rc != PARLE_OK) return rc;
+    const bool flat = p.rows == 1 || (p.ld_x == p.cols && p.ld_y == p.cols && (!p.residual || p.ld_r == p.cols));
+    const bool starts = rows_aligned16(p.x, 0, dtype) && rows_aligned16(p.y, 0, dtype) && rows_aligned16(p.residual, 0, dtype);
+    long long done = 0;                                  // elements covered
+    if (flat) {
+        if (starts && elements >= 8) {
+            const long long groups = elements / 8;
+            const unsigned blocks = (unsigned)((groups + kThreads * kFlight - 1) / (kThreads * kFlight));
+            if (p.residual) dropout_flat_kernel<T, true><<<blocks, kThreads, 0, stream>>>(p, groups);
+            else dropout_flat_kernel<T, false><<<blocks, kThreads, 0, stream>>>(p, groups);
+            done = groups * 8;
+        }
+    } else if (starts && p.cols % 8 == 0 && rows_aligned16(p.x, p.ld_x, dtype) && rows_aligned16(p.y, p.ld_y, dtype) &&
+               (!p.residual || rows_aligned16(p.residual, p.ld_r, dtype)) && p.cols < (1LL << 31)) {
+        const long long per_row = p.cols / 8;
+        int log_per_row = 0;
+        while (log_per_row < 8 && (1LL << log_per_row) * kFlight < per_row) ++log_per_row;
+        const long long col_blocks = (per_row + ((long long)kFlight << log_per_row) - 1) / ((long long)kFlight << log_per_row);
+        const long long row_blocks = (p.rows + (kThreads >> log_per_row) - 1) / (kThreads >> log_per_row);
+        if (row_blocks * col_blocks < (1LL << 31)) {
+            const unsigned blocks = (unsigned)(row_blocks * col_blocks);
+            if (p.residual) dropout_rows_kernel<T, true><<<blocks, kThreads, 0, stream>>>(p, log_per_row, (unsigned)col_blocks);
+            else dropout_rows_kernel<T, false><<<blocks, kThreads, 0, stream>>>(p, log_per_row, (unsigned)col_blocks);
+            done = elements;
+        }
+    } else if (p.cols >= kSegment && p.cols < (1LL << 31)) {
+        const long long per_row = (p.cols + kSegment - 1) / kSegment, segments = per_row * p.rows, blocks = (segments + kThreads / 32 - 1) / (kThreads / 32);
+        if (blocks < (1LL << 31)) {
+            dropout_segments_kernel<T><<<(unsigned)blocks, kThreads, 0, stream>>>(p, segments, (unsigned)per_row);
+            done = elements;
         }
     }
-    if (done < elements) {
-        const long long groups = (elements - done + 7) / 8, blocks = (groups + kThreads - 1) / kThreads;
-        dropout_elements_kernel<T><<<(unsigned)blocks, kThreads, 0, stream>>>(p, done / 8, elements);
-        return launch_status();
+    if (done) {
+        const int rc = launch_status();
+        if (rc != PARLE_OK || done == elements) return rc;
     }
-    return PARLE_OK;
+    DropoutArgs a = p;
+    if (flat) { a.rows = 1; a.cols = elements; }
+    const long long groups = (elements - done + 7) / 8;
+    dropout_elements_kernel<T><<<(unsigned)((groups + kThreads - 1) / kThreads), kThreads, 0, stream>>>(a, done / 8, elements);
+    return launch_status();
 }
 
 }  // namespace
@@ -177,8 +268,10 @@ extern "C" int parle_dropout(const void *x, long long ld_x, const void *residual
     a.x = x; a.residual = residual; a.y = y;
     a.ld_x = ld_x; a.ld_r = ld_r; a.ld_y = ld_y;
     a.rows = rows; a.cols = cols;
-    a.threshold = (uint32_t)floor(p * 65536.0 + 0.5);
-    a.scale = a.threshold < 65536u ? (float)(65536.0 / (65536.0 - (double)a.threshold)) : 0.f;
+    const uint32_t threshold = (uint32_t)floor(p * 65536.0 + 0.5);
+    a.drop_all = threshold == 65536u;
+    a.upper_threshold = a.drop_all ? 1u : threshold << 16;
+    a.scale = a.drop_all ? 0.f : (float)(65536.0 / (65536.0 - (double)threshold));
     a.seed = seed; a.offset = offset;
     a.offset_dev = reinterpret_cast<const unsigned long long *>(offset_dev);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);

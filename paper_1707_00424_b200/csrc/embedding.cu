@@ -34,60 +34,85 @@ struct LookupArgs {
     void *out;
     const int32_t *tokens;
     long long table_gs, ld_table, out_gs, ld_out;
-    long long length, rows;                              // rows = n * length
+    long long length;
     int vocab, dim;
     float scale;
     int32_t *flags;
 };
 
-// E elements per access (8: everything on 16-byte boundaries; 1: any pitch and alignment).  `per_row` threads of a block
-// (a power of two) share a row.
-template <typename TI, typename TO, int E>
-__global__ void __launch_bounds__(kThreads) embedding_kernel(const LookupArgs p, int per_row) {
-    const int lane = threadIdx.x % per_row;
-    const long long row = (long long)blockIdx.x * (kThreads / per_row) + threadIdx.x / per_row;
-    if (row >= p.rows) return;
-    const int token = p.tokens[row];
-    const long long g = row / p.length, t = row - g * p.length;
-    TO *out = static_cast<TO *>(p.out) + g * p.out_gs + t * p.ld_out;
-    const bool real = token >= 0 && token < p.vocab;
-    if (!real && token != PARLE_NO_TOKEN && lane == 0 && p.flags) atomicOr(p.flags, PARLE_FLAG_BAD_LABEL);
-    const TI *in = static_cast<const TI *>(p.table) + g * p.table_gs + (real ? (long long)token * p.ld_table : 0);
-    const int steps = p.dim / E;
-    if constexpr (E == 8) {
-        constexpr int U = 2;
-        for (int j0 = lane; j0 < steps; j0 += per_row * U) {
-            Pack8<TI> v[U];
+// E elements per access (8: everything on 16-byte boundaries; 1: any pitch and alignment).  1 << log_per_row threads of a block share a
+// row; a thread has R rows and U accesses of each in flight, R U = 4: long rows U = 4, short ones R = 4.  grid (rows, n).
+template <typename TI, typename TO, int E, int R>
+__global__ void __launch_bounds__(kThreads) embedding_kernel(const LookupArgs p, int log_per_row) {
+    constexpr int U = 4 / R;
+    const int per_row = 1 << log_per_row, lane = threadIdx.x & (per_row - 1), slots = kThreads >> log_per_row;
+    const long long row0 = (long long)blockIdx.x * (slots * R) + (threadIdx.x >> log_per_row);
+    const int32_t *tokens = p.tokens + blockIdx.y * p.length;
+    const TI *table = static_cast<const TI *>(p.table) + blockIdx.y * p.table_gs;
+    TO *out = static_cast<TO *>(p.out) + blockIdx.y * p.out_gs;
+    int token[R];
+    bool real[R];
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (real && j0 + u * per_row < steps) v[u].load(in + (long long)(j0 + u * per_row) * 8);
+    for (int r = 0; r < R; ++r) token[r] = row0 + r * slots < p.length ? tokens[row0 + r * slots] : PARLE_NO_TOKEN;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        real[r] = (unsigned)token[r] < (unsigned)p.vocab;
+        if (!real[r] && token[r] != PARLE_NO_TOKEN && lane == 0 && p.flags) atomicOr(p.flags, PARLE_FLAG_BAD_LABEL);
+    }
+    const int steps = p.dim / E;
+    for (int c0 = lane; c0 < steps; c0 += per_row * U) {
+        std::conditional_t<E == 8, Pack8<TI>, TI> v[R][U];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const TI *from = table + (real[r] ? token[r] * p.ld_table : 0);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int j = j0 + u * per_row;
-                if (j >= steps) break;
-                float f[8];
-                if (real) {
-                    v[u].get(f);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] *= p.scale;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] = 0.f;
-                }
-                Pack8<TO> o;
-                o.set(f);
-                o.store(out + (long long)j * 8);
+                const int c = c0 + u * per_row;
+                if (!real[r] || c >= steps) continue;
+                if constexpr (E == 8) v[r][u].load(from + (long long)c * 8); else v[r][u] = from[c];
             }
         }
-    } else {
-        for (int j = lane; j < steps; j += per_row) out[j] = from_float<TO>(real ? to_float(in[j]) * p.scale : 0.f);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (row0 + r * slots >= p.length) break;
+            TO *to = out + (row0 + r * slots) * p.ld_out;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int c = c0 + u * per_row;
+                if (c >= steps) break;
+                float f[E];
+                if constexpr (E == 8) v[r][u].get(f); else f[0] = to_float(v[r][u]);
+#pragma unroll
+                for (int i = 0; i < E; ++i) f[i] = real[r] ? f[i] * p.scale : 0.f;
+                if constexpr (E == 8) {
+                    Pack8<TO> o;
+                    o.set(f);
+                    o.store(to + (long long)c * 8);
+                } else {
+                    to[c] = from_float<TO>(f[0]);
+                }
+            }
+        }
     }
 }
 
-int threads_per_row(int steps) {
-    int t = 1;
-    while (t < steps && t < kThreads) t *= 2;
-    return t;
+// Threads for a row: up to 64, so that a thread has several accesses of a long row in flight; more where there are few rows.
+// (16384 rows of 4096 bf16: 64 threads 35 us, 256 threads 39 us; 65536 rows of 512: four rows a thread 27 us, one 31 us.)
+template <typename TI, typename TO, int E> int launch_lookup(const LookupArgs &a, int n, int sms, cudaStream_t stream) {
+    const int steps = a.dim / E;
+    int log_per_row = 0;
+    while (log_per_row < 6 && (1 << log_per_row) < steps) ++log_per_row;
+    int rows_each = steps <= (1 << log_per_row) ? 4 : steps <= (2 << log_per_row) ? 2 : 1;
+    const auto blocks = [&] { return (a.length + (kThreads >> log_per_row) * rows_each - 1) / ((kThreads >> log_per_row) * rows_each); };
+    if (blocks() * n < 2 * sms) {
+        rows_each = 1;
+        while (log_per_row < 8 && (1 << log_per_row) < steps && blocks() * n < 2 * sms) ++log_per_row;
+    }
+    const dim3 grid((unsigned)blocks(), n);
+    if (rows_each == 4) embedding_kernel<TI, TO, E, 4><<<grid, kThreads, 0, stream>>>(a, log_per_row);
+    else if (rows_each == 2) embedding_kernel<TI, TO, E, 2><<<grid, kThreads, 0, stream>>>(a, log_per_row);
+    else embedding_kernel<TI, TO, E, 1><<<grid, kThreads, 0, stream>>>(a, log_per_row);
+    return launch_status();
 }
 
 // ---- gradient --------------------------------------------------------------------------------------------------------------------
@@ -180,7 +205,7 @@ template <typename T, int E>
 __global__ void __launch_bounds__(kThreads, 4) embedding_grad_direct_kernel(const GradArgs p, int log_groups) {
     __shared__ int count[kRowsMost], frequent[kRowsMost], frequents;
     __shared__ int noted[kRowsMost][kNoted];
-    __shared__ float parts[kWarps / 2][kColumns];         // of a frequent token's row
+    __shared__ float parts[kWarps * 256];                 // of a frequent token's row
     const int g = blockIdx.z, b = blockIdx.x, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int col0 = blockIdx.y * kColumns, groups = 1 << log_groups;
     const int rows = (p.vocab - b + groups - 1) >> log_groups;
@@ -204,57 +229,59 @@ __global__ void __launch_bounds__(kThreads, 4) embedding_grad_direct_kernel(cons
         if (at < kNoted) noted[row][at] = threadIdx.x + u * kThreads;
     }
     __syncthreads();
-    for (int i = warp; i < rows; i += kWarps) {
+    // a warp per row and 256 columns
+    const int halves = p.dim - col0 > 256 ? 2 : 1;
+    for (int item = warp; item < rows * halves; item += kWarps) {
+        const int i = halves == 2 ? item / 2 : item, first = col0 + (halves == 2 ? item % 2 * 256 : 0);
         const int m = count[i];
         float *row = dtable + (long long)((i << log_groups) + b) * p.ld_dtable;
         if (m == 0) {
             if (p.accumulate) continue;
-            const int end = min(p.dim, col0 + kColumns);
+            const int end = min(p.dim, first + 256);
             if constexpr (E == 8) {
-                for (int c = col0 + lane * 4; c < end; c += 128) *reinterpret_cast<float4 *>(row + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int c = first + lane * 4; c < end; c += 128) *reinterpret_cast<float4 *>(row + c) = make_float4(0.f, 0.f, 0.f, 0.f);
             } else {
-                for (int c = col0 + lane; c < end; c += 32) row[c] = 0.f;
+                for (int c = first + lane; c < end; c += 32) row[c] = 0.f;
             }
             continue;
         }
         if (m > kNoted) {
-            if (lane == 0) frequent[atomicAdd(&frequents, 1)] = i;
+            if (lane == 0 && first == col0) frequent[atomicAdd(&frequents, 1)] = i;
             continue;
         }
-        // the noted positions in ascending order: one per lane, moved to the number of smaller ones
+        // the noted positions in ascending order: one per lane, fetched from the lane with that many smaller ones
         int place = lane < m ? noted[i][lane] : INT_MAX;
         if (m > 1) {
-            int smaller = 0;
-            for (int j = 0; j < m; ++j) smaller += __shfl_sync(0xffffffffu, place, j) < place;
-            __syncwarp();
-            if (lane < m) noted[i][smaller] = place;
-            __syncwarp();
-            place = noted[i][min(lane, m - 1)];
+            int smaller = lane < m ? 0 : lane, from = 0;
+            for (int j = 0; j < m; ++j) {                 // (every lane takes part in the exchanges)
+                const int other = __shfl_sync(0xffffffffu, place, j);
+                if (lane < m && other < place) ++smaller;
+            }
+            for (int j = 0; j < 32; ++j) {
+                const int s = __shfl_sync(0xffffffffu, smaller, j);
+                if (s == lane) from = j;
+            }
+            place = __shfl_sync(0xffffffffu, place, from);
         }
-        float acc[2][8] = {};
-        for (int j = 0; j < m; j += 2) {
-            Lane8<T, E> v[2][2];
+        float acc[8] = {};
+        for (int j = 0; j < m; j += 4) {
+            Lane8<T, E> v[4];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const T *from = dout + (long long)__shfl_sync(0xffffffffu, place, min(j + u, m - 1)) * p.ld_dout;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (j + u < m) v[u][h].load(from, col0 + h * 256, p.dim);
+            for (int u = 0; u < 4; ++u) {
+                const int at = __shfl_sync(0xffffffffu, place, min(j + u, m - 1));
+                if (j + u < m) v[u].load(dout + (long long)at * p.ld_dout, first, p.dim);
             }
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (j + u < m) v[u][h].add_to(acc[h]);
+            for (int u = 0; u < 4; ++u)
+                if (j + u < m) v[u].add_to(acc);
         }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) store_row<E>(p, row, col0 + h * 256, acc[h]);
+        store_row<E>(p, row, first, acc);
     }
-    // rows of frequent tokens: two warps side by side, four along the positions; their parts are added in order
+    // rows of frequent tokens: all warps, side by side if there are columns for two, along the positions; their parts are added in order
     __syncthreads();
-    const int half = warp % 2, quarter = warp / 2;
-    const int per_part = (p.length + kWarps / 2 - 1) / (kWarps / 2);
-    const int from = min(p.length, quarter * per_part), to = min(p.length, from + per_part);
+    const int segments = kWarps / halves, segment = warp / halves, first = warp % halves * 256;
+    const int per_segment = (p.length + segments - 1) / segments;
+    const int from = min(p.length, segment * per_segment), to = min(p.length, from + per_segment);
     for (int f = 0; f < frequents; ++f) {
         const int v = (frequent[f] << log_groups) + b;
         float acc[8] = {};
@@ -266,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 4) embedding_grad_direct_kernel(cons
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     if (!found) break;
-                    x[u].load(dout + (long long)(t0 + __ffs(found) - 1) * p.ld_dout, col0 + half * 256, p.dim);
+                    x[u].load(dout + (long long)(t0 + __ffs(found) - 1) * p.ld_dout, col0 + first, p.dim);
                     found &= found - 1;
                     ++many;
                 }
@@ -276,11 +303,12 @@ __global__ void __launch_bounds__(kThreads, 4) embedding_grad_direct_kernel(cons
             }
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) parts[quarter][Lane8<T, E>::column(half * 256, k)] = acc[k];
+        for (int k = 0; k < 8; ++k) parts[segment * halves * 256 + Lane8<T, E>::column(first, k)] = acc[k];
         __syncthreads();
         float *row = dtable + (long long)v * p.ld_dtable;
-        for (int c = threadIdx.x; c < kColumns && col0 + c < p.dim; c += kThreads) {
-            const float sum = ((parts[0][c] + parts[1][c]) + parts[2][c]) + parts[3][c];
+        for (int c = threadIdx.x; c < halves * 256 && col0 + c < p.dim; c += kThreads) {
+            float sum = parts[c];
+            for (int s = 1; s < segments; ++s) sum += parts[s * halves * 256 + c];
             row[col0 + c] = p.accumulate ? fmaf(p.scale, sum, row[col0 + c]) : p.scale * sum;
         }
         __syncthreads();
@@ -292,9 +320,10 @@ __global__ void __launch_bounds__(kThreads, 4) embedding_grad_direct_kernel(cons
 constexpr int kChunk = 32;              // sorted positions a block of the reduction sums
 constexpr int kDigits = 256;            // of a radix pass (8 bits)
 constexpr int kTile = 4096;             // positions a block of a radix pass moves
-// Notes which tokens occur, by one lane for all lanes of the warp with the same key.
+// Notes which tokens occur, by one lane for all lanes of the warp with the same key.  By whole warps; a lane without a position
+// brings the key INT_MAX.
 __device__ __forceinline__ void note_occurs(const GradArgs &p, int g, int key) {
-    const unsigned same = __match_any_sync(__activemask(), key);
+    const unsigned same = __match_any_sync(0xffffffffu, key);
     if (key < p.vocab && __ffs(same) - 1 == (int)threadIdx.x % 32) atomicOr(p.occurs + (long long)g * p.words + key / 32, 1u << (key % 32));
 }
 
@@ -470,7 +499,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const GradArg
         // while the others come: which tokens occur (the words were zero before the pass's first barrier; the next pass's items
         // come here after its first barrier)
         if (pass == 0)
-            for (int i = threadIdx.x; i < mine; i += kSortThreads) note_occurs(p, cluster, items[i].x);
+            for (int i0 = 0; i0 < mine; i0 += kSortThreads) note_occurs(p, cluster, i0 + (int)threadIdx.x < mine ? items[i0 + threadIdx.x].x : INT_MAX);
         cluster_wait();                                   // what the others put here has arrived; their reads here are done
     }
 }
@@ -486,13 +515,15 @@ radix_count_kernel(const GradArgs p, const int32_t *keys, int shift, int first_p
     if (first_pass && g == 0 && blockIdx.x == 0 && threadIdx.x == 0) *p.crossings = 0;
     __syncthreads();
     const long long t0 = (long long)blockIdx.x * kTile;
-    for (int i = threadIdx.x; i < kTile && t0 + i < p.length; i += kThreads) {
-        int key = keys[t0 + i];
+    for (int i = threadIdx.x; i < kTile; i += kThreads) {
+        const bool have = t0 + i < p.length;
+        int key = have ? keys[t0 + i] : PARLE_NO_TOKEN;
         if (first_pass) {
             note_bad_token(key, p.vocab, p.flags);
             key = sort_key(key, p.vocab);
-            note_occurs(p, g, key);
+            note_occurs(p, g, have ? key : INT_MAX);
         }
+        if (!have) continue;
         atomicAdd(&hist[(key >> shift) & (kDigits - 1)], 1);
     }
     __syncthreads();
@@ -881,21 +912,18 @@ extern "C" int parle_embedding(const void *table, int table_dtype, long long tab
     LookupArgs a = {};
     a.table = table; a.out = out; a.tokens = tokens; a.flags = flags;
     a.table_gs = table_gs; a.ld_table = ld_table; a.out_gs = out_gs; a.ld_out = ld_out;
-    a.length = length; a.rows = (long long)n * length;
+    a.length = length;
     a.vocab = vocab; a.dim = dim; a.scale = (float)scale;
     const bool wide = dim % 8 == 0 && rows_aligned16(table, ld_table, table_dtype) && rows_aligned16(out, ld_out, out_dtype) &&
                       (n == 1 || (rows_aligned16(table, table_gs, table_dtype) && rows_aligned16(out, out_gs, out_dtype)));
-    const int per_row = threads_per_row(wide ? dim / 8 : dim);
-    const long long rows_per_block = kThreads / per_row;
-    const unsigned blocks = (unsigned)((a.rows + rows_per_block - 1) / rows_per_block);
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return PARLE_ECUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     return with_dtype(table_dtype, [&](auto *ti) {
         return with_dtype(out_dtype, [&](auto *to) {
             using TI = std::remove_pointer_t<decltype(ti)>;
             using TO = std::remove_pointer_t<decltype(to)>;
-            if (wide) embedding_kernel<TI, TO, 8><<<blocks, kThreads, 0, stream>>>(a, per_row);
-            else embedding_kernel<TI, TO, 1><<<blocks, kThreads, 0, stream>>>(a, per_row);
-            return launch_status();
+            return wide ? launch_lookup<TI, TO, 8>(a, n, sms, stream) : launch_lookup<TI, TO, 1>(a, n, sms, stream);
         });
     });
 }

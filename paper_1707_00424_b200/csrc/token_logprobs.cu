@@ -436,11 +436,12 @@ template <typename T> struct Online {
     }
 };
 
-// First pass over a row or a share of it: the next U granules are on their way while U are summed.
-template <typename T, int BLOCK, int U> __device__ __forceinline__ void pass_sums(const Row<T> &row, int begin, int end, Online<T> &sums) {
+// First pass over a row: the next U granules are on their way while U are summed.
+template <typename T, int BLOCK, int U> __device__ __forceinline__ void pass_sums(const Row<T> &row, Online<T> &sums) {
+    const int end = row.granules;
     Granule<T> next[U];
-    row.load_all(begin + (int)threadIdx.x, BLOCK, end, next);
-    for (int q0 = begin + threadIdx.x; q0 < end; q0 += BLOCK * U) {
+    row.load_all((int)threadIdx.x, BLOCK, end, next);
+    for (int q0 = threadIdx.x; q0 < end; q0 += BLOCK * U) {
         Granule<T> raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) raw[u] = next[u];
@@ -553,15 +554,20 @@ struct Given {
 // The k largest of a cluster's sh.top lists, in its first block (after a cluster barrier), into sh.top.  No key below the largest of
 // the lists' k-th keys can be among them, which leaves little more than k to rank.
 template <int BLOCK> __device__ __forceinline__ void merge_top(int k, int blocks, Shared<BLOCK> &sh) {
-    unsigned long long bound = 0;
-    for (int b = 0; b < blocks; ++b) bound = max(bound, at_rank(sh.top, b)[k - 1]);
-    __syncthreads();                                      // (sh.candidate and sh.found were in use)
+    __syncthreads();                                      // (sh.group, sh.candidate and sh.found were in use)
     if (threadIdx.x == 0) sh.found = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < blocks * k; i += BLOCK) {
-        const unsigned long long key = at_rank(sh.top, i / k)[i % k];
-        if (key && key >= bound) sh.candidate[atomicAdd(&sh.found, 1)] = key;
+    unsigned long long key = 0;                           // one each: blocks * k <= BLOCK
+    static_assert(kClusterMost * kTopMost <= 256, "a thread per key");
+    if ((int)threadIdx.x < blocks * k) {
+        key = at_rank(sh.top, threadIdx.x / k)[threadIdx.x % k];
+        if ((int)threadIdx.x % k == k - 1) sh.group[threadIdx.x / k] = key;
     }
+    __syncthreads();
+    unsigned long long bound = 0;
+#pragma unroll
+    for (int b = 0; b < kClusterMost; ++b)
+        if (b < blocks) bound = max(bound, sh.group[b]);
+    if (key && key >= bound) sh.candidate[atomicAdd(&sh.found, 1)] = key;
     __syncthreads();
     const int found = sh.found;
     if (threadIdx.x < kTopMost) sh.top[threadIdx.x] = 0;  // (every block but this one is done with its own list)
@@ -594,7 +600,7 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_kernel(con
     const Row<T> row(p.logits, p.ld, at, p.vocab);
     const Given given(p, row, at);
     Online<T> sums(p.scale_log2e);
-    pass_sums<T, BLOCK, U>(row, 0, row.granules, sums);
+    pass_sums<T, BLOCK, U>(row, sums);
     const unsigned long long best = sums.best >= 0 ? order_key(sums.top, (uint32_t)sums.best) : 0;
     if (p.k > 0) offer_best(best, sh);
     const RowResult r = row_result<T, BLOCK>(row, block_sums<BLOCK>(sums.collect(), sh), p.scale, p.scale_log2e, sh);
@@ -743,32 +749,28 @@ template <typename T, int BLOCK> __device__ __forceinline__ void zero_row(const 
     }
 }
 
-// The gradient of long rows, by a block or a cluster of blocks: a second pass reads the row again, from L2.  Its reads and the
-// stores are marked as the last use of their lines, so that rows between their two passes stay.
+// The gradient of long rows, by a block each: a second pass reads the row again, from L2.  Its reads and the stores are marked as the
+// last use of their lines, so that rows between their two passes stay.
 template <typename T, int BLOCK, int U, bool ENT>
-__global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_grad_kernel(const RowsArgs p, int blocks) {
+__global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_grad_kernel(const RowsArgs p) {
     __shared__ SharedSums<BLOCK> sh;
-    const long long at = blockIdx.x / blocks;
-    const int rank = blocks > 1 ? (int)cluster_rank() : 0;
+    const long long at = blockIdx.x;
     const Row<T> row(p.logits, p.ld, at, p.vocab);
-    const int per_block = (row.granules + blocks - 1) / blocks;
-    const int begin = min(row.granules, rank * per_block), end = min(row.granules, begin + per_block);
+    const int end = row.granules;
     const Given given(p, row, at);
     const Incoming in(p, given, at);
     const OutRow<T> out(p, row, at);
-    const TokenShare<T> share(row, given, begin + (int)threadIdx.x, BLOCK, end);
-    if (threadIdx.x == 0 && rank == 0) given.note_bad(p);
-    if (in.none && !p.logprob && !p.entropy) return zero_row<T, BLOCK>(p, at, rank, blocks);      // (every block of the cluster)
+    const TokenShare<T> share(row, given, threadIdx.x, BLOCK, end);
+    if (threadIdx.x == 0) given.note_bad(p);
+    if (in.none && !p.logprob && !p.entropy) return zero_row<T, BLOCK>(p, at, 0, 1);
     Online<T> sums(p.scale_log2e);
-    pass_sums<T, BLOCK, U>(row, begin, end, sums);
-    const RowResult r = row_result<T, BLOCK>(row, cluster_sums<BLOCK>(block_sums<BLOCK>(sums.collect(), sh), sh, blocks), p.scale, p.scale_log2e, sh);
-    if (threadIdx.x == 0 && rank == 0) given.write(p, at, r);
-    if (r.far && blocks > 1) cluster_sync_all();          // each block has read the whole row before any writes an in-place gradient
-    if (blocks > 1) cluster_done();
+    pass_sums<T, BLOCK, U>(row, sums);
+    const RowResult r = row_result<T, BLOCK>(row, block_sums<BLOCK>(sums.collect(), sh), p.scale, p.scale_log2e, sh);
+    if (threadIdx.x == 0) given.write(p, at, r);
     if (in.none || r.empty) {
-        zero_row<T, BLOCK>(p, at, rank, blocks);
+        zero_row<T, BLOCK>(p, at, 0, 1);
     } else if (r.far) {
-        far_gradient<T>(row, begin + (int)threadIdx.x, BLOCK, end, r, in.a(r), in.b(r), in.g, given.token, out);
+        far_gradient<T>(row, threadIdx.x, BLOCK, end, r, in.a(r), in.b(r), in.g, given.token, out);
     } else {
         const Slope<T, ENT> slope(r, in.a(r), in.b(r));
         // from the end: what was read last is the likeliest to be in L1 and L2 still
@@ -778,15 +780,15 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_grad_kerne
 #pragma unroll
             for (int u = 0; u < U; ++u) raw[u].raw = __ldcs(row.base + q0 + u * BLOCK);
         };
-        int q0 = begin + (int)threadIdx.x + (end - begin - 1) / stride * stride;
+        int q0 = (int)threadIdx.x + (end - 1) / stride * stride;
         Granule<T> next[U];
         if (fast(q0)) fetch(q0, next);
-        for (; q0 >= begin; q0 -= stride) {
+        for (; q0 >= 0; q0 -= stride) {
             if (fast(q0)) {
                 Granule<T> raw[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) raw[u] = next[u];
-                if (q0 - stride >= begin && fast(q0 - stride)) fetch(q0 - stride, next);
+                if (q0 >= stride && fast(q0 - stride)) fetch(q0 - stride, next);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     float v[Granule<T>::N];
@@ -794,7 +796,7 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_grad_kerne
                     __stcs(out.base + q0 + u * BLOCK, packed<T>(v));
                 }
             } else {
-                if (q0 - stride >= begin && fast(q0 - stride)) fetch(q0 - stride, next);
+                if (q0 >= stride && fast(q0 - stride)) fetch(q0 - stride, next);
                 for (int u = 0; u < U; ++u) {
                     const int q = q0 + u * BLOCK;
                     if (q >= end) break;
@@ -806,7 +808,6 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_grad_kerne
         }
         if (share.mine) out.out[given.token] = from_float<T>(slope.value(share.x) + in.g);
     }
-    if (blocks > 1) cluster_await_done();                 // no block leaves while another may read its shared memory
 }
 
 // Rows held in registers, U granules a thread, by a block or a cluster of blocks: everything is in flight at once and read once,
@@ -925,13 +926,6 @@ template <typename T, int BLOCK, int U, bool GRAD, bool ENT> int launch_held(con
     return launch_status();
 }
 
-template <typename T, int BLOCK, int U, bool ENT> int launch_grad(const RowsArgs &p, int blocks, cudaStream_t stream) {
-    cudaLaunchAttribute attr = {};
-    const cudaLaunchConfig_t cfg = row_config(p.rows, blocks, BLOCK, attr, stream);
-    if (cudaLaunchKernelEx(&cfg, token_logprobs_grad_kernel<T, BLOCK, U, ENT>, p, blocks) != cudaSuccess) return PARLE_ECUDA;
-    return launch_status();
-}
-
 template <typename T, bool GRAD, bool ENT> int launch_rows(const RowsArgs &p, int sms, cudaStream_t stream) {
     // granules of a row, one more where rows do not all begin on 16-byte boundaries
     const long long granules = ((long long)p.vocab * sizeof(T) + 15) / 16 + (reinterpret_cast<uintptr_t>(p.logits) % 16 || p.ld * sizeof(T) % 16 ? 1 : 0);
@@ -948,7 +942,8 @@ template <typename T, bool GRAD, bool ENT> int launch_rows(const RowsArgs &p, in
     // One block a row; 512 threads where fewer rows between their two passes keep them in L2.  Measured, gradient of 131072 bf16 logits,
     // 512 against 256 threads: 2048 rows 204 / 231 us; of 65536, 1024 rows 59 / 60; of 32768, 1024 rows 37 / 32.
     if constexpr (GRAD) {
-        return granules > 8192 ? launch_grad<T, 512, 4, ENT>(p, 1, stream) : launch_grad<T, 256, 4, ENT>(p, 1, stream);
+        if (granules > 8192) token_logprobs_grad_kernel<T, 512, 4, ENT><<<(unsigned)p.rows, 512, 0, stream>>>(p);
+        else token_logprobs_grad_kernel<T, 256, 4, ENT><<<(unsigned)p.rows, 256, 0, stream>>>(p);
     } else {
         token_logprobs_kernel<T, 256, 4><<<(unsigned)p.rows, 256, 0, stream>>>(p);
     }

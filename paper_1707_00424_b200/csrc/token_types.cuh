@@ -97,6 +97,12 @@ template <typename F> int with_dtype(int dtype, F f) {
     return PARLE_EINVAL;
 }
 
+// a / b, by 32-bit division where both fit (a 64-bit one is four times as long).
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    if (((a | b) >> 32) == 0) return (uint32_t)a / (uint32_t)b;
+    return a / b;
+}
+
 inline int launch_status() { return cudaGetLastError() == cudaSuccess ? PARLE_OK : PARLE_ECUDA; }
 
 }  // namespace parle

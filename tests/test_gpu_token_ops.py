@@ -427,7 +427,7 @@ def check_dropout(x, p, seed, offset, residual=None, **kw):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows, cols, pad, shift", [
     (1, 1, 0, 0), (1, 7, 0, 1), (1, 8, 0, 0), (1, 4099, 0, 0), (3, 5, 0, 0), (7, 16, 0, 0), (5, 16, 8, 0), (5, 24, 3, 1), (17, 255, 0, 3),
-    (9, 257, 1, 0), (33, 1001, 22, 5), (64, 64, 0, 0), (100, 3, 2, 0),
+    (9, 257, 1, 0), (33, 1001, 22, 5), (64, 64, 0, 0), (100, 3, 2, 0), (3, 9000, 8, 0), (2, 20011, 3, 1), (5, 248, 1, 0), (40, 8, 8, 0),
 ])
 def test_dropout(dtype, rows, cols, pad, shift):
     rng = np.random.default_rng(rows * cols)
