@@ -867,10 +867,16 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kerne
     t = block_sums<BLOCK>(t, sh);
     if (!GRAD && p.k > 0) {
         const unsigned long long bound = top_bound(p.k, sh);
-        if (best && best >= bound) {
+        if (best && best >= bound) {                      // few threads, and mostly one granule of each: it is read again
+            unsigned reach = 0;
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (q0 + u * BLOCK < end) hand_on(row, raw[u], q0 + u * BLOCK, bound, sh);
+                if (order_key(raw[u].largest(), (uint32_t)(q0 + u * BLOCK)) >= bound) reach |= 1u << u;
+            while (reach) {
+                const int q = q0 + (__ffs(reach) - 1) * BLOCK;
+                reach &= reach - 1;
+                if (q < end) hand_on(row, row.load(q, end), q, bound, sh);
+            }
         }
         __syncthreads();
         rank_candidates(row, begin, end, p.k, sh);
