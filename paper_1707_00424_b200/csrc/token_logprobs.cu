@@ -945,13 +945,18 @@ template <typename T, bool GRAD, bool ENT> int launch_rows(const RowsArgs &p, in
     const long long blocks = (granules + 256 * U - 1) / (256 * U);
     if (granules > 4096 && blocks <= kClusterMost && p.rows * blocks <= (GRAD ? 4 : 2) * sms)
         return launch_held<T, 256, U, GRAD, ENT>(p, (int)blocks, stream);
-    // One block a row; 512 threads where fewer rows between their two passes keep them in L2.  Measured, gradient of 131072 bf16 logits,
-    // 512 against 256 threads: 2048 rows 204 / 231 us; of 65536, 1024 rows 59 / 60; of 32768, 1024 rows 37 / 32.
+    // One block a row.  More threads where fewer rows between the gradient's two passes keep them in L2, fewer where what a block does
+    // per row (joining sums, ranking) counts.  Measured: gradient of 2048 x 131072 bf16 logits with 512 / 256 threads 204 / 231 us, 1024 x
+    // 65536 59 / 60, 1024 x 32760 with 256 / 128 threads 33 / 30.5, 4096 x 10000 51 / 41; log probabilities with alternatives of 1024 x
+    // 32760 with 256 / 128 threads 23 / 27, 4096 x 20000 66 / 68, 4096 x 10000 49 / 35.
+    const unsigned rows = (unsigned)p.rows;
     if constexpr (GRAD) {
-        if (granules > 8192) token_logprobs_grad_kernel<T, 512, 4, ENT><<<(unsigned)p.rows, 512, 0, stream>>>(p);
-        else token_logprobs_grad_kernel<T, 256, 4, ENT><<<(unsigned)p.rows, 256, 0, stream>>>(p);
+        if (granules > 8192) token_logprobs_grad_kernel<T, 512, 4, ENT><<<rows, 512, 0, stream>>>(p);
+        else if (granules > 4096) token_logprobs_grad_kernel<T, 256, 4, ENT><<<rows, 256, 0, stream>>>(p);
+        else token_logprobs_grad_kernel<T, 128, 4, ENT><<<rows, 128, 0, stream>>>(p);
     } else {
-        token_logprobs_kernel<T, 256, 4><<<(unsigned)p.rows, 256, 0, stream>>>(p);
+        if (granules > 2048) token_logprobs_kernel<T, 256, 4><<<rows, 256, 0, stream>>>(p);
+        else token_logprobs_kernel<T, 128, 4><<<rows, 128, 0, stream>>>(p);
     }
     return launch_status();
 }
