@@ -358,7 +358,8 @@ int parle_softmax_ce_static(const float *logits, const int32_t *labels, int n, i
  * as PARLE_NO_TOKEN too and sets the bit PARLE_FLAG_BAD_LABEL in *flags (dev [1] int32 or NULL; a call only sets the
  * bit, the caller clears it).
  * EINVAL: NULL, a size, pitch, type or scalar out of range, outputs whose rows overlap.  EALIGN: a pointer not on a boundary of
- * its element.  ETOOBIG: more than PARLE_TOKEN_MAX_ROWS rows or PARLE_TOKEN_MAX_ELEMENTS elements.  ECUDA: a launch failed. */
+ * its element.  ETOOBIG: more than PARLE_TOKEN_MAX_ROWS positions or tokens (an eighth of it: rows of logits),
+ * PARLE_TOKEN_MAX_ELEMENTS elements of dropout, PARLE_EMBEDDING_MAX_DIM columns.  ECUDA: a launch failed. */
 #define PARLE_F32 0
 #define PARLE_BF16 1
 #define PARLE_F16 2
@@ -366,6 +367,7 @@ int parle_softmax_ce_static(const float *logits, const int32_t *labels, int n, i
 #define PARLE_TOP_MAX 32
 #define PARLE_TOKEN_MAX_ROWS (1LL << 30)
 #define PARLE_TOKEN_MAX_ELEMENTS (1LL << 40)
+#define PARLE_EMBEDDING_MAX_DIM (1 << 24)
 
 /* Row-wise log probabilities of logits x dev [rows, vocab], row pitch ld:
  *   log p_j = scale (x_j - m) - log sum_i exp(scale (x_i - m)),  m = max x    (scale = 1 / temperature, in [1e-6, 1e6])

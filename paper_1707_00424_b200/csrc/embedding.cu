@@ -889,6 +889,10 @@ bool valid_sizes(int n, long long length, int vocab, int dim) {
     return n >= 1 && n <= PARLE_MAX_REPLICAS && length >= 0 && vocab >= 1 && dim >= 1;
 }
 
+bool too_big(int n, long long length, int vocab, int dim) {
+    return length > PARLE_TOKEN_MAX_ROWS / n || vocab > PARLE_TOKEN_MAX_ROWS || dim > PARLE_EMBEDDING_MAX_DIM;
+}
+
 // Whether n groups of `rows` rows of dim elements, at these pitches, do not overlap: group after group, or row by row with the
 // groups side by side.
 bool separate_rows(int n, long long rows, int dim, long long gs, long long ld) {
@@ -903,7 +907,7 @@ extern "C" int parle_embedding(const void *table, int table_dtype, long long tab
                                const int32_t *tokens, long long length, double scale, void *out, int out_dtype,
                                long long out_gs, long long ld_out, int32_t *flags, void *cuda_stream) {
     if (!valid_sizes(n, length, vocab, dim) || !valid_dtype(table_dtype) || !valid_dtype(out_dtype) || !isfinite((float)scale)) return PARLE_EINVAL;
-    if (length > PARLE_TOKEN_MAX_ROWS / n) return PARLE_ETOOBIG;
+    if (too_big(n, length, vocab, dim)) return PARLE_ETOOBIG;
     if (ld_table < 0 || (n > 1 && table_gs < 0) || !separate_rows(n, length, dim, out_gs, ld_out)) return PARLE_EINVAL;
     if (length == 0) return PARLE_OK;
     if (!table || !tokens || !out) return PARLE_EINVAL;
@@ -929,7 +933,7 @@ extern "C" int parle_embedding(const void *table, int table_dtype, long long tab
 }
 
 extern "C" size_t parle_embedding_grad_workspace_bytes(int n, long long length, int vocab, int dim) {
-    if (!valid_sizes(n, length, vocab, dim) || length > PARLE_TOKEN_MAX_ROWS / n) return 0;
+    if (!valid_sizes(n, length, vocab, dim) || too_big(n, length, vocab, dim)) return 0;
     return plan_grad(n, length, vocab, dim).bytes;
 }
 
@@ -938,7 +942,7 @@ extern "C" int parle_embedding_grad(const void *dout, int dout_dtype, long long 
                                     long long ld_dtable, int accumulate, void *workspace, size_t workspace_bytes, int32_t *flags,
                                     void *cuda_stream) {
     if (!valid_sizes(n, length, vocab, dim) || !valid_dtype(dout_dtype) || !isfinite((float)scale)) return PARLE_EINVAL;
-    if (length > PARLE_TOKEN_MAX_ROWS / n) return PARLE_ETOOBIG;
+    if (too_big(n, length, vocab, dim)) return PARLE_ETOOBIG;
     if (ld_dout < 0 || (n > 1 && dout_gs < 0) || !separate_rows(n, vocab, dim, dtable_gs, ld_dtable) || !dtable) return PARLE_EINVAL;
     const GradPlan plan = plan_grad(n, length, vocab, dim);
     if (length > 0 && (!dout || !tokens || (!workspace && plan.bytes))) return PARLE_EINVAL;

@@ -948,14 +948,15 @@ template <typename T, bool GRAD, bool ENT> int launch_rows(const RowsArgs &p, in
     // One block a row.  More threads where fewer rows between the gradient's two passes keep them in L2, fewer where what a block does
     // per row (joining sums, ranking) counts.  Measured: gradient of 2048 x 131072 bf16 logits with 512 / 256 threads 204 / 231 us, 1024 x
     // 65536 59 / 60, 1024 x 32760 with 256 / 128 threads 33 / 30.5, 4096 x 10000 51 / 41; log probabilities with alternatives of 1024 x
-    // 32760 with 256 / 128 threads 23 / 27, 4096 x 20000 66 / 68, 4096 x 10000 49 / 35.
+    // 32760 with 256 / 128 threads 23 / 27, 4096 x 20000 66 / 68, 4096 x 10000 49 / 35, 128 x 131072 with 512 / 256 threads 12.6 / 16.7.
     const unsigned rows = (unsigned)p.rows;
     if constexpr (GRAD) {
         if (granules > 8192) token_logprobs_grad_kernel<T, 512, 4, ENT><<<rows, 512, 0, stream>>>(p);
         else if (granules > 4096) token_logprobs_grad_kernel<T, 256, 4, ENT><<<rows, 256, 0, stream>>>(p);
         else token_logprobs_grad_kernel<T, 128, 4, ENT><<<rows, 128, 0, stream>>>(p);
     } else {
-        if (granules > 2048) token_logprobs_kernel<T, 256, 4><<<rows, 256, 0, stream>>>(p);
+        if (granules > 2048 && p.rows <= 2 * sms) token_logprobs_kernel<T, 512, 4><<<rows, 512, 0, stream>>>(p);
+        else if (granules > 2048) token_logprobs_kernel<T, 256, 4><<<rows, 256, 0, stream>>>(p);
         else token_logprobs_kernel<T, 128, 4><<<rows, 128, 0, stream>>>(p);
     }
     return launch_status();

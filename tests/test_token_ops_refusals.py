@@ -58,12 +58,14 @@ def dropout(x=P, ld_x=8, residual=None, ld_r=0, y=2 * P, ld_y=8, dtype=F32, rows
     (embedding, dict(scale=math.inf), EINVAL), (embedding, dict(scale=1e39), EINVAL), (embedding, dict(ld_table=-4), EINVAL),
     (embedding, dict(table_gs=-32), EINVAL), (embedding, dict(ld_out=3), EINVAL), (embedding, dict(out_gs=19), EINVAL),
     (embedding, dict(out_gs=0), EINVAL), (embedding, dict(out_gs=4, ld_out=7), EINVAL),
-    (embedding, dict(length=1 << 30), ETOOBIG), (embedding, dict(table=P + 2), EALIGN), (embedding, dict(out=P + 1, out_dtype=F16), EALIGN),
+    (embedding, dict(length=1 << 30), ETOOBIG), (embedding, dict(vocab=(1 << 30) + 1), ETOOBIG), (embedding, dict(dim=(1 << 24) + 1), ETOOBIG),
+    (embedding, dict(table=P + 2), EALIGN), (embedding, dict(out=P + 1, out_dtype=F16), EALIGN),
     (embedding, dict(tokens=P + 2), EALIGN), (embedding, dict(flags=P + 3), EALIGN),
     (embedding_grad, dict(dout=None), EINVAL), (embedding_grad, dict(dtable=None), EINVAL), (embedding_grad, dict(workspace=None, length=20000, dout_gs=80000), EINVAL),
     (embedding_grad, dict(dtype=3), EINVAL), (embedding_grad, dict(scale=math.nan), EINVAL), (embedding_grad, dict(ld_dout=-1), EINVAL),
     (embedding_grad, dict(dtable_gs=31), EINVAL), (embedding_grad, dict(ld_dtable=3), EINVAL), (embedding_grad, dict(nbytes=64, length=20000), EWORKSPACE),
-    (embedding_grad, dict(length=1 << 30), ETOOBIG), (embedding_grad, dict(workspace=3 * P + 64), EALIGN),
+    (embedding_grad, dict(length=1 << 30), ETOOBIG), (embedding_grad, dict(vocab=(1 << 30) + 1), ETOOBIG),
+    (embedding_grad, dict(dim=(1 << 24) + 1), ETOOBIG), (embedding_grad, dict(workspace=3 * P + 64), EALIGN),
     (embedding_grad, dict(dout=P + 2), EALIGN), (embedding_grad, dict(dtable=P + 2), EALIGN),
     (dropout, dict(x=None), EINVAL), (dropout, dict(y=None), EINVAL), (dropout, dict(p=-0.1), EINVAL), (dropout, dict(p=1.1), EINVAL),
     (dropout, dict(p=math.nan), EINVAL), (dropout, dict(dtype=9), EINVAL), (dropout, dict(rows=-1), EINVAL), (dropout, dict(ld_y=7), EINVAL),
