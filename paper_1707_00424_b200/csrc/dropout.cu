@@ -84,7 +84,7 @@ template <typename T, bool RES> __device__ __forceinline__ Pack8<T> drop_group(c
 // many three-way xors for eight elements) takes most of the issue slots.
 constexpr int kFlight = 4;
 template <typename T, bool RES>
-__global__ void __launch_bounds__(kThreads) dropout_flat_kernel(const DropoutArgs p, long long groups) {
+__global__ void __launch_bounds__(kThreads) dropout_flat_kernel(const DropoutArgs p, long long groups, int rest) {
     const long long first = (long long)blockIdx.x * (kThreads * kFlight) + threadIdx.x;
     Pack8<T> x[kFlight], r[kFlight];
 #pragma unroll
@@ -100,6 +100,14 @@ __global__ void __launch_bounds__(kThreads) dropout_flat_kernel(const DropoutArg
         const long long g = first + u * kThreads;
         if (g >= groups) break;
         drop_group<T, RES>(p, x[u], r[u], (unsigned long long)g, offset).store(static_cast<T *>(p.y) + g * 8);
+    }
+    if (blockIdx.x == gridDim.x - 1 && (int)threadIdx.x < rest) {      // the elements behind the last whole group, a thread each
+        const long long e = groups * 8 + threadIdx.x;
+        const uint4 w = fields(p, (unsigned long long)groups, offset);
+        const uint32_t word = threadIdx.x < 2 ? w.x : threadIdx.x < 4 ? w.y : threadIdx.x < 6 ? w.z : w.w;
+        float v = dropped(to_float(static_cast<const T *>(p.x)[e]), (threadIdx.x % 2 ? word : word << 16) >= p.upper_threshold, p.scale);
+        if (RES) v += to_float(static_cast<const T *>(p.residual)[e]);
+        static_cast<T *>(p.y)[e] = from_float<T>(v);
     }
 }
 
@@ -169,11 +177,11 @@ __global__ void __launch_bounds__(kThreads) dropout_segments_kernel(const Dropou
     }
 }
 
-// Shorter rows, and the last elements of contiguous arrays: the same over 32 consecutive groups (256 elements in row-major order).
+// Shorter rows, and contiguous arrays off 16-byte boundaries: the same over 32 consecutive groups (256 elements in row-major order).
 template <typename T>
-__global__ void __launch_bounds__(kThreads) dropout_elements_kernel(const DropoutArgs p, long long group0, long long elements) {
+__global__ void __launch_bounds__(kThreads) dropout_elements_kernel(const DropoutArgs p, long long elements) {
     const int lane = threadIdx.x % 32;
-    const long long first = group0 + ((long long)blockIdx.x * (kThreads / 32) + threadIdx.x / 32) * 32, e0 = first * 8;
+    const long long first = ((long long)blockIdx.x * (kThreads / 32) + threadIdx.x / 32) * 32, e0 = first * 8;
     if (e0 >= elements) return;
     const long long row0 = quotient(e0, p.cols), col0 = e0 - row0 * p.cols;
     float x[8], r[8];
@@ -211,14 +219,15 @@ template <typename T> int launch_dropout(const DropoutArgs &p, int dtype, cudaSt
     const long long elements = p.rows * p.cols;
     const bool flat = p.rows == 1 || (p.ld_x == p.cols && p.ld_y == p.cols && (!p.residual || p.ld_r == p.cols));
     const bool starts = rows_aligned16(p.x, 0, dtype) && rows_aligned16(p.y, 0, dtype) && rows_aligned16(p.residual, 0, dtype);
-    long long done = 0;                                  // elements covered
+    bool done = false;
     if (flat) {
-        if (starts && elements >= 8) {
+        if (starts) {
             const long long groups = elements / 8;
-            const unsigned blocks = (unsigned)((groups + kThreads * kFlight - 1) / (kThreads * kFlight));
-            if (p.residual) dropout_flat_kernel<T, true><<<blocks, kThreads, 0, stream>>>(p, groups);
-            else dropout_flat_kernel<T, false><<<blocks, kThreads, 0, stream>>>(p, groups);
-            done = groups * 8;
+            const int rest = (int)(elements % 8);
+            const unsigned blocks = (unsigned)(groups / (kThreads * kFlight) + 1);
+            if (p.residual) dropout_flat_kernel<T, true><<<blocks, kThreads, 0, stream>>>(p, groups, rest);
+            else dropout_flat_kernel<T, false><<<blocks, kThreads, 0, stream>>>(p, groups, rest);
+            done = true;
         }
     } else if (starts && p.cols % 8 == 0 && rows_aligned16(p.x, p.ld_x, dtype) && rows_aligned16(p.y, p.ld_y, dtype) &&
                (!p.residual || rows_aligned16(p.residual, p.ld_r, dtype)) && p.cols < (1LL << 31)) {
@@ -231,23 +240,21 @@ template <typename T> int launch_dropout(const DropoutArgs &p, int dtype, cudaSt
             const unsigned blocks = (unsigned)(row_blocks * col_blocks);
             if (p.residual) dropout_rows_kernel<T, true><<<blocks, kThreads, 0, stream>>>(p, log_per_row, (unsigned)col_blocks);
             else dropout_rows_kernel<T, false><<<blocks, kThreads, 0, stream>>>(p, log_per_row, (unsigned)col_blocks);
-            done = elements;
+            done = true;
         }
     } else if (p.cols >= kSegment && p.cols < (1LL << 31)) {
         const long long per_row = (p.cols + kSegment - 1) / kSegment, segments = per_row * p.rows, blocks = (segments + kThreads / 32 - 1) / (kThreads / 32);
         if (blocks < (1LL << 31)) {
             dropout_segments_kernel<T><<<(unsigned)blocks, kThreads, 0, stream>>>(p, segments, (unsigned)per_row);
-            done = elements;
+            done = true;
         }
     }
-    if (done) {
-        const int rc = launch_status();
-        if (rc != PARLE_OK || done == elements) return rc;
+    if (!done) {
+        DropoutArgs a = p;
+        if (flat) { a.rows = 1; a.cols = elements; }
+        const long long groups = (elements + 7) / 8;
+        dropout_elements_kernel<T><<<(unsigned)((groups + kThreads - 1) / kThreads), kThreads, 0, stream>>>(a, elements);
     }
-    DropoutArgs a = p;
-    if (flat) { a.rows = 1; a.cols = elements; }
-    const long long groups = (elements - done + 7) / 8;
-    dropout_elements_kernel<T><<<(unsigned)((groups + kThreads - 1) / kThreads), kThreads, 0, stream>>>(a, done / 8, elements);
     return launch_status();
 }
 

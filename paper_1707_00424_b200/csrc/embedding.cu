@@ -140,7 +140,7 @@ __device__ __forceinline__ void note_bad_token(int token, int vocab, int32_t *fl
 // ---- direct gradient -------------------------------------------------------------------------------------------------------------
 
 constexpr int kDirectMost = 1024;       // longest sequence
-constexpr int kNoted = 32;              // positions of a row that are noted
+constexpr int kNoted = 16;              // positions of a row that are noted
 constexpr int kRowsMost = 64;           // table rows of a block
 constexpr int kColumns = 512;           // columns of a block
 constexpr int kWarps = kThreads / 32;
@@ -397,20 +397,6 @@ __global__ void __launch_bounds__(kThreads) rank_tokens_kernel(const GradArgs p,
 constexpr int kSortThreads = 512, kSorters = 8;          // a cluster sorts up to
 constexpr int kSortEach = 4096, kSortMost = kSorters * kSortEach;
 constexpr int kSortBits = 9;            // of a pass at most: a thread per digit
-
-__device__ __forceinline__ int cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return (int)r;
-}
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-// Address of another block's copy of a shared variable.
-template <typename V> __device__ __forceinline__ V *at_rank(V *p, int rank) {
-    uint64_t r;
-    asm volatile("mapa.u64 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<uint64_t>(p)), "r"(rank));
-    return reinterpret_cast<V *>(r);
-}
 
 // A cluster sorts a sequence: a stable radix sort, least significant digit first, every block with an eighth of the sequence in
 // shared memory.  A position goes to (positions with a lower digit) + (same digit, in an earlier block, warp, or place of the warp).
@@ -816,17 +802,6 @@ template <typename T, int E> int launch_direct(const GradArgs &a, int n, int sms
     return launch_status();
 }
 
-cudaLaunchConfig_t launch_config(dim3 grid, int threads, int bytes, cudaLaunchAttribute *attr, cudaStream_t stream) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = bytes;
-    cfg.stream = stream;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cfg;
-}
-
 template <typename T>
 int launch_sorted(GradArgs a, int n, const GradPlan &plan, bool wide, bool wide_table, char *ws, int sms, cudaStream_t stream) {
     int *keys[2], *places[2];
@@ -846,10 +821,7 @@ int launch_sorted(GradArgs a, int n, const GradPlan &plan, bool wide, bool wide_
         constexpr int bytes = 2 * kSortEach * (int)sizeof(int2);
         if (cudaFuncSetAttribute(sort_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return PARLE_ECUDA;
         cudaLaunchAttribute attr = {};
-        attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim.x = kSorters;
-        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-        const cudaLaunchConfig_t cfg = launch_config(dim3((unsigned)n * kSorters), kSortThreads, bytes, &attr, stream);
+        const cudaLaunchConfig_t cfg = cluster_config(dim3((unsigned)n * kSorters), kSortThreads, bytes, kSorters, &attr, stream);
         if (cudaLaunchKernelEx(&cfg, sort_tokens_kernel, a, plan.sort_passes, plan.sort_bits,
                                keys[0], places[0]) != cudaSuccess) return PARLE_ECUDA;
     } else {
@@ -873,15 +845,21 @@ int launch_sorted(GradArgs a, int n, const GradPlan &plan, bool wide, bool wide_
     const long long row_bytes = (long long)a.dim * 4;
     const int zero_rows = (int)std::max(1LL, std::min(256LL, 65536 / row_bytes));
     const long long zero_blocks = a.accumulate ? 0 : ((long long)a.vocab + zero_rows - 1) / zero_rows;
-    const dim3 grid((unsigned)(plan.chunks + zero_blocks), (a.dim + columns - 1) / columns, n);
+    const dim3 grid((unsigned)(plan.chunks + zero_blocks), (a.dim + columns - 1) / columns, n);      // (at most 2^14 column parts)
     cudaLaunchAttribute chained = {};
     chained.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     chained.val.programmaticStreamSerializationAllowed = 1;
-    const cudaLaunchConfig_t sums = launch_config(grid, kThreads, 0, &chained, stream);
+    cudaLaunchConfig_t cfg = {};
+    cfg.stream = stream;
+    cfg.attrs = &chained;
+    cfg.numAttrs = 1;
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(kThreads);
     const auto kernel = wide ? embedding_grad_kernel<T, 8> : embedding_grad_kernel<T, 1>;
-    if (cudaLaunchKernelEx(&sums, kernel, a, zero_rows, wide_table) != cudaSuccess) return PARLE_ECUDA;
-    const cudaLaunchConfig_t join = launch_config(dim3(2 * sms), kJoinThreads, 0, &chained, stream);
-    if (cudaLaunchKernelEx(&join, embedding_grad_join_kernel, a) != cudaSuccess) return PARLE_ECUDA;
+    if (cudaLaunchKernelEx(&cfg, kernel, a, zero_rows, wide_table) != cudaSuccess) return PARLE_ECUDA;
+    cfg.gridDim = dim3(2 * sms);
+    cfg.blockDim = dim3(kJoinThreads);
+    if (cudaLaunchKernelEx(&cfg, embedding_grad_join_kernel, a) != cudaSuccess) return PARLE_ECUDA;
     return launch_status();
 }
 
@@ -920,8 +898,8 @@ extern "C" int parle_embedding(const void *table, int table_dtype, long long tab
     a.vocab = vocab; a.dim = dim; a.scale = (float)scale;
     const bool wide = dim % 8 == 0 && rows_aligned16(table, ld_table, table_dtype) && rows_aligned16(out, ld_out, out_dtype) &&
                       (n == 1 || (rows_aligned16(table, table_gs, table_dtype) && rows_aligned16(out, out_gs, out_dtype)));
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return PARLE_ECUDA;
+    const int sms = current_sms();
+    if (sms < 0) return PARLE_ECUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     return with_dtype(table_dtype, [&](auto *ti) {
         return with_dtype(out_dtype, [&](auto *to) {
@@ -957,8 +935,8 @@ extern "C" int parle_embedding_grad(const void *dout, int dout_dtype, long long 
     a.scale = (float)scale; a.accumulate = accumulate != 0;
     const bool wide_table = dim % 4 == 0 && rows_aligned16(dtable, ld_dtable, PARLE_F32) && (n == 1 || dtable_gs % 4 == 0);
     const bool wide = wide_table && dim % 8 == 0 && rows_aligned16(dout, ld_dout, dout_dtype) && (n == 1 || rows_aligned16(dout, dout_gs, dout_dtype));
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return PARLE_ECUDA;
+    const int sms = current_sms();
+    if (sms < 0) return PARLE_ECUDA;
     return with_dtype(dout_dtype, [&](auto *tag) {
         using TD = std::remove_pointer_t<decltype(tag)>;
         if (plan.passes) return launch_sorted<TD>(a, n, plan, wide, wide_table, static_cast<char *>(workspace), sms, stream);

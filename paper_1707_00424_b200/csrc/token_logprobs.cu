@@ -226,23 +226,9 @@ __device__ __forceinline__ float key_value(unsigned long long key) {
 }
 __device__ __forceinline__ int key_token(unsigned long long key) { return (int)~(uint32_t)key; }
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
 __device__ __forceinline__ void cluster_sync_all() {
-    asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
-}
-// In two halves: says that this thread is done with the other blocks' shared memory / waits until all are.  (Relaxed: it orders no
-// memory, so nobody's stores in flight are waited for.)
-__device__ __forceinline__ void cluster_done() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
-__device__ __forceinline__ void cluster_await_done() { asm volatile("barrier.cluster.wait;" ::: "memory"); }
-// Address of another block's copy of a shared variable.
-template <typename V> __device__ __forceinline__ const V *at_rank(const V *p, uint32_t rank) {
-    uint64_t r;
-    asm volatile("mapa.u64 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<uint64_t>(p)), "r"(rank));
-    return reinterpret_cast<const V *>(r);
+    cluster_arrive();
+    cluster_wait();
 }
 
 template <int BLOCK> struct SharedSums {
@@ -351,6 +337,7 @@ __device__ __forceinline__ void rank_candidates(const Row<T> &row, int begin, in
             const int i = i0 + (int)threadIdx.x / PARTS;
             const unsigned long long key = i < found ? sh.candidate[i] : 0;
             int above = 0;
+#pragma unroll 8
             for (int j = threadIdx.x % PARTS; j < found; j += PARTS) above += sh.candidate[j] > key;
 #pragma unroll
             for (int o = PARTS / 2; o > 0; o >>= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
@@ -817,7 +804,7 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kerne
     __shared__ Shared<BLOCK> sh;
     constexpr int P = Granule<T>::N / 2;
     const long long at = blockIdx.x / blocks;
-    const int rank = blocks > 1 ? (int)cluster_rank() : 0;
+    const int rank = blocks > 1 ? cluster_rank() : 0;
     const Row<T> row(p.logits, p.ld, at, p.vocab);
     const int per_block = (row.granules + blocks - 1) / blocks;      // at most BLOCK * U
     const int begin = min(row.granules, rank * per_block), end = min(row.granules, begin + per_block);
@@ -908,26 +895,12 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kerne
         write_top(p, at, r, sh);
     }
     if (!GRAD && blocks > 1) cluster_done();
-    if (blocks > 1) cluster_await_done();                 // no block leaves while another may read its shared memory
-}
-
-// A launch of rows * blocks blocks, `blocks` of them a cluster.
-cudaLaunchConfig_t row_config(long long rows, int blocks, int threads, cudaLaunchAttribute &attr, cudaStream_t stream) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(rows * blocks));
-    cfg.blockDim = dim3(threads);
-    cfg.stream = stream;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = blocks;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = blocks > 1 ? 1 : 0;
-    return cfg;
+    if (blocks > 1) cluster_wait();                 // no block leaves while another may read its shared memory
 }
 
 template <typename T, int BLOCK, int U, bool GRAD, bool ENT> int launch_held(const RowsArgs &p, int blocks, cudaStream_t stream) {
     cudaLaunchAttribute attr = {};
-    const cudaLaunchConfig_t cfg = row_config(p.rows, blocks, BLOCK, attr, stream);
+    const cudaLaunchConfig_t cfg = cluster_config(dim3((unsigned)(p.rows * blocks)), BLOCK, 0, blocks, &attr, stream);
     if (cudaLaunchKernelEx(&cfg, token_logprobs_held_kernel<T, BLOCK, U, GRAD, ENT>, p, blocks) != cudaSuccess) return PARLE_ECUDA;
     return launch_status();
 }
@@ -936,6 +909,10 @@ template <typename T, bool GRAD, bool ENT> int launch_rows(const RowsArgs &p, in
     // granules of a row, one more where rows do not all begin on 16-byte boundaries
     const long long granules = ((long long)p.vocab * sizeof(T) + 15) / 16 + (reinterpret_cast<uintptr_t>(p.logits) % 16 || p.ld * sizeof(T) % 16 ? 1 : 0);
     constexpr int U = 8;
+    // Short rows: a warp each; two where so many alternatives are wanted that 32 groups set their bound too low.  Measured, 8192 x 500
+    // bf16 logits, a warp / two: 5 alternatives 16.5 / 29 us, 20: 23 / 33, 32: 91 / 35.
+    if constexpr (!GRAD)
+        if (p.k > 24 && granules <= 64 * 4) return launch_held<T, 64, 4, GRAD, ENT>(p, 1, stream);
     if (granules <= 32 * 4) return launch_held<T, 32, 4, GRAD, ENT>(p, 1, stream);
     if (granules <= 32 * U) return launch_held<T, 32, U, GRAD, ENT>(p, 1, stream);
     if (granules <= 128 * U) return launch_held<T, 128, U, GRAD, ENT>(p, 1, stream);
@@ -963,8 +940,8 @@ template <typename T, bool GRAD, bool ENT> int launch_rows(const RowsArgs &p, in
 }
 
 template <typename T> int launch_logprobs(const RowsArgs &p, bool grad, cudaStream_t stream) {
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return PARLE_ECUDA;
+    const int sms = current_sms();
+    if (sms < 0) return PARLE_ECUDA;
     if (!grad) return launch_rows<T, false, true>(p, sms, stream);
     return p.entropy || p.d_entropy ? launch_rows<T, true, true>(p, sms, stream) : launch_rows<T, true, false>(p, sms, stream);
 }

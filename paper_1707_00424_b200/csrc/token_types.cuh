@@ -3,6 +3,8 @@
 
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "common.cuh"
 
 namespace parle {
@@ -101,6 +103,51 @@ template <typename F> int with_dtype(int dtype, F f) {
 __device__ __forceinline__ long long quotient(long long a, long long b) {
     if (((a | b) >> 32) == 0) return (uint32_t)a / (uint32_t)b;
     return a / b;
+}
+
+// SMs of the current device; -1 if it cannot be asked.
+inline int current_sms() {
+    static std::atomic<int> known[64];
+    int dev = -1, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return -1;
+    if (dev < 64 && (sms = known[dev].load(std::memory_order_relaxed)) > 0) return sms;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return -1;
+    if (dev < 64) known[dev].store(sms, std::memory_order_relaxed);
+    return sms;
+}
+
+// ---- thread-block clusters ----
+
+__device__ __forceinline__ int cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return (int)r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+// Says that this thread is done with the other blocks' shared memory; cluster_wait() then waits until all are.  (Relaxed: it orders
+// no memory, so nobody's stores in flight are waited for.)
+__device__ __forceinline__ void cluster_done() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
+// Address of another block's copy of a shared variable.
+template <typename V> __device__ __forceinline__ V *at_rank(V *p, int rank) {
+    uint64_t r;
+    asm volatile("mapa.u64 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<uint64_t>(p)), "r"(rank));
+    return reinterpret_cast<V *>(r);
+}
+
+// A launch of blocks in clusters of `cluster` along x (1: none).  attr: room for the attribute.
+inline cudaLaunchConfig_t cluster_config(dim3 grid, int threads, size_t shared_bytes, int cluster, cudaLaunchAttribute *attr, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared_bytes;
+    cfg.stream = stream;
+    attr->id = cudaLaunchAttributeClusterDimension;
+    attr->val.clusterDim.x = cluster;
+    attr->val.clusterDim.y = attr->val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 1 : 0;
+    return cfg;
 }
 
 inline int launch_status() { return cudaGetLastError() == cudaSuccess ? PARLE_OK : PARLE_ECUDA; }
