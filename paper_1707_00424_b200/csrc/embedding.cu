@@ -481,12 +481,14 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const GradArg
                 places_out[(long long)cluster * p.length + place] = item.y;
             }
         }
-        cluster_arrive();
-        // while the others come: which tokens occur (the words were zero before the pass's first barrier; the next pass's items
-        // come here after its first barrier)
-        if (pass == 0)
-            for (int i0 = 0; i0 < mine; i0 += kSortThreads) note_occurs(p, cluster, i0 + (int)threadIdx.x < mine ? items[i0 + threadIdx.x].x : INT_MAX);
-        cluster_wait();                                   // what the others put here has arrived; their reads here are done
+        if (pass + 1 < passes) {
+            cluster_arrive();                             // what the others put here has arrived; their reads here are done
+        } else {
+            // (nobody waits for the results here.)  Which tokens occur: the words were zero before the pass's first barrier
+            cluster_done();
+            for (int i0 = 0; i0 < mine; i0 += kSortThreads) note_occurs(p, cluster, i0 + (int)threadIdx.x < mine ? in[i0 + threadIdx.x].x : INT_MAX);
+        }
+        cluster_wait();
     }
 }
 
