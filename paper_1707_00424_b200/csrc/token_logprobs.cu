@@ -579,7 +579,8 @@ __device__ __forceinline__ void write_top(const RowsArgs &p, long long at, const
     if (p.top_logprob) p.top_logprob[at * p.k + threadIdx.x] = undefined ? r.inv_s : real ? r.logprob(key_value(key)) : -INFINITY;
 }
 
-// Rows of any length, streamed: one block per row.
+// Rows of any length, streamed: one block per row.  2048 x 131072 bf16 logits: 88 us, 0.93 of the copy rate, without alternatives, 98-100
+// with eight; exponentials (a warp instruction takes 7.8 cycles of their pipe) and issue slots are both in use at 62-65 %.
 template <typename T, int BLOCK, int U>
 __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_kernel(const RowsArgs p) {
     __shared__ Shared<BLOCK> sh;
@@ -737,7 +738,8 @@ template <typename T, int BLOCK> __device__ __forceinline__ void zero_row(const 
 }
 
 // The gradient of long rows, by a block each: a second pass reads the row again, from L2.  Its reads and the stores are marked as the
-// last use of their lines, so that rows between their two passes stay.
+// last use of their lines, so that rows between their two passes stay (a fifth of them does not).  2048 x 131072 bf16 logits: 200-204 us;
+// two exponentials per logit take 116 us of their pipe, the bytes 164 us at the copy rate.
 template <typename T, int BLOCK, int U, bool ENT>
 __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_grad_kernel(const RowsArgs p) {
     __shared__ SharedSums<BLOCK> sh;
@@ -895,7 +897,7 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kerne
         write_top(p, at, r, sh);
     }
     if (!GRAD && blocks > 1) cluster_done();
-    if (blocks > 1) cluster_wait();                 // no block leaves while another may read its shared memory
+    if (blocks > 1) cluster_wait();                       // no block leaves while another may read its shared memory
 }
 
 template <typename T, int BLOCK, int U, bool GRAD, bool ENT> int launch_held(const RowsArgs &p, int blocks, cudaStream_t stream) {

@@ -245,6 +245,24 @@ def test_gradient_of_masked_and_undefined_rows(dtype, vocab, split):
         check_grad(x[cut].clone(), tokens[cut], g[cut] * 0, None, 1.0, inplace=True, outputs=True)
 
 
+def test_logprobs_beyond_32_bit_offsets():
+    rows, vocab = 33000, 131072                                            # 4.3e9 logits
+    x = torch.zeros(rows, vocab, dtype=torch.bfloat16, device=DEV)
+    pick = torch.tensor([0, 16383, 16384, 32767, 32768, rows - 1], device=DEV)
+    x[pick] = torch.randn(6, vocab, device=DEV).bfloat16()
+    t = torch.randint(0, vocab, (rows,), device=DEV, dtype=torch.int32)
+    lp, h, top, toplp = pb.token_logprobs(x, t, k=3)
+    few = pb.token_logprobs(x[pick].contiguous(), t[pick].contiguous(), k=3)
+    # the few rows are summed by other blocks: another order of the same sums
+    assert torch.allclose(lp[pick], few[0], atol=1e-5) and torch.allclose(h[pick], few[1], atol=1e-4) and torch.equal(top[pick], few[2])
+    g = torch.randn(rows, device=DEV)
+    want = pb.token_logprobs_grad(x[pick].contiguous(), t[pick].contiguous(), g[pick].contiguous())
+    pb.token_logprobs_grad(x, t, g, dlogits=x)
+    assert torch.allclose(x[pick].float(), want.float(), rtol=2 ** -7, atol=1e-7)       # a step of bf16
+    del x, want
+    torch.cuda.empty_cache()
+
+
 def test_rows_without_an_incoming_gradient_are_zero_whatever_their_logits():
     x = torch.full((3, 70001), math.nan, device=DEV, dtype=torch.bfloat16)
     x[1] = 1.0
@@ -279,6 +297,13 @@ def test_bad_tokens_set_the_flag_and_count_as_none():
     pb.token_logprobs_grad(x, t, torch.ones(4, device=DEV), flags=flags)
     pb.embedding(x, t % 4, flags=flags); pb.embedding(x, t.clamp(max=3), flags=flags); pb.embedding_grad(x, t, 30, flags=flags)
     assert flags.item() == 0
+    for length in (1500, 6000, 40000):                                    # each way of sorting
+        many, rows = torch.randint(-1, 30, (length,), dtype=torch.int32, device=DEV), torch.randn(length, 8, device=DEV)
+        want = pb.embedding_grad(rows, many, 30, flags=flags)
+        assert flags.item() == 0
+        wrong = torch.where(many == -1, torch.full_like(many, 30), many)
+        assert torch.equal(pb.embedding_grad(rows, wrong, 30, flags=flags), want) and flags.item() == pb.FLAG_BAD_LABEL
+        flags.zero_()
     bad = torch.tensor([30, -2, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device=DEV)
     for call in (lambda: pb.token_logprobs(x, bad, flags=flags)[0], lambda: pb.embedding(x, bad, flags=flags),
                  lambda: pb.embedding_grad(x, bad, 30, flags=flags), lambda: pb.token_logprobs_grad(x, bad, torch.ones(4, device=DEV), flags=flags)):
@@ -336,6 +361,21 @@ def test_embedding_beyond_32_bit_offsets():
     pb.embedding_grad(dout, last, 300000, 1.0, dtable=grad, accumulate=True)
     assert (grad[last.long()] == 3).all()
     del grad
+    torch.cuda.empty_cache()
+
+
+def test_embedding_gradient_of_an_input_beyond_32_bit_offsets():
+    length, vocab, dim = 540000, 700, 8192                                # 4.4e9 elements
+    dout = torch.zeros(length, dim, dtype=torch.bfloat16, device=DEV)
+    pick = [0, 262143, 262144, 524287, 524288, length - 1]
+    t = torch.randint(0, vocab, (length,), device=DEV, dtype=torch.int32)
+    want = torch.zeros(vocab, device=DEV)
+    for i, at in enumerate(pick):
+        dout[at] = i + 1
+        want[t[at]] += i + 1
+    got = pb.embedding_grad(dout, t, vocab)
+    assert torch.equal(got, want[:, None].expand(vocab, dim))
+    del dout, got
     torch.cuda.empty_cache()
 
 
