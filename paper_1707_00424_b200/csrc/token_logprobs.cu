@@ -600,20 +600,15 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_kernel(con
     const unsigned long long bound = top_bound(p.k, sh);
     if (best && best >= bound) sh.owner[atomicAdd(&sh.owners, 1)] = threadIdx.x;
     __syncthreads();
-    // the granules of the threads that reach the bound, read by all threads, four in flight
-    const int per_owner = (row.granules + BLOCK - 1) / BLOCK, items = sh.owners * per_owner;
-    for (int i0 = threadIdx.x; i0 < items; i0 += BLOCK * 4) {
-        Granule<T> raw[4];
-        int q[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = i0 + u * BLOCK;
-            q[u] = i < items ? sh.owner[i / per_owner] + (i % per_owner) * BLOCK : row.granules;
-            raw[u] = row.load(q[u], row.granules);
+    // the granules of the threads that reach the bound, a warp for each of these threads, two in flight per lane
+    const int owners = sh.owners;
+    for (int o = threadIdx.x / 32; o < owners; o += BLOCK / 32)
+        for (int q0 = sh.owner[o] + (int)threadIdx.x % 32 * BLOCK; q0 < row.granules; q0 += 64 * BLOCK) {
+            const int q1 = q0 + 32 * BLOCK;
+            const Granule<T> first = row.load(q0, row.granules), second = row.load(q1, row.granules);
+            hand_on(row, first, q0, bound, sh);
+            if (q1 < row.granules) hand_on(row, second, q1, bound, sh);
         }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) hand_on(row, raw[u], q[u], bound, sh);
-    }
     __syncthreads();
     rank_candidates(row, 0, row.granules, p.k, sh);
     write_top(p, at, r, sh);
