@@ -1,13 +1,15 @@
-"""Build libparle.so (sm_100a) in-tree with nvcc."""
+"""Build libparle.so (sm_100a) with nvcc and the token operators' Python module _token_ops.so with g++, both in-tree."""
 from __future__ import annotations
 
 import os
 import shutil
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libparle.so")
+MODULE = os.path.join(HERE, "_token_ops.so")
 SOURCES = ["parle_api.cu", "static_loss.cu", "token_logprobs.cu", "embedding.cu", "dropout.cu"]
 HEADERS = ["common.cuh", "mlp_simt.cuh", "umma_gemm.cuh", "umma_pair_gemm.cuh", "umma_wgrad_update.cuh", "umma_tf32x3.cuh", "update_kernels.cuh", "token_types.cuh"]
 
@@ -19,30 +21,52 @@ def _nvcc() -> str:
     raise RuntimeError("nvcc not found: the Parle CUDA library cannot be built")
 
 
-def _stale() -> bool:
-    if not os.path.exists(LIB):
+def _stale(target: str, sources) -> bool:
+    if not os.path.exists(target):
         return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS]
+    t = os.path.getmtime(target)
+    deps = [os.path.join(CSRC, f) for f in sources]
     deps.append(os.path.join(HERE, "..", "include", "parle.h"))
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _run(cmd) -> str:
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"{os.path.basename(cmd[0])} failed:\n" + res.stdout + res.stderr)
+    return res.stderr
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile the library if it is missing or older than its sources; return its path."""
-    if not force and not _stale():
+    if not force and not _stale(LIB, SOURCES + HEADERS):
         return LIB
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--threads", "0",
            "-shared", "-Xcompiler", "-fPIC", "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
     if verbose:
         cmd.insert(1, "-Xptxas=-v")
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
+    log = _run(cmd)
     if verbose:
-        print(res.stderr)
+        print(log)
     return LIB
+
+
+def build_module(force: bool = False) -> str:
+    """Compile the Python module of the token operators, which calls the library beside it, for the torch that is installed."""
+    build()
+    if not force and not _stale(MODULE, ["token_bindings.cpp"]):
+        return MODULE
+    import torch
+    at = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(_nvcc())))
+    _run([shutil.which("g++") or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DBUILT_FOR_TORCH="{torch.__version__}"', "-isystem", os.path.join(at, "include"),
+          "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(cuda, "include"), os.path.join(CSRC, "token_bindings.cpp"),
+          "-o", MODULE, "-L" + HERE, "-l:libparle.so", "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10",
+          "-Wl,-rpath,$ORIGIN"])
+    return MODULE
 
 
 if __name__ == "__main__":
     print(build(force=True, verbose=True))
+    print(build_module(force=True))
