@@ -13,6 +13,7 @@
 // common to every term of the row and to log S, so it cancels.
 #include <math.h>
 
+#include <algorithm>
 #include <initializer_list>
 #include <type_traits>
 
@@ -120,6 +121,18 @@ template <typename T> struct Granule {
         return r;
     }
     __device__ __forceinline__ float largest() const { return largest_of<T, 1>({*this}); }
+    // of the elements of even and of odd number
+    __device__ __forceinline__ void largest_two(float &even, float &odd) const {
+        if constexpr (sizeof(T) == 4) {
+            even = fmaxf(__uint_as_float(raw.x), __uint_as_float(raw.z));
+            odd = fmaxf(__uint_as_float(raw.y), __uint_as_float(raw.w));
+        } else {
+            using T2 = std::conditional_t<std::is_same<T, __half>::value, __half2, __nv_bfloat162>;
+            const T2 *h = reinterpret_cast<const T2 *>(&raw), m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+            even = to_float(m.x);
+            odd = to_float(m.y);
+        }
+    }
 };
 
 // Largest element of some granules; NaN is passed over (the sums carry it).
@@ -237,8 +250,9 @@ template <int BLOCK> struct SharedSums {
 };
 
 template <int BLOCK> struct Shared : SharedSums<BLOCK> {
-    static constexpr int kGroups = BLOCK < 64 ? BLOCK : 64;      // thread groups whose maxima bound the k-th largest logit from below
-    unsigned long long group[BLOCK];                      // the threads' best (logit, granule)
+    // groups of logits whose maxima bound the k-th largest from below (a warp's: 32, or two a thread)
+    static constexpr int kGroups = BLOCK < 64 ? BLOCK : 64;
+    alignas(16) unsigned long long group[BLOCK < 64 ? 64 : BLOCK];      // the threads' best (logit, granule)
     unsigned long long bound;
     int found, owners;
     int owner[BLOCK];
@@ -287,41 +301,61 @@ template <int BLOCK> __device__ __forceinline__ void offer_best(unsigned long lo
     if (threadIdx.x == 0) { sh.found = 0; sh.owners = 0; sh.bound = 0; }
 }
 
-// After it: the bound, as (logit, granule); 0 where fewer than k groups have a logit.
-template <int BLOCK> __device__ __forceinline__ unsigned long long top_bound(int k, Shared<BLOCK> &sh) {
-    constexpr int G = Shared<BLOCK>::kGroups, PARTS = BLOCK / G;
-    if constexpr (PARTS > 1) {
-        if (threadIdx.x < G) {
-            unsigned long long g = sh.group[threadIdx.x];
+// The same with two groups a thread, for rows of one warp: its logits of even and of odd number, as (logit, 2 granule + 0 or 1).
+__device__ __forceinline__ void offer_two(unsigned long long even, unsigned long long odd, Shared<32> &sh) {
+    offer_best<32>(even, sh);
+    sh.group[threadIdx.x + 32] = odd;
+}
+
+// After it: the bound, as (logit, granule); 0 where fewer than G groups' k have a logit.  No two groups' keys are the same, but for 0.
+template <int G, int BLOCK> __device__ __forceinline__ unsigned long long top_bound(int k, Shared<BLOCK> &sh) {
+    if constexpr (BLOCK < G) {                            // two groups a thread
+        const ulonglong2 g = *reinterpret_cast<const ulonglong2 *>(&sh.group[2 * threadIdx.x]);
+        int above0 = 0, above1 = 0;
 #pragma unroll
-            for (int t = threadIdx.x + G; t < BLOCK; t += G) g = max(g, sh.group[t]);
-            sh.group[threadIdx.x] = g;
+        for (int t = 0; t < G; t += 2) {
+            const ulonglong2 o = *reinterpret_cast<const ulonglong2 *>(&sh.group[t]);
+            above0 += (o.x > g.x) + (o.y > g.x);
+            above1 += (o.x > g.y) + (o.y > g.y);
         }
-        __syncthreads();
+        if (above0 == k - 1) sh.bound = g.x;
+        if (above1 == k - 1) sh.bound = g.y;
+    } else {
+        constexpr int PARTS = BLOCK / G;
+        if constexpr (PARTS > 1) {
+            if (threadIdx.x < G) {
+                unsigned long long g = sh.group[threadIdx.x];
+#pragma unroll
+                for (int t = threadIdx.x + G; t < BLOCK; t += G) g = max(g, sh.group[t]);
+                sh.group[threadIdx.x] = g;
+            }
+            __syncthreads();
+        }
+        const int i = threadIdx.x / PARTS, part = threadIdx.x % PARTS;
+        const unsigned long long g = sh.group[i];
+        int above = 0;
+#pragma unroll
+        for (int t = part; t < G; t += PARTS) above += sh.group[t] > g;
+#pragma unroll
+        for (int o = PARTS / 2; o > 0; o >>= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
+        if (above == k - 1 && part == 0) sh.bound = g;
     }
-    const int i = threadIdx.x / PARTS, part = threadIdx.x % PARTS;
-    const unsigned long long g = sh.group[i];
-    int above = 0;
-#pragma unroll
-    for (int t = part; t < G; t += PARTS) above += sh.group[t] > g || (sh.group[t] == g && t < i);
-#pragma unroll
-    for (int o = PARTS / 2; o > 0; o >>= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
-    if (above == k - 1 && part == 0) sh.bound = g;
     __syncthreads();
     return sh.bound;
 }
 
 // Hands on a granule's logits that reach the bound.
-template <typename T, int BLOCK>
+template <bool TWO = false, typename T, int BLOCK>
 __device__ __forceinline__ void hand_on(const Row<T> &row, const Granule<T> &raw, int q, unsigned long long bound, Shared<BLOCK> &sh) {
     constexpr int N = Granule<T>::N;
-    if (order_key(raw.largest(), (uint32_t)q) < bound) return;       // (a granule of NaN alone compares either way)
+    const uint32_t place = TWO ? 2 * q : q;
+    if (order_key(raw.largest(), place) < bound) return;  // (a granule of NaN alone compares either way)
     float v[N];
     raw.get(v);
     const int e0 = row.first_element(q);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        if (!(v[i] > -INFINITY) || order_key(v[i], (uint32_t)q) < bound) continue;      // (beside the row lies -inf)
+        if (!(v[i] > -INFINITY) || order_key(v[i], TWO ? place + i % 2 : place) < bound) continue;      // (beside the row lies -inf)
         const int at = atomicAdd(&sh.found, 1);
         if (at < kCandidates) sh.candidate[at] = order_key(v[i], (uint32_t)(e0 + i));
     }
@@ -597,7 +631,7 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_kernel(con
         given.note_bad(p);
     }
     if (p.k == 0) return;
-    const unsigned long long bound = top_bound(p.k, sh);
+    const unsigned long long bound = top_bound<Shared<BLOCK>::kGroups>(p.k, sh);
     if (best && best >= bound) sh.owner[atomicAdd(&sh.owners, 1)] = threadIdx.x;
     __syncthreads();
     // the granules of the threads that reach the bound, a warp for each of these threads, two in flight per lane
@@ -795,8 +829,9 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_grad_kerne
 }
 
 // Rows held in registers, U granules a thread, by a block or a cluster of blocks: everything is in flight at once and read once,
-// and the gradient is formed from what is held.  GRAD: the gradient (ENT: with an entropy's); else log probabilities, entropy, top.
-template <typename T, int BLOCK, int U, bool GRAD, bool ENT>
+// and the gradient is formed from what is held.  GRAD: the gradient (ENT: with an entropy's); else log probabilities, entropy, top
+// (TWO: from two groups a thread).
+template <typename T, int BLOCK, int U, bool GRAD, bool ENT, bool TWO>
 __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kernel(const RowsArgs p, int blocks) {
     __shared__ Shared<BLOCK> sh;
     constexpr int P = Granule<T>::N / 2;
@@ -813,16 +848,22 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kerne
     const TokenShare<T> share(row, given, q0, BLOCK, GRAD ? end : 0);
     Granule<T> raw[U];
     row.load_all(q0, BLOCK, end, raw);
-    float top = -INFINITY;
-    int best_granule = -1;
+    float top = -INFINITY, top_odd = -INFINITY;
+    int best_granule = -1, best_odd = -1;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const float v = raw[u].largest();
+        float v, odd;
+        if constexpr (TWO) {
+            raw[u].largest_two(v, odd);
+            if (odd > top_odd) { top_odd = odd; best_odd = q0 + u * BLOCK; }
+        } else {
+            v = raw[u].largest();
+        }
         if (v > top) { top = v; best_granule = q0 + u * BLOCK; }
     }
     const float c = p.scale_log2e;
     Sums t;
-    t.r = fmaxf(top * c, -kNear);
+    t.r = fmaxf((TWO ? fmaxf(top, top_odd) : top) * c, -kNear);
     {
         const uint32_t low = low_bound<T>(c);
         const float_pair c2 = pair(c, c), r2 = pair(-t.r, -t.r);
@@ -846,20 +887,26 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kerne
         split(s2, lo, hi); t.s = lo + hi;
         split(a2, lo, hi); t.a = lo + hi;
     }
-    const unsigned long long best = best_granule >= 0 ? order_key(top, (uint32_t)best_granule) : 0;
-    if (!GRAD && p.k > 0) offer_best(best, sh);
+    unsigned long long best = best_granule >= 0 ? order_key(top, (uint32_t)(TWO ? 2 * best_granule : best_granule)) : 0;
+    if constexpr (TWO) {
+        const unsigned long long odd = best_odd >= 0 ? order_key(top_odd, (uint32_t)(2 * best_odd + 1)) : 0;
+        offer_two(best, odd, sh);
+        best = max(best, odd);
+    } else if constexpr (!GRAD) {
+        if (p.k > 0) offer_best(best, sh);
+    }
     t = block_sums<BLOCK>(t, sh);
-    if (!GRAD && p.k > 0) {
-        const unsigned long long bound = top_bound(p.k, sh);
+    if constexpr (!GRAD) if (p.k > 0) {
+        const unsigned long long bound = top_bound<TWO ? 64 : Shared<BLOCK>::kGroups>(p.k, sh);
         if (best && best >= bound) {                      // few threads, and mostly one granule of each: it is read again
             unsigned reach = 0;
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (order_key(raw[u].largest(), (uint32_t)(q0 + u * BLOCK)) >= bound) reach |= 1u << u;
+                if (order_key(raw[u].largest(), (uint32_t)((TWO ? 2 : 1) * (q0 + u * BLOCK))) >= bound) reach |= 1u << u;
             while (reach) {
                 const int q = q0 + (__ffs(reach) - 1) * BLOCK;
                 reach &= reach - 1;
-                if (q < end) hand_on(row, row.load(q, end), q, bound, sh);
+                if (q < end) hand_on<TWO>(row, row.load(q, end), q, bound, sh);
             }
         }
         __syncthreads();
@@ -895,10 +942,10 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kerne
     if (blocks > 1) cluster_wait();                       // no block leaves while another may read its shared memory
 }
 
-template <typename T, int BLOCK, int U, bool GRAD, bool ENT> int launch_held(const RowsArgs &p, int blocks, cudaStream_t stream) {
+template <typename T, int BLOCK, int U, bool GRAD, bool ENT, bool TWO = false> int launch_held(const RowsArgs &p, int blocks, cudaStream_t stream) {
     cudaLaunchAttribute attr = {};
     const cudaLaunchConfig_t cfg = cluster_config(dim3((unsigned)(p.rows * blocks)), BLOCK, 0, blocks, &attr, stream);
-    if (cudaLaunchKernelEx(&cfg, token_logprobs_held_kernel<T, BLOCK, U, GRAD, ENT>, p, blocks) != cudaSuccess) return PARLE_ECUDA;
+    if (cudaLaunchKernelEx(&cfg, token_logprobs_held_kernel<T, BLOCK, U, GRAD, ENT, TWO>, p, blocks) != cudaSuccess) return PARLE_ECUDA;
     return launch_status();
 }
 
@@ -906,19 +953,33 @@ template <typename T, bool GRAD, bool ENT> int launch_rows(const RowsArgs &p, in
     // granules of a row, one more where rows do not all begin on 16-byte boundaries
     const long long granules = ((long long)p.vocab * sizeof(T) + 15) / 16 + (reinterpret_cast<uintptr_t>(p.logits) % 16 || p.ld * sizeof(T) % 16 ? 1 : 0);
     constexpr int U = 8;
-    // Short rows: a warp each; two where so many alternatives are wanted that 32 groups set their bound too low.  Measured, 8192 x 500
-    // bf16 logits, a warp / two: 5 alternatives 16.5 / 29 us, 20: 23 / 33, 32: 91 / 35.
+    // Short rows: a warp each; with two groups a thread where so many alternatives are wanted that 32 groups, or a very short row's
+    // fewer, set their bound too low.  Measured, with / without: 8192 x 500 bf16 logits, 20 alternatives 19.3 us without, 25: 22.3 / 23.8,
+    // 32: 24.4 / 88; 6827 x 150, 20: 16.8 / 46.
     if constexpr (!GRAD)
-        if (p.k > 24 && granules <= 64 * 4) return launch_held<T, 64, 4, GRAD, ENT>(p, 1, stream);
+        if (4LL * p.k > 3 * std::min(32LL, granules) && granules <= 32 * U)
+            return granules <= 32 * 4 ? launch_held<T, 32, 4, GRAD, ENT, true>(p, 1, stream) : launch_held<T, 32, U, GRAD, ENT, true>(p, 1, stream);
     if (granules <= 32 * 4) return launch_held<T, 32, 4, GRAD, ENT>(p, 1, stream);
     if (granules <= 32 * U) return launch_held<T, 32, U, GRAD, ENT>(p, 1, stream);
     if (granules <= 128 * U) return launch_held<T, 128, U, GRAD, ENT>(p, 1, stream);
+    // Few rows, held by larger blocks.  Measured, held / streamed: 148 rows of 12000 bf16 logits 6.2 / 6.3 us (gradient 4.9 / 5.3, one row
+    // 4.8 / 5.0); gradient of 26549 bf16 logits, 1 row 6.5 / 7.9, 148 rows 6.8 / 8.8, 296 rows 9.4 / 10.2, 592 rows 16.7 / 14.5 (log
+    // probabilities of 148 rows: 6.9 / 6.2).
+    if (granules <= 256 * U) {
+        if (p.rows <= sms) return launch_held<T, 256, U, GRAD, ENT>(p, 1, stream);
+    } else if (GRAD && granules <= 512 * U && p.rows <= 2 * sms) {
+        return launch_held<T, 512, U, GRAD, ENT>(p, 1, stream);
+    }
     // Few long rows: a cluster of up to 8 blocks each (a cluster costs some microseconds of its own).  Measured, 131072 bf16 logits,
     // cluster against one block: 1 row 6.5 / 10.8 us (gradient 8.4 / 16.7), 32 rows 8.6 / 11.8 (10.5 / 16.7), 64 rows 10.6 / 12.4
-    // (12.6 / 16.7), 128 rows 16.9 / 12.6 (20.9 / 16.6); 20000 bf16 logits, 1 row: 6.5 / 5.9 (8.0 / 7.5).
-    const long long blocks = (granules + 256 * U - 1) / (256 * U);
-    if (granules > 4096 && blocks <= kClusterMost && p.rows * blocks <= (GRAD ? 4 : 2) * sms)
-        return launch_held<T, 256, U, GRAD, ENT>(p, (int)blocks, stream);
+    // (12.6 / 16.7), 128 rows 16.9 / 12.6 (20.9 / 16.6); 20000 bf16 logits, 1 row: 6.5 / 5.9 (8.0 / 7.5).  131072 fp32 logits, blocks of
+    // 512 threads, 1 row: 7.7 / 10.8 (6.1 / 18.7); 96788 fp32 logits, 13 rows: 7.9 / 9.3 (6.5 / 15.7), 37 rows: - / 9.4 (8.9 / 15.7).
+    const long long blocks = (granules + 256 * U - 1) / (256 * U), large = (granules + 512 * U - 1) / (512 * U);
+    if (granules > 4096 && blocks <= kClusterMost) {
+        if (p.rows * blocks <= (GRAD ? 4 : 2) * sms) return launch_held<T, 256, U, GRAD, ENT>(p, (int)blocks, stream);
+    } else if (blocks > kClusterMost && large <= kClusterMost) {
+        if (p.rows * large <= (GRAD ? 2 : 1) * sms) return launch_held<T, 512, U, GRAD, ENT>(p, (int)large, stream);
+    }
     // One block a row.  More threads where fewer rows between the gradient's two passes keep them in L2, fewer where what a block does
     // per row (joining sums, ranking) counts.  Measured: gradient of 2048 x 131072 bf16 logits with 512 / 256 threads 204 / 231 us, 1024 x
     // 65536 59 / 60, 1024 x 32760 with 256 / 128 threads 33 / 30.5, 4096 x 10000 51 / 41; log probabilities with alternatives of 1024 x

@@ -678,3 +678,48 @@ def test_embedded_and_dropped_minibatches_through_an_inner_step():
     # the step's loss is the mean of -log p of its labels, both from the same logits: fp32 rounding of the step's own kernel
     assert torch.allclose(loss, -lp.mean(dim=1), rtol=1e-5, atol=1e-5)
     assert torch.equal(top.long(), logits.topk(5).indices) and (h > 0).all() and (toplp[..., 0] >= lp).all()
+
+
+# ---- rows by larger blocks, two groups of logits a thread -----------------------------------------------------------------------
+
+LONG = {torch.float32: 100003, torch.bfloat16: 200001, torch.float16: 200001}      # longer than eight blocks of 256 threads hold
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows, pad, shift, k", [(1, 0, 0, 32), (13, 1, 3, 8), (20, 0, 0, 0), (50, 0, 1, 5)])
+def test_logprobs_of_very_long_rows(dtype, rows, pad, shift, k):
+    x, tokens, rng = random_rows(rows, LONG[dtype], dtype, rows)
+    check_logprobs(strided(x, pad, shift), tokens, 0.7, k)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_masked_tied_and_undefined_rows_of_very_long_rows(dtype):
+    vocab = LONG[dtype]
+    x = special_rows(vocab, dtype)
+    tokens = np.array([(7 * r + 1) % vocab for r in range(x.shape[0])])
+    check_logprobs(x, tokens, 1.0, 9)
+    rng = np.random.default_rng(1)
+    g, h = rng.normal(size=x.shape[0]), rng.normal(size=x.shape[0])
+    for inplace in (False, True):
+        check_grad(x.clone(), tokens, g, h, 1.0, inplace=inplace)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows, granules, pad, shift", [(1, 1300, 0, 0), (148, 1025, 1, 1), (149, 2047, 0, 0), (1, 2049, 0, 0), (5, 4095, 3, 2),
+                                                        (296, 2100, 0, 0), (297, 2100, 0, 0), (3, 16700, 0, 0), (20, 20000, 5, 1)])
+def test_gradient_of_few_rows_by_larger_blocks(dtype, rows, granules, pad, shift):
+    vocab = granules * (4 if dtype == torch.float32 else 8) - 3
+    x, tokens, rng = random_rows(rows, vocab, dtype, granules)
+    tokens[rng.random(rows) < 0.2] = -1
+    g, h = rng.normal(size=rows), rng.normal(size=rows) * (rows % 2)
+    check_grad(x, tokens, g, h, 0.8, inplace=rows % 3 == 0, pad=pad, shift=shift)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows, vocab, pad, shift, k", [(300, 150, 0, 0, 20), (70, 150, 3, 1, 32), (50, 500, 0, 0, 25), (9, 1011, 0, 2, 32), (6, 2039, 0, 0, 32),
+                                                        (40, 33, 0, 0, 32), (40, 31, 1, 0, 32), (17, 8, 0, 0, 2), (17, 9, 0, 1, 2)])
+def test_many_alternatives_of_short_rows(dtype, rows, vocab, pad, shift, k):
+    x, tokens, rng = random_rows(rows, vocab, dtype, vocab)
+    x[::3] = x[::3].round()                                           # ties
+    x[1::3] = torch.where(torch.rand(x[1::3].shape, generator=torch.Generator().manual_seed(vocab)).to(DEV) < 0.8, -math.inf, x[1::3])
+    check_logprobs(strided(x, pad, shift), tokens, 1.0, k)
