@@ -723,3 +723,18 @@ def test_many_alternatives_of_short_rows(dtype, rows, vocab, pad, shift, k):
     x[::3] = x[::3].round()                                           # ties
     x[1::3] = torch.where(torch.rand(x[1::3].shape, generator=torch.Generator().manual_seed(vocab)).to(DEV) < 0.8, -math.inf, x[1::3])
     check_logprobs(strided(x, pad, shift), tokens, 1.0, k)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n, length, vocab, dim, pad", [
+    (1, 1025, 40, 256, 1), (1, 1056, 3, 257, 0), (2, 1100, 500, 511, 1), (1, 2000, 33, 512, 2), (1, 1500, 700, 513, 0), (1, 1300, 50, 769, 0),
+    (3, 1057, 9, 1023, 1), (1, 4200, 2000, 1025, 0), (1, 1040, 64, 2051, 0), (1, 9000, 11, 900, 4),
+])
+def test_embedding_gradient_of_rows_off_16_byte_boundaries(dtype, n, length, vocab, dim, pad):
+    """Skewed tokens: runs inside a chunk, over one border and over many."""
+    rng = np.random.default_rng(dim)
+    tokens = np.minimum(np.exp(rng.random((n, length)) * math.log(vocab + 1)) - 1, vocab - 1).astype(np.int32)
+    tokens[rng.random((n, length)) < 0.05] = -1
+    dout = torch.from_numpy(rng.normal(size=(n, length, dim + pad))).to(dtype).to(DEV)[:, :, :dim]
+    check_embedding_grad(dout, tokens, vocab, 0.9, pad=pad)
+    check_embedding_grad(dout, tokens, vocab, -1.7, accumulate=True, pad=pad)
