@@ -139,8 +139,121 @@ __global__ void __launch_bounds__(kThreads) dropout_rows_kernel(const DropoutArg
     }
 }
 
-// Any pitch and alignment, rows of at least kSegment elements: a warp takes kSegment elements of a row, which lie in at most 32
-// groups; every lane draws one group's numbers, then the warp walks over the elements 32 at a time, so that its accesses are
+// Eight elements as words.
+template <typename T> struct Words {
+    static constexpr int N = 2 * sizeof(T);               // words of eight elements
+    // N words of w from byte `at` on: 0 .. 15, even, the same in the whole warp
+    __device__ __forceinline__ static Pack8<T> from(uint32_t (&w)[N + 4], int at) {
+        if (at & 8) {
+#pragma unroll
+            for (int i = 0; i < N + 2; ++i) w[i] = w[i + 2];
+        }
+        if (at & 4) {
+#pragma unroll
+            for (int i = 0; i < N + 1; ++i) w[i] = w[i + 1];
+        }
+        if (sizeof(T) == 2 && (at & 2)) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+        }
+        Pack8<T> v;
+        uint32_t *to = reinterpret_cast<uint32_t *>(&v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) to[i] = w[i];
+        return v;
+    }
+};
+
+// A row, for a warp that takes some of it from `base` on.  Places are relative to that; the row lies at [low, high).
+template <typename T> struct Shifted {
+    const T *at;                                          // element `base` (may lie before the row)
+    int skew;                                             // bytes of it behind a 16-byte boundary
+    __device__ __forceinline__ Shifted(const void *array, long long ld, long long row, long long base) {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(array) + (uintptr_t)((row * ld + base) * (long long)sizeof(T));
+        at = reinterpret_cast<const T *>(a);
+        skew = (int)(a & 15);
+    }
+    // Elements o .. o + 7: from the 16-byte pieces that hold them, where those lie in the row; else one by one.
+    __device__ __forceinline__ Pack8<T> load(int o, int low, int high) const {
+        constexpr int S = sizeof(T);
+        if ((o - low) * S >= skew && (high - o - 8) * S >= ((16 - skew) & 15)) {
+            uint32_t w[Words<T>::N + 4];
+            const uint4 *from = reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(at + o) - skew);
+#pragma unroll
+            for (int i = 0; i < Words<T>::N / 4 + 1; ++i) {
+                const uint4 q = i < Words<T>::N / 4 || skew ? from[i] : make_uint4(0, 0, 0, 0);
+                w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+            }
+            return Words<T>::from(w, skew);
+        }
+        Pack8<T> v = {};
+        T *e = reinterpret_cast<T *>(&v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (o + i >= low && o + i < high) e[i] = at[o + i];
+        return v;
+    }
+};
+
+constexpr int kSteps = 4, kShifted = 96;                  // steps where there are many parts; shortest rows for many elements
+constexpr long long kFew = 1 << 18;
+// Any pitch and alignment: a warp takes 32 groups of a row at a time, a lane each, `steps` times.  Groups lie anywhere against 16-byte
+// boundaries, by the same number of bytes in all lanes: a lane loads the pieces that hold its group and shifts them, and stores the
+// piece that ends its left neighbour's group and begins its own.  Only at the ends of the row and of the 32 groups elements go one by one.
+// Bound by issue slots (shifting costs as much as the generator).  8192 x 4095 bf16 of pitch 4127 to 4095: 42 us, element by element 86;
+// with a residual, 4096 to 4095, 57 against 96; in one step a warp instead of four 54 and 66; 77 x 1001 2.4 against 3.3.
+template <typename T, bool RES>
+__global__ void __launch_bounds__(kThreads, 6) dropout_shifted_kernel(const DropoutArgs p, long long parts, long long per_row, int steps) {
+    const int lane = threadIdx.x % 32;
+    const long long s = (long long)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+    if (s >= parts) return;
+    const long long row = quotient(s, per_row), e0 = row * p.cols;
+    const long long base = (s - row * per_row) * steps * 256 - e0 % 8;
+    const Shifted<T> x(p.x, p.ld_x, row, base), r(p.residual, p.ld_r, row, base), y(p.y, p.ld_y, row, base);
+    const int shifted = y.skew / (int)sizeof(T);          // elements at a group's end that lie in the next lane's piece
+    const unsigned long long offset = call_offset(p);
+    const unsigned long long group = (unsigned long long)(e0 + base) / 8;
+    const int low = (int)max(-base, -1024LL), high = (int)min(p.cols - base, kSteps * 256 + 1024LL);      // (clipped where it does not matter)
+    for (int first = 0; first < min(steps * 256, high); first += 256) {
+        const int o = first + lane * 8;
+        const Pack8<T> in = x.load(o, low, high);
+        Pack8<T> add;
+        if (RES) add = r.load(o, low, high);
+        const Pack8<T> out = drop_group<T, RES>(p, in, add, group + o / 8, offset);
+        T *const to = const_cast<T *>(y.at) + o;
+        const bool whole = o >= low && o + 8 <= high;
+        if (y.skew == 0 && whole) {
+            out.store(to);
+            continue;
+        }
+        bool joined = false, joined_next = false;
+        if (y.skew) {
+            const unsigned wholes = __ballot_sync(0xffffffffu, whole);
+            const uint32_t *own = reinterpret_cast<const uint32_t *>(&out);
+            constexpr int N = Words<T>::N;
+            uint32_t w[N + 4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __shfl_up_sync(0xffffffffu, own[N - 4 + i], 1);
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[4 + i] = own[i];
+            const unsigned both = wholes & (wholes << 1); // lanes whose piece is all theirs and their neighbour's
+            joined = (both >> lane) & 1u;
+            joined_next = lane < 31 && ((both >> (lane + 1)) & 1u);
+            const Pack8<T> piece = Words<T>::from(w, 16 - y.skew);
+            if (joined) piece.store(to - shifted);
+        }
+        const T *e = reinterpret_cast<const T *>(&out);
+        const int from = joined ? 8 - shifted : 0, until = joined_next ? 8 - shifted : 8;
+        if (from < until) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i >= from && i < until && o + i >= low && o + i < high) to[i] = e[i];
+        }
+    }
+}
+
+// The same for many elements of fp32, whose single accesses are wide enough: a warp takes kSegment elements of a row, which lie in
+// at most 32 groups; every lane draws one group's numbers, then the warp walks over the elements 32 at a time, so that its accesses are
 // consecutive, and each lane fetches its element's keep bit from the lane that drew it.  All loads come before the stores (y may
 // be x).
 constexpr int kSegment = 248;
@@ -177,7 +290,7 @@ __global__ void __launch_bounds__(kThreads) dropout_segments_kernel(const Dropou
     }
 }
 
-// Shorter rows, and contiguous arrays off 16-byte boundaries: the same over 32 consecutive groups (256 elements in row-major order).
+// Many shorter rows: the same over 32 consecutive groups (256 elements in row-major order).
 template <typename T>
 __global__ void __launch_bounds__(kThreads) dropout_elements_kernel(const DropoutArgs p, long long elements) {
     const int lane = threadIdx.x % 32;
@@ -242,16 +355,28 @@ template <typename T> int launch_dropout(const DropoutArgs &p, int dtype, cudaSt
             else dropout_rows_kernel<T, false><<<blocks, kThreads, 0, stream>>>(p, log_per_row, (unsigned)col_blocks);
             done = true;
         }
-    } else if (p.cols >= kSegment && p.cols < (1LL << 31)) {
-        const long long per_row = (p.cols + kSegment - 1) / kSegment, segments = per_row * p.rows, blocks = (segments + kThreads / 32 - 1) / (kThreads / 32);
+    }
+    DropoutArgs a = p;
+    if (flat) { a.rows = 1; a.cols = elements; }
+    // Measured, shifted / element by element: 4096 x 33 bf16 with a residual 4.5 / 4.8 us, 8192 x 33 6.6 / 4.8, 8192 x 90 6.7 / 6.0, 8192 x 129
+    // fp16 5.6 / 6.8; fp32, 4096 x 4095 with a residual, shifted 39, by segments 31 (the floor).
+    const bool few = elements <= kFew;
+    if (!done && (few || (sizeof(T) == 2 && a.cols >= kShifted))) {
+        const int steps = a.rows * ((a.cols + 7 + 255) / 256) >= 20000 ? kSteps : 1;
+        const long long each = 256LL * steps, per_row = (a.cols + 7 + each - 1) / each, parts = per_row * a.rows, blocks = (parts + kThreads / 32 - 1) / (kThreads / 32);
         if (blocks < (1LL << 31)) {
-            dropout_segments_kernel<T><<<(unsigned)blocks, kThreads, 0, stream>>>(p, segments, (unsigned)per_row);
+            if (p.residual) dropout_shifted_kernel<T, true><<<(unsigned)blocks, kThreads, 0, stream>>>(a, parts, per_row, steps);
+            else dropout_shifted_kernel<T, false><<<(unsigned)blocks, kThreads, 0, stream>>>(a, parts, per_row, steps);
+            done = true;
+        }
+    } else if (!done && sizeof(T) == 4 && a.cols >= kSegment && a.cols < (1LL << 31)) {
+        const long long per_row = (a.cols + kSegment - 1) / kSegment, segments = per_row * a.rows, blocks = (segments + kThreads / 32 - 1) / (kThreads / 32);
+        if (blocks < (1LL << 31)) {
+            dropout_segments_kernel<T><<<(unsigned)blocks, kThreads, 0, stream>>>(a, segments, (unsigned)per_row);
             done = true;
         }
     }
     if (!done) {
-        DropoutArgs a = p;
-        if (flat) { a.rows = 1; a.cols = elements; }
         const long long groups = (elements + 7) / 8;
         dropout_elements_kernel<T><<<(unsigned)((groups + kThreads - 1) / kThreads), kThreads, 0, stream>>>(a, elements);
     }

@@ -738,3 +738,37 @@ def test_embedding_gradient_of_rows_off_16_byte_boundaries(dtype, n, length, voc
     dout = torch.from_numpy(rng.normal(size=(n, length, dim + pad))).to(dtype).to(DEV)[:, :, :dim]
     check_embedding_grad(dout, tokens, vocab, 0.9, pad=pad)
     check_embedding_grad(dout, tokens, vocab, -1.7, accumulate=True, pad=pad)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_dropout_of_rows_at_every_place_against_16_byte_boundaries(dtype):
+    rng = np.random.default_rng(8)
+    for shift in range(9):
+        for cols, pad in ((100, 1), (33, 0), (257, 5), (600, 3), (40, 4), (9, 2)):
+            x = torch.from_numpy(rng.normal(size=(5, cols))).to(dtype).to(DEV)
+            r = torch.from_numpy(rng.normal(size=(5, cols))).to(dtype).to(DEV)
+            want = pb.dropout(x, 0.4, 6, 1, residual=r)               # contiguous, on 16-byte boundaries
+            out = torch.full((5 * (cols + 3) + 40,), 7.0, dtype=dtype, device=DEV)
+            view = out[8 - shift:8 - shift + 5 * (cols + 3)].view(5, cols + 3)[:, :cols]
+            pb.dropout(strided(x, pad, shift), 0.4, 6, 1, residual=strided(r, pad + 1, 2 * shift + 1), out=view)
+            assert torch.equal(view, want)
+            left = torch.ones_like(out, dtype=torch.bool)
+            left[8 - shift:8 - shift + 5 * (cols + 3)].view(5, cols + 3)[:, :cols] = False
+            assert bool((out[left] == 7).all())                       # nothing beside the rows is written
+            for at in (strided(x, pad, shift), strided(x, 0, shift)):
+                assert torch.equal(pb.dropout(at, 0.4, 6, 1, residual=r, out=at), want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows, cols, pad, shift", [(5001, 1003, 2, 1), (9000, 33, 5, 0), (3000, 95, 1, 3), (2800, 96, 1, 0), (1, 300007, 0, 3), (700, 1001, 0, 1),
+                                                    (1100, 247, 0, 2), (1100, 248, 1, 0), (20100, 121, 0, 5)])
+def test_dropout_of_many_elements_off_16_byte_boundaries(dtype, rows, cols, pad, shift):
+    rng = np.random.default_rng(cols)
+    x = torch.from_numpy(rng.normal(size=(rows, cols))).to(dtype).to(DEV)
+    r = torch.from_numpy(rng.normal(size=(rows, cols))).to(dtype).to(DEV)
+    check_dropout(strided(x, pad, shift), 0.3, 99, 7)
+    a = strided(x, pad, shift)
+    check_dropout(strided(x, pad, shift), 0.3, 99, 7, residual=r, out=a)
+    assert torch.equal(pb.dropout(strided(x, pad, shift), 0.3, 99, 7, residual=strided(r, 1, shift + 2)), a)
+    b = strided(x, pad, shift)
+    assert torch.equal(pb.dropout(b, 0.3, 99, 7, residual=r, out=b), a)
