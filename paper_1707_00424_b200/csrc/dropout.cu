@@ -142,20 +142,9 @@ __global__ void __launch_bounds__(kThreads) dropout_rows_kernel(const DropoutArg
 // Eight elements as words.
 template <typename T> struct Words {
     static constexpr int N = 2 * sizeof(T);               // words of eight elements
-    // N words of w from byte `at` on: 0 .. 15, even, the same in the whole warp
+    // N words of w from byte `at` on, the same in the whole warp
     __device__ __forceinline__ static Pack8<T> from(uint32_t (&w)[N + 4], int at) {
-        if (at & 8) {
-#pragma unroll
-            for (int i = 0; i < N + 2; ++i) w[i] = w[i + 2];
-        }
-        if (at & 4) {
-#pragma unroll
-            for (int i = 0; i < N + 1; ++i) w[i] = w[i + 1];
-        }
-        if (sizeof(T) == 2 && (at & 2)) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
-        }
+        skip_bytes<N, sizeof(T) == 2>(w, at);
         Pack8<T> v;
         uint32_t *to = reinterpret_cast<uint32_t *>(&v);
 #pragma unroll

@@ -690,23 +690,40 @@ template <typename T> __device__ __forceinline__ uint4 packed(const float (&v)[G
     }
 }
 
-// Where a row of dlogits goes: by granule where it begins at the same place of 16 bytes as the logits, else by element.
+// Where a row of dlogits goes: by granule where it begins at the same place of 16 bytes as the logits, else in joined pieces.
 template <typename T> struct OutRow {
     static constexpr int N = Granule<T>::N;
     T *out;
-    uint4 *base;                                          // NULL: by element
+    uint4 *base;                                          // NULL: begins at another place
+    int skew;                                             // bytes of a granule's first element behind a 16-byte boundary
     __device__ __forceinline__ OutRow(const RowsArgs &p, const Row<T> &row, long long at) {
         out = static_cast<T *>(p.dlogits) + at * p.ld_d;
         const uintptr_t a = reinterpret_cast<uintptr_t>(out);
-        base = (a - reinterpret_cast<uintptr_t>(row.x())) % 16 == 0 ? reinterpret_cast<uint4 *>(a & ~(uintptr_t)15) : nullptr;
+        skew = (int)((a - reinterpret_cast<uintptr_t>(row.x())) & 15);
+        base = skew == 0 ? reinterpret_cast<uint4 *>(a & ~(uintptr_t)15) : nullptr;
     }
-    __device__ __noinline__ static void store_elements(T *out, int e0, int vocab, uint4 packed) {
+    // elements from .. until - 1 of a granule, those that lie in the row
+    __device__ __noinline__ static void store_elements(T *out, int e0, int vocab, uint4 packed, int from, int until) {
         const T *v = reinterpret_cast<const T *>(&packed);
-        for (int j = max(0, -e0); j < N && e0 + j < vocab; ++j) out[e0 + j] = v[j];
+        for (int j = max(from, -e0); j < until && e0 + j < vocab; ++j) out[e0 + j] = v[j];
     }
     __device__ __forceinline__ void store(const Row<T> &row, int q, bool whole, const float (&v)[N]) const {
         if (base && whole) base[q] = packed<T>(v);
-        else store_elements(out, row.first_element(q), row.vocab, packed<T>(v));
+        else store_elements(out, row.first_element(q), row.vocab, packed<T>(v), 0, N);
+    }
+    // By a whole warp, whose lanes bring consecutive granules (from `end` on none), with base == NULL: a lane stores the 16 bytes that
+    // end its left neighbour's granule and begin its own; what is at the ends goes by element.
+    __device__ __forceinline__ void store_joined(const Row<T> &row, int q, int end, const float (&v)[N]) const {
+        const uint4 own = packed<T>(v);
+        const int lane = threadIdx.x % 32, cut = (16 - skew) / (int)sizeof(T), e0 = row.first_element(q);
+        const unsigned wholes = __ballot_sync(0xffffffffu, q < end && row.whole(q)), both = wholes & (wholes << 1);
+        uint32_t w[8] = {__shfl_up_sync(0xffffffffu, own.x, 1), __shfl_up_sync(0xffffffffu, own.y, 1),
+                         __shfl_up_sync(0xffffffffu, own.z, 1), __shfl_up_sync(0xffffffffu, own.w, 1), own.x, own.y, own.z, own.w};
+        skip_bytes<4, sizeof(T) == 2>(w, 16 - skew);
+        const bool joined = (both >> lane) & 1u, next = lane < 31 && ((both >> (lane + 1)) & 1u);
+        if (joined) *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(out + e0) - skew) = make_uint4(w[0], w[1], w[2], w[3]);
+        const int from = joined ? cut : 0, until = next ? cut : N;
+        if (q < end && from < until) store_elements(out, e0, row.vocab, own, from, until);
     }
 };
 
@@ -768,7 +785,8 @@ template <typename T, int BLOCK> __device__ __forceinline__ void zero_row(const 
 
 // The gradient of long rows, by a block each: a second pass reads the row again, from L2.  Its reads and the stores are marked as the
 // last use of their lines, so that rows between their two passes stay (a fifth of them does not).  2048 x 131072 bf16 logits: 200-204 us;
-// two exponentials per logit take 116 us of their pipe, the bytes 164 us at the copy rate.
+// two exponentials per logit take 116 us of their pipe, the bytes 164 us at the copy rate.  Of 131071 at another pitch than dlogits:
+// 312 us, element by element 802.
 template <typename T, int BLOCK, int U, bool ENT>
 __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_grad_kernel(const RowsArgs p) {
     __shared__ SharedSums<BLOCK> sh;
@@ -789,6 +807,20 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_grad_kerne
         zero_row<T, BLOCK>(p, at, 0, 1);
     } else if (r.far) {
         far_gradient<T>(row, threadIdx.x, BLOCK, end, r, in.a(r), in.b(r), in.g, given.token, out);
+    } else if (!out.base) {
+        const Slope<T, ENT> slope(r, in.a(r), in.b(r));
+        for (int q0 = (int)threadIdx.x + (end - 1) / (BLOCK * U) * (BLOCK * U); q0 >= 0; q0 -= BLOCK * U) {      // (all threads as often)
+            Granule<T> raw[U];
+            row.load_all(q0, BLOCK, end, raw);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float v[Granule<T>::N];
+                slope.values(raw[u], v);
+                out.store_joined(row, q0 + u * BLOCK, end, v);
+            }
+        }
+        __syncwarp();                                     // (a neighbour may have written the token's place)
+        if (share.mine) out.out[given.token] = from_float<T>(slope.value(share.x) + in.g);
     } else {
         const Slope<T, ENT> slope(r, in.a(r), in.b(r));
         // from the end: what was read last is the likeliest to be in L1 and L2 still
@@ -829,8 +861,8 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_grad_kerne
 }
 
 // Rows held in registers, U granules a thread, by a block or a cluster of blocks: everything is in flight at once and read once,
-// and the gradient is formed from what is held.  GRAD: the gradient (ENT: with an entropy's); else log probabilities, entropy, top
-// (TWO: from two groups a thread).
+// and the gradient is formed from what is held.  GRAD: the gradient (ENT: with an entropy's; TWO: rows of
+// dlogits may begin at other places of 16 bytes than the logits); else log probabilities, entropy, top (TWO: from two groups a thread).
 template <typename T, int BLOCK, int U, bool GRAD, bool ENT, bool TWO>
 __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kernel(const RowsArgs p, int blocks) {
     __shared__ Shared<BLOCK> sh;
@@ -853,7 +885,7 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kerne
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         float v, odd;
-        if constexpr (TWO) {
+        if constexpr (TWO && !GRAD) {
             raw[u].largest_two(v, odd);
             if (odd > top_odd) { top_odd = odd; best_odd = q0 + u * BLOCK; }
         } else {
@@ -863,7 +895,7 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kerne
     }
     const float c = p.scale_log2e;
     Sums t;
-    t.r = fmaxf((TWO ? fmaxf(top, top_odd) : top) * c, -kNear);
+    t.r = fmaxf((TWO && !GRAD ? fmaxf(top, top_odd) : top) * c, -kNear);
     {
         const uint32_t low = low_bound<T>(c);
         const float_pair c2 = pair(c, c), r2 = pair(-t.r, -t.r);
@@ -888,7 +920,7 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kerne
         split(a2, lo, hi); t.a = lo + hi;
     }
     unsigned long long best = best_granule >= 0 ? order_key(top, (uint32_t)(TWO ? 2 * best_granule : best_granule)) : 0;
-    if constexpr (TWO) {
+    if constexpr (TWO && !GRAD) {
         const unsigned long long odd = best_odd >= 0 ? order_key(top_odd, (uint32_t)(2 * best_odd + 1)) : 0;
         offer_two(best, odd, sh);
         best = max(best, odd);
@@ -927,11 +959,13 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kerne
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int q = q0 + u * BLOCK;
-                if (q >= end) break;
+                if (!TWO || out.base ? q >= end : q - (int)threadIdx.x % 32 >= end) break;
                 float v[Granule<T>::N];
                 slope.values(raw[u], v);
-                out.store(row, q, row.whole(q), v);
+                if (!TWO || out.base) out.store(row, q, row.whole(q), v);
+                else out.store_joined(row, q, end, v);
             }
+            if (TWO) __syncwarp();                        // (a neighbour may have written the token's place)
             if (share.mine) out.out[given.token] = from_float<T>(slope.value(share.x) + in.g);
         }
     } else if (p.k > 0 && rank == 0) {
@@ -943,6 +977,9 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kerne
 }
 
 template <typename T, int BLOCK, int U, bool GRAD, bool ENT, bool TWO = false> int launch_held(const RowsArgs &p, int blocks, cudaStream_t stream) {
+    if constexpr (GRAD && !TWO)
+        if ((reinterpret_cast<uintptr_t>(p.logits) - reinterpret_cast<uintptr_t>(p.dlogits)) % 16 || (p.ld - p.ld_d) * sizeof(T) % 16)
+            return launch_held<T, BLOCK, U, GRAD, ENT, true>(p, blocks, stream);
     cudaLaunchAttribute attr = {};
     const cudaLaunchConfig_t cfg = cluster_config(dim3((unsigned)(p.rows * blocks)), BLOCK, 0, blocks, &attr, stream);
     if (cudaLaunchKernelEx(&cfg, token_logprobs_held_kernel<T, BLOCK, U, GRAD, ENT, TWO>, p, blocks) != cudaSuccess) return PARLE_ECUDA;
@@ -953,6 +990,10 @@ template <typename T, bool GRAD, bool ENT> int launch_rows(const RowsArgs &p, in
     // granules of a row, one more where rows do not all begin on 16-byte boundaries
     const long long granules = ((long long)p.vocab * sizeof(T) + 15) / 16 + (reinterpret_cast<uintptr_t>(p.logits) % 16 || p.ld * sizeof(T) % 16 ? 1 : 0);
     constexpr int U = 8;
+    // Alternatives of few short rows: four warps each.  Measured, four warps / one, 5 alternatives of 500 bf16 logits: 64 rows 4.3 / 4.8 us,
+    // 600 rows 5.0 / 5.5, 1200 rows 6.8 / 5.8; 20 of 1900: 4.2 / 7.8 (one row), 5.6 / 10.4 (300 rows), 8.7 / 10.9, 2400 rows 14.2 / 12.8.
+    if constexpr (!GRAD)
+        if (p.k > 0 && granules > 32 && granules <= 128 * 2 && p.rows <= (p.k > 12 ? 8 : 4) * sms) return launch_held<T, 128, 2, GRAD, ENT>(p, 1, stream);
     // Short rows: a warp each; with two groups a thread where so many alternatives are wanted that 32 groups, or a very short row's
     // fewer, set their bound too low.  Measured, with / without: 8192 x 500 bf16 logits, 20 alternatives 19.3 us without, 25: 22.3 / 23.8,
     // 32: 24.4 / 88; 6827 x 150, 20: 16.8 / 46.

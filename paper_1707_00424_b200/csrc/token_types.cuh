@@ -80,6 +80,22 @@ template <> struct Pack8<__half> {
     __device__ __forceinline__ void store(__half *p) const { *reinterpret_cast<uint4 *>(p) = a; }
 };
 
+// Moves the N words from byte `at` of w on (0 .. 15; even; a multiple of 4 but for HALVES) to its beginning.
+template <int N, bool HALVES> __device__ __forceinline__ void skip_bytes(uint32_t (&w)[N + 4], int at) {
+    if (at & 8) {
+#pragma unroll
+        for (int i = 0; i < N + 2; ++i) w[i] = w[i + 2];
+    }
+    if (at & 4) {
+#pragma unroll
+        for (int i = 0; i < N + 1; ++i) w[i] = w[i + 1];
+    }
+    if (HALVES && (at & 2)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    }
+}
+
 inline bool valid_dtype(int dtype) { return dtype == PARLE_F32 || dtype == PARLE_BF16 || dtype == PARLE_F16; }
 inline int dtype_bytes(int dtype) { return dtype == PARLE_F32 ? 4 : 2; }
 // Whether p lies on a boundary of its element type.

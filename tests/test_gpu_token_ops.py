@@ -772,3 +772,32 @@ def test_dropout_of_many_elements_off_16_byte_boundaries(dtype, rows, cols, pad,
     assert torch.equal(pb.dropout(strided(x, pad, shift), 0.3, 99, 7, residual=strided(r, 1, shift + 2)), a)
     b = strided(x, pad, shift)
     assert torch.equal(pb.dropout(b, 0.3, 99, 7, residual=r, out=b), a)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("x_shift, out_shift, x_pad, out_pad", [(0, 1, 0, 0), (1, 0, 0, 0), (0, 2, 0, 0), (3, 0, 4, 4), (0, 4, 0, 0), (0, 5, 1, 0), (7, 0, 0, 3), (2, 1, 8, 1)])
+def test_gradient_at_another_place_of_16_bytes_than_the_logits(dtype, x_shift, out_shift, x_pad, out_pad):
+    """The given token is each of a row's in turn; rows of a warp, of a block, of a cluster and streamed."""
+    rng = np.random.default_rng(x_shift * 8 + out_shift)
+    for rows, vocab in ((297, 297), (21, 21), (5, 1000), (4, 8000), (3, 17000), (2, 70001)):
+        x, tokens, _ = random_rows(rows, vocab, dtype, vocab)
+        tokens = np.arange(rows) if rows == vocab else (np.arange(rows) * 7919 + 13) % vocab
+        check_grad(strided(x, x_pad, x_shift), tokens, rng.normal(size=rows), rng.normal(size=rows), 1.1, pad=out_pad, shift=out_shift, outputs=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows, vocab", [(600, 8211), (300, 33001), (300, 70003)])
+def test_gradient_of_many_rows_at_another_pitch(dtype, rows, vocab):
+    """Against the same call at the same pitch, which the tests above hold to the oracle: the same bits."""
+    x, tokens, rng = random_rows(rows, vocab, dtype, 3)
+    tok = torch.from_numpy(np.asarray(tokens, np.int32)).to(DEV)
+    g, h = (torch.from_numpy(rng.normal(size=rows).astype(np.float32)).to(DEV) for _ in range(2))
+    g[::5] = 0
+    h[::5] = 0
+    want = pb.token_logprobs_grad(x, tok, g, h)
+    for pad, shift in ((1, 0), (3, 5), (8, 1)):
+        buf = torch.full((rows * (vocab + pad) + 16,), 5.0, dtype=dtype, device=DEV)
+        out = buf[shift:shift + rows * (vocab + pad)].view(rows, vocab + pad)
+        pb.token_logprobs_grad(x, tok, g, h, dlogits=out[:, :vocab])
+        assert torch.equal(out[:, :vocab], want)
+        assert bool((out[:, vocab:] == 5).all()) and bool((buf[:shift] == 5).all()) and bool((buf[shift + rows * (vocab + pad):] == 5).all())
