@@ -353,11 +353,17 @@ __device__ __forceinline__ void hand_on(const Row<T> &row, const Granule<T> &raw
     float v[N];
     raw.get(v);
     const int e0 = row.first_element(q);
+    uint32_t reach = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (v[i] > -INFINITY && order_key(v[i], TWO ? place + i % 2 : place) >= bound) reach |= 1u << i;      // (beside the row lies -inf)
+    if (!reach) return;
+    int at = atomicAdd(&sh.found, __popc(reach));
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        if (!(v[i] > -INFINITY) || order_key(v[i], TWO ? place + i % 2 : place) < bound) continue;      // (beside the row lies -inf)
-        const int at = atomicAdd(&sh.found, 1);
+        if (!((reach >> i) & 1u)) continue;
         if (at < kCandidates) sh.candidate[at] = order_key(v[i], (uint32_t)(e0 + i));
+        ++at;
     }
 }
 
@@ -634,15 +640,15 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_kernel(con
     const unsigned long long bound = top_bound<Shared<BLOCK>::kGroups>(p.k, sh);
     if (best && best >= bound) sh.owner[atomicAdd(&sh.owners, 1)] = threadIdx.x;
     __syncthreads();
-    // the granules of the threads that reach the bound, a warp for each of these threads, two in flight per lane
-    const int owners = sh.owners;
-    for (int o = threadIdx.x / 32; o < owners; o += BLOCK / 32)
-        for (int q0 = sh.owner[o] + (int)threadIdx.x % 32 * BLOCK; q0 < row.granules; q0 += 64 * BLOCK) {
-            const int q1 = q0 + 32 * BLOCK;
-            const Granule<T> first = row.load(q0, row.granules), second = row.load(q1, row.granules);
-            hand_on(row, first, q0, bound, sh);
-            if (q1 < row.granules) hand_on(row, second, q1, bound, sh);
-        }
+    // the granules of the threads that reach the bound, two in flight per thread
+    const int each = (row.granules + BLOCK - 1) / BLOCK, all = sh.owners * each;
+    const auto granule = [&](int i) { return i < all ? sh.owner[i / each] + i % each * BLOCK : row.granules; };
+    for (int i = threadIdx.x; i < all; i += 2 * BLOCK) {
+        const int q0 = granule(i), q1 = granule(i + BLOCK);
+        const Granule<T> first = row.load(q0, row.granules), second = row.load(q1, row.granules);
+        if (q0 < row.granules) hand_on(row, first, q0, bound, sh);
+        if (q1 < row.granules) hand_on(row, second, q1, bound, sh);
+    }
     __syncthreads();
     rank_candidates(row, 0, row.granules, p.k, sh);
     write_top(p, at, r, sh);
