@@ -714,7 +714,7 @@ template <typename T> struct OutRow {
         for (int j = max(from, -e0); j < until && e0 + j < vocab; ++j) out[e0 + j] = v[j];
     }
     __device__ __forceinline__ void store(const Row<T> &row, int q, bool whole, const float (&v)[N]) const {
-        if (base && whole) base[q] = packed<T>(v);
+        if (whole) base[q] = packed<T>(v);                // (then base is not NULL)
         else store_elements(out, row.first_element(q), row.vocab, packed<T>(v), 0, N);
     }
     // By a whole warp, whose lanes bring consecutive granules (from `end` on none), with base == NULL: a lane stores the 16 bytes that
@@ -761,6 +761,46 @@ __device__ __noinline__ void far_gradient(const Row<T> row, int first, int step,
     }
 }
 
+// The gradient of a row that may begin at another place of 16 bytes than the logits (and is not the logits themselves), by dlogits' 16-byte pieces: their logits lie in two
+// granules, the second of them the next lane's first.
+template <typename T, int BLOCK, bool ENT>
+__device__ __noinline__ void shifted_gradient(const Row<T> row, const RowResult r, float a, float b, float g, int token, T *out) {
+    constexpr int N = Granule<T>::N, S = sizeof(T), U = 2;
+    const Slope<T, ENT> slope(r, a, b);
+    const int skew = (int)((reinterpret_cast<uintptr_t>(row.x()) - reinterpret_cast<uintptr_t>(out)) & 15);      // of a piece's first logit
+    const int head = (int)((reinterpret_cast<uintptr_t>(out) & 15) / S), pieces = (head + row.vocab + N - 1) / N;
+    // pieces whose logits' granules lie in the row
+    const int low = head + (skew + S - 1) / S, high = head + row.vocab - N - (16 - skew) / S;
+    for (int j0 = (int)threadIdx.x + (pieces - 1) / (BLOCK * U) * (BLOCK * U); j0 >= 0; j0 -= BLOCK * U) {
+        uint4 first[U], second[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = (j0 + u * BLOCK) * N;
+            if (at < low || at > high) continue;
+            const uint4 *from = reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(row.x() + (at - head)) - skew);
+            first[u] = from[0];
+            second[u] = from[1];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = (j0 + u * BLOCK) * N, e0 = at - head;
+            if (at >= low && at <= high) {
+                uint32_t w[8] = {first[u].x, first[u].y, first[u].z, first[u].w, second[u].x, second[u].y, second[u].z, second[u].w};
+                skip_bytes<4, S == 2>(w, skew);
+                Granule<T> raw;
+                raw.raw = make_uint4(w[0], w[1], w[2], w[3]);
+                float v[N];
+                slope.values(raw, v);
+                __stcs(reinterpret_cast<uint4 *>(out + e0), packed<T>(v));
+            } else {
+                for (int e = max(0, e0); e < min(row.vocab, e0 + N); ++e) out[e] = from_float<T>(slope.value(row.x()[e]));
+            }
+        }
+    }
+    if (token >= 0 && (token + head) / N % BLOCK == (int)threadIdx.x)      // by the thread that wrote its piece
+        out[token] = from_float<T>(slope.value(row.x()[token]) + g);
+}
+
 // What a row of the gradient needs besides its sums.
 struct Incoming {
     float g, h;
@@ -791,9 +831,9 @@ template <typename T, int BLOCK> __device__ __forceinline__ void zero_row(const 
 
 // The gradient of long rows, by a block each: a second pass reads the row again, from L2.  Its reads and the stores are marked as the
 // last use of their lines, so that rows between their two passes stay (a fifth of them does not).  2048 x 131072 bf16 logits: 200-204 us;
-// two exponentials per logit take 116 us of their pipe, the bytes 164 us at the copy rate.  Of 131071 at another pitch than dlogits:
-// 312 us, element by element 802.
-template <typename T, int BLOCK, int U, bool ENT>
+// two exponentials per logit take 116 us of their pipe, the bytes 164 us at the copy rate.  SHIFTED: rows of
+// dlogits may begin at other places of 16 bytes than the logits; 2048 x 131071 of pitch 131072 to 131071: 243 us, element by element 802.
+template <typename T, int BLOCK, int U, bool ENT, bool SHIFTED>
 __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_grad_kernel(const RowsArgs p) {
     __shared__ SharedSums<BLOCK> sh;
     const long long at = blockIdx.x;
@@ -813,25 +853,13 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_grad_kerne
         zero_row<T, BLOCK>(p, at, 0, 1);
     } else if (r.far) {
         far_gradient<T>(row, threadIdx.x, BLOCK, end, r, in.a(r), in.b(r), in.g, given.token, out);
-    } else if (!out.base) {
-        const Slope<T, ENT> slope(r, in.a(r), in.b(r));
-        for (int q0 = (int)threadIdx.x + (end - 1) / (BLOCK * U) * (BLOCK * U); q0 >= 0; q0 -= BLOCK * U) {      // (all threads as often)
-            Granule<T> raw[U];
-            row.load_all(q0, BLOCK, end, raw);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                float v[Granule<T>::N];
-                slope.values(raw[u], v);
-                out.store_joined(row, q0 + u * BLOCK, end, v);
-            }
-        }
-        __syncwarp();                                     // (a neighbour may have written the token's place)
-        if (share.mine) out.out[given.token] = from_float<T>(slope.value(share.x) + in.g);
+    } else if constexpr (SHIFTED) {
+        shifted_gradient<T, BLOCK, ENT>(row, r, in.a(r), in.b(r), in.g, given.real ? given.token : -1, out.out);
     } else {
         const Slope<T, ENT> slope(r, in.a(r), in.b(r));
         // from the end: what was read last is the likeliest to be in L1 and L2 still
         const int stride = BLOCK * U;
-        const auto fast = [&](int q0) { return out.base && row.all_whole(q0, q0 + (U - 1) * BLOCK, end); };
+        const auto fast = [&](int q0) { return row.all_whole(q0, q0 + (U - 1) * BLOCK, end); };
         const auto fetch = [&](int q0, Granule<T> (&raw)[U]) {
 #pragma unroll
             for (int u = 0; u < U; ++u) raw[u].raw = __ldcs(row.base + q0 + u * BLOCK);
@@ -982,10 +1010,14 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_held_kerne
     if (blocks > 1) cluster_wait();                       // no block leaves while another may read its shared memory
 }
 
+// Whether rows of dlogits begin at other places of 16 bytes than the logits (never where they are the logits).
+template <typename T> bool begins_elsewhere(const RowsArgs &p) {
+    return (reinterpret_cast<uintptr_t>(p.logits) - reinterpret_cast<uintptr_t>(p.dlogits)) % 16 || (p.rows > 1 && (p.ld - p.ld_d) * (long long)sizeof(T) % 16);
+}
+
 template <typename T, int BLOCK, int U, bool GRAD, bool ENT, bool TWO = false> int launch_held(const RowsArgs &p, int blocks, cudaStream_t stream) {
     if constexpr (GRAD && !TWO)
-        if ((reinterpret_cast<uintptr_t>(p.logits) - reinterpret_cast<uintptr_t>(p.dlogits)) % 16 || (p.ld - p.ld_d) * sizeof(T) % 16)
-            return launch_held<T, BLOCK, U, GRAD, ENT, true>(p, blocks, stream);
+        if (begins_elsewhere<T>(p)) return launch_held<T, BLOCK, U, GRAD, ENT, true>(p, blocks, stream);
     cudaLaunchAttribute attr = {};
     const cudaLaunchConfig_t cfg = cluster_config(dim3((unsigned)(p.rows * blocks)), BLOCK, 0, blocks, &attr, stream);
     if (cudaLaunchKernelEx(&cfg, token_logprobs_held_kernel<T, BLOCK, U, GRAD, ENT, TWO>, p, blocks) != cudaSuccess) return PARLE_ECUDA;
@@ -1033,9 +1065,11 @@ template <typename T, bool GRAD, bool ENT> int launch_rows(const RowsArgs &p, in
     // 32760 with 256 / 128 threads 23 / 27, 4096 x 20000 66 / 68, 4096 x 10000 49 / 35, 128 x 131072 with 512 / 256 threads 12.6 / 16.7.
     const unsigned rows = (unsigned)p.rows;
     if constexpr (GRAD) {
-        if (granules > 8192) token_logprobs_grad_kernel<T, 512, 4, ENT><<<rows, 512, 0, stream>>>(p);
-        else if (granules > 4096) token_logprobs_grad_kernel<T, 256, 4, ENT><<<rows, 256, 0, stream>>>(p);
-        else token_logprobs_grad_kernel<T, 128, 4, ENT><<<rows, 128, 0, stream>>>(p);
+        const bool shifted = begins_elsewhere<T>(p);
+        const auto launch = [&](auto *kernel, auto *kernel_shifted, int threads) { (shifted ? kernel_shifted : kernel)<<<rows, threads, 0, stream>>>(p); };
+        if (granules > 8192) launch(token_logprobs_grad_kernel<T, 512, 4, ENT, false>, token_logprobs_grad_kernel<T, 512, 4, ENT, true>, 512);
+        else if (granules > 4096) launch(token_logprobs_grad_kernel<T, 256, 4, ENT, false>, token_logprobs_grad_kernel<T, 256, 4, ENT, true>, 256);
+        else launch(token_logprobs_grad_kernel<T, 128, 4, ENT, false>, token_logprobs_grad_kernel<T, 128, 4, ENT, true>, 128);
     } else {
         if (granules > 2048 && p.rows <= 2 * sms) token_logprobs_kernel<T, 512, 4><<<rows, 512, 0, stream>>>(p);
         else if (granules > 2048) token_logprobs_kernel<T, 256, 4><<<rows, 256, 0, stream>>>(p);
