@@ -801,3 +801,26 @@ def test_gradient_of_many_rows_at_another_pitch(dtype, rows, vocab):
         pb.token_logprobs_grad(x, tok, g, h, dlogits=out[:, :vocab])
         assert torch.equal(out[:, :vocab], want)
         assert bool((out[:, vocab:] == 5).all()) and bool((buf[:shift] == 5).all()) and bool((buf[shift + rows * (vocab + pad):] == 5).all())
+
+
+def test_beyond_32_bit_offsets_off_16_byte_boundaries():
+    n = (1 << 32) + 4099
+    x = torch.ones(n + 3, dtype=torch.bfloat16, device=DEV)
+    pb.dropout(x[3:], 0.5, 9, 1, out=x[3:])
+    assert bool((x[:3] == 1).all())
+    for first in (0, (1 << 31) - 40, (1 << 32) - 40, n - 100):
+        field = to.dropout_fields(100, 9, 1, first=first)
+        assert np.array_equal(f64(x[3 + first:103 + first]) > 0, field >= 32768)
+    del x
+    rows, vocab = 33000, 131071
+    logits = torch.zeros(rows, vocab + 1, dtype=torch.bfloat16, device=DEV)
+    logits[-3:].normal_()
+    dlogits = torch.ones(rows, vocab, dtype=torch.bfloat16, device=DEV)
+    tokens = torch.full((rows,), vocab - 1, dtype=torch.int32, device=DEV)
+    g = torch.zeros(rows, device=DEV)
+    g[-3:] = torch.tensor([1.0, -2.0, 0.5])                           # (rows without a gradient are not read)
+    pb.token_logprobs_grad(logits[:, :vocab], tokens, g, dlogits=dlogits)
+    want = pb.token_logprobs_grad(logits[-3:, :vocab].contiguous(), tokens[-3:], g[-3:])
+    assert torch.equal(dlogits[-3:], want) and not bool(dlogits[:-3].any())
+    del logits, dlogits
+    torch.cuda.empty_cache()
