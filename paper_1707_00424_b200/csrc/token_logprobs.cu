@@ -344,7 +344,10 @@ template <int G, int BLOCK> __device__ __forceinline__ unsigned long long top_bo
     return sh.bound;
 }
 
-// Hands on a granule's logits that reach the bound.
+// Hands on a granule's logits that reach the bound.  TWO: all of them at the even group's place, whatever their own group, since the
+// bound orders equal logits of one granule by group and the alternatives are ordered by token.  What is left behind is then smaller
+// than the bound's logit, or equal to it in a later granule: k larger or earlier ones exist.  (The thread that holds what is handed on
+// reaches the bound: if only the odd group's place does not, the bound is the thread's own even group.)
 template <bool TWO = false, typename T, int BLOCK>
 __device__ __forceinline__ void hand_on(const Row<T> &row, const Granule<T> &raw, int q, unsigned long long bound, Shared<BLOCK> &sh) {
     constexpr int N = Granule<T>::N;
@@ -356,7 +359,7 @@ __device__ __forceinline__ void hand_on(const Row<T> &row, const Granule<T> &raw
     uint32_t reach = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-        if (v[i] > -INFINITY && order_key(v[i], TWO ? place + i % 2 : place) >= bound) reach |= 1u << i;      // (beside the row lies -inf)
+        if (v[i] > -INFINITY && order_key(v[i], place) >= bound) reach |= 1u << i;      // (beside the row lies -inf)
     if (!reach) return;
     int at = atomicAdd(&sh.found, __popc(reach));
 #pragma unroll
