@@ -493,7 +493,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const GradArg
     }
 }
 
-// Longer sequences: the same sort by launches of its own, two a pass.  First: how often each digit occurs in a tile.
+// Longer sequences: the same sort by launches of its own, two a pass, or three.  First: how often each digit occurs in a tile.
 __global__ void __launch_bounds__(kThreads)
 radix_count_kernel(const GradArgs p, const int32_t *keys, int shift, int first_pass, int *counts) {
     __shared__ int hist[kDigits];
@@ -515,13 +515,43 @@ radix_count_kernel(const GradArgs p, const int32_t *keys, int shift, int first_p
         atomicAdd(&hist[(key >> shift) & (kDigits - 1)], 1);
     }
     __syncthreads();
-    counts[((long long)g * gridDim.x + blockIdx.x) * kDigits + threadIdx.x] = hist[threadIdx.x];
+    counts[((long long)g * (gridDim.x + 1) + blockIdx.x) * kDigits + threadIdx.x] = hist[threadIdx.x];
+}
+
+constexpr int kSummedTiles = 64;        // most tiles whose counts every block of a move adds up by itself
+constexpr int kScanDigits = 32, kScanThreads = 1024;
+
+// Of many tiles, the counts become the counts of the tiles before, and the row behind them the totals: a move then reads two rows, where
+// adding up all tiles' counts in every block takes reads that grow with the square of the length.  A block takes 32 digits of a
+// table, a lane each; its warps take a part of the tiles each.  grid (digits / 32, n).
+// Measured, added up by every block / scanned, 64 columns of bf16: 32769 positions 65 / 74 us, 65536 into 4000 rows 86 / 95, 131072 into
+// 50021 rows 119 / 128, 262144 (64 tiles) 187 / 186.
+__global__ void __launch_bounds__(kScanThreads) radix_scan_kernel(int *counts, int tiles) {
+    constexpr int W = kScanThreads / 32;
+    __shared__ int sums[W][kScanDigits];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    int *const c = counts + (long long)blockIdx.y * (tiles + 1) * kDigits + blockIdx.x * kScanDigits + lane;
+    const int each = (tiles + W - 1) / W, from = min(tiles, warp * each), to = min(tiles, from + each);
+    int sum = 0;
+#pragma unroll 8
+    for (int t = from; t < to; ++t) sum += c[(long long)t * kDigits];
+    sums[warp][lane] = sum;
+    __syncthreads();
+    int before = 0;
+    for (int w = 0; w < warp; ++w) before += sums[w][lane];
+    if (warp == W - 1) c[(long long)tiles * kDigits] = before + sum;
+#pragma unroll 8
+    for (int t = from; t < to; ++t) {
+        const int own = c[(long long)t * kDigits];
+        c[(long long)t * kDigits] = before;
+        before += own;
+    }
 }
 
 // Then: every position moves to (positions with a lower digit) + (same digit, earlier tile) + (same digit, earlier in the tile).
 // A warp owns kTile / 8 consecutive positions and ranks 32 at a time by matching digits.
 __global__ void __launch_bounds__(kThreads)
-radix_move_kernel(const int32_t *keys, const int *places, int length, int vocab, int shift, int first_pass, const int *counts,
+radix_move_kernel(const int32_t *keys, const int *places, int length, int vocab, int shift, int first_pass, const int *counts, int scanned,
                   int *keys_out, int *places_out) {
     __shared__ int warp_count[kWarps][kDigits];
     __shared__ int scan[kWarps];
@@ -537,11 +567,16 @@ radix_move_kernel(const int32_t *keys, const int *places, int length, int vocab,
     }
     // thread = digit: its total over all tiles, and over the tiles before this one
     int total = 0, earlier = 0;
-    const int *c = counts + (long long)g * gridDim.x * kDigits + threadIdx.x;
-    for (int b = 0; b < (int)gridDim.x; ++b) {
-        const int v = c[(long long)b * kDigits];
-        total += v;
-        if (b < (int)blockIdx.x) earlier += v;
+    const int *c = counts + (long long)g * (gridDim.x + 1) * kDigits + threadIdx.x;
+    if (scanned) {
+        total = c[(long long)gridDim.x * kDigits];
+        earlier = c[(long long)blockIdx.x * kDigits];
+    } else {
+        for (int b = 0; b < (int)gridDim.x; ++b) {
+            const int v = c[(long long)b * kDigits];
+            total += v;
+            if (b < (int)blockIdx.x) earlier += v;
+        }
     }
     int sum = total;                                      // inclusive scan over the digits
     for (int o = 1; o < 32; o <<= 1) {
@@ -817,7 +852,7 @@ GradPlan plan_grad(int n, long long length, int vocab, int dim) {
     if (length > kSortMost) p.tiles = (int)((length + kTile - 1) / kTile);
     for (int i = 0; i < (p.tiles ? 2 : 1); ++i) { p.keys[i] = at; at += ints; p.places[i] = at; at += ints; }
     p.counts = at;
-    at += round_up((size_t)n * p.tiles * kDigits * sizeof(int), 128);
+    if (p.tiles) at += round_up((size_t)n * (p.tiles + 1) * kDigits * sizeof(int), 128);      // (a row of totals behind the tiles')
     p.occurs = at;
     at += round_up((size_t)n * p.words * sizeof(uint32_t), 128);
     p.crossings = at;
@@ -868,7 +903,12 @@ int launch_sorted(GradArgs a, int n, const GradPlan &plan, bool wide, bool wide_
             const int to = pass ? 1 - sorted : 0;
             radix_count_kernel<<<grid, kThreads, 0, stream>>>(a, in, 8 * pass, pass == 0, counts);
             if ((rc = launch_status()) != PARLE_OK) return rc;
-            radix_move_kernel<<<grid, kThreads, 0, stream>>>(in, places[sorted], a.length, a.vocab, 8 * pass, pass == 0, counts, keys[to], places[to]);
+            const bool scanned = plan.tiles > kSummedTiles;
+            if (scanned) {
+                radix_scan_kernel<<<dim3(kDigits / kScanDigits, n), kScanThreads, 0, stream>>>(counts, plan.tiles);
+                if ((rc = launch_status()) != PARLE_OK) return rc;
+            }
+            radix_move_kernel<<<grid, kThreads, 0, stream>>>(in, places[sorted], a.length, a.vocab, 8 * pass, pass == 0, counts, scanned, keys[to], places[to]);
             if ((rc = launch_status()) != PARLE_OK) return rc;
             sorted = to;
         }
