@@ -8,8 +8,6 @@ from __future__ import annotations
 
 import os
 
-import torch
-
 from .binding import ParleError, lib
 
 NO_TOKEN = -1
@@ -21,6 +19,7 @@ def load():
     """The compiled module (built first if it is missing)."""
     global _MODULE
     if _MODULE is None:
+        import torch
         lib()
         from . import build
         if not os.path.exists(build.MODULE):
