@@ -1,9 +1,11 @@
 """Build libparle.so (sm_100a) with nvcc and the token operators' Python module _token_ops.so with g++, both in-tree."""
 from __future__ import annotations
 
+import hashlib
 import os
 import shutil
 import subprocess
+import sys
 import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -21,11 +23,11 @@ def _nvcc() -> str:
     raise RuntimeError("nvcc not found: the Parle CUDA library cannot be built")
 
 
-def _stale(target: str, sources) -> bool:
-    if not os.path.exists(target):
+def _stale() -> bool:
+    if not os.path.exists(LIB):
         return True
-    t = os.path.getmtime(target)
-    deps = [os.path.join(CSRC, f) for f in sources]
+    t = os.path.getmtime(LIB)
+    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS]
     deps.append(os.path.join(HERE, "..", "include", "parle.h"))
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -39,7 +41,7 @@ def _run(cmd) -> str:
 
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile the library if it is missing or older than its sources; return its path."""
-    if not force and not _stale(LIB, SOURCES + HEADERS):
+    if not force and not _stale():
         return LIB
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--threads", "0",
            "-shared", "-Xcompiler", "-fPIC", "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
@@ -51,16 +53,35 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def module_stamp() -> str:
+    """What the module has to be built from: its sources' contents, the torch and the Python that are running.  The compiler puts it into
+    the module, so that one built from anything else is known whatever the files' times are."""
+    import torch
+    h = hashlib.sha256(f"{torch.__version__} {sys.implementation.cache_tag}".encode())
+    for path in (os.path.join(CSRC, "token_bindings.cpp"), os.path.join(HERE, "..", "include", "parle.h")):
+        with open(path, "rb") as f:
+            h.update(f.read())
+    return "token operators of " + h.hexdigest()[:32]
+
+
+def _module_stale() -> bool:
+    if not os.path.exists(MODULE):
+        return True
+    with open(MODULE, "rb") as f:
+        return module_stamp().encode() not in f.read()
+
+
 def build_module(force: bool = False) -> str:
-    """Compile the Python module of the token operators, which calls the library beside it, for the torch that is installed."""
-    build()
-    if not force and not _stale(MODULE, ["token_bindings.cpp"]):
+    """Compile the Python module of the token operators, which calls the library beside it, if it is missing or was built from other sources or for
+    another torch or Python than the ones here; return its path."""
+    if not force and not _module_stale():
         return MODULE
+    build()
     import torch
     at = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(os.path.realpath(_nvcc())))
     _run([shutil.which("g++") or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
-          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DBUILT_FOR_TORCH="{torch.__version__}"', "-isystem", os.path.join(at, "include"),
+          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DBUILT_FROM="{module_stamp()}"', "-isystem", os.path.join(at, "include"),
           "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(cuda, "include"), os.path.join(CSRC, "token_bindings.cpp"),
           "-o", MODULE, "-L" + HERE, "-l:libparle.so", "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10",
           "-Wl,-rpath,$ORIGIN"])

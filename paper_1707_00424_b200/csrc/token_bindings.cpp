@@ -432,6 +432,6 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_token_ops", nullptr, -1, methods,
 
 PyMODINIT_FUNC PyInit__token_ops() {
     PyObject *m = PyModule_Create(&module);
-    if (m && PyModule_AddStringConstant(m, "torch_version", BUILT_FOR_TORCH) < 0) Py_CLEAR(m);
+    if (m && PyModule_AddStringConstant(m, "built_from", BUILT_FROM) < 0) Py_CLEAR(m);
     return m;
 }

@@ -6,8 +6,6 @@ current stream of the tensors' device: both in the module _token_ops (csrc/token
 for them; those not given are allocated with torch.  Tensors are strided as they come: only the last dimension has to be dense."""
 from __future__ import annotations
 
-import os
-
 from .binding import ParleError, lib
 
 NO_TOKEN = -1
@@ -16,17 +14,15 @@ _MODULE = None
 
 
 def load():
-    """The compiled module (built first if it is missing)."""
+    """The compiled module, built first if it is missing or was built from other sources or for another torch."""
     global _MODULE
     if _MODULE is None:
-        import torch
         lib()
         from . import build
-        if not os.path.exists(build.MODULE):
-            build.build_module()
+        build.build_module()
         from . import _token_ops as module
-        if module.torch_version != torch.__version__:
-            raise RuntimeError(f"_token_ops.so was built for torch {module.torch_version}, this is {torch.__version__}: build it again")
+        if module.built_from != build.module_stamp():
+            raise RuntimeError("_token_ops.so changed while it was loaded: start again")
         module.set_error(ParleError)
         _MODULE = module
     return _MODULE
