@@ -1,6 +1,8 @@
 """Build libparle.so (sm_100a) with nvcc and the token operators' Python module _token_ops.so with g++, both in-tree."""
 from __future__ import annotations
 
+import contextlib
+import fcntl
 import hashlib
 import os
 import shutil
@@ -39,17 +41,45 @@ def _run(cmd) -> str:
     return res.stderr
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile the library if it is missing or older than its sources; return its path."""
-    if not force and not _stale():
-        return LIB
+def _compile(cmd, target: str) -> str:
+    """Run a compiler for `target`, which changes at once and only when the whole of it is there."""
+    part = f"{target[:-len('.so')]}.{os.getpid()}.so"
+    try:
+        log = _run(cmd + ["-o", part])
+        os.replace(part, target)
+    finally:
+        if os.path.exists(part):
+            os.remove(part)
+    return log
+
+
+@contextlib.contextmanager
+def _one_at_a_time():
+    """Of the processes that build (ranks started together on a fresh tree), one builds and the others wait."""
+    fd = os.open(HERE, os.O_RDONLY)
+    try:
+        fcntl.flock(fd, fcntl.LOCK_EX)
+        yield
+    finally:
+        os.close(fd)
+
+
+def _compile_library(verbose: bool = False) -> None:
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--threads", "0",
-           "-shared", "-Xcompiler", "-fPIC", "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
+           "-shared", "-Xcompiler", "-fPIC"] + [os.path.join(CSRC, s) for s in SOURCES]
     if verbose:
         cmd.insert(1, "-Xptxas=-v")
-    log = _run(cmd)
+    log = _compile(cmd, LIB)
     if verbose:
         print(log)
+
+
+def build(force: bool = False, verbose: bool = False) -> str:
+    """Compile the library if it is missing or older than its sources; return its path."""
+    if force or _stale():
+        with _one_at_a_time():
+            if force or _stale():
+                _compile_library(verbose)
     return LIB
 
 
@@ -71,20 +101,25 @@ def _module_stale() -> bool:
         return module_stamp().encode() not in f.read()
 
 
-def build_module(force: bool = False) -> str:
-    """Compile the Python module of the token operators, which calls the library beside it, if it is missing or was built from other sources or for
-    another torch or Python than the ones here; return its path."""
-    if not force and not _module_stale():
-        return MODULE
-    build()
+def _compile_module() -> None:
     import torch
     at = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(os.path.realpath(_nvcc())))
-    _run([shutil.which("g++") or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
-          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DBUILT_FROM="{module_stamp()}"', "-isystem", os.path.join(at, "include"),
-          "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(cuda, "include"), os.path.join(CSRC, "token_bindings.cpp"),
-          "-o", MODULE, "-L" + HERE, "-l:libparle.so", "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10",
-          "-Wl,-rpath,$ORIGIN"])
+    _compile([shutil.which("g++") or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+              f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DBUILT_FROM="{module_stamp()}"', "-isystem", os.path.join(at, "include"),
+              "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(cuda, "include"), os.path.join(CSRC, "token_bindings.cpp"),
+              "-L" + HERE, "-l:libparle.so", "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"], MODULE)
+
+
+def build_module(force: bool = False) -> str:
+    """Compile the Python module of the token operators, which calls the library beside it, if it is missing or was built from other sources or for
+    another torch or Python than the ones here; return its path."""
+    if force or _module_stale():
+        with _one_at_a_time():
+            if _stale():
+                _compile_library()
+            if force or _module_stale():
+                _compile_module()
     return MODULE
 
 

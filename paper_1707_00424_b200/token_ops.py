@@ -17,9 +17,9 @@ def load():
     """The compiled module, built first if it is missing or was built from other sources or for another torch."""
     global _MODULE
     if _MODULE is None:
-        lib()
         from . import build
         build.build_module()
+        lib()
         from . import _token_ops as module
         if module.built_from != build.module_stamp():
             raise RuntimeError("_token_ops.so changed while it was loaded: start again")

@@ -67,3 +67,57 @@ def test_a_module_of_other_sources_or_for_another_torch_is_built_again(tmp_path)
             os.utime(here / "paper_1707_00424_b200" / built)
         assert load_in(here) == "compiles"
         changed.write_text(text)
+
+
+BUILD = """
+import os, sys, time
+sys.path.insert(0, '.')
+from paper_1707_00424_b200 import build
+def slowly(cmd):                                          # a compiler that writes its output in two halves
+    with open('compiled', 'a') as f:
+        f.write(os.path.basename(cmd[0]) + chr(10))
+    stamp = [c for c in cmd if 'BUILT_FROM' in c]
+    with open(cmd[cmd.index('-o') + 1], 'wb') as f:
+        f.write(b'first half ')
+        f.flush()
+        time.sleep(1.0)
+        f.write((build.module_stamp() if stamp else 'library').encode() + b' second half')
+    return ''
+build._run = slowly
+build.%s()
+"""
+
+
+def build_at_once(here, what, target, ranks=3):
+    """Several processes build; what a reader saw of the file meanwhile, and how often it was compiled."""
+    import time
+    path, seen = here / "paper_1707_00424_b200" / target, set()
+    path.unlink()
+    running = [subprocess.Popen([sys.executable, "-c", BUILD % what], cwd=here, stderr=subprocess.PIPE, text=True) for _ in range(ranks)]
+    while any(p.poll() is None for p in running):
+        if path.exists():
+            seen.add(path.read_bytes()[-11:])
+        time.sleep(0.01)
+    assert [p.returncode for p in running] == [0] * ranks, [p.stderr.read() for p in running]
+    compiled = (here / "compiled").read_text().split()
+    (here / "compiled").unlink()
+    left = [f for f in os.listdir(here / "paper_1707_00424_b200") if ".so" in f and f not in ("_token_ops.so", "libparle.so")]
+    return seen, compiled, left
+
+
+def test_processes_that_build_at_once_build_once_and_never_show_half_a_file(tmp_path):
+    here = copy_of_the_package(tmp_path)
+    for what, target in (("build_module", "_token_ops.so"), ("build", "libparle.so")):
+        seen, compiled, left = build_at_once(here, what, target)
+        assert seen <= {b"second half"} and len(compiled) == 1 and not left, (seen, compiled, left)
+
+
+def test_a_failed_build_leaves_the_old_file(tmp_path):
+    here = copy_of_the_package(tmp_path)
+    for what, target in (("build_module", "_token_ops.so"), ("build", "libparle.so")):
+        path = here / "paper_1707_00424_b200" / target
+        before = path.read_bytes()
+        code = BUILD.replace("time.sleep(1.0)", "raise RuntimeError('no')") % (what + "(force=True) or print")
+        r = subprocess.run([sys.executable, "-c", code], cwd=here, capture_output=True, text=True, timeout=600)
+        assert r.returncode != 0 and "RuntimeError: no" in r.stderr and path.read_bytes() == before
+        assert sorted(f for f in os.listdir(here / "paper_1707_00424_b200") if f.endswith(".so")) == ["_token_ops.so", "libparle.so"]
