@@ -14,6 +14,7 @@
 
 #include <limits.h>
 
+#include <initializer_list>
 #include <string>
 #include <vector>
 
@@ -56,6 +57,16 @@ struct Call {
             rc = f();
         }
         if (rc != PARLE_OK) fail(rc, name);
+    }
+
+    // Behind the call: the given ones of these results have been written, which autograd's check of saved tensors has to see.  (An inference
+    // tensor has no version; nothing saves it.)
+    static void written(std::initializer_list<PyObject *> results) {
+        for (PyObject *o : results) {
+            if (o == Py_None) continue;
+            const at::Tensor &t = THPVariable_Unpack(o);
+            if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+        }
     }
 
     // The tensor that decides the device, and the stream: `stream` or the device's current one.
@@ -246,6 +257,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const void *const logits_at = logits.data_ptr();
     c.run([&] { return parle_token_logprobs(logits_at, dtype, x.rows, vocab, x.pitch, tokens, scale, k, logprob_at, entropy_at,
                                  k ? top_token_at : nullptr, k ? top_logprob_at : nullptr, flags, c.stream); });
+    c.written({a[4], a[5], a[6], a[7], a[8]});
     PyObject *first = Py_None;
     if (a[1] != Py_None) first = logprob.take(); else Py_INCREF(first);
     return Py_BuildValue("(NNNN)", first, entropy.take(), top_token.take(), top_logprob.take());
@@ -277,6 +289,7 @@ PyObject *token_logprobs_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
     void *const d_at = d.data_ptr();
     c.run([&] { return parle_token_logprobs_grad(logits_at, dtype, x.rows, vocab, x.pitch, tokens, scale, d_logprob, d_entropy, logprob, entropy,
                                       d_at, y.pitch, flags, c.stream); });
+    c.written({a[5], a[6], a[7], a[8]});
     return dlogits.take();
     END_HANDLE_TH_ERRORS
 }
@@ -322,6 +335,7 @@ PyObject *embedding(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     const void *const table_at = table.data_ptr();
     void *const out_at = o.data_ptr();
     c.run([&] { return parle_embedding(table_at, table_dtype, in.gs, in.ld, n_int, vocab, dim, tokens_at, length, scale, out_at, out_dtype, to.gs, to.ld, flags, c.stream); });
+    c.written({a[3], a[5]});
     return out.take();
     END_HANDLE_TH_ERRORS
 }
@@ -379,6 +393,7 @@ PyObject *embedding_grad(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     float *const dtable_at = (float *)g.data_ptr();
     c.run([&] { return parle_embedding_grad(dout_at, dtype, in.gs, in.ld, tokens_at, n_int, length, vocab, dim_int, scale, dtable_at, to.gs, to.ld, accumulate,
                                  workspace, bytes, flags, c.stream); });
+    c.written({a[5], a[7], a[8]});
     return dtable.take();
     END_HANDLE_TH_ERRORS
 }
@@ -412,6 +427,7 @@ PyObject *dropout(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const void *const x_at = x.data_ptr();
     void *const out_at = y.data_ptr();
     c.run([&] { return parle_dropout(x_at, in.pitch, residual, ld_r, out_at, ld_y, dtype, in.rows, in.cols, p, seed, offset, offset_dev, c.stream); });
+    c.written({a[5]});
     return out.take();
     END_HANDLE_TH_ERRORS
 }

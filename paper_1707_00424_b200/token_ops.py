@@ -3,7 +3,11 @@ with entropy, top alternatives and gradient.
 
 Each function checks its tensors, then makes one call of the C ABI (include/parle.h has the definitions) on `stream`, or on the
 current stream of the tensors' device: both in the module _token_ops (csrc/token_bindings.cpp).  Results go to the tensors given
-for them; those not given are allocated with torch.  Tensors are strided as they come: only the last dimension has to be dense."""
+for them; those not given are allocated with torch.  Tensors are strided as they come: only the last dimension has to be dense.
+
+The functions stand outside autograd, as all of this package: what they return has no graph, whether an input requires a gradient or not;
+their gradients are calls of their own.  Tensors given for results count as modified in place, so that a backward pass of torch that
+saved one of them raises its usual error."""
 from __future__ import annotations
 
 from .binding import ParleError, lib
