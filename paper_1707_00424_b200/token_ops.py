@@ -54,7 +54,9 @@ def embedding(table, tokens, scale: float = 1.0, *, out=None, dtype=None, flags=
 
 
 def embedding_grad_workspace_bytes(n: int, length: int, vocab: int, dim: int) -> int:
-    """Bytes of scratch that embedding_grad() needs for n tables and `length` positions each."""
+    """Bytes of scratch that embedding_grad() needs for n tables and `length` positions each; 0 for sizes that it refuses."""
+    if min(n, length, vocab, dim) < 0 or max(n, vocab, dim) >= 1 << 31 or length >= 1 << 63:      # (ctypes would cut them off)
+        return 0
     return lib().parle_embedding_grad_workspace_bytes(n, length, vocab, dim)
 
 

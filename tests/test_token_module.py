@@ -121,3 +121,11 @@ def test_a_failed_build_leaves_the_old_file(tmp_path):
         r = subprocess.run([sys.executable, "-c", code], cwd=here, capture_output=True, text=True, timeout=600)
         assert r.returncode != 0 and "RuntimeError: no" in r.stderr and path.read_bytes() == before
         assert sorted(f for f in os.listdir(here / "paper_1707_00424_b200") if f.endswith(".so")) == ["_token_ops.so", "libparle.so"]
+
+
+def test_workspace_of_sizes_beyond_the_c_types_is_that_of_invalid_ones():
+    import paper_1707_00424_b200 as pb
+    size = pb.embedding_grad_workspace_bytes
+    assert size(1, 2000, 10, 4) > 0
+    for wrong in ((1 + (1 << 32), 2000, 10, 4), (1, 2000 + (1 << 64), 10, 4), (1, 2000, 10 + (1 << 32), 4), (1, 2000, 10, 4 + (1 << 32)), (1, -1, 10, 4), (1 - (1 << 32), 2000, 10, 4)):
+        assert size(*wrong) == 0, wrong
