@@ -9,8 +9,8 @@
 // Up to kDirectMost positions ("direct", one launch, no workspace): a block takes a set of table rows, looks through all the
 // tokens, notes for each of its rows the positions that hold its token, puts them in order and sums.
 //
-// More positions ("sorted"): one kernel sorts the positions by (token, position) in the shared memory of a cluster.  The sorted
-// sequence is then cut into chunks of kChunk positions; a block sums the runs of equal tokens in its chunk and writes the rows of
+// More positions ("sorted"): the positions are sorted by (token, position), up to kRankedMost by counting, up to kSortMost in the shared
+// memory of a cluster, beyond by launches of their own.  The sorted sequence is then cut into chunks of kChunk positions; a block sums the runs of equal tokens in its chunk and writes the rows of
 // those that begin and end there, while other blocks write zeros to the rows of tokens that do not occur.  A run that crosses a
 // chunk's border leaves one partial row per chunk, which a last kernel joins.  Work is shared out by position, so it does not
 // matter how often which token occurs.

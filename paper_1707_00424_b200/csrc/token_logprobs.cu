@@ -387,7 +387,8 @@ __device__ __forceinline__ void rank_candidates(const Row<T> &row, int begin, in
             if (i < found && above < k) sh.top[above] = key;
         }
     } else {
-        // too many logits above the bound (large ones gathered in few groups): one pass over the block's logits per rank
+        // too many logits above the bound (large ones gathered in few groups): one pass over the block's logits per rank.  200 rows of
+        // 65536 bf16 logits whose large ones lie in three of every 64 granules, 32 alternatives: 543 us, ordinary ones 12.5
         constexpr int N = Granule<T>::N;
         unsigned long long last = ~0ull;
         for (int r = 0; r < k; ++r) {
@@ -622,8 +623,8 @@ __device__ __forceinline__ void write_top(const RowsArgs &p, long long at, const
     if (p.top_logprob) p.top_logprob[at * p.k + threadIdx.x] = undefined ? r.inv_s : real ? r.logprob(key_value(key)) : -INFINITY;
 }
 
-// Rows of any length, streamed: one block per row.  2048 x 131072 bf16 logits: 88 us, 0.93 of the copy rate, without alternatives, 98-100
-// with eight; exponentials (a warp instruction takes 7.8 cycles of their pipe) and issue slots are both in use at 62-65 %.
+// Rows of any length, streamed: one block per row.  2048 x 131072 bf16 logits in a graph: 85 us without alternatives, 92 (0.89 of the copy
+// rate) where every call has other logits and so none in L2; 105 with eight alternatives, 138 with 32; called, some 3-5 us more.  Exponentials (a warp instruction takes 7.8 cycles of their pipe) and issue slots are both in use at 62-65 %.
 template <typename T, int BLOCK, int U>
 __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) token_logprobs_kernel(const RowsArgs p) {
     __shared__ Shared<BLOCK> sh;
@@ -833,7 +834,7 @@ template <typename T, int BLOCK> __device__ __forceinline__ void zero_row(const 
 }
 
 // The gradient of long rows, by a block each: a second pass reads the row again, from L2.  Its reads and the stores are marked as the
-// last use of their lines, so that rows between their two passes stay (a fifth of them does not).  2048 x 131072 bf16 logits: 200-204 us;
+// last use of their lines, so that rows between their two passes stay (a fifth of them does not).  2048 x 131072 bf16 logits: 204-211 us;
 // two exponentials per logit take 116 us of their pipe, the bytes 164 us at the copy rate.  SHIFTED: rows of
 // dlogits may begin at other places of 16 bytes than the logits; 2048 x 131071 of pitch 131072 to 131071: 243 us, element by element 802.
 template <typename T, int BLOCK, int U, bool ENT, bool SHIFTED>
@@ -1037,7 +1038,7 @@ template <typename T, bool GRAD, bool ENT> int launch_rows(const RowsArgs &p, in
         if (p.k > 0 && granules > 32 && granules <= 128 * 2 && p.rows <= (p.k > 12 ? 8 : 4) * sms) return launch_held<T, 128, 2, GRAD, ENT>(p, 1, stream);
     // Short rows: a warp each; with two groups a thread where so many alternatives are wanted that 32 groups, or a very short row's
     // fewer, set their bound too low.  Measured, with / without: 8192 x 500 bf16 logits, 20 alternatives 19.3 us without, 25: 22.3 / 23.8,
-    // 32: 24.4 / 88; 6827 x 150, 20: 16.8 / 46.
+    // 32: 23.6 / 88; 6827 x 150, 20: 15.9 / 46.
     if constexpr (!GRAD)
         if (4LL * p.k > 3 * std::min(32LL, granules) && granules <= 32 * U)
             return granules <= 32 * 4 ? launch_held<T, 32, 4, GRAD, ENT, true>(p, 1, stream) : launch_held<T, 32, U, GRAD, ENT, true>(p, 1, stream);
