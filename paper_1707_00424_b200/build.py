@@ -83,15 +83,22 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+MODULE_SOURCES = [os.path.join(CSRC, "token_bindings.cpp"), os.path.join(HERE, "..", "include", "parle.h")]
+
+
 def module_stamp() -> str:
-    """What the module has to be built from: its sources' contents, the torch and the Python that are running.  The compiler puts it into
-    the module, so that one built from anything else is known whatever the files' times are."""
+    """What the module has to be built from: the torch and the Python that are running and its sources' contents (nothing behind "of " where
+    there are only built files).  The compiler puts it into the module, so that one built from anything else is known whatever the
+    files' times are."""
     import torch
-    h = hashlib.sha256(f"{torch.__version__} {sys.implementation.cache_tag}".encode())
-    for path in (os.path.join(CSRC, "token_bindings.cpp"), os.path.join(HERE, "..", "include", "parle.h")):
+    stamp = f"token operators for torch {torch.__version__}, {sys.implementation.cache_tag}, of "
+    if not all(os.path.exists(path) for path in MODULE_SOURCES):
+        return stamp
+    h = hashlib.sha256()
+    for path in MODULE_SOURCES:
         with open(path, "rb") as f:
             h.update(f.read())
-    return "token operators of " + h.hexdigest()[:32]
+    return stamp + h.hexdigest()[:32]
 
 
 def _module_stale() -> bool:
@@ -115,6 +122,8 @@ def build_module(force: bool = False) -> str:
     """Compile the Python module of the token operators, which calls the library beside it, if it is missing or was built from other sources or for
     another torch or Python than the ones here; return its path."""
     if force or _module_stale():
+        if not os.path.exists(MODULE_SOURCES[0]):
+            raise RuntimeError(f"{MODULE} is missing or not built as \"{module_stamp()}..\", and its sources are not here to build it from")
         with _one_at_a_time():
             if _stale():
                 _compile_library()

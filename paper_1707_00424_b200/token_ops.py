@@ -25,7 +25,7 @@ def load():
         build.build_module()
         lib()
         from . import _token_ops as module
-        if module.built_from != build.module_stamp():
+        if not module.built_from.startswith(build.module_stamp()):
             raise RuntimeError("_token_ops.so changed while it was loaded: start again")
         module.set_error(ParleError)
         _MODULE = module

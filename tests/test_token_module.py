@@ -69,6 +69,16 @@ def test_a_module_of_other_sources_or_for_another_torch_is_built_again(tmp_path)
         changed.write_text(text)
 
 
+def test_built_files_are_loaded_without_their_sources(tmp_path):
+    import shutil
+    here = copy_of_the_package(tmp_path)
+    shutil.rmtree(here / "include")
+    shutil.rmtree(here / "paper_1707_00424_b200" / "csrc")
+    assert load_in(here) == "loaded"
+    r = subprocess.run([sys.executable, "-c", LOAD % "torch.__version__ = '0.1'"], cwd=here, capture_output=True, text=True, timeout=600)
+    assert r.returncode != 0 and "torch 0.1" in r.stderr
+
+
 BUILD = """
 import os, sys, time
 sys.path.insert(0, '.')
