@@ -428,6 +428,58 @@ int parle_dropout(const void *x, long long ld_x, const void *residual, long long
                   int dtype, long long rows, long long cols, double p, uint64_t seed, uint64_t offset,
                   const uint64_t *offset_dev, void *cuda_stream);
 
+/* What follows a gradient and what follows the logits, with the rules of the token operators above (streams, types, pitches, codes).
+ * Lists of tensors are host arrays, read before the call returns; a tensor is `size` consecutive elements (0: nothing to do). */
+typedef struct {
+    const void *grad;    /* dev [size] */
+    long long size;
+} parle_grad_tensor;
+
+/* norm (dev [1] fp32) <- sqrt(sum of the squares of all elements of the tensors, of one type), 0 for none.  The sum is as good as one in
+ * 64 bits over the whole range of the types and is added in one order: the same inputs give the same bits.  workspace dev, 128-byte aligned,
+ * >= parle_grad_norm_workspace_bytes() (0 for a bad list): scratch of this call alone until its work has finished. */
+size_t parle_grad_norm_workspace_bytes(const parle_grad_tensor *tensors, int count);
+int parle_grad_norm(const parle_grad_tensor *tensors, int count, int grad_dtype, float *norm, void *workspace, size_t workspace_bytes,
+                    void *cuda_stream);
+
+#define PARLE_NO_COPY -1
+#define PARLE_ADAMW_BLOCK 256
+typedef struct {
+    void *param;             /* dev [size], param_dtype */
+    const void *grad;        /* dev [size], grad_dtype */
+    void *exp_avg;           /* dev [size]: m, fp32, or its codes, one byte each */
+    void *exp_avg_sq;        /* dev [size]: v, fp32, or the codes of sqrt(v) */
+    float *exp_avg_scale;    /* dev [ceil(size / PARLE_ADAMW_BLOCK)], 8-bit moments only */
+    float *exp_avg_sq_scale; /* the same of sqrt(v) */
+    void *copy;              /* dev [size], copy_dtype; not read where that is PARLE_NO_COPY */
+    long long size;
+} parle_adamw_tensor;
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;  /* lr, weight_decay >= 0; betas in [0, 1); eps in [2^-60, 1] */
+    double grad_scale;       /* > 0; gradients are multiplied by it (1 / loss scale) */
+    double max_norm;         /* > 0; +INFINITY: no clipping */
+    long long step;          /* t = step + *step_dev, 1 in the first step */
+    const float *norm;       /* dev [1] or NULL: parle_grad_norm of the gradients as they are given; needed to clip */
+    const float *lr_dev;     /* dev [1] or NULL: lr is multiplied by it */
+    const int64_t *step_dev; /* dev [1] or NULL (0) */
+} parle_adamw_step;
+
+/* One AdamW step of every tensor of the list:
+ *   c = grad_scale min(1, max_norm / (grad_scale *norm)),  g = c grad,  m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2
+ *   param <- (1 - lr weight_decay) param - lr / (1 - beta1^t)  m / (sqrt(v / (1 - beta2^t)) + eps),     copy <- param in 16 bits
+ * in fp32, stored with one rounding.  Where *norm is no finite number nothing is written (the step is skipped), and PARLE_FLAG_NONFINITE
+ * is set in *flags (dev [1] int32 or NULL); it is set, too, where a new parameter is no finite number.  state_bits 32: moments are fp32.
+ * state_bits 8: m and sqrt(v) are e4m3 codes times a scale for each PARLE_ADAMW_BLOCK consecutive elements, the largest magnitude / 448
+ * (0, with codes of 0, where all magnitudes are below 2^-100; NaN where one is no finite number).  A magnitude y / scale between two codes
+ * goes to the upper one where its distance from the lower, in parts of theirs, plus u / 2^24 is at least 1: u = (12664745 i + 9560335 t) mod 2^24
+ * for m, 2^24 - 1 - u for sqrt(v), i the element's number in its tensor; a root above 0 is held as at least the smallest code.  Over the
+ * steps this rounds to neither side: moments that move by less than a code's distance a step move all the same.
+ * All zeros are the state of no steps, in both forms.  Arrays may not overlap; an array that begins where another begins is EINVAL.
+ * copy_dtype: PARLE_BF16 or PARLE_F16 beside fp32 parameters, else PARLE_NO_COPY.  step_dev and lr_dev are read when the kernel runs: a
+ * captured step that is replayed moves on when the caller advances them. */
+int parle_adamw(const parle_adamw_tensor *tensors, int count, int param_dtype, int grad_dtype, int copy_dtype, int state_bits,
+                const parle_adamw_step *step, int32_t *flags, void *cuda_stream);
+
 /* Kernels launched by this context since creation (for accounting). */
 long long parle_launch_count(const parle_ctx *ctx);
 

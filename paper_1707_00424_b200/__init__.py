@@ -8,3 +8,4 @@ from .binding import (  # noqa: F401
 from .token_ops import (  # noqa: F401
     NO_TOKEN, TOP_MAX, dropout, embedding, embedding_grad, embedding_grad_workspace_bytes, token_logprobs, token_logprobs_grad,
 )
+from .optimizer_ops import adamw, adamw_state, grad_norm  # noqa: F401

@@ -35,6 +35,19 @@ class _Buffers(C.Structure):
                 ("xbar", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
+class GradTensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("size", C.c_longlong)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("param", "grad", "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale", "copy")] + [("size", C.c_longlong)]
+
+
+class AdamwStep(C.Structure):
+    _fields_ = [(name, C.c_double) for name in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale", "max_norm")] + [
+        ("step", C.c_longlong), ("norm", C.c_void_p), ("lr_dev", C.c_void_p), ("step_dev", C.c_void_p)]
+
+
 def library_path() -> str:
     return os.path.join(_HERE, "libparle.so")
 
@@ -96,6 +109,9 @@ def lib() -> C.CDLL:
         "parle_embedding_grad_workspace_bytes": (sz, [ci, ll, ci, ci]),
         "parle_embedding_grad": (ci, [vp, ci, ll, ll, vp, ci, ll, ci, ci, cd, vp, ll, ll, ci, vp, sz, vp, vp]),
         "parle_dropout": (ci, [vp, ll, vp, ll, vp, ll, ci, ll, ll, cd, C.c_uint64, C.c_uint64, vp, vp]),
+        "parle_grad_norm_workspace_bytes": (sz, [C.POINTER(GradTensor), ci]),
+        "parle_grad_norm": (ci, [C.POINTER(GradTensor), ci, ci, vp, vp, sz, vp]),
+        "parle_adamw": (ci, [C.POINTER(AdamwTensor), ci, ci, ci, ci, ci, C.POINTER(AdamwStep), vp, vp]),
         "parle_launch_count": (C.c_longlong, [vp]),
         "parle_last_cuda_error": (ci, [vp]),
         "parle_strerror": (C.c_char_p, [ci]),

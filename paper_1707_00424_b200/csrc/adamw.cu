@@ -1,0 +1,413 @@
+// parle_adamw: one AdamW step (Loshchilov, Hutter, "Decoupled weight decay regularization", 2019) of a list of tensors, moments in 32 or
+// in 8 bits.
+//
+//   g = c grad,  m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p = (1 - lr wd) p - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
+//
+// Every element is read once and written once: bound by DRAM, 28 bytes an fp32 element with 32-bit moments, 10 to 16 with 8-bit ones.
+// All arithmetic is fp32; the root and the reciprocal are the hardware's (2^-22 of the step, which moves p by far less than p's own
+// rounding).
+//
+// 8-bit moments.  256 elements, a warp's eight a lane, share an fp32 scale; codes are e4m3 (range 2^-9 .. 448) of m and of r = sqrt(v),
+// whose range is half of v's in powers of two.  A code's neighbours are 6 to 12 % away, but b2 = 0.999 moves v by 0.1 % a step: rounded to
+// nearest, r would stay on its code for good.  So the value between two codes goes to the upper one when the rest reaches a threshold that
+// runs evenly through [0, 1) from step to step and from element to element, u = frac(i a + t b) with a, b powers of the plastic
+// number's inverse (Weyl's equidistribution; Roberts' choice of a, b): a drift of f codes a step moves the code in a share f of the
+// steps.  24 bits of u: with 8, as in the hardware's stochastic conversion, f itself (0.008 a step) would be rounded to 0.4 % of a code.
+// The threshold is a function of (i, t): no random state, the same call gives the same bits.
+#include <math.h>
+#include <stdlib.h>
+
+#include <type_traits>
+
+#include "tensor_list.cuh"
+
+using namespace parle;
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBlock = 256;                              // elements that share a scale
+constexpr float kLargest = 448.f;                        // of e4m3
+constexpr float kNothing = 0x1p-100f;                    // a block whose values all lie below this holds zeros
+constexpr uint32_t kWeylI = 12664745, kWeylT = 9560335;  // 2^24 / p and 2^24 / p^2, p the plastic number; odd: all 2^24 thresholds occur
+constexpr int kSteps = 2;                                // groups of a thread in a chunk
+constexpr int kChunk = kThreads * 8 * kSteps;
+
+struct Entry {
+    void *param, *exp_avg, *exp_avg_sq, *copy;
+    const void *grad;
+    float *exp_avg_scale, *exp_avg_sq_scale;
+    long long size_shift;                                // size << 4 | shift << 1 | whether whole groups lie on 16-byte boundaries
+};
+template <int CAP> struct List {
+    int count;
+    uint32_t first[CAP];                                 // first chunk of each entry
+    Entry entry[CAP];
+};
+constexpr int kFew = 24, kMany = 440;                    // a launch takes 32764 bytes of arguments at most
+
+struct StepArgs {
+    float b1, one_minus_b1, b2, one_minus_b2, eps;
+    float rate, root_scale, decay;                       // lr / (1 - b1^t), 1 / sqrt(1 - b2^t), 1 - lr wd, where neither step_dev nor lr_dev is given
+    float grad_scale, max_norm;
+    double lr, weight_decay, log_b1, log_b2;
+    long long step;
+    const float *norm, *lr_dev;
+    const long long *step_dev;
+    int32_t *flags;
+};
+
+struct NoCopy {};
+template <typename T> struct Limit;                      // magnitudes below it are finite once rounded to the type
+template <> struct Limit<float> { static constexpr float value = INFINITY; };
+template <> struct Limit<NoCopy> { static constexpr float value = INFINITY; };
+template <> struct Limit<__nv_bfloat16> { static constexpr float value = 0x1.ffp127f; };
+template <> struct Limit<__half> { static constexpr float value = 65520.f; };
+
+struct Scalars {                                         // what a block needs beside its elements
+    float c, rate, root_scale, decay;
+    uint32_t weyl;                                       // t's part of the threshold
+    bool skip;
+};
+
+__device__ __forceinline__ float root(float v) {
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float reciprocal(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+__device__ __forceinline__ Scalars scalars(const StepArgs &a) {
+    __shared__ Scalars shared;
+    Scalars s{a.grad_scale, a.rate, a.root_scale, a.decay, (uint32_t)a.step * kWeylT, false};
+    if (a.step_dev || a.lr_dev) {                        // (the same for all blocks)
+        if (threadIdx.x == 0) {
+            const long long t = a.step + (a.step_dev ? *a.step_dev : 0);
+            const double lr = a.lr * (a.lr_dev ? (double)*a.lr_dev : 1.0);
+            s.rate = (float)(lr / -expm1((double)t * a.log_b1));
+            s.root_scale = (float)(1.0 / sqrt(-expm1((double)t * a.log_b2)));
+            s.decay = (float)(1.0 - lr * a.weight_decay);
+            s.weyl = (uint32_t)t * kWeylT;
+            shared = s;
+        }
+        __syncthreads();
+        s = shared;
+    }
+    if (a.norm) {
+        const float norm = *a.norm;
+        s.skip = !(fabsf(norm) < INFINITY);
+        s.c *= fminf(1.f, __fdiv_rn(a.max_norm, norm * a.grad_scale));
+        if (s.skip && a.flags && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.flags, PARLE_FLAG_NONFINITE);
+    }
+    return s;
+}
+
+// Two e4m3 codes as fp32.
+__device__ __forceinline__ float2 decode2(uint32_t codes) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)codes));
+    return __half22float2(*reinterpret_cast<const __half2 *>(&h));
+}
+__device__ __forceinline__ void decode8(uint2 codes, float scale, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = decode2((i < 2 ? codes.x : codes.y) >> (i % 2 * 16));
+        v[2 * i] = f.x * scale;
+        v[2 * i + 1] = f.y * scale;
+    }
+}
+// A code in the top byte.  y in [0, 448]; times 2^-120 its exponent is fp32's, subnormal where the code is: 20 bits lie below the code, 24
+// with the shift, where the threshold is added.
+__device__ __forceinline__ uint32_t code_above(float y, uint32_t threshold) { return (__float_as_uint(y * 0x1p-120f) << 4) + threshold; }
+__device__ __forceinline__ uint32_t top_bytes(const uint32_t *t) {
+    return __byte_perm(__byte_perm(t[0], t[1], 0x0073), __byte_perm(t[2], t[3], 0x0073), 0x5410);
+}
+
+// The scale of a block of a warp from the largest magnitude of each lane (as bits: what is not finite is largest); inverse: what values
+// are multiplied by (rounded down: no product is above 448).
+__device__ __forceinline__ float block_scale(uint32_t largest, float *inverse) {
+    const float top = __uint_as_float(__reduce_max_sync(0xffffffffu, largest));
+    const bool none = top < kNothing, finite = top < INFINITY;
+    *inverse = none || !finite ? 0.f : __fdiv_rd(kLargest, top);
+    return none ? 0.f : finite ? __fdiv_rn(top, kLargest) : NAN;
+}
+
+template <typename P, typename G, typename C, int BITS, class L>
+__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ L list, const __grid_constant__ StepArgs a) {
+    const Scalars s = scalars(a);
+    if (s.skip) return;
+    const int index = entry_of(list, blockIdx.x);
+    const Entry &t = list.entry[index];
+    const long long n = t.size_shift >> 4;
+    const int shift = (int)(t.size_shift >> 1) & 7;
+    const bool aligned = t.size_shift & 1;
+    P *const param = static_cast<P *>(t.param);
+    const G *const grad = static_cast<const G *>(t.grad);
+    bool ok = true;
+    long long e0 = (long long)(blockIdx.x - list.first[index]) * kChunk + threadIdx.x * 8 - shift;
+    for (int step = 0; step < kSteps; ++step, e0 += kThreads * 8) {
+        if (BITS == 8 ? e0 - (int)(threadIdx.x % 32) * 8 >= n : e0 >= n) break;      // (whole warps: a block's lanes meet below)
+        const bool whole = aligned && e0 >= 0 && e0 + 8 <= n;
+        float p[8], g[8], m[8], v[8];
+        if (whole) {
+            Pack8<P> pp;
+            Pack8<G> gg;
+            pp.load(param + e0);
+            gg.load(grad + e0);
+            if (BITS == 32) {
+                Pack8<float> mm, vv;
+                mm.load(static_cast<const float *>(t.exp_avg) + e0);
+                vv.load(static_cast<const float *>(t.exp_avg_sq) + e0);
+                mm.get(m);
+                vv.get(v);
+            } else {
+                const uint2 mc = *reinterpret_cast<const uint2 *>(static_cast<const char *>(t.exp_avg) + e0);
+                const uint2 rc = *reinterpret_cast<const uint2 *>(static_cast<const char *>(t.exp_avg_sq) + e0);
+                decode8(mc, t.exp_avg_scale[e0 / kBlock], m);
+                decode8(rc, t.exp_avg_sq_scale[e0 / kBlock], v);
+            }
+            pp.get(p);
+            gg.get(g);
+        } else {
+            load_some(param, e0, n, p);
+            load_some(grad, e0, n, g);
+            if (BITS == 32) {
+                load_some(static_cast<const float *>(t.exp_avg), e0, n, m);
+                load_some(static_cast<const float *>(t.exp_avg_sq), e0, n, v);
+            } else {
+                uint32_t mc[2] = {0, 0}, rc[2] = {0, 0};
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (e0 + i < n) {
+                        mc[i / 4] |= (uint32_t)static_cast<const unsigned char *>(t.exp_avg)[e0 + i] << (i % 4 * 8);
+                        rc[i / 4] |= (uint32_t)static_cast<const unsigned char *>(t.exp_avg_sq)[e0 + i] << (i % 4 * 8);
+                    }
+                const long long block = min(e0, n - 1) / kBlock;
+                decode8(make_uint2(mc[0], mc[1]), t.exp_avg_scale[block], m);
+                decode8(make_uint2(rc[0], rc[1]), t.exp_avg_sq_scale[block], v);
+                if (e0 >= n) {                           // (a scale may be NaN: lanes behind the end hold zeros all the same)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) m[i] = v[i] = 0.f;
+                }
+            }
+        }
+        float r[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            g[i] *= s.c;
+            if (BITS == 8) v[i] *= v[i];
+            m[i] = fmaf(a.b1, m[i], a.one_minus_b1 * g[i]);
+            v[i] = fmaf(a.b2, v[i], a.one_minus_b2 * g[i] * g[i]);
+            r[i] = root(v[i]);
+            p[i] = fmaf(p[i], s.decay, -s.rate * (m[i] * reciprocal(fmaf(r[i], s.root_scale, a.eps))));
+            ok &= fabsf(p[i]) < fminf(Limit<P>::value, Limit<C>::value);
+        }
+        uint2 mc, rc;
+        if (BITS == 8) {
+            uint32_t m_top = 0, r_top = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool there = whole || e0 + i < n;
+                m_top = max(m_top, there ? __float_as_uint(m[i]) & 0x7fffffffu : 0u);
+                r_top = max(r_top, there ? __float_as_uint(r[i]) & 0x7fffffffu : 0u);
+            }
+            float m_inverse, r_inverse;
+            const float m_scale = block_scale(m_top, &m_inverse), r_scale = block_scale(r_top, &r_inverse);
+            if (threadIdx.x % 32 == 0) {
+                t.exp_avg_scale[e0 / kBlock] = m_scale;
+                t.exp_avg_sq_scale[e0 / kBlock] = r_scale;
+            }
+            uint32_t mt[8], rt[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t u = ((uint32_t)(e0 + i) * kWeylI + s.weyl) & 0xffffffu;
+                mt[i] = m_inverse == 0.f ? 0u : code_above(fabsf(m[i]) * m_inverse, u) | (__float_as_uint(m[i]) & 0x80000000u);
+                rt[i] = r_inverse == 0.f ? 0u : code_above(r[i] * r_inverse, u ^ 0xffffffu);
+                if (r_inverse != 0.f && r[i] > 0.f) rt[i] = max(rt[i], 1u << 24);     // else m would be divided by eps alone one day
+            }
+            mc = make_uint2(top_bytes(mt), top_bytes(mt + 4));
+            rc = make_uint2(top_bytes(rt), top_bytes(rt + 4));
+        }
+        if (whole) {
+            Pack8<P> pp;
+            pp.set(p);
+            pp.store(param + e0);
+            if (BITS == 32) {
+                Pack8<float> mm, vv;
+                mm.set(m);
+                vv.set(v);
+                mm.store(static_cast<float *>(t.exp_avg) + e0);
+                vv.store(static_cast<float *>(t.exp_avg_sq) + e0);
+            } else {
+                *reinterpret_cast<uint2 *>(static_cast<char *>(t.exp_avg) + e0) = mc;
+                *reinterpret_cast<uint2 *>(static_cast<char *>(t.exp_avg_sq) + e0) = rc;
+            }
+            if constexpr (!std::is_same<C, NoCopy>::value) {
+                Pack8<C> cc;
+                cc.set(p);
+                cc.store(static_cast<C *>(t.copy) + e0);
+            }
+        } else {
+            store_some(param, e0, n, p);
+            if (BITS == 32) {
+                store_some(static_cast<float *>(t.exp_avg), e0, n, m);
+                store_some(static_cast<float *>(t.exp_avg_sq), e0, n, v);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (e0 + i < n) {
+                        static_cast<unsigned char *>(t.exp_avg)[e0 + i] = (unsigned char)((i < 4 ? mc.x : mc.y) >> (i % 4 * 8));
+                        static_cast<unsigned char *>(t.exp_avg_sq)[e0 + i] = (unsigned char)((i < 4 ? rc.x : rc.y) >> (i % 4 * 8));
+                    }
+            }
+            if constexpr (!std::is_same<C, NoCopy>::value) store_some(static_cast<C *>(t.copy), e0, n, p);
+        }
+    }
+    if (a.flags && !ok) atomicOr(a.flags, PARLE_FLAG_NONFINITE);
+}
+
+// Whether an address occurs twice among those given to see().  Room for the addresses is on the stack for a list of one launch's size.
+class Addresses {
+    static constexpr int kSmall = 4096;
+    uintptr_t small_[kSmall];
+    uintptr_t *slot_ = small_;
+    size_t mask_ = kSmall - 1;
+
+  public:
+    ~Addresses() {
+        if (slot_ != small_) free(slot_);
+    }
+    bool prepare(size_t addresses) {
+        size_t slots = kSmall;
+        while (slots < 2 * addresses) slots *= 2;
+        if (slots > kSmall && !(slot_ = static_cast<uintptr_t *>(malloc(slots * sizeof(uintptr_t))))) {
+            slot_ = small_;
+            return false;
+        }
+        mask_ = slots - 1;
+        for (size_t i = 0; i < slots; ++i) slot_[i] = 0;
+        return true;
+    }
+    bool see(const void *p) {
+        const uintptr_t key = reinterpret_cast<uintptr_t>(p);
+        for (size_t i = (size_t)((key * 0x9E3779B97F4A7C15ull) >> 20) & mask_;; i = (i + 1) & mask_) {
+            if (slot_[i] == key) return true;
+            if (slot_[i] == 0) {
+                slot_[i] = key;
+                return false;
+            }
+        }
+    }
+};
+
+template <typename P, typename G, typename C, int BITS, class L> int launch_list(const L &list, const StepArgs &a, unsigned chunks, cudaStream_t stream) {
+    adamw_kernel<P, G, C, BITS, L><<<chunks, kThreads, 0, stream>>>(list, a);
+    return launch_status();
+}
+
+template <int CAP, typename P, typename G, typename C, int BITS>
+int launch_all(const parle_adamw_tensor *tensors, int count, const StepArgs &a, cudaStream_t stream) {
+    List<CAP> list;
+    list.count = 0;
+    unsigned chunks = 0;
+    for (int i = 0;; ++i) {
+        const bool end = i == count;
+        const long long n = end ? 0 : tensors[i].size;
+        const long long more = (n + 7 + kChunk - 1) / kChunk;
+        if (list.count && (end || list.count == CAP || chunks + more >= 1LL << 31)) {
+            const int rc = launch_list<P, G, C, BITS>(list, a, chunks, stream);
+            if (rc != PARLE_OK) return rc;
+            list.count = 0;
+            chunks = 0;
+        }
+        if (end) return PARLE_OK;
+        if (n == 0) continue;
+        const parle_adamw_tensor &t = tensors[i];
+        // 32-bit moments: groups are cut where all arrays' are, if they agree on that; 8-bit ones: at every eighth element
+        const int shift = BITS == 8 ? 0 : group_shift(t.param, sizeof(P));
+        bool aligned = group_shift(t.param, sizeof(P)) == shift && group_shift(t.grad, sizeof(G)) == shift;
+        if (BITS == 32) aligned = aligned && group_shift(t.exp_avg, 4) == shift && group_shift(t.exp_avg_sq, 4) == shift;
+        else aligned = aligned && group_shift(t.exp_avg, 1) == 0 && group_shift(t.exp_avg_sq, 1) == 0;
+        if constexpr (!std::is_same<C, NoCopy>::value) aligned = aligned && group_shift(t.copy, sizeof(C)) == shift;
+        list.first[list.count] = chunks;
+        list.entry[list.count++] = {t.param, t.exp_avg, t.exp_avg_sq, t.copy, t.grad, t.exp_avg_scale, t.exp_avg_sq_scale,
+                                    n << 4 | (aligned ? shift : 0) << 1 | (aligned ? 1 : 0)};
+        chunks += (unsigned)((n + (aligned ? shift : 0) + kChunk - 1) / kChunk);
+    }
+}
+
+template <typename P, typename G, typename C>
+int launch_bits(const parle_adamw_tensor *tensors, int count, int bits, const StepArgs &a, cudaStream_t stream) {
+    if (bits == 8) return count <= kFew ? launch_all<kFew, P, G, C, 8>(tensors, count, a, stream) : launch_all<kMany, P, G, C, 8>(tensors, count, a, stream);
+    return count <= kFew ? launch_all<kFew, P, G, C, 32>(tensors, count, a, stream) : launch_all<kMany, P, G, C, 32>(tensors, count, a, stream);
+}
+
+}  // namespace
+
+extern "C" int parle_adamw(const parle_adamw_tensor *tensors, int count, int param_dtype, int grad_dtype, int copy_dtype, int state_bits,
+                           const parle_adamw_step *step, int32_t *flags, void *cuda_stream) {
+    if (count < 0 || (count && !tensors) || !step || !valid_dtype(param_dtype) || !valid_dtype(grad_dtype)) return PARLE_EINVAL;
+    if (state_bits != 8 && state_bits != 32) return PARLE_EINVAL;
+    if (copy_dtype != PARLE_NO_COPY && (param_dtype != PARLE_F32 || (copy_dtype != PARLE_BF16 && copy_dtype != PARLE_F16))) return PARLE_EINVAL;
+    const parle_adamw_step &h = *step;
+    const float lr = (float)h.lr, decay = (float)(1.0 - h.lr * h.weight_decay), grad_scale = (float)h.grad_scale;
+    if (!(h.lr >= 0.0 && isfinite(lr)) || !(h.beta1 >= 0.0 && h.beta1 < 1.0) || !(h.beta2 >= 0.0 && h.beta2 < 1.0)) return PARLE_EINVAL;
+    if (!(h.eps >= 0x1p-60 && h.eps <= 1.0) || !(h.weight_decay >= 0.0 && isfinite(decay))) return PARLE_EINVAL;
+    if (!(grad_scale > 0.f && isfinite(grad_scale)) || !(h.max_norm > 0.0) || (float)h.max_norm == 0.f) return PARLE_EINVAL;
+    if (!(h.norm || h.max_norm == INFINITY)) return PARLE_EINVAL;
+    if (h.step_dev ? h.step < 0 : h.step < 1) return PARLE_EINVAL;
+    if (reinterpret_cast<uintptr_t>(h.norm) % 4 || reinterpret_cast<uintptr_t>(h.lr_dev) % 4 || reinterpret_cast<uintptr_t>(h.step_dev) % 8 ||
+        reinterpret_cast<uintptr_t>(flags) % 4) return PARLE_EALIGN;
+    const bool copies = copy_dtype != PARLE_NO_COPY;
+    for (int i = 0; i < count; ++i) {
+        const parle_adamw_tensor &t = tensors[i];
+        if (t.size < 0) return PARLE_EINVAL;
+        if (t.size == 0) continue;
+        if (t.size > PARLE_TOKEN_MAX_ELEMENTS) return PARLE_ETOOBIG;
+        if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq || (copies && !t.copy)) return PARLE_EINVAL;
+        if (state_bits == 8 && (!t.exp_avg_scale || !t.exp_avg_sq_scale)) return PARLE_EINVAL;
+        uintptr_t off = reinterpret_cast<uintptr_t>(t.param) % dtype_bytes(param_dtype) | reinterpret_cast<uintptr_t>(t.grad) % dtype_bytes(grad_dtype);
+        if (copies) off |= reinterpret_cast<uintptr_t>(t.copy) % 2;
+        if (state_bits == 32) off |= (reinterpret_cast<uintptr_t>(t.exp_avg) | reinterpret_cast<uintptr_t>(t.exp_avg_sq)) % 4;
+        else off |= (reinterpret_cast<uintptr_t>(t.exp_avg_scale) | reinterpret_cast<uintptr_t>(t.exp_avg_sq_scale)) % 4;
+        if (off) return PARLE_EALIGN;
+    }
+    // The same array twice would be stepped by two blocks at once.
+    Addresses seen;
+    if (count > (1 << 26) || !seen.prepare((size_t)count * 6)) return PARLE_ETOOBIG;
+    for (int i = 0; i < count; ++i) {
+        const parle_adamw_tensor &t = tensors[i];
+        if (t.size == 0) continue;
+        if (seen.see(t.param) || seen.see(t.exp_avg) || seen.see(t.exp_avg_sq) || (copies && seen.see(t.copy))) return PARLE_EINVAL;
+        if (state_bits == 8 && (seen.see(t.exp_avg_scale) || seen.see(t.exp_avg_sq_scale))) return PARLE_EINVAL;
+    }
+    StepArgs a = {};
+    a.b1 = (float)h.beta1; a.one_minus_b1 = (float)(1.0 - h.beta1);
+    a.b2 = (float)h.beta2; a.one_minus_b2 = (float)(1.0 - h.beta2);
+    a.eps = (float)h.eps;
+    a.log_b1 = log(h.beta1); a.log_b2 = log(h.beta2);    // (-inf for 0: b^t = 0)
+    a.lr = h.lr; a.weight_decay = h.weight_decay; a.step = h.step;
+    if (!h.step_dev) {
+        a.rate = (float)(h.lr / -expm1((double)h.step * a.log_b1));
+        a.root_scale = (float)(1.0 / sqrt(-expm1((double)h.step * a.log_b2)));
+    }
+    a.decay = decay;
+    a.grad_scale = grad_scale; a.max_norm = (float)h.max_norm;
+    a.norm = h.norm; a.lr_dev = h.lr_dev; a.step_dev = reinterpret_cast<const long long *>(h.step_dev); a.flags = flags;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    return with_dtype(param_dtype, [&](auto *p) {
+        return with_dtype(grad_dtype, [&](auto *g) {
+            using P = std::remove_pointer_t<decltype(p)>;
+            using G = std::remove_pointer_t<decltype(g)>;
+            if constexpr (std::is_same<P, float>::value) {
+                if (copy_dtype == PARLE_BF16) return launch_bits<P, G, __nv_bfloat16>(tensors, count, state_bits, a, stream);
+                if (copy_dtype == PARLE_F16) return launch_bits<P, G, __half>(tensors, count, state_bits, a, stream);
+            }
+            return launch_bits<P, G, NoCopy>(tensors, count, state_bits, a, stream);
+        });
+    });
+}

@@ -432,6 +432,147 @@ PyObject *dropout(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// A list or tuple of tensors; None: none.
+struct Tensors {
+    PyObject *items = nullptr;
+    Py_ssize_t n = 0;
+    Tensors(const Call &c, const char *what, PyObject *o, Py_ssize_t want = -1) {
+        if (o == Py_None) return;
+        if (!PyList_Check(o) && !PyTuple_Check(o)) c.refuse(std::string(what) + " has to be a list or tuple of tensors, not " + Py_TYPE(o)->tp_name);
+        items = o;
+        n = PySequence_Fast_GET_SIZE(o);
+        if (want >= 0 && n != want) c.refuse(std::to_string(n) + " " + what + " for " + std::to_string(want) + " tensors");
+    }
+    explicit operator bool() const { return items; }
+    PyObject *object(Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(items, i); }
+};
+
+// The type of tensor i of a list, the same for all of it; contiguous, of this shape, on the call's device.
+const at::Tensor &member(const Call &c, const char *what, const Tensors &list, Py_ssize_t i, const at::Tensor *like, at::ScalarType type) {
+    const at::Tensor &t = c.tensor(what, list.object(i));
+    if (t.scalar_type() != type || !t.is_contiguous() || (like && t.sizes() != like->sizes()) || t.get_device() != c.index) {
+        const std::string name = std::string(what) + "[" + std::to_string(i) + "]";
+        c.here(name.c_str(), t);
+        c.refuse(name + " is " + Call::describe(t) + ": a contiguous " + c10::toString(type) + " tensor" + (like ? " like " + Call::describe(*like) : "") + " is needed");
+    }
+    return t;
+}
+
+// grads, out, workspace, stream
+PyObject *grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    if (!expects(n_args, 4)) return nullptr;
+    Call c("parle_grad_norm");
+    const Tensors grads(c, "grads", a[0]);
+    if (grads.n == 0) c.refuse("grads has to hold a tensor");
+    if (grads.n > INT_MAX) c.refuse("too many tensors");
+    const at::Tensor &first = c.first("grads[0]", grads.object(0), a[3]);
+    const at::ScalarType type = first.scalar_type();
+    const int dtype = c.dtype("grads[0]", first);
+    std::vector<parle_grad_tensor> list((size_t)grads.n);
+    for (Py_ssize_t i = 0; i < grads.n; ++i) {
+        const at::Tensor &t = member(c, "grads", grads, i, nullptr, type);
+        list[i] = {t.data_ptr(), (long long)t.numel()};
+    }
+    Result out(a[1]);
+    if (!out.given) out.made = c.make({}, at::kFloat);
+    float *const norm = (float *)c.word("out", out.given ? out.given : Py_None, at::kFloat, at::kFloat);
+    float *const norm_at = out.given ? norm : (float *)out.made.data_ptr();
+    at::Tensor scratch;
+    void *workspace = nullptr;
+    size_t bytes = 0;
+    if (a[2] == Py_None) {
+        bytes = parle_grad_norm_workspace_bytes(list.data(), (int)grads.n);
+        if (bytes) {
+            scratch = c.make({(int64_t)bytes}, at::kByte);
+            workspace = scratch.data_ptr();
+        }
+    } else {
+        const at::Tensor &w = c.tensor("workspace", a[2]);
+        c.here("workspace", w);
+        if (!w.is_contiguous()) c.refuse("workspace is not contiguous");
+        workspace = w.data_ptr();
+        bytes = w.nbytes();
+    }
+    c.run([&] { return parle_grad_norm(list.data(), (int)grads.n, dtype, norm_at, workspace, bytes, c.stream); });
+    c.written({a[1], a[2]});
+    return out.take();
+    END_HANDLE_TH_ERRORS
+}
+
+// params, grads, exp_avg, exp_avg_sq, exp_avg_scales, exp_avg_sq_scales, copies, step, lr, beta1, beta2, eps, weight_decay, grad_scale,
+// norm, max_norm, step_dev, lr_dev, flags, stream
+PyObject *adamw(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    if (!expects(n_args, 20)) return nullptr;
+    Call c("parle_adamw");
+    const Tensors params(c, "params", a[0]);
+    if (params.n == 0) c.refuse("params has to hold a tensor");
+    if (params.n > INT_MAX) c.refuse("too many tensors");
+    const char *const names[7] = {"params", "grads", "exp_avg", "exp_avg_sq", "exp_avg_scales", "exp_avg_sq_scales", "copies"};
+    const Tensors lists[7] = {params, {c, names[1], a[1], params.n}, {c, names[2], a[2], params.n}, {c, names[3], a[3], params.n}, {c, names[4], a[4], params.n},
+                              {c, names[5], a[5], params.n}, {c, names[6], a[6], params.n}};
+    const at::Tensor &first = c.first("params[0]", params.object(0), a[19]);
+    at::ScalarType types[7];
+    for (int k = 0; k < 4; ++k) {
+        if (!lists[k]) c.refuse(std::string(names[k]) + " are needed");
+        types[k] = k ? c.tensor(names[k], lists[k].object(0)).scalar_type() : first.scalar_type();
+    }
+    const int param_dtype = c.dtype("params[0]", first), grad_dtype = c.dtype("grads[0]", c.tensor("grads", lists[1].object(0)));
+    if (types[2] != types[3] || (types[2] != at::kFloat && types[2] != at::kFloat8_e4m3fn))
+        c.refuse(std::string("exp_avg is ") + c10::toString(types[2]) + ", exp_avg_sq " + c10::toString(types[3]) + ": both Float or both Float8_e4m3fn are needed");
+    const int bits = types[2] == at::kFloat ? 32 : 8;
+    types[4] = types[5] = at::kFloat;
+    for (int k = 4; k < 6; ++k)
+        if ((bool)lists[k] != (bits == 8)) c.refuse(std::string(names[k]) + (bits == 8 ? " are needed beside 8-bit moments" : " belong to 8-bit moments"));
+    int copy_dtype = PARLE_NO_COPY;
+    if (lists[6]) {
+        const at::Tensor &t = c.tensor("copies", lists[6].object(0));
+        types[6] = t.scalar_type();
+        copy_dtype = c.dtype("copies[0]", t);
+        if (copy_dtype == PARLE_F32 || param_dtype != PARLE_F32) c.refuse("copies are 16-bit ones of fp32 params");
+    }
+    std::vector<parle_adamw_tensor> list((size_t)params.n);
+    for (Py_ssize_t i = 0; i < params.n; ++i) {
+        const at::Tensor &p = member(c, names[0], params, i, nullptr, types[0]);
+        parle_adamw_tensor &t = list[i];
+        t.size = p.numel();
+        t.param = p.data_ptr();
+        t.grad = member(c, names[1], lists[1], i, &p, types[1]).data_ptr();
+        t.exp_avg = member(c, names[2], lists[2], i, &p, types[2]).data_ptr();
+        t.exp_avg_sq = member(c, names[3], lists[3], i, &p, types[3]).data_ptr();
+        t.exp_avg_scale = t.exp_avg_sq_scale = nullptr;
+        if (bits == 8)
+            for (int k = 4; k < 6; ++k) {
+                const at::Tensor &s = member(c, names[k], lists[k], i, nullptr, at::kFloat);
+                if (s.numel() != (t.size + PARLE_ADAMW_BLOCK - 1) / PARLE_ADAMW_BLOCK)
+                    c.refuse(std::string(names[k]) + "[" + std::to_string(i) + "] is " + Call::describe(s) + ": a scale for each 256 of " + std::to_string(t.size) + " elements is needed");
+                (k == 4 ? t.exp_avg_scale : t.exp_avg_sq_scale) = (float *)s.data_ptr();
+            }
+        t.copy = lists[6] ? member(c, names[6], lists[6], i, &p, types[6]).data_ptr() : nullptr;
+    }
+    parle_adamw_step h;
+    h.step = c.integer("step", a[7], 0, LLONG_MAX);
+    h.lr = c.number("lr", a[8]);
+    h.beta1 = c.number("beta1", a[9]);
+    h.beta2 = c.number("beta2", a[10]);
+    h.eps = c.number("eps", a[11]);
+    h.weight_decay = c.number("weight_decay", a[12]);
+    h.grad_scale = c.number("grad_scale", a[13]);
+    h.norm = (const float *)c.word("norm", a[14], at::kFloat, at::kFloat);
+    h.max_norm = a[15] == Py_None ? std::numeric_limits<double>::infinity() : c.number("max_norm", a[15]);
+    h.step_dev = (const int64_t *)c.word("step_dev", a[16], at::kLong, at::kLong);
+    h.lr_dev = (const float *)c.word("lr_dev", a[17], at::kFloat, at::kFloat);
+    int32_t *const flags = (int32_t *)c.word("flags", a[18], at::kInt, at::kInt);
+    c.run([&] { return parle_adamw(list.data(), (int)params.n, param_dtype, grad_dtype, copy_dtype, bits, &h, flags, c.stream); });
+    c.written({a[18]});
+    for (int k = 0; k < 7; ++k)
+        if (k != 1 && lists[k])
+            for (Py_ssize_t i = 0; i < params.n; ++i) c.written({lists[k].object(i)});
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject *set_error(PyObject *, PyObject *type) {
     Py_INCREF(type);
     Py_XDECREF(g_error);
@@ -440,7 +581,7 @@ PyObject *set_error(PyObject *, PyObject *type) {
 }
 
 #define FASTCALL(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {FASTCALL(token_logprobs), FASTCALL(token_logprobs_grad), FASTCALL(embedding), FASTCALL(embedding_grad), FASTCALL(dropout),
+PyMethodDef methods[] = {FASTCALL(token_logprobs), FASTCALL(token_logprobs_grad), FASTCALL(embedding), FASTCALL(embedding_grad), FASTCALL(dropout), FASTCALL(grad_norm), FASTCALL(adamw),
                          {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_token_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
