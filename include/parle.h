@@ -480,6 +480,30 @@ typedef struct {
 int parle_adamw(const parle_adamw_tensor *tensors, int count, int param_dtype, int grad_dtype, int copy_dtype, int state_bits,
                 const parle_adamw_step *step, int32_t *flags, void *cuda_stream);
 
+#define PARLE_FLAG_BAD_SAMPLING 8   /* a row's parameters or random number were out of range (parle_sample_tokens) */
+typedef struct {             /* of all rows, or of each: where an array (dev [rows], 4-byte aligned) is given, the number beside it is not looked at */
+    double scale;            /* inverse temperature, in [1e-6, 1e6] */
+    double top_p, min_p;     /* in [0, 1]; 1 and 0: no limit */
+    int top_k;               /* 0: no limit; 1: the largest logit */
+    const float *scales, *top_ps, *min_ps;   /* NaN, and scales out of range, make the row invalid; top_p >= 1, min_p <= 0: no limit */
+    const int32_t *top_ks;   /* <= 0: no limit */
+} parle_sampling;
+
+/* A token of each row of logits x dev [rows, vocab], row pitch ld, by a given random number u dev [rows] fp32 in [0, 1).  With m the row's
+ * largest logit, w_j = exp(scale (x_j - m)), and tokens ranked by logit, of equal logits the lower token first (all parameters in fp32):
+ *   K    the first top_k of the ranking (logits of -inf are never kept)
+ *   P    the shortest beginning of K whose weights' sum is at least top_p times K's, and at least the first
+ *   kept the tokens of P with w_j >= min_p (as scale (x_j - m) >= log min_p)
+ *   token dev [rows] int32            the first kept token j, by number, with sum_{kept i <= j} w_i > u sum_kept w
+ *   logprob dev [rows] fp32 or NULL   log of its weight over the sum of the kept ones'
+ *   kept dev [rows] int32 or NULL     how many are kept
+ * Weights are formed in fp64 and added exactly as whole numbers of 2^-44 (of less above 2^19 tokens): the same inputs give the same
+ * tokens.  Tokens of a weight below 2^-45 can be kept, but are never sampled.  A row of -inf alone: PARLE_NO_TOKEN, -inf, 0.  A row with NaN or
+ * +inf: PARLE_NO_TOKEN, NaN, 0.  The same for an invalid row (NaN among its parameters, scale out of range, u not in [0, 1)), which also
+ * sets PARLE_FLAG_BAD_SAMPLING in *flags (dev [1] int32 or NULL). */
+int parle_sample_tokens(const void *logits, int dtype, long long rows, int vocab, long long ld, const float *u,
+                        const parle_sampling *sampling, int32_t *token, float *logprob, int32_t *kept, int32_t *flags, void *cuda_stream);
+
 /* Kernels launched by this context since creation (for accounting). */
 long long parle_launch_count(const parle_ctx *ctx);
 

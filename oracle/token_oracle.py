@@ -125,3 +125,36 @@ def dropout(x, p: float, seed: int, offset: int, residual=None):
     y = np.zeros(x.shape)
     y[keep] = np.asarray(x, np.float64)[keep] * 65536 / (65536 - threshold) if threshold < 65536 else 0
     return y if residual is None else y + np.asarray(residual, np.float64)
+
+
+def sample(x, u: float, scale: float = 1.0, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0):
+    """One row: (token, log probability among the kept, number kept, how near a comparison of sums was, relative to the sums).  Parameters as
+    fp32 numbers; a row or parameters without an answer give NO_TOKEN, NaN or -inf, 0, 1."""
+    x = np.asarray(x, np.float64)
+    u, scale, top_p, min_p = (float(np.float32(v)) for v in (u, scale, top_p, min_p))
+    bad = not (float(np.float32(1e-6)) <= scale <= 1e6 and 0 <= u < 1) or math.isnan(top_p) or math.isnan(min_p)
+    if bad or np.isnan(x).any() or np.isposinf(x).any():
+        return NO_TOKEN, math.nan, 0, 1.0
+    best = x.max()
+    if best == -np.inf:
+        return NO_TOKEN, -math.inf, 0, 1.0
+    order = np.lexsort((np.arange(len(x)), -x))
+    order = order[x[order] > -np.inf]
+    if top_k > 0:
+        order = order[:top_k]
+    near = 1.0
+    w = np.exp(scale * (x[order] - best))
+    kept = len(order)
+    if top_p < 1:
+        sums = np.cumsum(w)
+        kept = int((sums < top_p * sums[-1]).sum()) + 1
+        near = np.abs(sums - top_p * sums[-1]).min() / sums[-1]
+    if min_p > 0:
+        kept = min(kept, int((x[order] >= best + math.log(min(min_p, 1.0)) / scale).sum()))
+    tokens = np.sort(order[:kept])
+    w = np.exp(scale * (x[tokens] - best))
+    sums = np.cumsum(w)
+    at = int((sums <= u * sums[-1]).sum())
+    at = min(at, int(np.flatnonzero(w).max()))             # (u below 1 by less than the sums' rounding)
+    near = min(near, np.abs(sums[:-1] - u * sums[-1]).min() / sums[-1] if kept > 1 else 1.0)
+    return int(tokens[at]), float(scale * (x[tokens[at]] - best) - math.log(sums[-1])), kept, float(near)

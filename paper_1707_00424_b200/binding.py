@@ -11,7 +11,7 @@ import os
 from typing import Optional, Sequence
 
 GEMM_FP32, GEMM_BF16 = 0, 1
-FLAG_NONFINITE, FLAG_WAIT_LIMIT, FLAG_BAD_LABEL = 1, 2, 4
+FLAG_NONFINITE, FLAG_WAIT_LIMIT, FLAG_BAD_LABEL, FLAG_BAD_SAMPLING = 1, 2, 4, 8
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB: Optional[C.CDLL] = None
@@ -46,6 +46,11 @@ class AdamwTensor(C.Structure):
 class AdamwStep(C.Structure):
     _fields_ = [(name, C.c_double) for name in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale", "max_norm")] + [
         ("step", C.c_longlong), ("norm", C.c_void_p), ("lr_dev", C.c_void_p), ("step_dev", C.c_void_p)]
+
+
+class Sampling(C.Structure):
+    _fields_ = [("scale", C.c_double), ("top_p", C.c_double), ("min_p", C.c_double), ("top_k", C.c_int)] + [
+        (name, C.c_void_p) for name in ("scales", "top_ps", "min_ps", "top_ks")]
 
 
 def library_path() -> str:
@@ -112,6 +117,7 @@ def lib() -> C.CDLL:
         "parle_grad_norm_workspace_bytes": (sz, [C.POINTER(GradTensor), ci]),
         "parle_grad_norm": (ci, [C.POINTER(GradTensor), ci, ci, vp, vp, sz, vp]),
         "parle_adamw": (ci, [C.POINTER(AdamwTensor), ci, ci, ci, ci, ci, C.POINTER(AdamwStep), vp, vp]),
+        "parle_sample_tokens": (ci, [vp, ci, ll, ci, ll, vp, C.POINTER(Sampling), vp, vp, vp, vp, vp]),
         "parle_launch_count": (C.c_longlong, [vp]),
         "parle_last_cuda_error": (ci, [vp]),
         "parle_strerror": (C.c_char_p, [ci]),

@@ -1,0 +1,541 @@
+// parle_sample_tokens: a token of each row of logits, with temperature, top-k, top-p and min-p, from one given random number a row.
+//
+// With m the row's largest logit, weights w_j = exp(scale (x_j - m)) and ranks by (logit descending, token ascending): the tokens kept are a
+// prefix of the ranking, {x > T} and the first of the tokens with x = T by number; the one sampled is the first kept token, by number,
+// at which the sum of kept weights exceeds u times their total.
+//
+// A token is right or wrong, and with 10^5 tokens u lies within 10^-6 of one of the sums' steps in every tenth row: sums of fp32
+// exponentials would give another token there than the definition.  So weights are formed in fp64, 2^(k/32) from a table times a
+// polynomial of degree 5 (Taylor's, to 3 10^-15), and kept as whole numbers of 2^-44: their sums are exact and the same in any order, whichever
+// threads and atomics form them.  u times the total is formed exactly, too (128 bits).
+//
+// T is found by histograms: first of scale (m - x) in steps of 1/32, then of the logits' bits within the step that holds the border, 11
+// bits at a time.  A bin's 64-bit sum is two 32-bit words in shared memory, the carry passed on by the adding thread.  A row is read by
+// one block, or by a cluster of up to eight where there are few rows.
+#include <math.h>
+
+#include <type_traits>
+
+#include "token_types.cuh"
+
+using namespace parle;
+
+namespace {
+
+constexpr int kBins = 2048, kSegments = 1024;
+constexpr uint32_t kNegInf = 0x007fffffu;                // key of -inf
+
+struct SampleArgs {
+    const void *logits;
+    long long rows, ld;
+    int vocab;
+    float scale, top_p, min_p;
+    int top_k;
+    const float *u, *scales, *top_ps, *min_ps;
+    const int32_t *top_ks;
+    int32_t *token, *kept, *flags;
+    float *logprob;
+    int granules;                                        // of a block's part of a row
+    int seg_steps;                                       // a segment is 32 x seg_steps granules
+    int frac_bits;                                       // weights are whole numbers of 2^-frac_bits
+};
+
+typedef unsigned long long u64;
+
+// Logits as unsigned numbers of the same order; -0 counts as 0.
+__device__ __forceinline__ uint32_t key_of(float x) {
+    const uint32_t b = __float_as_uint(x + 0.f);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
+
+// f total, f in [0, 1), exactly: rounded down or up to a whole number.
+__device__ __forceinline__ u64 part_of(u64 total, float f, bool up) {
+    if (!(f > 0.f)) return 0;
+    const uint32_t b = __float_as_uint(f), e = b >> 23;
+    const u64 mantissa = (b & 0x7fffffu) | (e ? 0x800000u : 0u);
+    const int s = 150 - (e ? (int)e : 1);                // f = mantissa 2^-s, s >= 24
+    const u64 low = total * mantissa, high = __umul64hi(total, mantissa);
+    u64 whole, rest;
+    if (s >= 128) { whole = 0; rest = low | high; }
+    else if (s >= 64) { whole = high >> (s - 64); rest = low | (s == 64 ? 0 : high << (128 - s)); }
+    else { whole = high << (64 - s) | low >> s; rest = low << (64 - s); }
+    return whole + (up && rest ? 1 : 0);
+}
+
+struct Weigher {                                         // w(x) = exp(scale (x - best)) as a whole number of 2^-frac_bits
+    double best, c, one;                                 // c: 32 scale log2 e; one: whose last bit is 2^-frac_bits
+    float least;                                         // logits below it weigh nothing
+    const double *table;                                 // 2^(i / 32), in shared memory
+    __device__ __forceinline__ u64 operator()(float x) const {
+        const double t = ((double)fmaxf(x, least) - best) * c;
+        const double shifted = t + 6755399441055744.0;   // 1.5 2^52: rounds to a whole number
+        const int n = __double2loint(shifted);
+        const double r = t - (shifted - 6755399441055744.0);
+        constexpr double y = 0.69314718055994530942 / 32;
+        double p = fma(r, y * y * y * y * y / 120, y * y * y * y / 24);
+        p = fma(p, r, y * y * y / 6);
+        p = fma(p, r, y * y / 2);
+        p = fma(p, r, y);
+        p = fma(p, r, 1.0);
+        p *= table[n & 31];
+        p = __hiloint2double(__double2hiint(p) + ((n >> 5) << 20), __double2loint(p));
+        return x < least ? 0 : (u64)(__double_as_longlong(p + one) - __double_as_longlong(one));
+    }
+};
+
+// A row in granules of eight logits, cut at memory's 16-byte boundaries.
+template <typename T> struct Row {
+    const T *x;
+    int vocab, skew;                                     // logits of the first granule before the row
+    __device__ __forceinline__ void load(int granule, float (&v)[8]) const {
+        const long long e0 = (long long)granule * 8 - skew;
+        if (e0 >= 0 && e0 + 8 <= vocab) {
+            Pack8<T> p;
+            p.load(x + e0);
+            p.get(v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = e0 + i >= 0 && e0 + i < vocab ? to_float(x[e0 + i]) : -INFINITY;
+        }
+    }
+};
+
+struct Cut {                                             // kept: logits of keys above `key`, and the first `ties` of those with it
+    uint32_t key;
+    u64 ties;
+};
+
+struct Part {                                            // what a block found out about its part of the row
+    float best;
+    u64 mass;
+    uint32_t count, ties;
+};
+
+template <int THREADS> struct Shared {
+    double table[32];
+    union {
+        uint32_t hist[2][kBins];
+        struct {
+            u64 mass[kSegments];
+            uint32_t ties[kSegments];
+        } seg;
+    };
+    u64 scan[THREADS / 32];
+    float maxima[THREADS / 32];
+    Part part;
+    struct {
+        u64 above, total;
+        int bin;
+        uint32_t low, high;
+    } found;
+    struct {
+        u64 target;
+        uint32_t ties_before;
+        int segment;
+    } hit;
+};
+
+// Every thread of the row's blocks has come here, and sees what the others wrote.
+__device__ __forceinline__ void all_meet(int blocks) {
+    if (blocks == 1) __syncthreads();
+    else {
+        cluster_arrive();
+        cluster_wait();
+    }
+}
+
+__device__ __forceinline__ u64 shfl_up64(u64 v, int by) { return __shfl_up_sync(0xffffffffu, v, by); }
+
+// Exclusive sum over the block's threads; *total: of all.
+template <int THREADS> __device__ __forceinline__ u64 block_scan(u64 v, u64 (&scratch)[THREADS / 32], u64 *total) {
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    u64 sum = v;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const u64 below = shfl_up64(sum, o);
+        if (lane >= o) sum += below;
+    }
+    __syncthreads();                                     // (scratch may still be read from the last call)
+    if (lane == 31) scratch[warp] = sum;
+    __syncthreads();
+    u64 before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+        const u64 s = scratch[w];
+        if (w < warp) before += s;
+        all += s;
+    }
+    *total = all;
+    return before + sum - v;
+}
+
+template <typename T, int THREADS> struct Sampler {
+    static constexpr int kPer = kBins / THREADS;
+    Shared<THREADS> &sh;
+    Row<T> row;
+    int blocks, rank, begin, end;                        // the row's blocks; this one's granules
+    float scale, best;
+    Weigher weigh;
+
+    __device__ __forceinline__ int step_of(float x) const { return min(kBins - 1, (int)((best - x) * scale * 32.f)); }
+
+    template <class F> __device__ __forceinline__ void each(F f) const {
+        for (int g = begin + (int)threadIdx.x; g < end; g += THREADS) {
+            float v[8];
+            row.load(g, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f(v[i]);
+        }
+    }
+
+    // Adds w to bin b: a count, or a 64-bit number in two words.
+    template <bool MASS> __device__ __forceinline__ void add(int b, u64 w) {
+        if (!MASS) {
+            atomicAdd(&sh.hist[0][b], 1u);
+        } else {
+            const uint32_t low = (uint32_t)w, before = atomicAdd(&sh.hist[0][b], low), high = (uint32_t)(w >> 32) + (before + low < low ? 1u : 0u);
+            if (high) atomicAdd(&sh.hist[1][b], high);
+        }
+    }
+    __device__ __forceinline__ void clear() {
+        for (int i = threadIdx.x; i < 2 * kBins; i += THREADS) (&sh.hist[0][0])[i] = 0;
+        __syncthreads();
+    }
+    // The first bin at which `above` and the bins up to it, of all blocks, reach the target; target(total) may depend on the total.  -1 if none does.
+    template <bool MASS, class F> __device__ __forceinline__ void find(u64 above, F target) {
+        all_meet(blocks);
+        u64 bin[kPer], sum = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int b = threadIdx.x * kPer + i;
+            u64 s = 0;
+            for (int r = 0; r < blocks; ++r) {
+                const Shared<THREADS> *other = blocks == 1 ? &sh : at_rank(&sh, r);
+                s += other->hist[0][b];
+                if (MASS) s += (u64)other->hist[1][b] << 32;
+            }
+            sum += bin[i] = s;
+        }
+        if (threadIdx.x == 0) sh.found.bin = -1;
+        u64 total;
+        u64 before = above + block_scan<THREADS>(sum, sh.scan, &total);
+        const u64 goal = target(total);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (before < goal && before + bin[i] >= goal) {
+                sh.found.bin = threadIdx.x * kPer + i;
+                sh.found.above = before;
+            }
+            before += bin[i];
+        }
+        if (threadIdx.x == 0) sh.found.total = total;
+        all_meet(blocks);                                // (the histograms are read, found is written)
+    }
+
+    // The cut at which counts (or weights) of logits with keys above `floor` reach a goal, goal(total).  False if all together do not.
+    template <bool MASS, class F> __device__ __forceinline__ bool narrow(uint32_t floor, F goal_of, Cut *cut, u64 *goal) {
+        clear();
+        each([&](float x) {
+            if (key_of(x) > floor) add<MASS>(step_of(x), MASS ? weigh(x) : 1);
+        });
+        u64 want = 0;
+        find<MASS>(0, [&](u64 total) { return want = goal_of(total); });
+        *goal = want;
+        int bin = sh.found.bin;
+        if (bin < 0) return false;
+        u64 above = sh.found.above;
+        if (threadIdx.x < 2) {                           // the bin's keys: the smallest one of a step up to `bin`, and of a step before it
+            const int step = bin - (int)threadIdx.x;
+            uint32_t low = floor + 1, high = key_of(best) + 1;
+            while (low < high) {
+                const uint32_t mid = low + (high - low) / 2;
+                if (step_of(value_of(mid)) <= step) high = mid; else low = mid + 1;
+            }
+            if (threadIdx.x == 0) sh.found.low = low; else sh.found.high = low - 1;
+        }
+        __syncthreads();
+        uint32_t low = sh.found.low, high = sh.found.high;
+        for (;;) {
+            const uint32_t range = high - low;
+            const int shift = max(0, 32 - __clz(range) - 11);      // (range >> shift) < 2048
+            clear();
+            each([&](float x) {
+                const uint32_t key = key_of(x);
+                if (key >= low && key <= high) add<MASS>((int)((high - key) >> shift), MASS ? weigh(x) : 1);
+            });
+            find<MASS>(above, [&](u64) { return want; });
+            bin = sh.found.bin;                          // (there is one: the interval holds the border)
+            above = sh.found.above;
+            const uint32_t top = high - ((uint32_t)bin << shift);
+            if (shift == 0) {
+                cut->key = top;
+                cut->ties = MASS ? (want - above + weigh(value_of(top)) - 1) / max(weigh(value_of(top)), (u64)1) : want - above;
+                return true;
+            }
+            const uint32_t width = (1u << shift) - 1;
+            low = top - low > width ? top - width : low;
+            high = top;
+        }
+    }
+};
+
+template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__ SampleArgs a, int blocks) {
+    __shared__ Shared<THREADS> sh;
+    const int rank = blocks == 1 ? 0 : cluster_rank();
+    const long long r = blockIdx.x / blocks;
+    const T *const x = static_cast<const T *>(a.logits) + r * a.ld;
+    Row<T> row{x, a.vocab, (int)(reinterpret_cast<uintptr_t>(x) % 16 / sizeof(T))};
+    const int all = (a.vocab + row.skew + 7) / 8, begin = min(all, rank * a.granules), end = min(all, begin + a.granules);
+    const float scale = a.scales ? a.scales[r] : a.scale, top_p = a.top_ps ? a.top_ps[r] : a.top_p, min_p = a.min_ps ? a.min_ps[r] : a.min_p, u = a.u[r];
+    const int top_k = a.top_ks ? a.top_ks[r] : a.top_k;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    if (threadIdx.x < 32) sh.table[threadIdx.x] = exp2((double)threadIdx.x / 32);
+
+    Sampler<T, THREADS> s{sh, row, blocks, rank, begin, end, scale, -INFINITY, {}};
+    const auto largest = [](float v, float w) {          // NaN if either is
+        float m;
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(v), "f"(w));
+        return m;
+    };
+    float best = -INFINITY;
+    s.each([&](float v) { best = largest(best, v); });
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) best = largest(best, __shfl_xor_sync(0xffffffffu, best, o));
+    if (lane == 0) sh.maxima[warp] = best;
+    __syncthreads();
+    for (int w = 0; w < THREADS / 32; ++w) best = largest(best, sh.maxima[w]);
+    if (blocks > 1) {
+        if (threadIdx.x == 0) sh.part.best = best;
+        all_meet(blocks);
+        for (int o = 0; o < blocks; ++o) best = largest(best, at_rank(&sh, o)->part.best);
+        all_meet(blocks);                                // (nobody leaves while its word is read)
+    }
+    const bool valid = scale >= 1e-6f && scale <= 1e6f && top_p == top_p && min_p == min_p && u >= 0.f && u < 1.f;
+    if (!valid || !(fabsf(best) < INFINITY)) {
+        if (rank == 0 && threadIdx.x == 0) {
+            a.token[r] = PARLE_NO_TOKEN;
+            if (a.logprob) a.logprob[r] = valid && best == -INFINITY ? -INFINITY : NAN;
+            if (a.kept) a.kept[r] = 0;
+            if (!valid && a.flags) atomicOr(a.flags, PARLE_FLAG_BAD_SAMPLING);
+        }
+        return;
+    }
+    s.best = best;
+    s.weigh.best = best;
+    s.weigh.c = 32.0 * 1.44269504088896340736 * scale;
+    s.weigh.one = __hiloint2double((1023 + 52 - a.frac_bits) << 20, 0);
+    s.weigh.least = best - 45.f / scale;                 // (e^-45 < 2^-64)
+    s.weigh.table = sh.table;
+
+    Cut cut{kNegInf, 0};
+    u64 goal;
+    const auto tighter = [&](const Cut &c) {
+        if (c.key > cut.key || (c.key == cut.key && c.ties < cut.ties)) cut = c;
+    };
+    if (top_k > 0 && top_k < a.vocab) {
+        Cut c;
+        if (s.template narrow<false>(kNegInf, [&](u64) { return (u64)top_k; }, &c, &goal)) cut = c;
+    }
+    if (top_p < 1.f) {
+        const u64 tied = cut.ties ? s.weigh(value_of(cut.key)) : 0;
+        Cut c;
+        const bool inside = s.template narrow<true>(cut.key, [&](u64 total) { return max((u64)1, part_of(total + cut.ties * tied, top_p, true)); }, &c, &goal);
+        if (inside) cut = c;
+        else if (tied) cut.ties = (goal - sh.found.total + tied - 1) / tied;
+    }
+    if (min_p > 0.f) {
+        const double least = (double)best + log((double)fminf(min_p, 1.f)) / scale;
+        float f = (float)least;
+        if ((double)f < least) f = value_of(key_of(f) + 1);
+        tighter(Cut{key_of(f) - 1, 0});
+    }
+
+    // Sums of the kept weights by segments of the row, in its order.
+    const int segments = (end - begin + 32 * a.seg_steps - 1) / (32 * a.seg_steps);
+    __syncthreads();
+    u64 mass = 0;
+    uint32_t count = 0, ties = 0;
+    for (int g = warp; g < segments; g += THREADS / 32) {
+        u64 m = 0;
+        uint32_t t = 0;
+        for (int i = 0; i < a.seg_steps; ++i) {
+            const int at = begin + (g * a.seg_steps + i) * 32 + lane;
+            if (at >= end) continue;
+            float v[8];
+            row.load(at, v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t key = key_of(v[k]);
+                if (key > cut.key) {
+                    m += s.weigh(v[k]);
+                    ++count;
+                } else if (key == cut.key) ++t;
+            }
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m += __shfl_xor_sync(0xffffffffu, m, o);
+        t = __reduce_add_sync(0xffffffffu, t);
+        if (lane == 0) {
+            sh.seg.mass[g] = m;
+            sh.seg.ties[g] = t;
+            mass += m;
+            ties += t;
+        }
+    }
+    count = __reduce_add_sync(0xffffffffu, count);
+    // the block's own sums
+    if (threadIdx.x == 0) sh.part = Part{best, 0, 0, 0};
+    __syncthreads();
+    if (lane == 0) {
+        atomicAdd(&sh.part.mass, mass);
+        atomicAdd(&sh.part.count, count);
+        atomicAdd(&sh.part.ties, ties);
+    }
+    all_meet(blocks);
+    const u64 tied = cut.ties ? s.weigh(value_of(cut.key)) : 0;
+    const auto of_ties = [&](u64 before, uint32_t there) { return before >= cut.ties ? (u64)0 : min(cut.ties - before, (u64)there); };
+    u64 total = 0, mass_before = 0, ties_before = 0, all_ties = 0, kept = 0, own = 0;
+    for (int o = 0; o < blocks; ++o) {
+        const Part p = blocks == 1 ? sh.part : at_rank(&sh, o)->part;
+        const u64 taken = of_ties(all_ties, p.ties), there = p.mass + taken * tied;
+        if (o == rank) { mass_before = total; ties_before = all_ties; own = there; }
+        total += there;
+        all_ties += p.ties;
+        kept += p.count + taken;
+    }
+    const u64 target = min(part_of(total, u, false), total - 1);
+    if (target >= mass_before && target - mass_before < own) {      // the token lies in this block's part
+        constexpr int kPer = kSegments / THREADS;
+        u64 t[kPer], m[kPer], sum = 0, any;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int g = threadIdx.x * kPer + i;
+            sum += t[i] = g < segments ? sh.seg.ties[g] : 0;
+        }
+        u64 before = ties_before + block_scan<THREADS>(sum, sh.scan, &any);
+        sum = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int g = threadIdx.x * kPer + i;
+            sum += m[i] = (g < segments ? sh.seg.mass[g] : 0) + of_ties(before, (uint32_t)t[i]) * tied;
+            before += t[i];
+        }
+        for (int i = 0; i < kPer; ++i) before -= t[i];
+        u64 below = mass_before + block_scan<THREADS>(sum, sh.scan, &any);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (target >= below && target - below < m[i]) {
+                sh.hit.segment = threadIdx.x * kPer + i;
+                sh.hit.target = target - below;
+                sh.hit.ties_before = (uint32_t)min(before, (u64)0xffffffffu);
+            }
+            below += m[i];
+            before += t[i];
+        }
+        __syncthreads();
+        if (warp == 0) {
+            u64 rest = sh.hit.target, tb = sh.hit.ties_before;
+            for (int i = 0; i < a.seg_steps; ++i) {
+                const int at = begin + (sh.hit.segment * a.seg_steps + i) * 32 + lane;
+                float v[8];
+                uint32_t mine = 0;
+                u64 w[8], sum = 0;
+                if (at < end) row.load(at, v);
+                else
+                    for (int k = 0; k < 8; ++k) v[k] = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) mine += key_of(v[k]) == cut.key;
+                uint32_t upto = mine;
+#pragma unroll
+                for (int o = 1; o < 32; o *= 2) {
+                    const uint32_t b = __shfl_up_sync(0xffffffffu, upto, o);
+                    if (lane >= o) upto += b;
+                }
+                u64 at_tie = tb + upto - mine;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint32_t key = key_of(v[k]);
+                    w[k] = key > cut.key ? s.weigh(v[k]) : key == cut.key && at_tie++ < cut.ties ? tied : 0;
+                    sum += w[k];
+                }
+                u64 sums = sum;
+#pragma unroll
+                for (int o = 1; o < 32; o *= 2) {
+                    const u64 b = shfl_up64(sums, o);
+                    if (lane >= o) sums += b;
+                }
+                u64 before_lane = sums - sum;
+                if (rest >= before_lane && rest < sums) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if (rest >= before_lane && rest - before_lane < w[k]) {
+                            a.token[r] = at * 8 - row.skew + k;
+                            if (a.logprob) a.logprob[r] = (float)(((double)v[k] - best) * scale - log((double)total * exp2(-(double)a.frac_bits)));
+                        }
+                        before_lane += w[k];
+                    }
+                }
+                const u64 whole = __shfl_sync(0xffffffffu, sums, 31);
+                if (rest < whole) break;
+                rest -= whole;
+                tb += __shfl_sync(0xffffffffu, upto, 31);
+            }
+        }
+    }
+    if (rank == 0 && threadIdx.x == 0 && a.kept) a.kept[r] = (int32_t)kept;
+    if (blocks > 1) all_meet(blocks);                    // (nobody leaves while its sums are read)
+}
+
+template <typename T, int THREADS> int launch_sample(SampleArgs a, int blocks, cudaStream_t stream) {
+    const int granules = a.vocab / 8 + 2;                // wherever a row begins
+    a.seg_steps = 1;
+    for (;;) {
+        const int each = 32 * a.seg_steps;
+        a.granules = ((granules + blocks - 1) / blocks + each - 1) / each * each;
+        if (a.granules / each <= kSegments) break;
+        a.seg_steps *= 2;
+    }
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = cluster_config(dim3((unsigned)(a.rows * blocks)), THREADS, 0, blocks, &attr, stream);
+    if (cudaLaunchKernelEx(&cfg, sample_kernel<T, THREADS>, a, blocks) != cudaSuccess) {
+        cudaGetLastError();
+        return PARLE_ECUDA;
+    }
+    return PARLE_OK;
+}
+
+bool aligned4(const void *p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
+
+}  // namespace
+
+extern "C" int parle_sample_tokens(const void *logits, int dtype, long long rows, int vocab, long long ld, const float *u,
+                                   const parle_sampling *sampling, int32_t *token, float *logprob, int32_t *kept, int32_t *flags, void *cuda_stream) {
+    if (!valid_dtype(dtype) || rows < 0 || vocab < 1 || (rows > 1 && ld < 0) || !sampling) return PARLE_EINVAL;
+    const parle_sampling &h = *sampling;
+    const float scale = (float)h.scale, top_p = (float)h.top_p, min_p = (float)h.min_p;
+    if (!h.scales && !(h.scale >= 1e-6 && h.scale <= 1e6)) return PARLE_EINVAL;
+    if (!h.top_ks && h.top_k < 0) return PARLE_EINVAL;
+    if ((!h.top_ps && !(h.top_p >= 0.0 && h.top_p <= 1.0)) || (!h.min_ps && !(h.min_p >= 0.0 && h.min_p <= 1.0))) return PARLE_EINVAL;
+    if (rows == 0) return PARLE_OK;
+    if (!logits || !u || !token) return PARLE_EINVAL;
+    if (rows > PARLE_TOKEN_MAX_ROWS / 8 || vocab > 1 << 30) return PARLE_ETOOBIG;
+    if (!element_aligned(logits, dtype) || !aligned4(u) || !aligned4(h.scales) || !aligned4(h.top_ks) || !aligned4(h.top_ps) || !aligned4(h.min_ps) ||
+        !aligned4(token) || !aligned4(logprob) || !aligned4(kept) || !aligned4(flags)) return PARLE_EALIGN;
+    SampleArgs a = {};
+    a.logits = logits; a.rows = rows; a.ld = ld; a.vocab = vocab;
+    a.scale = fminf(fmaxf(scale, 1e-6f), 1e6f); a.top_p = top_p; a.min_p = min_p; a.top_k = h.top_k;
+    a.u = u; a.scales = h.scales; a.top_ks = h.top_ks; a.top_ps = h.top_ps; a.min_ps = h.min_ps;
+    a.token = token; a.logprob = logprob; a.kept = kept; a.flags = flags;
+    a.frac_bits = 44;
+    while (a.frac_bits > 8 && ((unsigned long long)vocab >> (63 - a.frac_bits))) --a.frac_bits;      // sums stay below 2^63
+    const int sms = current_sms();
+    if (sms < 0) return PARLE_ECUDA;
+    int blocks = 1;
+    while (blocks < 8 && rows * blocks * 2 <= 2 * sms && vocab / blocks >= 16384) blocks *= 2;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    return with_dtype(dtype, [&](auto *tag) {
+        using T = std::remove_pointer_t<decltype(tag)>;
+        return vocab <= 4096 ? launch_sample<T, 128>(a, blocks, stream) : launch_sample<T, 512>(a, blocks, stream);
+    });
+}

@@ -294,6 +294,43 @@ PyObject *token_logprobs_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// logits, u, scale, top_k, top_p, min_p, token, logprob, kept, flags, stream
+PyObject *sample_tokens(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!expects(n, 11)) return nullptr;
+    Call c("parle_sample_tokens");
+    const at::Tensor &logits = c.first("logits", a[0], a[10]);
+    const int dtype = c.dtype("logits", logits);
+    const Call::Rows x = c.rows("logits", logits, 0);
+    const at::IntArrayRef lead = logits.sizes().slice(0, logits.dim() - 1);
+    const float *u = (const float *)c.dense("u", c.tensor("u", a[1]), lead, at::kFloat);
+    parle_sampling h = {1.0, 1.0, 0.0, 0, nullptr, nullptr, nullptr, nullptr};
+    const auto either = [&](const char *what, PyObject *o, double &number, const float *&array) {
+        if (THPVariable_Check(o)) array = (const float *)c.dense(what, c.tensor(what, o), lead, at::kFloat);
+        else number = c.number(what, o);
+    };
+    either("scale", a[2], h.scale, h.scales);
+    if (THPVariable_Check(a[3])) h.top_ks = (const int32_t *)c.dense("top_k", c.tensor("top_k", a[3]), lead, at::kInt);
+    else h.top_k = (int)c.integer("top_k", a[3], 0, INT_MAX);
+    either("top_p", a[4], h.top_p, h.top_ps);
+    either("min_p", a[5], h.min_p, h.min_ps);
+    Result token(a[6]), logprob(a[7]), kept(a[8]);
+    const auto place = [&](const char *what, Result &r, at::ScalarType type) {
+        if (!r.given) r.made = c.make(lead, type);
+        return c.dense(what, r.given ? c.tensor(what, r.given) : r.made, lead, type);
+    };
+    int32_t *token_at = (int32_t *)place("token", token, at::kInt);
+    float *logprob_at = (float *)place("logprob", logprob, at::kFloat);
+    int32_t *kept_at = (int32_t *)place("kept", kept, at::kInt);
+    int32_t *flags = (int32_t *)c.word("flags", a[9], at::kInt, at::kInt);
+    const int vocab = int_size(c, "vocab", x.cols);
+    const void *const logits_at = logits.data_ptr();
+    c.run([&] { return parle_sample_tokens(logits_at, dtype, x.rows, vocab, x.pitch, u, &h, token_at, logprob_at, kept_at, flags, c.stream); });
+    c.written({a[6], a[7], a[8], a[9]});
+    return Py_BuildValue("(NNN)", token.take(), logprob.take(), kept.take());
+    END_HANDLE_TH_ERRORS
+}
+
 struct Tables {
     long long gs, ld;
 };
@@ -581,7 +618,7 @@ PyObject *set_error(PyObject *, PyObject *type) {
 }
 
 #define FASTCALL(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {FASTCALL(token_logprobs), FASTCALL(token_logprobs_grad), FASTCALL(embedding), FASTCALL(embedding_grad), FASTCALL(dropout), FASTCALL(grad_norm), FASTCALL(adamw),
+PyMethodDef methods[] = {FASTCALL(token_logprobs), FASTCALL(token_logprobs_grad), FASTCALL(embedding), FASTCALL(embedding_grad), FASTCALL(dropout), FASTCALL(sample_tokens), FASTCALL(grad_norm), FASTCALL(adamw),
                          {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_token_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

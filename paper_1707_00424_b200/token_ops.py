@@ -1,5 +1,5 @@
 """Token operators of libparle.so: embedding lookup and its gradient, counter-based dropout, log probabilities of given tokens
-with entropy, top alternatives and gradient.
+with entropy, top alternatives and gradient, sampling of tokens.
 
 Each function checks its tensors, then makes one call of the C ABI (include/parle.h has the definitions) on `stream`, or on the
 current stream of the tensors' device: both in the module _token_ops (csrc/token_bindings.cpp).  Results go to the tensors given
@@ -45,6 +45,14 @@ def token_logprobs_grad(logits, tokens=None, d_logprob=None, d_entropy=None, sca
     """dlogits of sum(d_logprob * logprob + d_entropy * entropy) (parle_token_logprobs_grad); dlogits may be logits itself.
     logprob and entropy are formed in the same pass when given."""
     return (_MODULE or load()).token_logprobs_grad(logits, tokens, d_logprob, d_entropy, scale, dlogits, logprob, entropy, flags, stream)
+
+
+def sample_tokens(logits, u, *, scale=1.0, top_k=0, top_p=1.0, min_p=0.0, token=None, logprob=None, kept=None, flags=None, stream=None):
+    """(token, logprob, kept) of logits [..., vocab] by random numbers u [...] (fp32, in [0, 1)) (parle_sample_tokens): a token sampled at
+    the inverse temperature `scale` among the top_k most probable (0: all), of these the most probable that make up top_p, of these those
+    at least min_p times as probable as the best; its log probability among them, and their number.  scale, top_k, top_p and min_p are
+    numbers, or tensors [...] (fp32; int32 for top_k) with one for each row."""
+    return (_MODULE or load()).sample_tokens(logits, u, scale, top_k, top_p, min_p, token, logprob, kept, flags, stream)
 
 
 def embedding(table, tokens, scale: float = 1.0, *, out=None, dtype=None, flags=None, stream=None):
