@@ -22,7 +22,7 @@ using namespace parle;
 
 namespace {
 
-constexpr int kBins = 2048, kSegments = 1024;
+constexpr int kBins = 2048, kSegments = 1024, kList = 1024;
 constexpr uint32_t kNegInf = 0x007fffffu;                // key of -inf
 
 struct SampleArgs {
@@ -67,20 +67,21 @@ struct Weigher {                                         // w(x) = exp(scale (x 
     double best, c, one;                                 // c: 32 scale log2 e; one: whose last bit is 2^-frac_bits
     float least;                                         // logits below it weigh nothing
     const double *table;                                 // 2^(i / 32), in shared memory
+    // 2^(n / 32) from the table, e^y of the rest, |y| <= ln 2 / 64 = h, by Taylor's polynomial of degree 5 whose last term is spread over y and y^3
+    // (Chebyshev's economisation: 16 z^5 - 20 z^3 + 5 z is at most 1): off by h^5 / 1920 = 8 10^-14.  Nine operations in fp64.
     __device__ __forceinline__ u64 operator()(float x) const {
-        const double t = ((double)fmaxf(x, least) - best) * c;
-        const double shifted = t + 6755399441055744.0;   // 1.5 2^52: rounds to a whole number
+        constexpr double y = 0.69314718055994530942 / 32, h = y / 2;
+        const double d = (double)fmaxf(x, least) - best;
+        const double shifted = fma(d, c, 6755399441055744.0);      // 1.5 2^52: rounds to a whole number
         const int n = __double2loint(shifted);
-        const double r = t - (shifted - 6755399441055744.0);
-        constexpr double y = 0.69314718055994530942 / 32;
-        double p = fma(r, y * y * y * y * y / 120, y * y * y * y / 24);
-        p = fma(p, r, y * y * y / 6);
+        const double r = fma(d, c, 6755399441055744.0 - shifted);
+        double p = fma(r, y * y * y * y / 24, y * y * y * (1.0 / 6 + h * h / 96));
         p = fma(p, r, y * y / 2);
-        p = fma(p, r, y);
+        p = fma(p, r, y * (1.0 - h * h * h * h / 384));
         p = fma(p, r, 1.0);
-        p *= table[n & 31];
-        p = __hiloint2double(__double2hiint(p) + ((n >> 5) << 20), __double2loint(p));
-        return x < least ? 0 : (u64)(__double_as_longlong(p + one) - __double_as_longlong(one));
+        const double power = table[n & 31];
+        p = fma(p, __hiloint2double(__double2hiint(power) + ((n >> 5) << 20), __double2loint(power)), one);
+        return x < least ? 0 : (u64)(__double_as_longlong(p) - __double_as_longlong(one));
     }
 };
 
@@ -108,9 +109,13 @@ struct Cut {                                             // kept: logits of keys
 
 struct Part {                                            // what a block found out about its part of the row
     float best;
+    uint32_t bound;                                      // key that as many logits of the part reach as were asked for
+    double sum;                                          // of weights, in fp32's precision
     u64 mass;
     uint32_t count, ties;
 };
+
+enum Outcome { kDone, kNeedTotal, kNeedAll };            // of a list of the largest logits: sampled from; the weights' total is needed exactly; too short
 
 template <int THREADS> struct Shared {
     double table[32];
@@ -121,8 +126,15 @@ template <int THREADS> struct Shared {
             uint32_t ties[kSegments];
         } seg;
     };
+    u64 list[kList];                                     // ~key << 32 | token
+    u64 weight[kList];
+    u64 sums[kList];
     u64 scan[THREADS / 32];
+    double scan_f[THREADS / 32];
     float maxima[THREADS / 32];
+    float minima[THREADS / 32];
+    uint32_t listed;
+    int outcome;
     Part part;
     struct {
         u64 above, total;
@@ -186,6 +198,20 @@ template <typename T, int THREADS> struct Sampler {
             row.load(g, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) f(v[i]);
+        }
+    }
+
+    // As each(), with the token's number; only where f's logits reach `floor`.
+    template <class F> __device__ __forceinline__ void each_from(float floor, F f) const {
+        for (int g = begin + (int)threadIdx.x; g < end; g += THREADS) {
+            float v[8];
+            row.load(g, v);
+            float most = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+            if (most >= floor) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (v[i] >= floor && v[i] > -INFINITY) f(v[i], g * 8 - row.skew + i);
+            }
         }
     }
 
@@ -278,9 +304,130 @@ template <typename T, int THREADS> struct Sampler {
             high = top;
         }
     }
+
+    // A key that at least `wanted` of the block's logits reach, and not many more: found among the threads' largest ones (as many threads reach
+    // it).  The least key of a number where there are fewer such threads.
+    __device__ __forceinline__ uint32_t bound(float mine, float least, float most, int wanted) const {
+        const uint32_t key = key_of(mine);
+        uint32_t low = key_of(least), high = key_of(most) + 1;
+        if (low <= kNegInf) low = kNegInf + 1;
+        if (__syncthreads_count(key >= low) < wanted) return kNegInf + 1;
+        while (high - low > 1) {
+            const uint32_t mid = low + (high - low) / 2;
+            const int reach = __syncthreads_count(key >= mid);
+            if (reach >= wanted) {
+                low = mid;
+                if (reach <= wanted + wanted / 8) break;
+            } else high = mid;
+        }
+        return low;
+    }
+
+    // Sorts list[0 .. n), in steps of neighbours, squares and halves (Batcher's bitonic sort).
+    __device__ __forceinline__ void sort(int n) {
+        int size = 2;
+        while (size < n) size *= 2;
+        for (int i = n + (int)threadIdx.x; i < size; i += THREADS) sh.list[i] = ~0ull;
+        for (int run = 2; run <= size; run *= 2)
+            for (int apart = run / 2; apart > 0; apart /= 2) {
+                __syncthreads();
+                for (int p = threadIdx.x; p < size / 2; p += THREADS) {
+                    const int i = 2 * p - (p & (apart - 1)), j = i + apart;
+                    const u64 x = sh.list[i], y = sh.list[j];
+                    if ((x > y) == ((i & run) == 0)) {
+                        sh.list[i] = y;
+                        sh.list[j] = x;
+                    }
+                }
+            }
+        __syncthreads();
+    }
+
+    // sums[i] = value(0) + .. + value(i), i < n.
+    template <class F> __device__ __forceinline__ void running(int n, F value) {
+        const int per = (n + THREADS - 1) / THREADS, first = min(n, (int)threadIdx.x * per), last = min(n, first + per);
+        u64 sum = 0, all;
+        for (int i = first; i < last; ++i) sum += value(i);
+        u64 before = block_scan<THREADS>(sum, sh.scan, &all);
+        for (int i = first; i < last; ++i) sh.sums[i] = before += value(i);
+        __syncthreads();
+    }
+
+    __device__ __forceinline__ int how_many(int n, u64 limit) const {      // of sums[0 .. n) are below limit
+        int count = 0;
+        for (int i = 0; i < n; i += THREADS) count += __syncthreads_count(i + (int)threadIdx.x < n && sh.sums[i + threadIdx.x] < limit);
+        return count;
+    }
+
+    // Samples from the n largest logits, in list[], if these hold all that is kept.  complete: whatever is not in the list is below min_p.  top_k
+    // (0: none) is at most n, or the list complete.  total_low, total_high: bounds of the weights' total where no top_k gives it, equal where it
+    // is known.
+    __device__ __forceinline__ Outcome from_list(const SampleArgs &a, long long r, int n, bool complete, int top_k, float top_p, u64 total_low, u64 total_high, uint32_t least_key, float u) {
+        sort(n);
+        for (int i = threadIdx.x; i < n; i += THREADS) sh.weight[i] = weigh(value_of(~(uint32_t)(sh.list[i] >> 32)));
+        running(n, [&](int i) { return sh.weight[i]; });
+        int kept = top_k > 0 ? min(top_k, n) : n;
+        if (top_p < 1.f) {
+            if (top_k > 0) total_low = total_high = sh.sums[kept - 1];
+            const u64 low = max((u64)1, part_of(total_low, top_p, true)), high = max((u64)1, part_of(total_high, top_p, true)), all = sh.sums[kept - 1];
+            if (high > all) {                            // (for a top_k, what is asked for is there)
+                if (low <= all) return kNeedTotal;
+                if (!complete) return kNeedAll;
+            } else {
+                const int some = how_many(kept, low) + 1;
+                if (low != high && how_many(kept, high) + 1 != some) return kNeedTotal;
+                kept = some;
+            }
+        } else if (top_k == 0 && !complete) return kNeedAll;
+        if (least_key) {
+            int reach = 0;
+            for (int i = 0; i < kept; i += THREADS) reach += __syncthreads_count(i + (int)threadIdx.x < kept && ~(uint32_t)(sh.list[i + threadIdx.x] >> 32) >= least_key);
+            kept = reach;
+        }
+        const u64 total = sh.sums[kept - 1], target = min(part_of(total, u, false), total - 1);
+        const auto answer = [&](uint32_t key, uint32_t token) {
+            a.token[r] = (int32_t)token;
+            if (a.logprob) a.logprob[r] = (float)(((double)value_of(key) - best) * scale - log((double)total * exp2(-(double)a.frac_bits)));
+            if (a.kept) a.kept[r] = kept;
+        };
+        if (kept <= 128) {                               // each kept token adds up those before it
+            if ((int)threadIdx.x < kept) {
+                const uint32_t token = (uint32_t)sh.list[threadIdx.x];
+                const u64 own = sh.weight[threadIdx.x];
+                u64 before = 0;
+                for (int i = 0; i < kept; ++i) before += (uint32_t)sh.list[i] < token ? sh.weight[i] : 0;
+                if (target >= before && target - before < own) answer(~(uint32_t)(sh.list[threadIdx.x] >> 32), token);
+            }
+            return kDone;
+        }
+        __syncthreads();
+        u64 mine[kList / THREADS];                       // by number: (token, place in weight[])
+#pragma unroll
+        for (int k = 0; k < kList / THREADS; ++k) {
+            const int i = k * THREADS + threadIdx.x;
+            if (i < kept) mine[k] = sh.list[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kList / THREADS; ++k) {
+            const int i = k * THREADS + threadIdx.x;
+            if (i < kept) {
+                sh.list[i] = (u64)(uint32_t)mine[k] << 32 | (uint32_t)i;
+                sh.seg.ties[i] = ~(uint32_t)(mine[k] >> 32);      // the key
+            }
+        }
+        __syncthreads();
+        sort(kept);
+        running(kept, [&](int i) { return sh.weight[(uint32_t)sh.list[i]]; });
+        for (int i = threadIdx.x; i < kept; i += THREADS) {
+            const int place = (int)(uint32_t)sh.list[i];
+            if (target < sh.sums[i] && target >= sh.sums[i] - sh.weight[place]) answer(sh.seg.ties[place], (uint32_t)(sh.list[i] >> 32));
+        }
+        return kDone;
+    }
 };
 
-template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__ SampleArgs a, int blocks) {
+template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_kernel(const __grid_constant__ SampleArgs a, int blocks) {
     __shared__ Shared<THREADS> sh;
     const int rank = blocks == 1 ? 0 : cluster_rank();
     const long long r = blockIdx.x / blocks;
@@ -298,17 +445,38 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS) sa
         asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(v), "f"(w));
         return m;
     };
-    float best = -INFINITY;
-    s.each([&](float v) { best = largest(best, v); });
+    float mine = -INFINITY;
+    s.each([&](float v) { mine = largest(mine, v); });
+    float best = mine, least = mine;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) best = largest(best, __shfl_xor_sync(0xffffffffu, best, o));
-    if (lane == 0) sh.maxima[warp] = best;
+    for (int o = 16; o > 0; o >>= 1) {
+        best = largest(best, __shfl_xor_sync(0xffffffffu, best, o));
+        least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
+    }
+    if (lane == 0) {
+        sh.maxima[warp] = best;
+        sh.minima[warp] = least;
+    }
+    if (threadIdx.x == 0) sh.listed = 0;
     __syncthreads();
-    for (int w = 0; w < THREADS / 32; ++w) best = largest(best, sh.maxima[w]);
+    for (int w = 0; w < THREADS / 32; ++w) {
+        best = largest(best, sh.maxima[w]);
+        least = fminf(least, sh.minima[w]);
+    }
+    // The largest logits are listed where they may be all that is kept: as many as top_k, or some for top_p to be reached by.
+    const bool by_k = top_k > 0 && top_k <= THREADS / 2, some = by_k || (top_k <= 0 && top_p < 1.f);
+    uint32_t bound = kNegInf + 1;
+    if (some && fabsf(best) < INFINITY) bound = s.bound(mine, least, best, by_k ? top_k : THREADS / 2);
     if (blocks > 1) {
-        if (threadIdx.x == 0) sh.part.best = best;
+        if (threadIdx.x == 0) {
+            sh.part.best = best;
+            sh.part.bound = bound;
+        }
         all_meet(blocks);
-        for (int o = 0; o < blocks; ++o) best = largest(best, at_rank(&sh, o)->part.best);
+        for (int o = 0; o < blocks; ++o) {
+            best = largest(best, at_rank(&sh, o)->part.best);
+            bound = max(bound, at_rank(&sh, o)->part.bound);
+        }
         all_meet(blocks);                                // (nobody leaves while its word is read)
     }
     const bool valid = scale >= 1e-6f && scale <= 1e6f && top_p == top_p && min_p == min_p && u >= 0.f && u < 1.f;
@@ -328,11 +496,112 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS) sa
     s.weigh.least = best - 45.f / scale;                 // (e^-45 < 2^-64)
     s.weigh.table = sh.table;
 
+    uint32_t least_key = 0;                              // of min_p
+    if (min_p > 0.f) {
+        const double low = (double)best + log((double)fminf(min_p, 1.f)) / scale;
+        float f = (float)low;
+        if ((double)f < low) f = value_of(key_of(f) + 1);
+        least_key = max(key_of(f), kNegInf + 1);
+    }
+
+    if (some || (least_key && top_p >= 1.f)) {
+        const bool lower = by_k && top_p < 1.f;          // top_k's weights are all needed for top_p
+        const uint32_t from = some ? (lower ? bound : max(bound, least_key)) : least_key;
+        const bool complete = from <= max(least_key, kNegInf + 1);
+        const bool total = some && !by_k;
+        const float floor = value_of(from);
+        const auto note = [&](float v, int token) {
+            const uint32_t at = atomicAdd(&sh.listed, 1u);
+            if (at < kList) sh.list[at] = (u64)~key_of(v) << 32 | (uint32_t)token;
+        };
+        double sum = 0.0;
+        if (total) {                                     // and the total, in fp32's precision
+            const float c = scale * 1.44269504f;
+            for (int g = begin + (int)threadIdx.x; g < end; g += THREADS) {
+                float v[8], part = 0.f;
+                row.load(g, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float e;
+                    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"((v[i] - best) * c));
+                    part += e;
+                }
+                sum += part;
+                const float most = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+                if (most >= floor) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (v[i] >= floor && v[i] > -INFINITY) note(v[i], g * 8 - row.skew + i);
+                }
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (lane == 0) sh.scan_f[warp] = sum;
+        } else s.each_from(floor, note);
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            sum = 0.0;
+            if (total)
+                for (int w = 0; w < THREADS / 32; ++w) sum += sh.scan_f[w];
+            sh.part.sum = sum;
+        }
+        all_meet(blocks);
+        Outcome outcome = kNeedAll;
+        int n = 0;
+        for (int o = 0; o < blocks; ++o) n += (int)min((uint32_t)kList + 1, blocks == 1 ? sh.listed : at_rank(&sh, o)->listed);
+        if (n <= kList) {
+            u64 low = 0, high = 0;
+            if (total) {
+                sum = 0.0;
+                for (int o = 0; o < blocks; ++o) sum += (blocks == 1 ? &sh : at_rank(&sh, o))->part.sum;
+                // An exponential is off by 2^-22, its argument t by 3 roundings, eight of them added by 7: (2^-22 + 2^-24 (2.1 |t| + 8)) w; and
+                // sum w |t| is at most sum w log2(vocab / sum w), as no distribution's entropy is above log2 vocab.
+                const double off = sum * 0x1p-24 * (14.0 + 2.1 * max(0.0, log2((double)a.vocab / sum))), unit = exp2((double)a.frac_bits);
+                low = (u64)((sum - off) * unit);
+                high = (u64)((sum + off) * unit) + (u64)a.vocab;
+            }
+            if (rank == 0) {
+                for (int o = 1, at = (int)sh.listed; o < blocks; ++o) {
+                    const Shared<THREADS> *other = at_rank(&sh, o);
+                    const int there = (int)other->listed;
+                    for (int i = threadIdx.x; i < there; i += THREADS) sh.list[at + i] = other->list[i];
+                    at += there;
+                }
+                __syncthreads();
+                outcome = s.from_list(a, r, n, complete, max(top_k, 0), top_p, low, high, least_key, u);
+                if (blocks > 1 && threadIdx.x == 0) sh.outcome = outcome;
+            }
+            all_meet(blocks);
+            if (blocks > 1) {
+                outcome = (Outcome)at_rank(&sh, 0)->outcome;
+                all_meet(blocks);
+            }
+            if (outcome == kDone) return;
+            if (outcome == kNeedTotal) {                 // (the list stays as it is: sorted, at rank 0)
+                u64 mass = 0;
+                s.each([&](float v) { mass += s.weigh(v); });
+                u64 all;
+                block_scan<THREADS>(mass, sh.scan, &all);
+                if (threadIdx.x == 0) sh.part.mass = all;
+                all_meet(blocks);
+                if (rank == 0) {
+                    all = 0;
+                    for (int o = 0; o < blocks; ++o) all += (blocks == 1 ? &sh : at_rank(&sh, o))->part.mass;
+                    outcome = s.from_list(a, r, n, complete, 0, top_p, all, all, least_key, u);
+                    if (blocks > 1 && threadIdx.x == 0) sh.outcome = outcome;
+                }
+                all_meet(blocks);
+                if (blocks > 1) {
+                    outcome = (Outcome)at_rank(&sh, 0)->outcome;
+                    all_meet(blocks);
+                }
+                if (outcome == kDone) return;
+            }
+        } else all_meet(blocks);                         // (the numbers listed are read)
+    }
+
     Cut cut{kNegInf, 0};
     u64 goal;
-    const auto tighter = [&](const Cut &c) {
-        if (c.key > cut.key || (c.key == cut.key && c.ties < cut.ties)) cut = c;
-    };
     if (top_k > 0 && top_k < a.vocab) {
         Cut c;
         if (s.template narrow<false>(kNegInf, [&](u64) { return (u64)top_k; }, &c, &goal)) cut = c;
@@ -344,12 +613,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS) sa
         if (inside) cut = c;
         else if (tied) cut.ties = (goal - sh.found.total + tied - 1) / tied;
     }
-    if (min_p > 0.f) {
-        const double least = (double)best + log((double)fminf(min_p, 1.f)) / scale;
-        float f = (float)least;
-        if ((double)f < least) f = value_of(key_of(f) + 1);
-        tighter(Cut{key_of(f) - 1, 0});
-    }
+    if (least_key > cut.key) cut = Cut{least_key - 1, 0};
 
     // Sums of the kept weights by segments of the row, in its order.
     const int segments = (end - begin + 32 * a.seg_steps - 1) / (32 * a.seg_steps);

@@ -471,28 +471,50 @@ PyObject *dropout(PyObject *, PyObject *const *a, Py_ssize_t n) {
 
 // A list or tuple of tensors; None: none.
 struct Tensors {
-    PyObject *items = nullptr;
+    PyObject **items = nullptr;
     Py_ssize_t n = 0;
     Tensors(const Call &c, const char *what, PyObject *o, Py_ssize_t want = -1) {
         if (o == Py_None) return;
         if (!PyList_Check(o) && !PyTuple_Check(o)) c.refuse(std::string(what) + " has to be a list or tuple of tensors, not " + Py_TYPE(o)->tp_name);
-        items = o;
         n = PySequence_Fast_GET_SIZE(o);
+        static PyObject *none[1] = {nullptr};
+        items = n ? PySequence_Fast_ITEMS(o) : none;
         if (want >= 0 && n != want) c.refuse(std::to_string(n) + " " + what + " for " + std::to_string(want) + " tensors");
     }
     explicit operator bool() const { return items; }
-    PyObject *object(Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(items, i); }
+    PyObject *object(Py_ssize_t i) const { return items[i]; }
 };
 
-// The type of tensor i of a list, the same for all of it; contiguous, of this shape, on the call's device.
-const at::Tensor &member(const Call &c, const char *what, const Tensors &list, Py_ssize_t i, const at::Tensor *like, at::ScalarType type) {
-    const at::Tensor &t = c.tensor(what, list.object(i));
-    if (t.scalar_type() != type || !t.is_contiguous() || (like && t.sizes() != like->sizes()) || t.get_device() != c.index) {
-        const std::string name = std::string(what) + "[" + std::to_string(i) + "]";
-        c.here(name.c_str(), t);
-        c.refuse(name + " is " + Call::describe(t) + ": a contiguous " + c10::toString(type) + " tensor" + (like ? " like " + Call::describe(*like) : "") + " is needed");
+// The tensors of a list, checked: all of this type, contiguous, on the call's device, of the shapes of `like`'s if that is given; their
+// addresses go to place(i, tensor, address).  A list of some hundreds is checked faster than its kernel runs only if its objects, which lie
+// anywhere, are fetched ahead.
+template <class F> void members(const Call &c, const char *what, const Tensors &list, at::ScalarType type, const Tensors *like, F place) {
+    const caffe2::TypeMeta meta = c10::scalarTypeToTypeMeta(type);
+    constexpr Py_ssize_t kAhead = 4;
+    for (Py_ssize_t i = 0; i < list.n; ++i) {
+        if (i + 2 * kAhead < list.n) __builtin_prefetch(list.items[i + 2 * kAhead]);
+        if (i + kAhead < list.n && THPVariable_Check(list.items[i + kAhead])) {
+            const char *const next = reinterpret_cast<const char *>(THPVariable_Unpack(list.items[i + kAhead]).unsafeGetTensorImpl());
+            for (size_t line = 0; line < sizeof(at::TensorImpl); line += 64) __builtin_prefetch(next + line);
+        }
+        const at::Tensor &t = c.tensor(what, list.items[i]);
+        const at::TensorImpl *const impl = t.unsafeGetTensorImpl();
+        const at::Tensor *const same = like ? &THPVariable_Unpack(like->items[i]) : nullptr;
+        if (t.dtype() != meta || !t.is_contiguous() || !t.is_cuda() || t.get_device() != c.index || (same && impl->sizes() != same->sizes())) {
+            const std::string name = std::string(what) + "[" + std::to_string(i) + "]";
+            c.here(name.c_str(), t);
+            c.refuse(name + " is " + Call::describe(t) + ": a contiguous " + c10::toString(type) + " tensor" + (same ? " like " + Call::describe(*same) : "") + " is needed");
+        }
+        place(i, (long long)t.numel(), t.data_ptr());
     }
-    return t;
+}
+
+// As Call::written(), for a list.
+void written(const Tensors &list) {
+    for (Py_ssize_t i = 0; i < list.n; ++i) {
+        const at::Tensor &t = THPVariable_Unpack(list.items[i]);
+        if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    }
 }
 
 // grads, out, workspace, stream
@@ -507,10 +529,7 @@ PyObject *grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     const at::ScalarType type = first.scalar_type();
     const int dtype = c.dtype("grads[0]", first);
     std::vector<parle_grad_tensor> list((size_t)grads.n);
-    for (Py_ssize_t i = 0; i < grads.n; ++i) {
-        const at::Tensor &t = member(c, "grads", grads, i, nullptr, type);
-        list[i] = {t.data_ptr(), (long long)t.numel()};
-    }
+    members(c, "grads", grads, type, nullptr, [&](Py_ssize_t i, long long size, void *p) { list[i] = {p, size}; });
     Result out(a[1]);
     if (!out.given) out.made = c.make({}, at::kFloat);
     float *const norm = (float *)c.word("out", out.given ? out.given : Py_None, at::kFloat, at::kFloat);
@@ -570,24 +589,18 @@ PyObject *adamw(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
         if (copy_dtype == PARLE_F32 || param_dtype != PARLE_F32) c.refuse("copies are 16-bit ones of fp32 params");
     }
     std::vector<parle_adamw_tensor> list((size_t)params.n);
-    for (Py_ssize_t i = 0; i < params.n; ++i) {
-        const at::Tensor &p = member(c, names[0], params, i, nullptr, types[0]);
-        parle_adamw_tensor &t = list[i];
-        t.size = p.numel();
-        t.param = p.data_ptr();
-        t.grad = member(c, names[1], lists[1], i, &p, types[1]).data_ptr();
-        t.exp_avg = member(c, names[2], lists[2], i, &p, types[2]).data_ptr();
-        t.exp_avg_sq = member(c, names[3], lists[3], i, &p, types[3]).data_ptr();
-        t.exp_avg_scale = t.exp_avg_sq_scale = nullptr;
-        if (bits == 8)
-            for (int k = 4; k < 6; ++k) {
-                const at::Tensor &s = member(c, names[k], lists[k], i, nullptr, at::kFloat);
-                if (s.numel() != (t.size + PARLE_ADAMW_BLOCK - 1) / PARLE_ADAMW_BLOCK)
-                    c.refuse(std::string(names[k]) + "[" + std::to_string(i) + "] is " + Call::describe(s) + ": a scale for each 256 of " + std::to_string(t.size) + " elements is needed");
-                (k == 4 ? t.exp_avg_scale : t.exp_avg_sq_scale) = (float *)s.data_ptr();
-            }
-        t.copy = lists[6] ? member(c, names[6], lists[6], i, &p, types[6]).data_ptr() : nullptr;
-    }
+    members(c, names[0], params, types[0], nullptr, [&](Py_ssize_t i, long long size, void *p) { list[i] = {p, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, size}; });
+    members(c, names[1], lists[1], types[1], &params, [&](Py_ssize_t i, long long, void *p) { list[i].grad = p; });
+    members(c, names[2], lists[2], types[2], &params, [&](Py_ssize_t i, long long, void *p) { list[i].exp_avg = p; });
+    members(c, names[3], lists[3], types[3], &params, [&](Py_ssize_t i, long long, void *p) { list[i].exp_avg_sq = p; });
+    for (int k = 4; k < 6; ++k)
+        members(c, names[k], lists[k], types[k], nullptr, [&](Py_ssize_t i, long long scales, void *p) {
+            if (scales != (list[i].size + PARLE_ADAMW_BLOCK - 1) / PARLE_ADAMW_BLOCK)
+                c.refuse(std::string(names[k]) + "[" + std::to_string(i) + "] has " + std::to_string(scales) + " numbers: one for each " + std::to_string(PARLE_ADAMW_BLOCK) + " of " +
+                         std::to_string(list[i].size) + " elements is needed");
+            (k == 4 ? list[i].exp_avg_scale : list[i].exp_avg_sq_scale) = (float *)p;
+        });
+    members(c, names[6], lists[6], lists[6] ? types[6] : at::kFloat, &params, [&](Py_ssize_t i, long long, void *p) { list[i].copy = p; });
     parle_adamw_step h;
     h.step = c.integer("step", a[7], 0, LLONG_MAX);
     h.lr = c.number("lr", a[8]);
@@ -604,8 +617,7 @@ PyObject *adamw(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     c.run([&] { return parle_adamw(list.data(), (int)params.n, param_dtype, grad_dtype, copy_dtype, bits, &h, flags, c.stream); });
     c.written({a[18]});
     for (int k = 0; k < 7; ++k)
-        if (k != 1 && lists[k])
-            for (Py_ssize_t i = 0; i < params.n; ++i) c.written({lists[k].object(i)});
+        if (k != 1) written(lists[k]);
     Py_RETURN_NONE;
     END_HANDLE_TH_ERRORS
 }
