@@ -65,13 +65,22 @@ __device__ __forceinline__ u64 part_of(u64 total, float f, bool up) {
 
 struct Weigher {                                         // w(x) = exp(scale (x - best)) as a whole number of 2^-frac_bits
     double best, c, one;                                 // c: 32 scale log2 e; one: whose last bit is 2^-frac_bits
-    float least;                                         // logits below it weigh nothing
+    float least;                                         // it and all logits below weigh nothing
     const double *table;                                 // 2^(i / 32), in shared memory
+    __device__ __forceinline__ void set(float best_, float scale, int frac_bits, const double *table_) {
+        best = best_;
+        table = table_;
+        one = __hiloint2double((1023 + 52 - frac_bits) << 20, 0);
+        // e^-45 < 2^-64.  Where best - 45 / scale is best again, the next number below weighs nothing, and is taken for as little as fits.
+        least = fminf(best_ - 45.f / scale, value_of(key_of(best_) - 1));
+        c = fmin(32.0 * 1.44269504088896340736 * scale, 4096.0 / (best - (double)least));
+    }
     // 2^(n / 32) from the table, e^y of the rest, |y| <= ln 2 / 64 = h, by Taylor's polynomial of degree 5 whose last term is spread over y and y^3
     // (Chebyshev's economisation: 16 z^5 - 20 z^3 + 5 z is at most 1): off by h^5 / 1920 = 8 10^-14.  Nine operations in fp64.
-    __device__ __forceinline__ u64 operator()(float x) const {
+    // raw(): of x >= least, with the bits of `one` still on it
+    __device__ __forceinline__ u64 raw(float x) const {
         constexpr double y = 0.69314718055994530942 / 32, h = y / 2;
-        const double d = (double)fmaxf(x, least) - best;
+        const double d = (double)x - best;
         const double shifted = fma(d, c, 6755399441055744.0);      // 1.5 2^52: rounds to a whole number
         const int n = __double2loint(shifted);
         const double r = fma(d, c, 6755399441055744.0 - shifted);
@@ -81,41 +90,90 @@ struct Weigher {                                         // w(x) = exp(scale (x 
         p = fma(p, r, 1.0);
         const double power = table[n & 31];
         p = fma(p, __hiloint2double(__double2hiint(power) + ((n >> 5) << 20), __double2loint(power)), one);
-        return x < least ? 0 : (u64)(__double_as_longlong(p) - __double_as_longlong(one));
+        return (u64)__double_as_longlong(p);
     }
+    __device__ __forceinline__ u64 operator()(float x) const { return raw(fmaxf(x, least)) - (u64)__double_as_longlong(one); }
 };
 
-// A row in granules of eight logits, cut at memory's 16-byte boundaries.
+// A row in granules of eight logits, cut at memory's 16-byte boundaries.  `flat`: all logits are -inf or the lowest number (a row that is masked
+// altogether); the latter are then taken for 0, so that there is a number below the largest logit, always.
 template <typename T> struct Row {
     const T *x;
     int vocab, skew;                                     // logits of the first granule before the row
-    __device__ __forceinline__ void load(int granule, float (&v)[8]) const {
-        const long long e0 = (long long)granule * 8 - skew;
-        if (e0 >= 0 && e0 + 8 <= vocab) {
-            Pack8<T> p;
-            p.load(x + e0);
+    bool flat;
+    __device__ __forceinline__ long long first(int granule) const { return (long long)granule * 8 - skew; }
+    __device__ __forceinline__ bool whole(int granule) const { return first(granule) >= 0 && first(granule) + 8 <= vocab; }
+    __device__ __forceinline__ float at(long long token) const {
+        const float v = token >= 0 && token < vocab ? to_float(x[token]) : -INFINITY;
+        return flat && v > -INFINITY ? 0.f : v;
+    }
+    __device__ __forceinline__ Pack8<T> fetch(int granule, int end) const {      // early; nothing where it is not whole
+        Pack8<T> p = {};
+        if (granule < end && whole(granule)) p.load(x + first(granule));
+        return p;
+    }
+    __device__ __forceinline__ void get(const Pack8<T> &p, int granule, float (&v)[8]) const {
+        if (whole(granule)) {
             p.get(v);
+            if (flat) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = v[i] > -INFINITY ? 0.f : v[i];
+            }
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = e0 + i >= 0 && e0 + i < vocab ? to_float(x[e0 + i]) : -INFINITY;
+            for (int i = 0; i < 8; ++i) v[i] = at(first(granule) + i);
         }
     }
+    __device__ __forceinline__ void load(int granule, float (&v)[8]) const { get(fetch(granule, granule + 1), granule, v); }
 };
 
-struct Cut {                                             // kept: logits of keys above `key`, and the first `ties` of those with it
-    uint32_t key;
+__device__ __forceinline__ float largest(float v, float w) {      // NaN if either is
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(v), "f"(w));
+    return m;
+}
+__device__ __forceinline__ __nv_bfloat162 largest(__nv_bfloat162 v, __nv_bfloat162 w) { return __hmax2_nan(v, w); }
+__device__ __forceinline__ __half2 largest(__half2 v, __half2 w) { return __hmax2_nan(v, w); }
+// The largest of granules of 16-bit logits in pairs (half the instructions), of fp32 ones one by one.
+template <typename T> struct Pair;
+template <> struct Pair<__nv_bfloat16> { typedef __nv_bfloat162 type; };
+template <> struct Pair<__half> { typedef __half2 type; };
+template <typename T> struct Largest {
+    typename Pair<T>::type pair;
+    __device__ __forceinline__ Largest() { pair.x = pair.y = from_float<T>(-INFINITY); }
+    __device__ __forceinline__ void take(const Pack8<T> &p) {
+        typedef typename Pair<T>::type P2;
+        const P2 *h = reinterpret_cast<const P2 *>(&p);
+        pair = largest(pair, largest(largest(h[0], h[1]), largest(h[2], h[3])));
+    }
+    __device__ __forceinline__ float get() const { return largest(to_float(pair.x), to_float(pair.y)); }
+};
+template <> struct Largest<float> {
+    float most = -INFINITY;
+    __device__ __forceinline__ void take(const Pack8<float> &p) {
+        most = largest(most, largest(largest(largest(p.a.x, p.a.y), largest(p.a.z, p.a.w)), largest(largest(p.b.x, p.b.y), largest(p.b.z, p.b.w))));
+    }
+    __device__ __forceinline__ float get() const { return most; }
+};
+
+struct Cut {                                             // kept: logits of keys above `key`, and the first `ties` of those with it;
+    uint32_t key;                                        // by_last: of those, the ones up to token `last`
     u64 ties;
+    bool by_last;
+    uint32_t last;
 };
 
 struct Part {                                            // what a block found out about its part of the row
     float best;
     uint32_t bound;                                      // key that as many logits of the part reach as were asked for
     double sum;                                          // of weights, in fp32's precision
-    u64 mass;
+    u64 mass, above;
     uint32_t count, ties;
 };
 
 enum Outcome { kDone, kNeedTotal, kNeedAll };            // of a list of the largest logits: sampled from; the weights' total is needed exactly; too short
+
+enum Settled { kNot, kSums, kCutOnly };                  // a border was not found; with the segments' sums; without them
 
 template <int THREADS> struct Shared {
     double table[32];
@@ -134,13 +192,22 @@ template <int THREADS> struct Shared {
     float maxima[THREADS / 32];
     float minima[THREADS / 32];
     uint32_t listed;
-    int outcome;
+    Outcome outcome;
     Part part;
     struct {
         u64 above, total;
         int bin;
         uint32_t low, high;
     } found;
+    struct {
+        u64 before, upto;                                // logits in the steps before the bracket, and up to its end
+        int from, to;
+    } bracket;
+    struct {                                             // by rank 0: what is kept, with its last token
+        Settled settled;
+        uint32_t key, last;
+        u64 kept, ties;
+    } choice;
     struct {
         u64 target;
         uint32_t ties_before;
@@ -192,27 +259,85 @@ template <typename T, int THREADS> struct Sampler {
 
     __device__ __forceinline__ int step_of(float x) const { return min(kBins - 1, (int)((best - x) * scale * 32.f)); }
 
-    template <class F> __device__ __forceinline__ void each(F f) const {
-        for (int g = begin + (int)threadIdx.x; g < end; g += THREADS) {
-            float v[8];
-            row.load(g, v);
+    // f(granule, logits) for each granule of the block's part, some in flight.
+    template <class F> __device__ __forceinline__ void each_granule(F f) const {
+        constexpr int kFlight = sizeof(T) == 2 ? 4 : 2;
+        for (int g = begin + (int)threadIdx.x; g < end; g += THREADS * kFlight) {
+            Pack8<T> p[kFlight];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f(v[i]);
-        }
-    }
-
-    // As each(), with the token's number; only where f's logits reach `floor`.
-    template <class F> __device__ __forceinline__ void each_from(float floor, F f) const {
-        for (int g = begin + (int)threadIdx.x; g < end; g += THREADS) {
-            float v[8];
-            row.load(g, v);
-            float most = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
-            if (most >= floor) {
+            for (int i = 0; i < kFlight; ++i) p[i] = row.fetch(g + i * THREADS, end);
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (v[i] >= floor && v[i] > -INFINITY) f(v[i], g * 8 - row.skew + i);
+            for (int i = 0; i < kFlight; ++i) {
+                if (g + i * THREADS >= end) break;
+                float v[8];
+                row.get(p[i], g + i * THREADS, v);
+                f(g + i * THREADS, v);
             }
         }
+    }
+    template <class F> __device__ __forceinline__ void each(F f) const {
+        each_granule([&](int, const float (&v)[8]) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f(v[i]);
+        });
+    }
+    __device__ __forceinline__ float largest_logit() const {
+        float mine = -INFINITY;
+        Largest<T> most;
+        constexpr int kFlight = 4;
+        for (int g = begin + (int)threadIdx.x; g < end; g += THREADS * kFlight) {
+            Pack8<T> p[kFlight];
+#pragma unroll
+            for (int i = 0; i < kFlight; ++i) p[i] = row.fetch(g + i * THREADS, end);
+#pragma unroll
+            for (int i = 0; i < kFlight; ++i) {
+                if (g + i * THREADS >= end) break;
+                if (row.whole(g + i * THREADS)) most.take(p[i]);
+                else {
+#pragma unroll 1
+                    for (int k = 0; k < 8; ++k) mine = largest(mine, row.at(row.first(g + i * THREADS) + k));
+                }
+            }
+        }
+        return largest(mine, most.get());
+    }
+    // f(segment, granule, logits, sum) for the granules of each segment, a warp's granules side by side and the whole warp in each call (behind the
+    // part's end with logits of -inf); then done(segment, sum of the lanes' sums).
+    template <class F, class G> __device__ __forceinline__ void each_segment(int seg_steps, F f, G done) const {
+        const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, segments = (end - begin + 32 * seg_steps - 1) / (32 * seg_steps);
+        int at = begin + warp * seg_steps * 32 + lane;
+        Pack8<T> next = row.fetch(at, end);
+        for (int g = warp; g < segments; g += THREADS / 32) {
+            u64 m = 0;
+            for (int i = 0; i < seg_steps; ++i) {
+                const Pack8<T> p = next;
+                const int now = at;
+                at += i + 1 < seg_steps ? 32 : 32 + (THREADS / 32 - 1) * seg_steps * 32;
+                next = row.fetch(at, end);
+                float v[8];
+                if (now < end) row.get(p, now, v);
+                else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] = -INFINITY;
+                }
+                f(g, now, v, m);
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) m += __shfl_xor_sync(0xffffffffu, m, o);
+            done(g, m);
+        }
+    }
+    __device__ __forceinline__ static float most_of(const float (&v)[8]) {
+        return fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+    }
+    // Lists the granule's logits in [low, high].
+    __device__ __forceinline__ void note(int granule, const float (&v)[8], float low, float high) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (v[k] >= low && v[k] <= high && v[k] > -INFINITY) {
+                const uint32_t place = atomicAdd(&sh.listed, 1u);
+                if (place < kList) sh.list[place] = (u64)~key_of(v[k]) << 32 | (uint32_t)(row.first(granule) + k);
+            }
     }
 
     // Adds w to bin b: a count, or a 64-bit number in two words.
@@ -347,6 +472,7 @@ template <typename T, int THREADS> struct Sampler {
     template <class F> __device__ __forceinline__ void running(int n, F value) {
         const int per = (n + THREADS - 1) / THREADS, first = min(n, (int)threadIdx.x * per), last = min(n, first + per);
         u64 sum = 0, all;
+        __syncthreads();                                 // (what value() reads is written)
         for (int i = first; i < last; ++i) sum += value(i);
         u64 before = block_scan<THREADS>(sum, sh.scan, &all);
         for (int i = first; i < last; ++i) sh.sums[i] = before += value(i);
@@ -425,14 +551,278 @@ template <typename T, int THREADS> struct Sampler {
         }
         return kDone;
     }
+
+    // Steps of 1/128 for counts.
+    static constexpr int kCounts = 2 * kBins;
+    __device__ __forceinline__ float count_place_of(float x) const { return fminf((best - x) * scale * 128.f, kCounts - 1); }
+    __device__ __forceinline__ int count_step_of(float x) const { return (int)count_place_of(x); }
+    // The smallest key above `floor` of a step up to `step`.
+    __device__ __forceinline__ uint32_t first_key(uint32_t floor, int step) const {
+        uint32_t low = floor + 1, high = key_of(best) + 1;
+        while (low < high) {
+            const uint32_t mid = low + (high - low) / 2;
+            if (count_step_of(value_of(mid)) <= step) high = mid; else low = mid + 1;
+        }
+        return low;
+    }
+
+    // What is kept of the logits above `floor` (and the first `ties` of it): by top_p, else by top_k (then floor is -inf's).  Counts by steps say near
+    // which one the border lies; for top_p every eighth logit's place within its step is added up, too: sums by counts and mean places are
+    // off by some 10^-5.  What is known already saves counting: `known` logits from `known_key` on, of the sum known_sum, and the sum of all
+    // (0: not known; in units of 2^-30).  One more pass adds up the weights, exactly, of all logits and of those above the steps around the border,
+    // these by segments, and lists the logits between, whose ranking gives the border (and shows whether the guess was right).
+    __device__ __forceinline__ Settled general(int seg_steps, uint32_t floor, u64 ties, int top_k, float top_p, uint32_t least_key, int known, uint32_t known_key,
+                                               u64 known_sum, u64 known_total) {
+        constexpr int kPer = kBins / THREADS;            // bins of a thread: kPer, and as many of the second half
+        uint32_t *const counts = &sh.hist[0][0];
+        uint32_t *const places = reinterpret_cast<uint32_t *>(sh.weight);      // (unused meanwhile, as long as counts)
+        static_assert(sizeof(sh.weight) + sizeof(sh.sums) >= kCounts * sizeof(uint32_t), "");
+        for (int i = threadIdx.x; i < kCounts; i += THREADS) counts[i] = places[i] = 0;
+        __syncthreads();
+        const float floor_value = value_of(floor), ceiling = known ? value_of(known_key) : INFINITY;
+        float low_value = floor_value;
+        // Logits that weigh less than (1 - top_p) total / vocab are all together less than what top_p leaves out.
+        if (known_total) low_value = fmaxf(low_value, best + (logf((1.f - top_p) * 0.999f * ((float)known_total * 0x1p-30f) / row.vocab)) / scale);
+        each_granule([&](int, const float (&v)[8]) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (v[i] > low_value && v[i] < ceiling) {
+                    const float t = count_place_of(v[i]);
+                    const int b = (int)t;
+                    atomicAdd(&counts[b], 1u);
+                    if (i == 0 && top_p < 1.f) atomicAdd(&places[b], 1u << 20 | (uint32_t)((t - b) * 256.f));
+                }
+            }
+        });
+        if (threadIdx.x == 0) {
+            sh.listed = 0;
+            sh.found.bin = -1;
+        }
+        all_meet(blocks);
+        uint32_t n[2 * kPer];
+        float place[2 * kPer];
+        u64 sum = 0, count;
+#pragma unroll
+        for (int i = 0; i < 2 * kPer; ++i) {
+            const int b = threadIdx.x * 2 * kPer + i;
+            uint32_t p = 0, samples = 0;
+            n[i] = 0;
+            for (int o = 0; o < blocks; ++o) {
+                const Shared<THREADS> *other = blocks == 1 ? &sh : at_rank(&sh, o);
+                n[i] += (&other->hist[0][0])[b];
+                const uint32_t q = reinterpret_cast<const uint32_t *>(other->weight)[b];
+                p += q & 0xfffffu;
+                samples += q >> 20;
+            }
+            place[i] = samples ? fminf(p / (256.f * samples), 1.f) : 0.5f;
+            sum += n[i];
+        }
+        const u64 before = known + block_scan<THREADS>(sum, sh.scan, &count);
+        if (top_p < 1.f) {
+            const auto weight = [&](float step) { return exp2f(step * (-1.44269504f / 128)) * 0x1p30f; };
+            u64 part[2 * kPer], sum = 0, all;
+#pragma unroll
+            for (int i = 0; i < 2 * kPer; ++i) sum += part[i] = (u64)(n[i] * weight(threadIdx.x * 2 * kPer + i + place[i]));
+            u64 at = known_sum + block_scan<THREADS>(sum, sh.scan, &all);
+            all += known_sum;
+            const u64 tied = ties * (u64)weight((best - floor_value) * scale * 128.f);
+            const u64 goal = part_of(known_total ? known_total : all + tied, top_p, true), low = max((u64)1, goal - (goal >> 13)), high = max((u64)1, min(goal + (goal >> 13), all));
+#pragma unroll
+            for (int i = 0; i < 2 * kPer; ++i) {
+                if (at < low && at + part[i] >= low) sh.found.bin = threadIdx.x * 2 * kPer + i;
+                if (at < high && at + part[i] >= high) sh.found.low = threadIdx.x * 2 * kPer + i;
+                at += part[i];
+            }
+        } else {
+            u64 at = before;
+            if (count <= (u64)top_k && threadIdx.x == 0) sh.found.bin = -2;
+#pragma unroll
+            for (int i = 0; i < 2 * kPer; ++i) {
+                if (count > (u64)top_k && at < (u64)top_k && at + n[i] >= (u64)top_k) sh.found.bin = sh.found.low = threadIdx.x * 2 * kPer + i;
+                at += n[i];
+            }
+        }
+        __syncthreads();
+        int from = sh.found.bin, to = (int)sh.found.low;
+        if (from == -2) {                                // top_k does not bind
+            if (threadIdx.x == 0) {
+                sh.choice.key = floor;
+                sh.choice.ties = ties;
+            }
+            all_meet(blocks);
+            return kCutOnly;
+        }
+        const auto bounds = [&](u64 first, u64 last) {   // steps and numbers of the logits first + 1 .. last of the ranking
+            u64 at = before;
+#pragma unroll
+            for (int i = 0; i < 2 * kPer; ++i) {
+                const u64 next = at + n[i];
+                if (at <= first && next > first) {
+                    sh.bracket.from = threadIdx.x * 2 * kPer + i;
+                    sh.bracket.before = at;
+                }
+                if (at < last && next >= last) {
+                    sh.bracket.to = threadIdx.x * 2 * kPer + i;
+                    sh.bracket.upto = next;
+                }
+                at = next;
+            }
+        };
+        u64 at = before;
+#pragma unroll
+        for (int i = 0; i < 2 * kPer; ++i) {
+            if ((int)threadIdx.x * 2 * kPer + i == from) {
+                sh.bracket.from = from;
+                sh.bracket.before = at;
+            }
+            at += n[i];
+            if ((int)threadIdx.x * 2 * kPer + i == to) {
+                sh.bracket.to = to;
+                sh.bracket.upto = at;
+            }
+        }
+        __syncthreads();
+        u64 above_count = sh.bracket.before, upto = sh.bracket.upto;
+        if (from >= 0 && upto - above_count < kList && top_p < 1.f) {      // some more, as sums of few logits are less exact
+            const u64 more = (kList - (upto - above_count)) / 4;
+            __syncthreads();
+            bounds(above_count - min(above_count - known, more), min(upto + more, known + count));
+            __syncthreads();
+            if (sh.bracket.upto - sh.bracket.before <= kList) {
+                from = sh.bracket.from;
+                to = sh.bracket.to;
+                above_count = sh.bracket.before;
+                upto = sh.bracket.upto;
+            }
+        }
+        all_meet(blocks);                                // (the histograms are read)
+        if (from < 0 || upto - above_count > kList) return kNot;
+        if (threadIdx.x < 2) {
+            const uint32_t key = first_key(floor, threadIdx.x == 0 ? to : from - 1);
+            if (threadIdx.x == 0) sh.found.low = key; else sh.found.high = known ? min(key, known_key) - 1 : key - 1;
+        }
+        __syncthreads();
+        const float low = value_of(sh.found.low), high = value_of(sh.found.high);
+        const int lane = threadIdx.x % 32;
+        const u64 one = (u64)__double_as_longlong(weigh.one);
+        const float weightless = fmaxf(top_p < 1.f ? floor_value : high, weigh.least);
+        u64 total = 0, above = 0;
+        each_segment(seg_steps, [&](int, int at, const float (&v)[8], u64 &m) {
+            bool some = false, any = top_p < 1.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                some |= v[k] >= low && v[k] <= high;
+                any |= v[k] > high;
+            }
+            if (__any_sync(0xffffffffu, any)) {
+                u64 all = 0, most = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const u64 w = weigh.raw(v[k] > weightless ? v[k] : weigh.least);
+                    all += w;
+                    most += v[k] > high ? w : one;
+                }
+                total += all - 8 * one;
+                m += most - 8 * one;
+            }
+            if (some) note(at, v, low, high);
+        }, [&](int g, u64 m) {
+            if (lane == 0) {
+                sh.seg.mass[g] = m;
+                above += m;
+            }
+        });
+        u64 all_total, all_above;
+        block_scan<THREADS>(total, sh.scan, &all_total);
+        block_scan<THREADS>(above, sh.scan, &all_above);
+        if (threadIdx.x == 0) {
+            sh.part.mass = all_total;
+            sh.part.above = all_above;
+        }
+        all_meet(blocks);
+        int n_list = (int)sh.listed;
+        const int own_list = n_list;
+        if (rank == 0) {
+            total = above = 0;
+            int listed = 0;
+            for (int o = 0; o < blocks; ++o) {
+                const Shared<THREADS> *other = blocks == 1 ? &sh : at_rank(&sh, o);
+                total += other->part.mass;
+                above += other->part.above;
+                listed += (int)min(other->listed, (uint32_t)kList + 1);
+            }
+            const bool fits = listed <= kList;
+            for (int o = 1; fits && o < blocks; ++o) {
+                const Shared<THREADS> *other = at_rank(&sh, o);
+                const int there = (int)other->listed;
+                for (int i = threadIdx.x; i < there; i += THREADS) sh.list[n_list + i] = other->list[i];
+                n_list += there;
+            }
+            if (!fits) n_list = 0;
+            __syncthreads();
+            sort(n_list);
+            for (int i = threadIdx.x; i < n_list; i += THREADS) sh.weight[i] = weigh(value_of(~(uint32_t)(sh.list[i] >> 32)));
+            running(n_list, [&](int i) { return sh.weight[i]; });
+            Settled settled = fits && n_list ? kSums : kNot;
+            int kept = top_k - (int)above_count;         // of the list
+            uint32_t key = floor;
+            u64 taken = 0;
+            if (settled == kSums && top_p < 1.f) {
+                const u64 tied = ties ? weigh(value_of(floor)) : 0, goal = max((u64)1, part_of(total + ties * tied, top_p, true));
+                if (goal <= above) settled = kNot;
+                else {
+                    kept = how_many(n_list, goal - above) + 1;
+                    if (kept > n_list) {                 // beyond the list: among the ties of floor, or the guess was wrong
+                        settled = upto == count + known && tied ? kCutOnly : kNot;
+                        if (settled == kCutOnly) taken = (goal - total + tied - 1) / tied;
+                    }
+                }
+            }
+            if (settled == kSums) {
+                if (least_key) {
+                    int reach = 0;
+                    for (int i = 0; i < kept; i += THREADS) reach += __syncthreads_count(i + (int)threadIdx.x < kept && ~(uint32_t)(sh.list[i + threadIdx.x] >> 32) >= least_key);
+                    kept = reach;
+                }
+                if (kept == 0) {                         // min_p cuts above the list
+                    settled = kCutOnly;
+                    key = least_key - 1;
+                } else key = ~(uint32_t)(sh.list[kept - 1] >> 32);
+            }
+            if (threadIdx.x == 0) {
+                sh.choice.settled = settled;
+                sh.choice.key = key;
+                sh.choice.ties = taken;
+                sh.choice.last = settled == kSums ? (uint32_t)sh.list[kept - 1] : 0;
+                sh.choice.kept = above_count + kept;
+            }
+        }
+        all_meet(blocks);
+        if (blocks > 1 && rank > 0) {
+            if (threadIdx.x == 0) sh.choice = at_rank(&sh, 0)->choice;
+            __syncthreads();
+        }
+        if (blocks > 1) all_meet(blocks);
+        if (sh.choice.settled == kSums) {                // the kept ones of the list, to their segments
+            const int mine = rank == 0 ? n_list : own_list;
+            for (int i = threadIdx.x; i < mine; i += THREADS) {
+                const uint32_t key = ~(uint32_t)(sh.list[i] >> 32), token = (uint32_t)sh.list[i];
+                const int granule = (int)((token + row.skew) / 8);
+                if (granule >= begin && granule < end && (key > sh.choice.key || (key == sh.choice.key && token <= sh.choice.last)))
+                    atomicAdd(&sh.seg.mass[(granule - begin) / (32 * seg_steps)], weigh(value_of(key)));
+            }
+            __syncthreads();
+        }
+        return sh.choice.settled;
+    }
 };
 
-template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_kernel(const __grid_constant__ SampleArgs a, int blocks) {
+template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 2 : 4) sample_kernel(const __grid_constant__ SampleArgs a, int blocks) {
     __shared__ Shared<THREADS> sh;
     const int rank = blocks == 1 ? 0 : cluster_rank();
     const long long r = blockIdx.x / blocks;
     const T *const x = static_cast<const T *>(a.logits) + r * a.ld;
-    Row<T> row{x, a.vocab, (int)(reinterpret_cast<uintptr_t>(x) % 16 / sizeof(T))};
+    Row<T> row{x, a.vocab, (int)(reinterpret_cast<uintptr_t>(x) % 16 / sizeof(T)), false};
     const int all = (a.vocab + row.skew + 7) / 8, begin = min(all, rank * a.granules), end = min(all, begin + a.granules);
     const float scale = a.scales ? a.scales[r] : a.scale, top_p = a.top_ps ? a.top_ps[r] : a.top_p, min_p = a.min_ps ? a.min_ps[r] : a.min_p, u = a.u[r];
     const int top_k = a.top_ks ? a.top_ks[r] : a.top_k;
@@ -440,13 +830,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
     if (threadIdx.x < 32) sh.table[threadIdx.x] = exp2((double)threadIdx.x / 32);
 
     Sampler<T, THREADS> s{sh, row, blocks, rank, begin, end, scale, -INFINITY, {}};
-    const auto largest = [](float v, float w) {          // NaN if either is
-        float m;
-        asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(v), "f"(w));
-        return m;
-    };
-    float mine = -INFINITY;
-    s.each([&](float v) { mine = largest(mine, v); });
+    float mine = s.largest_logit();
     float best = mine, least = mine;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -463,21 +847,31 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
         best = largest(best, sh.maxima[w]);
         least = fminf(least, sh.minima[w]);
     }
-    // The largest logits are listed where they may be all that is kept: as many as top_k, or some for top_p to be reached by.
+    // The largest logits are listed where they may be all that is kept: as many as top_k, or some for top_p to be reached by.  Of several blocks
+    // each finds its share of them; or all of them, where one has not that many logits.
     const bool by_k = top_k > 0 && top_k <= THREADS / 2, some = by_k || (top_k <= 0 && top_p < 1.f);
+    const int wanted = by_k ? top_k : THREADS / 2;
     uint32_t bound = kNegInf + 1;
-    if (some && fabsf(best) < INFINITY) bound = s.bound(mine, least, best, by_k ? top_k : THREADS / 2);
+    if (some && fabsf(best) < INFINITY) bound = s.bound(mine, least, best, (wanted + blocks - 1) / blocks);
     if (blocks > 1) {
         if (threadIdx.x == 0) {
             sh.part.best = best;
             sh.part.bound = bound;
         }
         all_meet(blocks);
+        const float own_best = best;
         for (int o = 0; o < blocks; ++o) {
             best = largest(best, at_rank(&sh, o)->part.best);
-            bound = max(bound, at_rank(&sh, o)->part.bound);
+            bound = min(bound, at_rank(&sh, o)->part.bound);
         }
         all_meet(blocks);                                // (nobody leaves while its word is read)
+        if (some && bound == kNegInf + 1 && fabsf(best) < INFINITY) {
+            bound = s.bound(mine, least, own_best, wanted);
+            if (threadIdx.x == 0) sh.part.bound = bound;
+            all_meet(blocks);
+            for (int o = 0; o < blocks; ++o) bound = max(bound, at_rank(&sh, o)->part.bound);
+            all_meet(blocks);
+        }
     }
     const bool valid = scale >= 1e-6f && scale <= 1e6f && top_p == top_p && min_p == min_p && u >= 0.f && u < 1.f;
     if (!valid || !(fabsf(best) < INFINITY)) {
@@ -489,12 +883,13 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
         }
         return;
     }
+    if (best == -3.402823466e38f) {
+        s.row.flat = row.flat = true;
+        bound = kNegInf + 1;
+        best = 0.f;
+    }
     s.best = best;
-    s.weigh.best = best;
-    s.weigh.c = 32.0 * 1.44269504088896340736 * scale;
-    s.weigh.one = __hiloint2double((1023 + 52 - a.frac_bits) << 20, 0);
-    s.weigh.least = best - 45.f / scale;                 // (e^-45 < 2^-64)
-    s.weigh.table = sh.table;
+    s.weigh.set(best, scale, a.frac_bits, sh.table);
 
     uint32_t least_key = 0;                              // of min_p
     if (min_p > 0.f) {
@@ -504,22 +899,20 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
         least_key = max(key_of(f), kNegInf + 1);
     }
 
+    int known = 0;                                       // logits from known_key on, listed
+    uint32_t known_key = 0;
+    u64 known_sum = 0, known_total = 0;                  // of weights, in units of 2^-30; 0: not known
     if (some || (least_key && top_p >= 1.f)) {
         const bool lower = by_k && top_p < 1.f;          // top_k's weights are all needed for top_p
         const uint32_t from = some ? (lower ? bound : max(bound, least_key)) : least_key;
         const bool complete = from <= max(least_key, kNegInf + 1);
         const bool total = some && !by_k;
         const float floor = value_of(from);
-        const auto note = [&](float v, int token) {
-            const uint32_t at = atomicAdd(&sh.listed, 1u);
-            if (at < kList) sh.list[at] = (u64)~key_of(v) << 32 | (uint32_t)token;
-        };
         double sum = 0.0;
         if (total) {                                     // and the total, in fp32's precision
             const float c = scale * 1.44269504f;
-            for (int g = begin + (int)threadIdx.x; g < end; g += THREADS) {
-                float v[8], part = 0.f;
-                row.load(g, v);
+            s.each_granule([&](int g, const float (&v)[8]) {
+                float part = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     float e;
@@ -527,17 +920,14 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
                     part += e;
                 }
                 sum += part;
-                const float most = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
-                if (most >= floor) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (v[i] >= floor && v[i] > -INFINITY) note(v[i], g * 8 - row.skew + i);
-                }
-            }
+                if (s.most_of(v) >= floor) s.note(g, v, floor, best);
+            });
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
             if (lane == 0) sh.scan_f[warp] = sum;
-        } else s.each_from(floor, note);
+        } else s.each_granule([&](int g, const float (&v)[8]) {
+            if (s.most_of(v) >= floor) s.note(g, v, floor, best);
+        });
         __syncthreads();
         if (threadIdx.x == 0) {
             sum = 0.0;
@@ -549,17 +939,18 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
         Outcome outcome = kNeedAll;
         int n = 0;
         for (int o = 0; o < blocks; ++o) n += (int)min((uint32_t)kList + 1, blocks == 1 ? sh.listed : at_rank(&sh, o)->listed);
+        u64 low = 0, high = 0;
+        if (total) {
+            sum = 0.0;
+            for (int o = 0; o < blocks; ++o) sum += (blocks == 1 ? &sh : at_rank(&sh, o))->part.sum;
+            // An exponential is off by 2^-22, its argument t by 3 roundings, eight of them added by 7: (2^-22 + 2^-24 (2.1 |t| + 8)) w; and
+            // sum w |t| is at most sum w log2(vocab / sum w), as no distribution's entropy is above log2 vocab.
+            const double off = sum * 0x1p-24 * (14.0 + 2.1 * max(0.0, log2((double)a.vocab / sum))), unit = exp2((double)a.frac_bits);
+            low = (u64)((sum - off) * unit);
+            high = (u64)((sum + off) * unit) + (u64)a.vocab;
+            known_total = (u64)(sum * 0x1p30);
+        }
         if (n <= kList) {
-            u64 low = 0, high = 0;
-            if (total) {
-                sum = 0.0;
-                for (int o = 0; o < blocks; ++o) sum += (blocks == 1 ? &sh : at_rank(&sh, o))->part.sum;
-                // An exponential is off by 2^-22, its argument t by 3 roundings, eight of them added by 7: (2^-22 + 2^-24 (2.1 |t| + 8)) w; and
-                // sum w |t| is at most sum w log2(vocab / sum w), as no distribution's entropy is above log2 vocab.
-                const double off = sum * 0x1p-24 * (14.0 + 2.1 * max(0.0, log2((double)a.vocab / sum))), unit = exp2((double)a.frac_bits);
-                low = (u64)((sum - off) * unit);
-                high = (u64)((sum + off) * unit) + (u64)a.vocab;
-            }
             if (rank == 0) {
                 for (int o = 1, at = (int)sh.listed; o < blocks; ++o) {
                     const Shared<THREADS> *other = at_rank(&sh, o);
@@ -569,13 +960,18 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
                 }
                 __syncthreads();
                 outcome = s.from_list(a, r, n, complete, max(top_k, 0), top_p, low, high, least_key, u);
-                if (blocks > 1 && threadIdx.x == 0) sh.outcome = outcome;
             }
-            all_meet(blocks);
-            if (blocks > 1) {
-                outcome = (Outcome)at_rank(&sh, 0)->outcome;
+            const auto agree = [&] {                     // on rank 0's outcome
+                if (threadIdx.x == 0) {
+                    sh.outcome = outcome;
+                    sh.part.above = sh.sums[n - 1];
+                }
                 all_meet(blocks);
-            }
+                outcome = (blocks == 1 ? &sh : at_rank(&sh, 0))->outcome;
+                known_sum = (blocks == 1 ? &sh : at_rank(&sh, 0))->part.above >> (a.frac_bits - 30);
+                all_meet(blocks);
+            };
+            agree();
             if (outcome == kDone) return;
             if (outcome == kNeedTotal) {                 // (the list stays as it is: sorted, at rank 0)
                 u64 mass = 0;
@@ -588,68 +984,91 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
                     all = 0;
                     for (int o = 0; o < blocks; ++o) all += (blocks == 1 ? &sh : at_rank(&sh, o))->part.mass;
                     outcome = s.from_list(a, r, n, complete, 0, top_p, all, all, least_key, u);
-                    if (blocks > 1 && threadIdx.x == 0) sh.outcome = outcome;
                 }
-                all_meet(blocks);
-                if (blocks > 1) {
-                    outcome = (Outcome)at_rank(&sh, 0)->outcome;
-                    all_meet(blocks);
-                }
+                agree();
                 if (outcome == kDone) return;
+            }
+            if (total && outcome == kNeedAll) {
+                known = n;
+                known_key = from;
             }
         } else all_meet(blocks);                         // (the numbers listed are read)
     }
 
-    Cut cut{kNegInf, 0};
+    Cut cut{kNegInf, 0, false, 0};
     u64 goal;
-    if (top_k > 0 && top_k < a.vocab) {
+    bool summed = false;                                 // the segments' sums are there
+    const bool limited = top_k > 0 && top_k < a.vocab;
+    if (limited && top_p < 1.f) {
         Cut c;
-        if (s.template narrow<false>(kNegInf, [&](u64) { return (u64)top_k; }, &c, &goal)) cut = c;
+        if (s.template narrow<false>(kNegInf, [&](u64) { return (u64)top_k; }, &c, &goal)) cut = Cut{c.key, c.ties, false, 0};
     }
-    if (top_p < 1.f) {
-        const u64 tied = cut.ties ? s.weigh(value_of(cut.key)) : 0;
-        Cut c;
-        const bool inside = s.template narrow<true>(cut.key, [&](u64 total) { return max((u64)1, part_of(total + cut.ties * tied, top_p, true)); }, &c, &goal);
-        if (inside) cut = c;
-        else if (tied) cut.ties = (goal - sh.found.total + tied - 1) / tied;
+    if (limited || top_p < 1.f) {
+        const Settled settled = s.general(a.seg_steps, cut.key, cut.ties, limited ? top_k : 0, top_p, least_key, known, known_key, known ? known_sum : 0, known_total);
+        if (settled == kSums) {
+            cut = Cut{sh.choice.key, 0, true, sh.choice.last};
+            summed = true;
+        } else if (settled == kCutOnly) {
+            cut = Cut{sh.choice.key, sh.choice.ties, false, 0};
+        } else if (top_p < 1.f) {
+            const u64 tied = cut.ties ? s.weigh(value_of(cut.key)) : 0;
+            Cut c;
+            const bool inside = s.template narrow<true>(cut.key, [&](u64 total) { return max((u64)1, part_of(total + cut.ties * tied, top_p, true)); }, &c, &goal);
+            if (inside) cut = Cut{c.key, c.ties, false, 0};
+            else if (tied) cut.ties = (goal - sh.found.total + tied - 1) / tied;
+        } else {
+            Cut c;
+            if (s.template narrow<false>(kNegInf, [&](u64) { return (u64)top_k; }, &c, &goal)) cut = Cut{c.key, c.ties, false, 0};
+        }
     }
-    if (least_key > cut.key) cut = Cut{least_key - 1, 0};
+    if (least_key > cut.key) cut = Cut{least_key - 1, 0, false, 0};
 
     // Sums of the kept weights by segments of the row, in its order.
     const int segments = (end - begin + 32 * a.seg_steps - 1) / (32 * a.seg_steps);
-    __syncthreads();
     u64 mass = 0;
     uint32_t count = 0, ties = 0;
-    for (int g = warp; g < segments; g += THREADS / 32) {
-        u64 m = 0;
+    if (summed) {
+        for (int g = threadIdx.x; g < segments; g += THREADS) {
+            mass += sh.seg.mass[g];
+            sh.seg.ties[g] = 0;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
+    } else {
+        __syncthreads();
+        const float border = value_of(cut.key), weightless = fmaxf(border, s.weigh.least);
+        const u64 one = (u64)__double_as_longlong(s.weigh.one);
         uint32_t t = 0;
-        for (int i = 0; i < a.seg_steps; ++i) {
-            const int at = begin + (g * a.seg_steps + i) * 32 + lane;
-            if (at >= end) continue;
-            float v[8];
-            row.load(at, v);
+        s.each_segment(a.seg_steps, [&](int, int, const float (&v)[8], u64 &m) {
+            bool some = false;
+            if (cut.ties) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) t += v[k] == border;
+            }
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const uint32_t key = key_of(v[k]);
-                if (key > cut.key) {
-                    m += s.weigh(v[k]);
-                    ++count;
-                } else if (key == cut.key) ++t;
+                some |= v[k] > border;
+                count += v[k] > border;
             }
-        }
+            if (!__any_sync(0xffffffffu, some)) return;
+            u64 part = 0;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m += __shfl_xor_sync(0xffffffffu, m, o);
-        t = __reduce_add_sync(0xffffffffu, t);
-        if (lane == 0) {
-            sh.seg.mass[g] = m;
-            sh.seg.ties[g] = t;
-            mass += m;
-            ties += t;
-        }
+            for (int k = 0; k < 8; ++k) part += s.weigh.raw(v[k] > weightless ? v[k] : s.weigh.least);
+            m += part - 8 * one;
+        }, [&](int g, u64 m) {
+            const uint32_t equal = cut.ties ? __reduce_add_sync(0xffffffffu, t) : 0;
+            t = 0;
+            if (lane == 0) {
+                sh.seg.mass[g] = m;
+                sh.seg.ties[g] = equal;
+                mass += m;
+                ties += equal;
+            }
+        });
+        count = __reduce_add_sync(0xffffffffu, count);
     }
-    count = __reduce_add_sync(0xffffffffu, count);
     // the block's own sums
-    if (threadIdx.x == 0) sh.part = Part{best, 0, 0, 0};
+    if (threadIdx.x == 0) sh.part = Part{best, 0, 0.0, 0, 0, 0, 0};
     __syncthreads();
     if (lane == 0) {
         atomicAdd(&sh.part.mass, mass);
@@ -657,7 +1076,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
         atomicAdd(&sh.part.ties, ties);
     }
     all_meet(blocks);
-    const u64 tied = cut.ties ? s.weigh(value_of(cut.key)) : 0;
+    const u64 tied = cut.ties || cut.by_last ? s.weigh(value_of(cut.key)) : 0;
     const auto of_ties = [&](u64 before, uint32_t there) { return before >= cut.ties ? (u64)0 : min(cut.ties - before, (u64)there); };
     u64 total = 0, mass_before = 0, ties_before = 0, all_ties = 0, kept = 0, own = 0;
     for (int o = 0; o < blocks; ++o) {
@@ -668,6 +1087,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
         all_ties += p.ties;
         kept += p.count + taken;
     }
+    if (summed) kept = sh.choice.kept;
     const u64 target = min(part_of(total, u, false), total - 1);
     if (target >= mass_before && target - mass_before < own) {      // the token lies in this block's part
         constexpr int kPer = kSegments / THREADS;
@@ -720,7 +1140,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const uint32_t key = key_of(v[k]);
-                    w[k] = key > cut.key ? s.weigh(v[k]) : key == cut.key && at_tie++ < cut.ties ? tied : 0;
+                    w[k] = key > cut.key ? s.weigh(v[k]) : key == cut.key && (cut.by_last ? (uint32_t)(row.first(at) + k) <= cut.last : at_tie++ < cut.ties) ? tied : 0;
                     sum += w[k];
                 }
                 u64 sums = sum;
@@ -734,7 +1154,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, 10
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         if (rest >= before_lane && rest - before_lane < w[k]) {
-                            a.token[r] = at * 8 - row.skew + k;
+                            a.token[r] = (int32_t)(row.first(at) + k);
                             if (a.logprob) a.logprob[r] = (float)(((double)v[k] - best) * scale - log((double)total * exp2(-(double)a.frac_bits)));
                         }
                         before_lane += w[k];
