@@ -66,7 +66,7 @@ __device__ __forceinline__ u64 part_of(u64 total, float f, bool up) {
 struct Weigher {                                         // w(x) = exp(scale (x - best)) as a whole number of 2^-frac_bits
     double best, c, one;                                 // c: 32 scale log2 e; one: whose last bit is 2^-frac_bits
     float least;                                         // it and all logits below weigh nothing
-    const double *table;                                 // 2^(i / 32), in shared memory
+    const double *table;                                 // 2^(i / 32), in shared memory; less i 2^15 in the upper word, which n 2^15 adds
     __device__ __forceinline__ void set(float best_, float scale, int frac_bits, const double *table_) {
         best = best_;
         table = table_;
@@ -75,21 +75,21 @@ struct Weigher {                                         // w(x) = exp(scale (x 
         least = fminf(best_ - 45.f / scale, value_of(key_of(best_) - 1));
         c = fmin(32.0 * 1.44269504088896340736 * scale, 4096.0 / (best - (double)least));
     }
-    // 2^(n / 32) from the table, e^y of the rest, |y| <= ln 2 / 64 = h, by Taylor's polynomial of degree 5 whose last term is spread over y and y^3
+    // 2^(n / 32) from the table and its exponent, e^y of the rest, |y| <= ln 2 / 64 = h, by Taylor's polynomial of degree 5 whose last term is spread over y and y^3
     // (Chebyshev's economisation: 16 z^5 - 20 z^3 + 5 z is at most 1): off by h^5 / 1920 = 8 10^-14.  Nine operations in fp64.
     // raw(): of x >= least, with the bits of `one` still on it
     __device__ __forceinline__ u64 raw(float x) const {
         constexpr double y = 0.69314718055994530942 / 32, h = y / 2;
         const double d = (double)x - best;
         const double shifted = fma(d, c, 6755399441055744.0);      // 1.5 2^52: rounds to a whole number
-        const int n = __double2loint(shifted);
+        const int n8 = __double2loint(shifted) << 3;
         const double r = fma(d, c, 6755399441055744.0 - shifted);
         double p = fma(r, y * y * y * y / 24, y * y * y * (1.0 / 6 + h * h / 96));
         p = fma(p, r, y * y / 2);
         p = fma(p, r, y * (1.0 - h * h * h * h / 384));
         p = fma(p, r, 1.0);
-        const double power = table[n & 31];
-        p = fma(p, __hiloint2double(__double2hiint(power) + ((n >> 5) << 20), __double2loint(power)), one);
+        const double power = *reinterpret_cast<const double *>(reinterpret_cast<const char *>(table) + (n8 & 0xf8));
+        p = fma(p, __hiloint2double(__double2hiint(power) + (n8 << 12), __double2loint(power)), one);
         return (u64)__double_as_longlong(p);
     }
     __device__ __forceinline__ u64 operator()(float x) const { return raw(fmaxf(x, least)) - (u64)__double_as_longlong(one); }
@@ -177,14 +177,14 @@ enum Settled { kNot, kSums, kCutOnly };                  // a border was not fou
 
 template <int THREADS> struct Shared {
     double table[32];
-    union {
+    union alignas(16) {
         uint32_t hist[2][kBins];
         struct {
             u64 mass[kSegments];
             uint32_t ties[kSegments];
         } seg;
     };
-    u64 list[kList];                                     // ~key << 32 | token
+    alignas(16) u64 list[kList];                                     // ~key << 32 | token
     u64 weight[kList];
     u64 sums[kList];
     u64 scan[THREADS / 32];
@@ -259,10 +259,39 @@ template <typename T, int THREADS> struct Sampler {
 
     __device__ __forceinline__ int step_of(float x) const { return min(kBins - 1, (int)((best - x) * scale * 32.f)); }
 
+    __device__ __forceinline__ Shared<THREADS> *block(int o) const { return blocks == 1 ? &sh : at_rank(&sh, o); }
+    // f(o, value(block o)) for the row's blocks: a word of another block's shared memory takes some 200 ns, so all are fetched first.
+    template <class V, class F> __device__ __forceinline__ void of_blocks(V value, F f) const {
+        typedef decltype(value(sh)) W;
+        if (blocks == 1) {
+            f(0, value(sh));
+            return;
+        }
+        W w[8];
+#pragma unroll
+        for (int o = 0; o < 8; ++o)
+            if (o < blocks) w[o] = value(*at_rank(&sh, o));
+#pragma unroll
+        for (int o = 0; o < 8; ++o)
+            if (o < blocks) f(o, w[o]);
+    }
+    // f(o, i, words) for four words after another of an array in the blocks' shared memory, the thread's N x 4 ones.
+    template <int N, class A, class F> __device__ __forceinline__ void of_arrays(A array, F f) const {
+#pragma unroll 2
+        for (int o = 0; o < blocks; ++o) {
+            const uint4 *const from = reinterpret_cast<const uint4 *>(array(*block(o))) + threadIdx.x * N;
+            uint4 w[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = from[i];
+#pragma unroll
+            for (int i = 0; i < N; ++i) f(i, w[i]);
+        }
+    }
+
     // f(granule, logits) for each granule of the block's part, some in flight.
-    template <class F> __device__ __forceinline__ void each_granule(F f) const {
+    template <class F> __device__ __forceinline__ void each_granule(F f, int first = 0) const {
         constexpr int kFlight = sizeof(T) == 2 ? 4 : 2;
-        for (int g = begin + (int)threadIdx.x; g < end; g += THREADS * kFlight) {
+        for (int g = begin + first + (int)threadIdx.x; g < end; g += THREADS * kFlight) {
             Pack8<T> p[kFlight];
 #pragma unroll
             for (int i = 0; i < kFlight; ++i) p[i] = row.fetch(g + i * THREADS, end);
@@ -281,26 +310,86 @@ template <typename T, int THREADS> struct Sampler {
             for (int i = 0; i < 8; ++i) f(v[i]);
         });
     }
-    __device__ __forceinline__ float largest_logit() const {
+    // The first granules of a thread stay in registers.
+    static constexpr int kHeld = sizeof(T) == 2 ? 4 : 2;
+    __device__ __forceinline__ void fetch_first(Pack8<T> (&held)[kHeld]) const {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) held[i] = row.fetch(begin + (int)threadIdx.x + i * THREADS, end);
+    }
+    template <class F> __device__ __forceinline__ void each_held(const Pack8<T> (&held)[kHeld], F f) const {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int g = begin + (int)threadIdx.x + i * THREADS;
+            if (g >= end) break;
+            float v[8];
+            row.get(held[i], g, v);
+            f(g, v);
+        }
+    }
+    __device__ __forceinline__ float largest_of(const Pack8<T> (&p)[kHeld], int g) const {
         float mine = -INFINITY;
         Largest<T> most;
-        constexpr int kFlight = 4;
-        for (int g = begin + (int)threadIdx.x; g < end; g += THREADS * kFlight) {
-            Pack8<T> p[kFlight];
 #pragma unroll
-            for (int i = 0; i < kFlight; ++i) p[i] = row.fetch(g + i * THREADS, end);
-#pragma unroll
-            for (int i = 0; i < kFlight; ++i) {
-                if (g + i * THREADS >= end) break;
-                if (row.whole(g + i * THREADS)) most.take(p[i]);
-                else {
+        for (int i = 0; i < kHeld; ++i) {
+            if (g + i * THREADS >= end) break;
+            if (row.whole(g + i * THREADS)) most.take(p[i]);
+            else {
 #pragma unroll 1
-                    for (int k = 0; k < 8; ++k) mine = largest(mine, row.at(row.first(g + i * THREADS) + k));
-                }
+                for (int k = 0; k < 8; ++k) mine = largest(mine, row.at(row.first(g + i * THREADS) + k));
             }
         }
         return largest(mine, most.get());
     }
+    __device__ __forceinline__ float largest_of_rest() const {
+        float mine = -INFINITY;
+        for (int g = begin + kHeld * THREADS + (int)threadIdx.x; g < end; g += THREADS * kHeld) {
+            Pack8<T> p[kHeld];
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) p[i] = row.fetch(g + i * THREADS, end);
+            mine = largest(mine, largest_of(p, g));
+        }
+        return mine;
+    }
+    // The row's largest logit, from the threads'.
+    __device__ __forceinline__ float all_largest(float mine) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) mine = largest(mine, __shfl_xor_sync(0xffffffffu, mine, o));
+        __syncthreads();
+        if (threadIdx.x % 32 == 0) sh.maxima[threadIdx.x / 32] = mine;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < THREADS / 32; ++w) mine = largest(mine, sh.maxima[w]);
+        if (blocks > 1) {
+            if (threadIdx.x == 0) sh.part.best = mine;
+            all_meet(blocks);
+            of_blocks([](const Shared<THREADS> &b) { return b.part.best; }, [&](int, float v) { mine = largest(mine, v); });
+            all_meet(blocks);                            // (nobody leaves while its word is read)
+        }
+        return mine;
+    }
+    // The least key that min_p leaves, if `top` is the largest logit.
+    __device__ __forceinline__ uint32_t least_of(float top, float min_p) const {
+        if (!(min_p > 0.f)) return 0;
+        const double low = (double)top + log((double)fminf(min_p, 1.f)) / scale;
+        float f = (float)low;
+        if ((double)f < low) f = value_of(key_of(f) + 1);
+        return max(key_of(f), kNegInf + 1);
+    }
+    // Of a granule: its logits in [low, inf) are listed; returns the sum of the weights, relative to `top`, in fp32's precision.
+    __device__ __forceinline__ float list_and_sum(int g, const float (&v)[8], float low, bool sum, float top, float c) {
+        float part = 0.f;
+        if (sum) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float e;
+                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"((v[i] - top) * c));
+                part += e;
+            }
+        }
+        if (most_of(v) >= low) note(g, v, low, INFINITY);
+        return part;
+    }
+
     // f(segment, granule, logits, sum) for the granules of each segment, a warp's granules side by side and the whole warp in each call (behind the
     // part's end with logits of -inf); then done(segment, sum of the lanes' sums).
     template <class F, class G> __device__ __forceinline__ void each_segment(int seg_steps, F f, G done) const {
@@ -356,18 +445,17 @@ template <typename T, int THREADS> struct Sampler {
     // The first bin at which `above` and the bins up to it, of all blocks, reach the target; target(total) may depend on the total.  -1 if none does.
     template <bool MASS, class F> __device__ __forceinline__ void find(u64 above, F target) {
         all_meet(blocks);
-        u64 bin[kPer], sum = 0;
+        u64 bin[kPer] = {}, sum = 0;
+        const auto put = [&](int i, const uint4 &w, int shift) {
+            bin[4 * i] += (u64)w.x << shift;
+            bin[4 * i + 1] += (u64)w.y << shift;
+            bin[4 * i + 2] += (u64)w.z << shift;
+            bin[4 * i + 3] += (u64)w.w << shift;
+        };
+        of_arrays<kPer / 4>([](const Shared<THREADS> &b) { return b.hist[0]; }, [&](int i, const uint4 &w) { put(i, w, 0); });
+        if (MASS) of_arrays<kPer / 4>([](const Shared<THREADS> &b) { return b.hist[1]; }, [&](int i, const uint4 &w) { put(i, w, 32); });
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int b = threadIdx.x * kPer + i;
-            u64 s = 0;
-            for (int r = 0; r < blocks; ++r) {
-                const Shared<THREADS> *other = blocks == 1 ? &sh : at_rank(&sh, r);
-                s += other->hist[0][b];
-                if (MASS) s += (u64)other->hist[1][b] << 32;
-            }
-            sum += bin[i] = s;
-        }
+        for (int i = 0; i < kPer; ++i) sum += bin[i];
         if (threadIdx.x == 0) sh.found.bin = -1;
         u64 total;
         u64 before = above + block_scan<THREADS>(sum, sh.scan, &total);
@@ -448,24 +536,76 @@ template <typename T, int THREADS> struct Sampler {
         return low;
     }
 
-    // Sorts list[0 .. n), in steps of neighbours, squares and halves (Batcher's bitonic sort).
-    __device__ __forceinline__ void sort(int n) {
-        int size = 2;
-        while (size < n) size *= 2;
-        for (int i = n + (int)threadIdx.x; i < size; i += THREADS) sh.list[i] = ~0ull;
-        for (int run = 2; run <= size; run *= 2)
-            for (int apart = run / 2; apart > 0; apart /= 2) {
-                __syncthreads();
-                for (int p = threadIdx.x; p < size / 2; p += THREADS) {
-                    const int i = 2 * p - (p & (apart - 1)), j = i + apart;
-                    const u64 x = sh.list[i], y = sh.list[j];
-                    if ((x > y) == ((i & run) == 0)) {
-                        sh.list[i] = y;
-                        sh.list[j] = x;
+    // The blocks' lists, one behind the other, in the first one's; their length.
+    __device__ __forceinline__ int merge() {
+        int n = 0, first[8] = {}, there[8] = {};
+        of_blocks([](const Shared<THREADS> &b) { return b.listed; }, [&](int o, uint32_t count) {
+            first[o] = n;
+            there[o] = (int)count;
+            n += (int)count;
+        });
+        if (blocks > 1) {
+            // an entry a thread, so that all are fetched at once
+            for (int i = threadIdx.x; i < n; i += THREADS) {
+                int o = 0, at = i;
+#pragma unroll
+                for (int k = 1; k < 8; ++k)
+                    if (k < blocks && i >= first[k]) {
+                        o = k;
+                        at = i - first[k];
                     }
+                if (o) sh.list[i] = at_rank(&sh, o)->list[at];
+            }
+        }
+        __syncthreads();
+        return n;
+    }
+
+    // Sorts list[0 .. n), all different: runs of 32 by a warp each (Batcher's bitonic sort, between lanes), then each entry's place is the sum of its
+    // places in all runs, found by halving.  (Barriers between all the steps of one bitonic sort took five times as long: 11000 cycles for 100 entries.)
+    __device__ __forceinline__ void sort(int n) {
+        constexpr int kEach = kList / THREADS;
+        const int lane = threadIdx.x % 32, runs = (n + 31) / 32;
+        __syncthreads();
+        for (int run = threadIdx.x / 32; run < runs; run += THREADS / 32) {
+            const int i = run * 32 + lane;
+            u64 x = i < n ? sh.list[i] : ~0ull;
+#pragma unroll
+            for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+                for (int apart = size / 2; apart > 0; apart /= 2) {
+                    const u64 y = __shfl_xor_sync(0xffffffffu, x, apart);
+                    const bool lower = (lane & apart) == 0, rising = (lane & size) == 0;
+                    x = (x < y) == (lower == rising) ? x : y;
+                }
+            sh.list[i] = x;
+        }
+        __syncthreads();
+        if (runs > 1) {
+            u64 mine[kEach];
+            int place[kEach];
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) {
+                const int i = k * THREADS + (int)threadIdx.x;
+                if (i >= n) break;
+                mine[k] = sh.list[i];
+                place[k] = i % 32;
+#pragma unroll 4
+                for (int run = 0; run < runs; ++run) {
+                    if (run == i / 32) continue;
+                    const u64 *const other = sh.list + run * 32;
+                    int below = 0;
+#pragma unroll
+                    for (int step = 16; step > 0; step /= 2) below += other[below + step - 1] < mine[k] ? step : 0;
+                    place[k] += below + (other[below] < mine[k] ? 1 : 0);
                 }
             }
-        __syncthreads();
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < kEach; ++k)
+                if (k * THREADS + (int)threadIdx.x < n) sh.list[place[k]] = mine[k];
+            __syncthreads();
+        }
     }
 
     // sums[i] = value(0) + .. + value(i), i < n.
@@ -599,22 +739,25 @@ template <typename T, int THREADS> struct Sampler {
             sh.found.bin = -1;
         }
         all_meet(blocks);
-        uint32_t n[2 * kPer];
-        float place[2 * kPer];
+        uint32_t n[2 * kPer] = {}, samples[2 * kPer] = {};
+        float place[2 * kPer] = {};
         u64 sum = 0, count;
+        of_arrays<kPer / 2>([](const Shared<THREADS> &b) { return b.hist[0]; }, [&](int i, const uint4 &w) {
+            n[4 * i] += w.x; n[4 * i + 1] += w.y; n[4 * i + 2] += w.z; n[4 * i + 3] += w.w;
+        });
+        if (top_p < 1.f) {
+            of_arrays<kPer / 2>([](const Shared<THREADS> &b) { return b.weight; }, [&](int i, const uint4 &w) {
+                const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    place[4 * i + k] += q[k] & 0xfffffu;
+                    samples[4 * i + k] += q[k] >> 20;
+                }
+            });
+        }
 #pragma unroll
         for (int i = 0; i < 2 * kPer; ++i) {
-            const int b = threadIdx.x * 2 * kPer + i;
-            uint32_t p = 0, samples = 0;
-            n[i] = 0;
-            for (int o = 0; o < blocks; ++o) {
-                const Shared<THREADS> *other = blocks == 1 ? &sh : at_rank(&sh, o);
-                n[i] += (&other->hist[0][0])[b];
-                const uint32_t q = reinterpret_cast<const uint32_t *>(other->weight)[b];
-                p += q & 0xfffffu;
-                samples += q >> 20;
-            }
-            place[i] = samples ? fminf(p / (256.f * samples), 1.f) : 0.5f;
+            place[i] = samples[i] ? fminf(place[i] / (256.f * samples[i]), 1.f) : 0.5f;
             sum += n[i];
         }
         const u64 before = known + block_scan<THREADS>(sum, sh.scan, &count);
@@ -745,21 +888,11 @@ template <typename T, int THREADS> struct Sampler {
         if (rank == 0) {
             total = above = 0;
             int listed = 0;
-            for (int o = 0; o < blocks; ++o) {
-                const Shared<THREADS> *other = blocks == 1 ? &sh : at_rank(&sh, o);
-                total += other->part.mass;
-                above += other->part.above;
-                listed += (int)min(other->listed, (uint32_t)kList + 1);
-            }
+            of_blocks([](const Shared<THREADS> &b) { return b.part.mass; }, [&](int, u64 m) { total += m; });
+            of_blocks([](const Shared<THREADS> &b) { return b.part.above; }, [&](int, u64 m) { above += m; });
+            of_blocks([](const Shared<THREADS> &b) { return b.listed; }, [&](int o, uint32_t n) { listed += (int)min(n, (uint32_t)kList + 1); });
             const bool fits = listed <= kList;
-            for (int o = 1; fits && o < blocks; ++o) {
-                const Shared<THREADS> *other = at_rank(&sh, o);
-                const int there = (int)other->listed;
-                for (int i = threadIdx.x; i < there; i += THREADS) sh.list[n_list + i] = other->list[i];
-                n_list += there;
-            }
-            if (!fits) n_list = 0;
-            __syncthreads();
+            n_list = fits ? merge() : 0;
             sort(n_list);
             for (int i = threadIdx.x; i < n_list; i += THREADS) sh.weight[i] = weigh(value_of(~(uint32_t)(sh.list[i] >> 32)));
             running(n_list, [&](int i) { return sh.weight[i]; });
@@ -825,180 +958,215 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
     Row<T> row{x, a.vocab, (int)(reinterpret_cast<uintptr_t>(x) % 16 / sizeof(T)), false};
     const int all = (a.vocab + row.skew + 7) / 8, begin = min(all, rank * a.granules), end = min(all, begin + a.granules);
     const float scale = a.scales ? a.scales[r] : a.scale, top_p = a.top_ps ? a.top_ps[r] : a.top_p, min_p = a.min_ps ? a.min_ps[r] : a.min_p, u = a.u[r];
-    const int top_k = a.top_ks ? a.top_ks[r] : a.top_k;
+    int top_k = a.top_ks ? a.top_ks[r] : a.top_k;
+    if (top_k >= a.vocab) top_k = 0;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    if (threadIdx.x < 32) sh.table[threadIdx.x] = exp2((double)threadIdx.x / 32);
+    if (threadIdx.x < 32) {
+        const double power = exp2((double)threadIdx.x / 32);
+        sh.table[threadIdx.x] = __hiloint2double(__double2hiint(power) - ((int)threadIdx.x << 15), __double2loint(power));
+    }
 
     Sampler<T, THREADS> s{sh, row, blocks, rank, begin, end, scale, -INFINITY, {}};
-    float mine = s.largest_logit();
-    float best = mine, least = mine;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        best = largest(best, __shfl_xor_sync(0xffffffffu, best, o));
-        least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
-    }
-    if (lane == 0) {
-        sh.maxima[warp] = best;
-        sh.minima[warp] = least;
-    }
+    // The first granules of each thread: the largest of their logits serves as a first guess.  The largest logits are listed where they may be all
+    // that is kept: as many as top_k, or some for top_p to be reached by; how large they have to be, the threads' largest ones of the first granules
+    // tell (each block its share of them), so that one pass over the row finds them; three standard deviations more of them, where the first
+    // granules are not all.
+    Pack8<T> held[s.kHeld];
+    s.fetch_first(held);
     if (threadIdx.x == 0) sh.listed = 0;
-    __syncthreads();
-    for (int w = 0; w < THREADS / 32; ++w) {
-        best = largest(best, sh.maxima[w]);
-        least = fminf(least, sh.minima[w]);
-    }
-    // The largest logits are listed where they may be all that is kept: as many as top_k, or some for top_p to be reached by.  Of several blocks
-    // each finds its share of them; or all of them, where one has not that many logits.
-    const bool by_k = top_k > 0 && top_k <= THREADS / 2, some = by_k || (top_k <= 0 && top_p < 1.f);
-    const int wanted = by_k ? top_k : THREADS / 2;
+    float mine = s.largest_of(held, begin + (int)threadIdx.x);
+    const bool rest = a.granules > s.kHeld * THREADS, limited = top_k > 0;
+    const bool by_k = top_k > 0 && top_k <= THREADS / 2, some = by_k || (top_k <= 0 && top_p < 1.f), unlimited = !limited && top_p >= 1.f && !(min_p > 0.f);
+    const int share = ((by_k ? top_k : THREADS / 2) + blocks - 1) / blocks;
+    float guess;
     uint32_t bound = kNegInf + 1;
-    if (some && fabsf(best) < INFINITY) bound = s.bound(mine, least, best, (wanted + blocks - 1) / blocks);
+    {
+        float most = mine, least = mine;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            most = largest(most, __shfl_xor_sync(0xffffffffu, most, o));
+            least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
+        }
+        if (lane == 0) {
+            sh.maxima[warp] = most;
+            sh.minima[warp] = least;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < THREADS / 32; ++w) {
+            most = largest(most, sh.maxima[w]);
+            least = fminf(least, sh.minima[w]);
+        }
+        if (some && fabsf(most) < INFINITY) {
+            const float expected = share * min(1.f, (float)(s.kHeld * THREADS) / a.granules);
+            bound = s.bound(mine, least, most, rest ? min(share, (int)(expected + 3.f * sqrtf(expected)) + 2) : share);
+        }
+        guess = most;
+    }
     if (blocks > 1) {
         if (threadIdx.x == 0) {
-            sh.part.best = best;
+            sh.part.best = guess;
             sh.part.bound = bound;
         }
         all_meet(blocks);
-        const float own_best = best;
-        for (int o = 0; o < blocks; ++o) {
-            best = largest(best, at_rank(&sh, o)->part.best);
-            bound = min(bound, at_rank(&sh, o)->part.bound);
-        }
-        all_meet(blocks);                                // (nobody leaves while its word is read)
-        if (some && bound == kNegInf + 1 && fabsf(best) < INFINITY) {
-            bound = s.bound(mine, least, own_best, wanted);
-            if (threadIdx.x == 0) sh.part.bound = bound;
-            all_meet(blocks);
-            for (int o = 0; o < blocks; ++o) bound = max(bound, at_rank(&sh, o)->part.bound);
-            all_meet(blocks);
-        }
+        s.of_blocks([](const Shared<THREADS> &b) { return make_uint2(__float_as_uint(b.part.best), b.part.bound); }, [&](int, uint2 w) {
+            guess = largest(guess, __uint_as_float(w.x));
+            bound = min(bound, w.y);
+        });
+        all_meet(blocks);                                // (nobody leaves while its words are read)
     }
+    const float lowest = -3.402823466e38f;
+    const bool lists = some || (min_p > 0.f && top_p >= 1.f), summing = top_k <= 0 && top_p < 1.f, blind = !(guess > lowest && guess < INFINITY);
+    const bool lower = by_k && top_p < 1.f;              // top_k's weights are all needed for top_p
+    uint32_t from = 0;
+    const auto list_from = [&](uint32_t least_key) { from = some ? (lower ? bound : max(bound, least_key)) : least_key; };
+    const float log2_scale = scale * 1.44269504f;
+    double sum = 0.0;
+    if (lists && !blind) {
+        list_from(s.least_of(guess, min_p));
+        const float floor = value_of(from);
+        s.each_held(held, [&](int g, const float (&v)[8]) { sum += s.list_and_sum(g, v, floor, summing, guess, log2_scale); });
+        s.each_granule([&](int g, const float (&v)[8]) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mine = largest(mine, v[i]);
+            sum += s.list_and_sum(g, v, floor, summing, guess, log2_scale);
+        }, s.kHeld * THREADS);
+    } else if (rest && (!unlimited || blind)) mine = largest(mine, s.largest_of_rest());
+    // (An unlimited row's other logits are read once, for their weights relative to the guess, see below.)
+    float best = rest && (!unlimited || blind) ? s.all_largest(mine) : guess;
     const bool valid = scale >= 1e-6f && scale <= 1e6f && top_p == top_p && min_p == min_p && u >= 0.f && u < 1.f;
-    if (!valid || !(fabsf(best) < INFINITY)) {
+    const auto no_answer = [&] {
         if (rank == 0 && threadIdx.x == 0) {
             a.token[r] = PARLE_NO_TOKEN;
             if (a.logprob) a.logprob[r] = valid && best == -INFINITY ? -INFINITY : NAN;
             if (a.kept) a.kept[r] = 0;
             if (!valid && a.flags) atomicOr(a.flags, PARLE_FLAG_BAD_SAMPLING);
         }
-        return;
-    }
-    if (best == -3.402823466e38f) {
+    };
+    if (!valid || !(fabsf(best) < INFINITY)) return no_answer();
+    if (best == lowest) {
         s.row.flat = row.flat = true;
-        bound = kNegInf + 1;
         best = 0.f;
     }
     s.best = best;
     s.weigh.set(best, scale, a.frac_bits, sh.table);
-
-    uint32_t least_key = 0;                              // of min_p
-    if (min_p > 0.f) {
-        const double low = (double)best + log((double)fminf(min_p, 1.f)) / scale;
-        float f = (float)low;
-        if ((double)f < low) f = value_of(key_of(f) + 1);
-        least_key = max(key_of(f), kNegInf + 1);
-    }
+    const uint32_t least_key = s.least_of(best, min_p);
 
     int known = 0;                                       // logits from known_key on, listed
     uint32_t known_key = 0;
     u64 known_sum = 0, known_total = 0;                  // of weights, in units of 2^-30; 0: not known
-    if (some || (least_key && top_p >= 1.f)) {
-        const bool lower = by_k && top_p < 1.f;          // top_k's weights are all needed for top_p
-        const uint32_t from = some ? (lower ? bound : max(bound, least_key)) : least_key;
-        const bool complete = from <= max(least_key, kNegInf + 1);
-        const bool total = some && !by_k;
-        const float floor = value_of(from);
-        double sum = 0.0;
-        if (total) {                                     // and the total, in fp32's precision
-            const float c = scale * 1.44269504f;
-            s.each_granule([&](int g, const float (&v)[8]) {
-                float part = 0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float e;
-                    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"((v[i] - best) * c));
-                    part += e;
+    for (int attempt = blind ? 1 : 0; lists && attempt < 2; ++attempt) {
+        float top = guess;                               // the weights summed are relative to it
+        if (attempt == 1) {                              // all logits are looked at for the bound
+            bound = kNegInf + 1;
+            if (some) {
+                if (row.flat) mine = mine > -INFINITY ? 0.f : mine;
+                bound = s.bound(mine, lowest, best, share);
+                if (blocks > 1) {                        // each block its share, or one of them all, where another has not that many logits
+                    const uint32_t all = s.bound(mine, lowest, best, share * blocks);
+                    if (threadIdx.x == 0) {
+                        sh.part.bound = bound;
+                        sh.part.count = all;
+                    }
+                    all_meet(blocks);
+                    uint32_t one = 0;
+                    s.of_blocks([](const Shared<THREADS> &b) { return make_uint2(b.part.bound, b.part.count); }, [&](int, uint2 w) {
+                        bound = min(bound, w.x);
+                        one = max(one, w.y);
+                    });
+                    bound = max(bound, one);
                 }
-                sum += part;
-                if (s.most_of(v) >= floor) s.note(g, v, floor, best);
-            });
+            }
+            list_from(least_key);
+            __syncthreads();
+            if (threadIdx.x == 0) sh.listed = 0;
+            all_meet(blocks);
+            top = best;
+            sum = 0.0;
+            const float floor = value_of(from);
+            s.each_granule([&](int g, const float (&v)[8]) { sum += s.list_and_sum(g, v, floor, summing, best, log2_scale); });
+        }
+        if (summing) {
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            __syncthreads();
             if (lane == 0) sh.scan_f[warp] = sum;
-        } else s.each_granule([&](int g, const float (&v)[8]) {
-            if (s.most_of(v) >= floor) s.note(g, v, floor, best);
-        });
+        }
         __syncthreads();
         if (threadIdx.x == 0) {
             sum = 0.0;
-            if (total)
+            if (summing)
                 for (int w = 0; w < THREADS / 32; ++w) sum += sh.scan_f[w];
             sh.part.sum = sum;
         }
         all_meet(blocks);
-        Outcome outcome = kNeedAll;
+        const bool complete = from <= max(least_key, kNegInf + 1);
         int n = 0;
-        for (int o = 0; o < blocks; ++o) n += (int)min((uint32_t)kList + 1, blocks == 1 ? sh.listed : at_rank(&sh, o)->listed);
+        s.of_blocks([](const Shared<THREADS> &b) { return b.listed; }, [&](int, uint32_t k) { n += (int)min((uint32_t)kList + 1, k); });
         u64 low = 0, high = 0;
-        if (total) {
+        bool fits = n <= kList && !(by_k && n < top_k && !complete);
+        if (summing) {
             sum = 0.0;
-            for (int o = 0; o < blocks; ++o) sum += (blocks == 1 ? &sh : at_rank(&sh, o))->part.sum;
-            // An exponential is off by 2^-22, its argument t by 3 roundings, eight of them added by 7: (2^-22 + 2^-24 (2.1 |t| + 8)) w; and
-            // sum w |t| is at most sum w log2(vocab / sum w), as no distribution's entropy is above log2 vocab.
-            const double off = sum * 0x1p-24 * (14.0 + 2.1 * max(0.0, log2((double)a.vocab / sum))), unit = exp2((double)a.frac_bits);
-            low = (u64)((sum - off) * unit);
-            high = (u64)((sum + off) * unit) + (u64)a.vocab;
-            known_total = (u64)(sum * 0x1p30);
-        }
-        if (n <= kList) {
-            if (rank == 0) {
-                for (int o = 1, at = (int)sh.listed; o < blocks; ++o) {
-                    const Shared<THREADS> *other = at_rank(&sh, o);
-                    const int there = (int)other->listed;
-                    for (int i = threadIdx.x; i < there; i += THREADS) sh.list[at + i] = other->list[i];
-                    at += there;
-                }
-                __syncthreads();
-                outcome = s.from_list(a, r, n, complete, max(top_k, 0), top_p, low, high, least_key, u);
+            s.of_blocks([](const Shared<THREADS> &b) { return b.part.sum; }, [&](int, double p) { sum += p; });
+            const double off_by = ((double)best - top) * log2_scale;
+            if (!(sum < 1e30) || off_by > 60.0) fits = false;
+            else {
+                // An exponential is off by 2^-22, its argument t by 3 roundings, eight of them added by 7: (2^-22 + 2^-24 (2.1 |t| + 8)) w; and
+                // sum w |t|, t relative to the largest logit, is at most sum w log2(vocab / sum w), as no distribution's entropy is above log2 vocab.
+                sum *= exp2(-off_by);
+                const double off = sum * 0x1p-24 * (14.0 + 2.1 * (max(0.0, log2((double)a.vocab / sum)) + off_by)), unit = exp2((double)a.frac_bits);
+                low = (u64)((sum - off) * unit);
+                high = (u64)((sum + off) * unit) + (u64)a.vocab;
+                known_total = (u64)(sum * 0x1p30);
             }
-            const auto agree = [&] {                     // on rank 0's outcome
-                if (threadIdx.x == 0) {
-                    sh.outcome = outcome;
-                    sh.part.above = sh.sums[n - 1];
-                }
-                all_meet(blocks);
-                outcome = (blocks == 1 ? &sh : at_rank(&sh, 0))->outcome;
-                known_sum = (blocks == 1 ? &sh : at_rank(&sh, 0))->part.above >> (a.frac_bits - 30);
-                all_meet(blocks);
-            };
+        }
+        if (!fits) {
+            all_meet(blocks);                            // (the blocks' numbers are read)
+            if (!rest) break;                            // (the bound was that of all logits)
+            continue;
+        }
+        Outcome outcome = kNeedAll;
+        if (rank == 0) {
+            s.merge();
+            outcome = s.from_list(a, r, n, complete, max(top_k, 0), top_p, low, high, least_key, u);
+        }
+        const auto agree = [&] {                         // on rank 0's outcome
+            if (threadIdx.x == 0) {
+                sh.outcome = outcome;
+                sh.part.above = sh.sums[n - 1];
+            }
+            all_meet(blocks);
+            outcome = s.block(0)->outcome;
+            known_sum = s.block(0)->part.above >> (a.frac_bits - 30);
+            all_meet(blocks);
+        };
+        agree();
+        if (outcome == kDone) return;
+        if (outcome == kNeedTotal) {                     // (the list stays as it is: sorted, at rank 0)
+            u64 mass = 0;
+            s.each([&](float v) { mass += s.weigh(v); });
+            u64 all;
+            block_scan<THREADS>(mass, sh.scan, &all);
+            if (threadIdx.x == 0) sh.part.mass = all;
+            all_meet(blocks);
+            if (rank == 0) {
+                all = 0;
+                s.of_blocks([](const Shared<THREADS> &b) { return b.part.mass; }, [&](int, u64 m) { all += m; });
+                outcome = s.from_list(a, r, n, complete, 0, top_p, all, all, least_key, u);
+            }
             agree();
             if (outcome == kDone) return;
-            if (outcome == kNeedTotal) {                 // (the list stays as it is: sorted, at rank 0)
-                u64 mass = 0;
-                s.each([&](float v) { mass += s.weigh(v); });
-                u64 all;
-                block_scan<THREADS>(mass, sh.scan, &all);
-                if (threadIdx.x == 0) sh.part.mass = all;
-                all_meet(blocks);
-                if (rank == 0) {
-                    all = 0;
-                    for (int o = 0; o < blocks; ++o) all += (blocks == 1 ? &sh : at_rank(&sh, o))->part.mass;
-                    outcome = s.from_list(a, r, n, complete, 0, top_p, all, all, least_key, u);
-                }
-                agree();
-                if (outcome == kDone) return;
-            }
-            if (total && outcome == kNeedAll) {
-                known = n;
-                known_key = from;
-            }
-        } else all_meet(blocks);                         // (the numbers listed are read)
+        }
+        if (summing) {
+            known = n;
+            known_key = from;
+        }
+        break;
     }
 
     Cut cut{kNegInf, 0, false, 0};
     u64 goal;
     bool summed = false;                                 // the segments' sums are there
-    const bool limited = top_k > 0 && top_k < a.vocab;
     if (limited && top_p < 1.f) {
         Cut c;
         if (s.template narrow<false>(kNegInf, [&](u64) { return (u64)top_k; }, &c, &goal)) cut = Cut{c.key, c.ties, false, 0};
@@ -1036,35 +1204,82 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
         for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
     } else {
         __syncthreads();
-        const float border = value_of(cut.key), weightless = fmaxf(border, s.weigh.least);
         const u64 one = (u64)__double_as_longlong(s.weigh.one);
-        uint32_t t = 0;
-        s.each_segment(a.seg_steps, [&](int, int, const float (&v)[8], u64 &m) {
-            bool some = false;
-            if (cut.ties) {
+        if (unlimited) {
+            // All logits are kept.  Where the largest one is not known yet, weights are relative to the guess, and the largest logit is found beside
+            // them; the sums stand if they fit (w < 2^7, their sum below 2^62), else they are formed again.
+            for (;;) {
+                sum = 0.0;
+                s.each_segment(a.seg_steps, [&](int, int, const float (&v)[8], u64 &m) {
+                    u64 part = 0;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) t += v[k] == border;
+                    for (int k = 0; k < 8; ++k) {
+                        part += s.weigh.raw(fmaxf(v[k], s.weigh.least));
+                        count += v[k] > -INFINITY;
+                        mine = largest(mine, v[k]);
+                    }
+                    m += part - 8 * one;
+                }, [&](int g, u64 m) {
+                    if (lane == 0) {
+                        sh.seg.mass[g] = m;
+                        sh.seg.ties[g] = 0;
+                        mass += m;
+                        sum += (double)m;
+                    }
+                });
+                if (!rest || blind) break;
+                if (lane == 0) sh.scan_f[warp] = sum;
+                const float top = s.all_largest(mine);   // (a barrier between)
+                if (!(fabsf(top) < INFINITY)) {
+                    best = top;
+                    return no_answer();
+                }
+                if (top == best) break;
+                if (threadIdx.x == 0) {
+                    sum = 0.0;
+                    for (int w = 0; w < THREADS / 32; ++w) sum += sh.scan_f[w];
+                    sh.part.sum = sum;
+                }
+                all_meet(blocks);
+                sum = 0.0;
+                s.of_blocks([](const Shared<THREADS> &b) { return b.part.sum; }, [&](int, double p) { sum += p; });
+                all_meet(blocks);
+                if (((double)top - best) * scale < 4.8 && sum < 0x1p62) break;
+                s.best = best = top;
+                s.weigh.set(best, scale, a.frac_bits, sh.table);
+                mass = 0;
+                count = 0;
             }
+        } else {
+            const float border = value_of(cut.key), weightless = fmaxf(border, s.weigh.least);
+            uint32_t t = 0;
+            s.each_segment(a.seg_steps, [&](int, int, const float (&v)[8], u64 &m) {
+                bool some = false;
+                if (cut.ties) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                some |= v[k] > border;
-                count += v[k] > border;
-            }
-            if (!__any_sync(0xffffffffu, some)) return;
-            u64 part = 0;
+                    for (int k = 0; k < 8; ++k) t += v[k] == border;
+                }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) part += s.weigh.raw(v[k] > weightless ? v[k] : s.weigh.least);
-            m += part - 8 * one;
-        }, [&](int g, u64 m) {
-            const uint32_t equal = cut.ties ? __reduce_add_sync(0xffffffffu, t) : 0;
-            t = 0;
-            if (lane == 0) {
-                sh.seg.mass[g] = m;
-                sh.seg.ties[g] = equal;
-                mass += m;
-                ties += equal;
-            }
-        });
+                for (int k = 0; k < 8; ++k) {
+                    some |= v[k] > border;
+                    count += v[k] > border;
+                }
+                if (!__any_sync(0xffffffffu, some)) return;
+                u64 part = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) part += s.weigh.raw(v[k] > weightless ? v[k] : s.weigh.least);
+                m += part - 8 * one;
+            }, [&](int g, u64 m) {
+                const uint32_t equal = cut.ties ? __reduce_add_sync(0xffffffffu, t) : 0;
+                t = 0;
+                if (lane == 0) {
+                    sh.seg.mass[g] = m;
+                    sh.seg.ties[g] = equal;
+                    mass += m;
+                    ties += equal;
+                }
+            });
+        }
         count = __reduce_add_sync(0xffffffffu, count);
     }
     // the block's own sums
@@ -1079,14 +1294,13 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
     const u64 tied = cut.ties || cut.by_last ? s.weigh(value_of(cut.key)) : 0;
     const auto of_ties = [&](u64 before, uint32_t there) { return before >= cut.ties ? (u64)0 : min(cut.ties - before, (u64)there); };
     u64 total = 0, mass_before = 0, ties_before = 0, all_ties = 0, kept = 0, own = 0;
-    for (int o = 0; o < blocks; ++o) {
-        const Part p = blocks == 1 ? sh.part : at_rank(&sh, o)->part;
+    s.of_blocks([](const Shared<THREADS> &b) { return b.part; }, [&](int o, const Part &p) {
         const u64 taken = of_ties(all_ties, p.ties), there = p.mass + taken * tied;
         if (o == rank) { mass_before = total; ties_before = all_ties; own = there; }
         total += there;
         all_ties += p.ties;
         kept += p.count + taken;
-    }
+    });
     if (summed) kept = sh.choice.kept;
     const u64 target = min(part_of(total, u, false), total - 1);
     if (target >= mass_before && target - mass_before < own) {      // the token lies in this block's part
