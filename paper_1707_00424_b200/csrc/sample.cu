@@ -66,6 +66,7 @@ __device__ __forceinline__ u64 part_of(u64 total, float f, bool up) {
 struct Weigher {                                         // w(x) = exp(scale (x - best)) as a whole number of 2^-frac_bits
     double best, c, one;                                 // c: 32 scale log2 e; one: whose last bit is 2^-frac_bits
     float least;                                         // it and all logits below weigh nothing
+    float most;                                          // logits above `best` that raw() may be used for (where best is a guess): w < 2^7
     const double *table;                                 // 2^(i / 32), in shared memory; less i 2^15 in the upper word, which n 2^15 adds
     __device__ __forceinline__ void set(float best_, float scale, int frac_bits, const double *table_) {
         best = best_;
@@ -74,11 +75,19 @@ struct Weigher {                                         // w(x) = exp(scale (x 
         // e^-45 < 2^-64.  Where best - 45 / scale is best again, the next number below weighs nothing, and is taken for as little as fits.
         least = fminf(best_ - 45.f / scale, value_of(key_of(best_) - 1));
         c = fmin(32.0 * 1.44269504088896340736 * scale, 4096.0 / (best - (double)least));
+        most = best_ + 4.8f / scale;
     }
     // 2^(n / 32) from the table and its exponent, e^y of the rest, |y| <= ln 2 / 64 = h, by Taylor's polynomial of degree 5 whose last term is spread over y and y^3
     // (Chebyshev's economisation: 16 z^5 - 20 z^3 + 5 z is at most 1): off by h^5 / 1920 = 8 10^-14.  Nine operations in fp64.
-    // raw(): of x >= least, with the bits of `one` still on it
-    __device__ __forceinline__ u64 raw(float x) const {
+    // raw(): of least <= x <= most, with the bits of `one` still on it
+    __device__ __forceinline__ u64 raw(float x) const { return (u64)__double_as_longlong(formed(x, one)); }
+    __device__ __forceinline__ u64 operator()(float x) const {
+        if (x > most) return __double2ull_rn(formed(x, 0.0) * __hiloint2double(2 * 1023 + 52 - (__double2hiint(one) >> 20) << 20, 0));
+        return raw(fmaxf(x, least)) - (u64)__double_as_longlong(one);
+    }
+
+  private:
+    __device__ __forceinline__ double formed(float x, double more) const {
         constexpr double y = 0.69314718055994530942 / 32, h = y / 2;
         const double d = (double)x - best;
         const double shifted = fma(d, c, 6755399441055744.0);      // 1.5 2^52: rounds to a whole number
@@ -89,10 +98,8 @@ struct Weigher {                                         // w(x) = exp(scale (x 
         p = fma(p, r, y * (1.0 - h * h * h * h / 384));
         p = fma(p, r, 1.0);
         const double power = *reinterpret_cast<const double *>(reinterpret_cast<const char *>(table) + (n8 & 0xf8));
-        p = fma(p, __hiloint2double(__double2hiint(power) + (n8 << 12), __double2loint(power)), one);
-        return (u64)__double_as_longlong(p);
+        return fma(p, __hiloint2double(__double2hiint(power) + (n8 << 12), __double2loint(power)), more);
     }
-    __device__ __forceinline__ u64 operator()(float x) const { return raw(fmaxf(x, least)) - (u64)__double_as_longlong(one); }
 };
 
 // A row in granules of eight logits, cut at memory's 16-byte boundaries.  `flat`: all logits are -inf or the lowest number (a row that is masked
@@ -124,6 +131,8 @@ template <typename T> struct Row {
             for (int i = 0; i < 8; ++i) v[i] = at(first(granule) + i);
         }
     }
+    // The largest of a granule as fetched; NaN if one is.  (Not of flat rows.)
+    __device__ __forceinline__ float most(const Pack8<T> &p, int granule) const;
     __device__ __forceinline__ void load(int granule, float (&v)[8]) const { get(fetch(granule, granule + 1), granule, v); }
 };
 
@@ -155,6 +164,18 @@ template <> struct Largest<float> {
     }
     __device__ __forceinline__ float get() const { return most; }
 };
+
+template <typename T> __device__ __forceinline__ float Row<T>::most(const Pack8<T> &p, int granule) const {
+    if (whole(granule)) {
+        Largest<T> m;
+        m.take(p);
+        return m.get();
+    }
+    float m = -INFINITY;
+#pragma unroll 1
+    for (int k = 0; k < 8; ++k) m = largest(m, at(first(granule) + k));
+    return m;
+}
 
 struct Cut {                                             // kept: logits of keys above `key`, and the first `ties` of those with it;
     uint32_t key;                                        // by_last: of those, the ones up to token `last`
@@ -288,9 +309,9 @@ template <typename T, int THREADS> struct Sampler {
         }
     }
 
-    // f(granule, logits) for each granule of the block's part, some in flight.
+    // f(granule, its raw form) for each granule of the block's part, some in flight.
     template <class F> __device__ __forceinline__ void each_granule(F f, int first = 0) const {
-        constexpr int kFlight = sizeof(T) == 2 ? 4 : 2;
+        constexpr int kFlight = 2;
         for (int g = begin + first + (int)threadIdx.x; g < end; g += THREADS * kFlight) {
             Pack8<T> p[kFlight];
 #pragma unroll
@@ -298,14 +319,14 @@ template <typename T, int THREADS> struct Sampler {
 #pragma unroll
             for (int i = 0; i < kFlight; ++i) {
                 if (g + i * THREADS >= end) break;
-                float v[8];
-                row.get(p[i], g + i * THREADS, v);
-                f(g + i * THREADS, v);
+                f(g + i * THREADS, p[i]);
             }
         }
     }
     template <class F> __device__ __forceinline__ void each(F f) const {
-        each_granule([&](int, const float (&v)[8]) {
+        each_granule([&](int g, const Pack8<T> &p) {
+            float v[8];
+            row.get(p, g, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) f(v[i]);
         });
@@ -321,9 +342,7 @@ template <typename T, int THREADS> struct Sampler {
         for (int i = 0; i < kHeld; ++i) {
             const int g = begin + (int)threadIdx.x + i * THREADS;
             if (g >= end) break;
-            float v[8];
-            row.get(held[i], g, v);
-            f(g, v);
+            f(g, held[i]);
         }
     }
     __device__ __forceinline__ float largest_of(const Pack8<T> (&p)[kHeld], int g) const {
@@ -375,22 +394,29 @@ template <typename T, int THREADS> struct Sampler {
         if ((double)f < low) f = value_of(key_of(f) + 1);
         return max(key_of(f), kNegInf + 1);
     }
-    // Of a granule: its logits in [low, inf) are listed; returns the sum of the weights, relative to `top`, in fp32's precision.
-    __device__ __forceinline__ float list_and_sum(int g, const float (&v)[8], float low, bool sum, float top, float c) {
+    // Of a granule: its logits from `low` on are listed; returns the sum of the weights, relative to `top`, in fp32's precision.  mine: the thread's
+    // largest logit.
+    __device__ __forceinline__ float list_and_sum(int g, const Pack8<T> &p, float low, bool sum, float top, float c, float &mine) {
+        const float most = row.flat ? top : row.most(p, g);
+        mine = largest(mine, most);
         float part = 0.f;
-        if (sum) {
+        if (sum || most >= low) {
+            float v[8];
+            row.get(p, g, v);
+            if (sum) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float e;
-                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"((v[i] - top) * c));
-                part += e;
+                for (int i = 0; i < 8; ++i) {
+                    float e;
+                    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"((v[i] - top) * c));
+                    part += e;
+                }
             }
+            if (most >= low) note(g, v, low, INFINITY);
         }
-        if (most_of(v) >= low) note(g, v, low, INFINITY);
         return part;
     }
 
-    // f(segment, granule, logits, sum) for the granules of each segment, a warp's granules side by side and the whole warp in each call (behind the
+    // f(granule, raw form, logits, sum) for the granules of each segment, a warp's granules side by side and the whole warp in each call (behind the
     // part's end with logits of -inf); then done(segment, sum of the lanes' sums).
     template <class F, class G> __device__ __forceinline__ void each_segment(int seg_steps, F f, G done) const {
         const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, segments = (end - begin + 32 * seg_steps - 1) / (32 * seg_steps);
@@ -409,15 +435,12 @@ template <typename T, int THREADS> struct Sampler {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) v[k] = -INFINITY;
                 }
-                f(g, now, v, m);
+                f(now, p, v, m);
             }
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) m += __shfl_xor_sync(0xffffffffu, m, o);
             done(g, m);
         }
-    }
-    __device__ __forceinline__ static float most_of(const float (&v)[8]) {
-        return fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
     }
     // Lists the granule's logits in [low, high].
     __device__ __forceinline__ void note(int granule, const float (&v)[8], float low, float high) {
@@ -723,7 +746,9 @@ template <typename T, int THREADS> struct Sampler {
         float low_value = floor_value;
         // Logits that weigh less than (1 - top_p) total / vocab are all together less than what top_p leaves out.
         if (known_total) low_value = fmaxf(low_value, best + (logf((1.f - top_p) * 0.999f * ((float)known_total * 0x1p-30f) / row.vocab)) / scale);
-        each_granule([&](int, const float (&v)[8]) {
+        each_granule([&](int g, const Pack8<T> &p) {
+            float v[8];
+            row.get(p, g, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 if (v[i] > low_value && v[i] < ceiling) {
@@ -850,7 +875,7 @@ template <typename T, int THREADS> struct Sampler {
         const u64 one = (u64)__double_as_longlong(weigh.one);
         const float weightless = fmaxf(top_p < 1.f ? floor_value : high, weigh.least);
         u64 total = 0, above = 0;
-        each_segment(seg_steps, [&](int, int at, const float (&v)[8], u64 &m) {
+        each_segment(seg_steps, [&](int at, const Pack8<T> &, const float (&v)[8], u64 &m) {
             bool some = false, any = top_p < 1.f;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
@@ -1025,12 +1050,9 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
     if (lists && !blind) {
         list_from(s.least_of(guess, min_p));
         const float floor = value_of(from);
-        s.each_held(held, [&](int g, const float (&v)[8]) { sum += s.list_and_sum(g, v, floor, summing, guess, log2_scale); });
-        s.each_granule([&](int g, const float (&v)[8]) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) mine = largest(mine, v[i]);
-            sum += s.list_and_sum(g, v, floor, summing, guess, log2_scale);
-        }, s.kHeld * THREADS);
+        const auto take = [&](int g, const Pack8<T> &p) { sum += s.list_and_sum(g, p, floor, summing, guess, log2_scale, mine); };
+        s.each_held(held, take);
+        s.each_granule(take, s.kHeld * THREADS);
     } else if (rest && (!unlimited || blind)) mine = largest(mine, s.largest_of_rest());
     // (An unlimited row's other logits are read once, for their weights relative to the guess, see below.)
     float best = rest && (!unlimited || blind) ? s.all_largest(mine) : guess;
@@ -1084,7 +1106,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
             top = best;
             sum = 0.0;
             const float floor = value_of(from);
-            s.each_granule([&](int g, const float (&v)[8]) { sum += s.list_and_sum(g, v, floor, summing, best, log2_scale); });
+            s.each_granule([&](int g, const Pack8<T> &p) { sum += s.list_and_sum(g, p, floor, summing, best, log2_scale, mine); });
         }
         if (summing) {
 #pragma unroll
@@ -1102,7 +1124,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
         all_meet(blocks);
         const bool complete = from <= max(least_key, kNegInf + 1);
         int n = 0;
-        s.of_blocks([](const Shared<THREADS> &b) { return b.listed; }, [&](int, uint32_t k) { n += (int)min((uint32_t)kList + 1, k); });
+        s.of_blocks([](const Shared<THREADS> &b) { return b.listed; }, [&](int, uint32_t k) { n += (int)min(2u * kList + 1, k); });
         u64 low = 0, high = 0;
         bool fits = n <= kList && !(by_k && n < top_k && !complete);
         if (summing) {
@@ -1122,7 +1144,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
         }
         if (!fits) {
             all_meet(blocks);                            // (the blocks' numbers are read)
-            if (!rest) break;                            // (the bound was that of all logits)
+            if (!rest || (!some && n > 2 * kList)) break;      // (the bound was that of all logits; min_p leaves far too many)
             continue;
         }
         Outcome outcome = kNeedAll;
@@ -1207,18 +1229,23 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
         const u64 one = (u64)__double_as_longlong(s.weigh.one);
         if (unlimited) {
             // All logits are kept.  Where the largest one is not known yet, weights are relative to the guess, and the largest logit is found beside
-            // them; the sums stand if they fit (w < 2^7, their sum below 2^62), else they are formed again.
+            // them; the sums stand if they fit (below 2^62), else they are formed again.
             for (;;) {
                 sum = 0.0;
-                s.each_segment(a.seg_steps, [&](int, int, const float (&v)[8], u64 &m) {
-                    u64 part = 0;
+                s.each_segment(a.seg_steps, [&](int g, const Pack8<T> &p, const float (&v)[8], u64 &m) {
+                    const float most = g >= end ? -INFINITY : row.flat ? best : row.most(p, g);
+                    mine = largest(mine, most);
+                    if (most > s.weigh.most) {
+#pragma unroll 1
+                        for (int k = 0; k < 8; ++k) m += s.weigh(row.at(row.first(g) + k));
+                    } else {
+                        u64 part = 0;
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        part += s.weigh.raw(fmaxf(v[k], s.weigh.least));
-                        count += v[k] > -INFINITY;
-                        mine = largest(mine, v[k]);
+                        for (int k = 0; k < 8; ++k) part += s.weigh.raw(fmaxf(v[k], s.weigh.least));
+                        m += part - 8 * one;
                     }
-                    m += part - 8 * one;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) count += v[k] > -INFINITY;
                 }, [&](int g, u64 m) {
                     if (lane == 0) {
                         sh.seg.mass[g] = m;
@@ -1244,7 +1271,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
                 sum = 0.0;
                 s.of_blocks([](const Shared<THREADS> &b) { return b.part.sum; }, [&](int, double p) { sum += p; });
                 all_meet(blocks);
-                if (((double)top - best) * scale < 4.8 && sum < 0x1p62) break;
+                if (((double)top - best) * scale < 12.0 && sum < 0x1p62) break;
                 s.best = best = top;
                 s.weigh.set(best, scale, a.frac_bits, sh.table);
                 mass = 0;
@@ -1253,7 +1280,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
         } else {
             const float border = value_of(cut.key), weightless = fmaxf(border, s.weigh.least);
             uint32_t t = 0;
-            s.each_segment(a.seg_steps, [&](int, int, const float (&v)[8], u64 &m) {
+            s.each_segment(a.seg_steps, [&](int, const Pack8<T> &, const float (&v)[8], u64 &m) {
                 bool some = false;
                 if (cut.ties) {
 #pragma unroll
