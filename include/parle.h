@@ -472,7 +472,8 @@ typedef struct {
  * state_bits 8: m and sqrt(v) are e4m3 codes times a scale for each PARLE_ADAMW_BLOCK consecutive elements, the largest magnitude / 448
  * (0, with codes of 0, where all magnitudes are below 2^-100; NaN where one is no finite number).  A magnitude y / scale between two codes
  * goes to the upper one where its distance from the lower, in parts of theirs, plus u / 2^24 is at least 1: u = (12664745 i + 9560335 t) mod 2^24
- * for m, 2^24 - 1 - u for sqrt(v), i the element's number in its tensor; a root above 0 is held as at least the smallest code.  Over the
+ * for m, 2^24 - 1 - u for sqrt(v), i the element's number in its tensor; a root above 0 is held as at least the smallest
+ * code, one below 2^-63 counts as 0.  Over the
  * steps this rounds to neither side: moments that move by less than a code's distance a step move all the same.
  * All zeros are the state of no steps, in both forms.  Arrays may not overlap; an array that begins where another begins is EINVAL.
  * copy_dtype: PARLE_BF16 or PARLE_F16 beside fp32 parameters, else PARLE_NO_COPY.  step_dev and lr_dev are read when the kernel runs: a

@@ -30,8 +30,8 @@ constexpr int kBlock = 256;                              // elements that share 
 constexpr float kLargest = 448.f;                        // of e4m3
 constexpr float kNothing = 0x1p-100f;                    // a block whose values all lie below this holds zeros
 constexpr uint32_t kWeylI = 12664745, kWeylT = 9560335;  // 2^24 / p and 2^24 / p^2, p the plastic number; odd: all 2^24 thresholds occur
-constexpr int kSteps = 2;                                // groups of a thread in a chunk
-constexpr int kChunk = kThreads * 8 * kSteps;
+constexpr int kSteps32 = 2, kSteps8 = 4;                 // groups of a thread in a chunk
+constexpr int kChunk32 = kThreads * 8 * kSteps32, kChunk8 = kThreads * 8 * kSteps8;
 
 struct Entry {
     void *param, *exp_avg, *exp_avg_sq, *copy;
@@ -74,6 +74,16 @@ __device__ __forceinline__ float root(float v) {
     float r;
     asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
+}
+__device__ __forceinline__ float coarse_root(float v) { // 0 below 2^-126
+    float r;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float larger(float v, float w) {      // NaN if either is
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(v), "f"(w));
+    return m;
 }
 __device__ __forceinline__ float reciprocal(float v) {
     float r;
@@ -120,24 +130,168 @@ __device__ __forceinline__ void decode8(uint2 codes, float scale, float (&v)[8])
         v[2 * i + 1] = f.y * scale;
     }
 }
-// A code in the top byte.  y in [0, 448]; times 2^-120 its exponent is fp32's, subnormal where the code is: 20 bits lie below the code, 24
-// with the shift, where the threshold is added.
-__device__ __forceinline__ uint32_t code_above(float y, uint32_t threshold) { return (__float_as_uint(y * 0x1p-120f) << 4) + threshold; }
+// A code in the top byte.  y in [0, 448] 2^-120: its exponent is fp32's, subnormal where the code is: 20 bits lie below the code, 24 with the shift,
+// where the threshold is added.
+__device__ __forceinline__ uint32_t code_above(float y, uint32_t threshold) { return (__float_as_uint(y) << 4) + threshold; }
 __device__ __forceinline__ uint32_t top_bytes(const uint32_t *t) {
     return __byte_perm(__byte_perm(t[0], t[1], 0x0073), __byte_perm(t[2], t[3], 0x0073), 0x5410);
 }
 
-// The scale of a block of a warp from the largest magnitude of each lane (as bits: what is not finite is largest); inverse: what values
-// are multiplied by (rounded down: no product is above 448).
-__device__ __forceinline__ float block_scale(uint32_t largest, float *inverse) {
-    const float top = __uint_as_float(__reduce_max_sync(0xffffffffu, largest));
+// The scale of a block of a warp from the largest magnitude of each lane (NaN if one is); factor: what values are multiplied by to lie in
+// [0, 448] 2^-120 (rounded down: no product is above).  Values from 2^14 on are scaled first, so that the factor is no subnormal number.
+__device__ __forceinline__ float block_scale(float largest, float (&x)[8], float *factor) {
+    float top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(largest)));      // (as bits, what is no number is largest)
     const bool none = top < kNothing, finite = top < INFINITY;
-    *inverse = none || !finite ? 0.f : __fdiv_rd(kLargest, top);
-    return none ? 0.f : finite ? __fdiv_rn(top, kLargest) : NAN;
+    const float scale = none ? 0.f : finite ? __fdiv_rn(top, kLargest) : NAN;
+    if (top >= 0x1p14f) {
+        top *= 0x1p-120f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= 0x1p-120f;
+        *factor = finite ? __fdiv_rd(kLargest * 0x1p-120f, top) : 0.f;
+    } else *factor = none ? 0.f : __fdiv_rd(kLargest * 0x1p-120f, top);
+    return scale;
 }
 
-template <typename P, typename G, typename C, int BITS, class L>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ L list, const __grid_constant__ StepArgs a) {
+// One step of eight elements with moments in 8 bits, a whole warp's block: v comes as the root, mc and rc as the old codes, and go as the new ones.
+__device__ __forceinline__ void step8(const StepArgs &a, const Scalars &s, float limit, long long e0, float m_scale, float r_scale, float (&p)[8], float (&g)[8], uint2 &mc, uint2 &rc, long long n,
+                                      bool whole, float *new_m_scale, float *new_r_scale, bool &ok) {
+    float m[8], r[8], m_top = 0.f, r_top = 0.f;
+    decode8(mc, m_scale, m);
+    decode8(rc, r_scale, r);
+    if (!whole) {                                        // (a scale may be NaN: behind the end there are zeros all the same)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (e0 + i >= n) m[i] = r[i] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        g[i] *= s.c;
+        m[i] = fmaf(a.b1, m[i], a.one_minus_b1 * g[i]);
+        r[i] = coarse_root(fmaf(a.b2, r[i] * r[i], a.one_minus_b2 * (g[i] * g[i])));
+        p[i] = fmaf(p[i], s.decay, -s.rate * (m[i] * reciprocal(fmaf(r[i], s.root_scale, a.eps))));
+        ok &= fabsf(p[i]) < limit;
+        m_top = larger(m_top, fabsf(m[i]));
+        r_top = larger(r_top, r[i]);
+    }
+    float m_factor, r_factor;
+    *new_m_scale = block_scale(m_top, m, &m_factor);
+    *new_r_scale = block_scale(r_top, r, &r_factor);
+    uint32_t mt[8], rt[8];
+    const uint32_t first = (uint32_t)e0 * kWeylI + s.weyl;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t u = (first + i * kWeylI) & 0xffffffu;
+        // (__fmul_rn: products written with * came out as zeros from CUDA 12.9's assembler at its default level)
+        mt[i] = code_above(__fmul_rn(fabsf(m[i]), m_factor), u) | (__float_as_uint(m[i]) & 0x80000000u);
+        rt[i] = code_above(__fmul_rn(r[i], r_factor), u ^ 0xffffffu);
+        if (r[i] > 0.f) rt[i] = max(rt[i], 1u << 24);    // else m would be divided by eps alone one day
+    }
+    mc = make_uint2(top_bytes(mt), top_bytes(mt + 4));
+    rc = make_uint2(top_bytes(rt), top_bytes(rt + 4));
+}
+
+// What a thread loads for eight elements, so that it can be fetched early.
+template <typename P, typename G> struct Raw8 {
+    Pack8<P> p;
+    Pack8<G> g;
+    uint2 mc, rc;
+    float m_scale, r_scale;
+    __device__ __forceinline__ void load(const Entry &t, long long e0) {
+        p.load(static_cast<const P *>(t.param) + e0);
+        g.load(static_cast<const G *>(t.grad) + e0);
+        mc = *reinterpret_cast<const uint2 *>(static_cast<const char *>(t.exp_avg) + e0);
+        rc = *reinterpret_cast<const uint2 *>(static_cast<const char *>(t.exp_avg_sq) + e0);
+        m_scale = t.exp_avg_scale[e0 / kBlock];
+        r_scale = t.exp_avg_sq_scale[e0 / kBlock];
+    }
+};
+
+template <typename P, typename G, typename C, class L>
+__global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant__ L list, const __grid_constant__ StepArgs a) {
+    const Scalars s = scalars(a);
+    if (s.skip) return;
+    const int index = entry_of(list, blockIdx.x);
+    const Entry &t = list.entry[index];
+    const long long n = t.size_shift >> 4, first = (long long)(blockIdx.x - list.first[index]) * kChunk8;
+    P *const param = static_cast<P *>(t.param);
+    char *const m_codes = static_cast<char *>(t.exp_avg), *const r_codes = static_cast<char *>(t.exp_avg_sq);
+    const float limit = fminf(Limit<P>::value, Limit<C>::value);
+    bool ok = true;
+    float m_scale, r_scale;
+    if ((t.size_shift & 1) && first + kChunk8 <= n) {    // a whole chunk on 16-byte boundaries: the next elements are fetched early
+        long long e0 = first + threadIdx.x * 8;
+        Raw8<P, G> raw;
+        raw.load(t, e0);
+#pragma unroll 1
+        for (int step = 0; step < kSteps8; ++step, e0 += kThreads * 8) {
+            Raw8<P, G> now = raw;
+            if (step + 1 < kSteps8) raw.load(t, e0 + kThreads * 8);
+            float p[8], g[8];
+            now.p.get(p);
+            now.g.get(g);
+            step8(a, s, limit, e0, now.m_scale, now.r_scale, p, g, now.mc, now.rc, n, true, &m_scale, &r_scale, ok);
+            now.p.set(p);
+            now.p.store(param + e0);
+            *reinterpret_cast<uint2 *>(m_codes + e0) = now.mc;
+            *reinterpret_cast<uint2 *>(r_codes + e0) = now.rc;
+            if (threadIdx.x % 32 == 0) {
+                t.exp_avg_scale[e0 / kBlock] = m_scale;
+                t.exp_avg_sq_scale[e0 / kBlock] = r_scale;
+            }
+            if constexpr (!std::is_same<C, NoCopy>::value) {
+                Pack8<C> c;
+                c.set(p);
+                c.store(static_cast<C *>(t.copy) + e0);
+            }
+        }
+    } else {
+        long long e0 = first + threadIdx.x * 8;
+#pragma unroll 1
+        for (int step = 0; step < kSteps8; ++step, e0 += kThreads * 8) {
+            if (e0 - (int)(threadIdx.x % 32) * 8 >= n) break;      // (whole warps: a block's lanes meet)
+            const bool whole = (t.size_shift & 1) && e0 + 8 <= n;
+            Raw8<P, G> raw = {};
+            float p[8], g[8];
+            if (whole) {
+                raw.load(t, e0);
+                raw.p.get(p);
+                raw.g.get(g);
+            } else {
+                load_some(param, e0, n, p);
+                load_some(static_cast<const G *>(t.grad), e0, n, g);
+                uint32_t c[4] = {};
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (e0 + i < n) {
+                        c[i / 4] |= (uint32_t)(unsigned char)m_codes[e0 + i] << (i % 4 * 8);
+                        c[2 + i / 4] |= (uint32_t)(unsigned char)r_codes[e0 + i] << (i % 4 * 8);
+                    }
+                raw.mc = make_uint2(c[0], c[1]);
+                raw.rc = make_uint2(c[2], c[3]);
+                const long long block = min(e0, n - 1) / kBlock;
+                raw.m_scale = t.exp_avg_scale[block];
+                raw.r_scale = t.exp_avg_sq_scale[block];
+            }
+            step8(a, s, limit, e0, raw.m_scale, raw.r_scale, p, g, raw.mc, raw.rc, n, whole, &m_scale, &r_scale, ok);
+            if (threadIdx.x % 32 == 0) {
+                t.exp_avg_scale[e0 / kBlock] = m_scale;
+                t.exp_avg_sq_scale[e0 / kBlock] = r_scale;
+            }
+            store_some(param, e0, n, p);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (e0 + i < n) {
+                    m_codes[e0 + i] = (char)((i < 4 ? raw.mc.x : raw.mc.y) >> (i % 4 * 8));
+                    r_codes[e0 + i] = (char)((i < 4 ? raw.rc.x : raw.rc.y) >> (i % 4 * 8));
+                }
+            if constexpr (!std::is_same<C, NoCopy>::value) store_some(static_cast<C *>(t.copy), e0, n, p);
+        }
+    }
+    if (a.flags && !ok) atomicOr(a.flags, PARLE_FLAG_NONFINITE);
+}
+
+template <typename P, typename G, typename C, class L>
+__global__ void __launch_bounds__(kThreads) adamw32_kernel(const __grid_constant__ L list, const __grid_constant__ StepArgs a) {
     const Scalars s = scalars(a);
     if (s.skip) return;
     const int index = entry_of(list, blockIdx.x);
@@ -147,105 +301,49 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
     const bool aligned = t.size_shift & 1;
     P *const param = static_cast<P *>(t.param);
     const G *const grad = static_cast<const G *>(t.grad);
+    float *const exp_avg = static_cast<float *>(t.exp_avg), *const exp_avg_sq = static_cast<float *>(t.exp_avg_sq);
+    const float limit = fminf(Limit<P>::value, Limit<C>::value);
     bool ok = true;
-    long long e0 = (long long)(blockIdx.x - list.first[index]) * kChunk + threadIdx.x * 8 - shift;
-    for (int step = 0; step < kSteps; ++step, e0 += kThreads * 8) {
-        if (BITS == 8 ? e0 - (int)(threadIdx.x % 32) * 8 >= n : e0 >= n) break;      // (whole warps: a block's lanes meet below)
+    long long e0 = (long long)(blockIdx.x - list.first[index]) * kChunk32 + threadIdx.x * 8 - shift;
+    for (int step = 0; step < kSteps32; ++step, e0 += kThreads * 8) {
+        if (e0 >= n) break;
         const bool whole = aligned && e0 >= 0 && e0 + 8 <= n;
         float p[8], g[8], m[8], v[8];
         if (whole) {
             Pack8<P> pp;
             Pack8<G> gg;
+            Pack8<float> mm, vv;
             pp.load(param + e0);
             gg.load(grad + e0);
-            if (BITS == 32) {
-                Pack8<float> mm, vv;
-                mm.load(static_cast<const float *>(t.exp_avg) + e0);
-                vv.load(static_cast<const float *>(t.exp_avg_sq) + e0);
-                mm.get(m);
-                vv.get(v);
-            } else {
-                const uint2 mc = *reinterpret_cast<const uint2 *>(static_cast<const char *>(t.exp_avg) + e0);
-                const uint2 rc = *reinterpret_cast<const uint2 *>(static_cast<const char *>(t.exp_avg_sq) + e0);
-                decode8(mc, t.exp_avg_scale[e0 / kBlock], m);
-                decode8(rc, t.exp_avg_sq_scale[e0 / kBlock], v);
-            }
+            mm.load(exp_avg + e0);
+            vv.load(exp_avg_sq + e0);
             pp.get(p);
             gg.get(g);
+            mm.get(m);
+            vv.get(v);
         } else {
             load_some(param, e0, n, p);
             load_some(grad, e0, n, g);
-            if (BITS == 32) {
-                load_some(static_cast<const float *>(t.exp_avg), e0, n, m);
-                load_some(static_cast<const float *>(t.exp_avg_sq), e0, n, v);
-            } else {
-                uint32_t mc[2] = {0, 0}, rc[2] = {0, 0};
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (e0 + i < n) {
-                        mc[i / 4] |= (uint32_t)static_cast<const unsigned char *>(t.exp_avg)[e0 + i] << (i % 4 * 8);
-                        rc[i / 4] |= (uint32_t)static_cast<const unsigned char *>(t.exp_avg_sq)[e0 + i] << (i % 4 * 8);
-                    }
-                const long long block = min(e0, n - 1) / kBlock;
-                decode8(make_uint2(mc[0], mc[1]), t.exp_avg_scale[block], m);
-                decode8(make_uint2(rc[0], rc[1]), t.exp_avg_sq_scale[block], v);
-                if (e0 >= n) {                           // (a scale may be NaN: lanes behind the end hold zeros all the same)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) m[i] = v[i] = 0.f;
-                }
-            }
+            load_some(exp_avg, e0, n, m);
+            load_some(exp_avg_sq, e0, n, v);
         }
-        float r[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             g[i] *= s.c;
-            if (BITS == 8) v[i] *= v[i];
             m[i] = fmaf(a.b1, m[i], a.one_minus_b1 * g[i]);
-            v[i] = fmaf(a.b2, v[i], a.one_minus_b2 * g[i] * g[i]);
-            r[i] = root(v[i]);
-            p[i] = fmaf(p[i], s.decay, -s.rate * (m[i] * reciprocal(fmaf(r[i], s.root_scale, a.eps))));
-            ok &= fabsf(p[i]) < fminf(Limit<P>::value, Limit<C>::value);
-        }
-        uint2 mc, rc;
-        if (BITS == 8) {
-            uint32_t m_top = 0, r_top = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const bool there = whole || e0 + i < n;
-                m_top = max(m_top, there ? __float_as_uint(m[i]) & 0x7fffffffu : 0u);
-                r_top = max(r_top, there ? __float_as_uint(r[i]) & 0x7fffffffu : 0u);
-            }
-            float m_inverse, r_inverse;
-            const float m_scale = block_scale(m_top, &m_inverse), r_scale = block_scale(r_top, &r_inverse);
-            if (threadIdx.x % 32 == 0) {
-                t.exp_avg_scale[e0 / kBlock] = m_scale;
-                t.exp_avg_sq_scale[e0 / kBlock] = r_scale;
-            }
-            uint32_t mt[8], rt[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t u = ((uint32_t)(e0 + i) * kWeylI + s.weyl) & 0xffffffu;
-                mt[i] = m_inverse == 0.f ? 0u : code_above(fabsf(m[i]) * m_inverse, u) | (__float_as_uint(m[i]) & 0x80000000u);
-                rt[i] = r_inverse == 0.f ? 0u : code_above(r[i] * r_inverse, u ^ 0xffffffu);
-                if (r_inverse != 0.f && r[i] > 0.f) rt[i] = max(rt[i], 1u << 24);     // else m would be divided by eps alone one day
-            }
-            mc = make_uint2(top_bytes(mt), top_bytes(mt + 4));
-            rc = make_uint2(top_bytes(rt), top_bytes(rt + 4));
+            v[i] = fmaf(a.b2, v[i], a.one_minus_b2 * (g[i] * g[i]));
+            p[i] = fmaf(p[i], s.decay, -s.rate * (m[i] * reciprocal(fmaf(root(v[i]), s.root_scale, a.eps))));
+            ok &= fabsf(p[i]) < limit;
         }
         if (whole) {
             Pack8<P> pp;
+            Pack8<float> mm, vv;
             pp.set(p);
+            mm.set(m);
+            vv.set(v);
             pp.store(param + e0);
-            if (BITS == 32) {
-                Pack8<float> mm, vv;
-                mm.set(m);
-                vv.set(v);
-                mm.store(static_cast<float *>(t.exp_avg) + e0);
-                vv.store(static_cast<float *>(t.exp_avg_sq) + e0);
-            } else {
-                *reinterpret_cast<uint2 *>(static_cast<char *>(t.exp_avg) + e0) = mc;
-                *reinterpret_cast<uint2 *>(static_cast<char *>(t.exp_avg_sq) + e0) = rc;
-            }
+            mm.store(exp_avg + e0);
+            vv.store(exp_avg_sq + e0);
             if constexpr (!std::is_same<C, NoCopy>::value) {
                 Pack8<C> cc;
                 cc.set(p);
@@ -253,17 +351,8 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
             }
         } else {
             store_some(param, e0, n, p);
-            if (BITS == 32) {
-                store_some(static_cast<float *>(t.exp_avg), e0, n, m);
-                store_some(static_cast<float *>(t.exp_avg_sq), e0, n, v);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (e0 + i < n) {
-                        static_cast<unsigned char *>(t.exp_avg)[e0 + i] = (unsigned char)((i < 4 ? mc.x : mc.y) >> (i % 4 * 8));
-                        static_cast<unsigned char *>(t.exp_avg_sq)[e0 + i] = (unsigned char)((i < 4 ? rc.x : rc.y) >> (i % 4 * 8));
-                    }
-            }
+            store_some(exp_avg, e0, n, m);
+            store_some(exp_avg_sq, e0, n, v);
             if constexpr (!std::is_same<C, NoCopy>::value) store_some(static_cast<C *>(t.copy), e0, n, p);
         }
     }
@@ -305,12 +394,14 @@ class Addresses {
 };
 
 template <typename P, typename G, typename C, int BITS, class L> int launch_list(const L &list, const StepArgs &a, unsigned chunks, cudaStream_t stream) {
-    adamw_kernel<P, G, C, BITS, L><<<chunks, kThreads, 0, stream>>>(list, a);
+    if constexpr (BITS == 8) adamw8_kernel<P, G, C, L><<<chunks, kThreads, 0, stream>>>(list, a);
+    else adamw32_kernel<P, G, C, L><<<chunks, kThreads, 0, stream>>>(list, a);
     return launch_status();
 }
 
 template <int CAP, typename P, typename G, typename C, int BITS>
 int launch_all(const parle_adamw_tensor *tensors, int count, const StepArgs &a, cudaStream_t stream) {
+    constexpr int kChunk = BITS == 8 ? kChunk8 : kChunk32;
     List<CAP> list;
     list.count = 0;
     unsigned chunks = 0;
