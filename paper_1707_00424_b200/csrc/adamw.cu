@@ -25,13 +25,14 @@ using namespace parle;
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads32 = 256, kThreads8 = 128;
 constexpr int kBlock = 256;                              // elements that share a scale
 constexpr float kLargest = 448.f;                        // of e4m3
 constexpr float kNothing = 0x1p-100f;                    // a block whose values all lie below this holds zeros
 constexpr uint32_t kWeylI = 12664745, kWeylT = 9560335;  // 2^24 / p and 2^24 / p^2, p the plastic number; odd: all 2^24 thresholds occur
-constexpr int kSteps32 = 2, kSteps8 = 4;                 // groups of a thread in a chunk
-constexpr int kChunk32 = kThreads * 8 * kSteps32, kChunk8 = kThreads * 8 * kSteps8;
+constexpr int kSteps32 = 2, kSteps8 = 8;                 // groups of a thread in a chunk
+constexpr int kChunk32 = kThreads32 * 8 * kSteps32, kChunk8 = kThreads8 * 8 * kSteps8;
+constexpr int kStages = 4;                               // of them in shared memory, 8-bit moments
 
 struct Entry {
     void *param, *exp_avg, *exp_avg_sq, *copy;
@@ -48,6 +49,7 @@ constexpr int kFew = 24, kMany = 440;                    // a launch takes 32764
 
 struct StepArgs {
     float b1, one_minus_b1, b2, one_minus_b2, eps;
+    float root_b2, root_one_minus_b2;
     float rate, root_scale, decay;                       // lr / (1 - b1^t), 1 / sqrt(1 - b2^t), 1 - lr wd, where neither step_dev nor lr_dev is given
     float grad_scale, max_norm;
     double lr, weight_decay, log_b1, log_b2;
@@ -122,14 +124,6 @@ __device__ __forceinline__ float2 decode2(uint32_t codes) {
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)codes));
     return __half22float2(*reinterpret_cast<const __half2 *>(&h));
 }
-__device__ __forceinline__ void decode8(uint2 codes, float scale, float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = decode2((i < 2 ? codes.x : codes.y) >> (i % 2 * 16));
-        v[2 * i] = f.x * scale;
-        v[2 * i + 1] = f.y * scale;
-    }
-}
 // A code in the top byte.  y in [0, 448] 2^-120: its exponent is fp32's, subnormal where the code is: 20 bits lie below the code, 24 with the shift,
 // where the threshold is added.
 __device__ __forceinline__ uint32_t code_above(float y, uint32_t threshold) { return (__float_as_uint(y) << 4) + threshold; }
@@ -152,23 +146,55 @@ __device__ __forceinline__ float block_scale(float largest, float (&x)[8], float
     return scale;
 }
 
-// One step of eight elements with moments in 8 bits, a whole warp's block: v comes as the root, mc and rc as the old codes, and go as the new ones.
-__device__ __forceinline__ void step8(const StepArgs &a, const Scalars &s, float limit, long long e0, float m_scale, float r_scale, float (&p)[8], float (&g)[8], uint2 &mc, uint2 &rc, long long n,
-                                      bool whole, float *new_m_scale, float *new_r_scale, bool &ok) {
+// Pairs of fp32 numbers: their instructions run at the rate of single ones, but take half of the issue slots, which bound this kernel.
+typedef unsigned long long Two;
+__device__ __forceinline__ Two two(float x, float y) {
+    Two t;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(t) : "f"(x), "f"(y));
+    return t;
+}
+__device__ __forceinline__ void split(Two t, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(t)); }
+__device__ __forceinline__ Two mul(Two a, Two b) {
+    Two t;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(t) : "l"(a), "l"(b));
+    return t;
+}
+__device__ __forceinline__ Two mul_add(Two a, Two b, Two c) {
+    Two t;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(t) : "l"(a), "l"(b), "l"(c));
+    return t;
+}
+
+// One step of eight elements with moments in 8 bits, a whole warp's block: mc and rc come as the old codes and go as the new ones.  The old
+// moments' factors b1 and sqrt(b2) go into their scales, c and the roots of the new ones' into what g is multiplied by.
+__device__ __forceinline__ void step8(const StepArgs &a, const Scalars &s, float limit, long long e0, float m_scale, float r_scale, float (&p)[8], const float (&g)[8], uint2 &mc, uint2 &rc,
+                                      long long n, bool whole, float *new_m_scale, float *new_r_scale, bool &ok) {
     float m[8], r[8], m_top = 0.f, r_top = 0.f;
-    decode8(mc, m_scale, m);
-    decode8(rc, r_scale, r);
-    if (!whole) {                                        // (a scale may be NaN: behind the end there are zeros all the same)
+    const float ms = m_scale * a.b1, rs = r_scale * a.root_b2, k1 = s.c * a.one_minus_b1, k2 = s.c * a.root_one_minus_b2;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (e0 + i >= n) m[i] = r[i] = 0.f;
+    for (int i = 0; i < 4; ++i) {
+        const float2 cm = decode2((i < 2 ? mc.x : mc.y) >> (i % 2 * 16)), cr = decode2((i < 2 ? rc.x : rc.y) >> (i % 2 * 16));
+        Two old_m = mul(two(cm.x, cm.y), two(ms, ms)), old_r = mul(two(cr.x, cr.y), two(rs, rs));
+        if (!whole) {                                    // (a scale may be NaN: behind the end there are zeros all the same)
+            float x, y;
+            const bool first = e0 + 2 * i < n, second = e0 + 2 * i + 1 < n;
+            split(old_m, x, y);
+            old_m = two(first ? x : 0.f, second ? y : 0.f);
+            split(old_r, x, y);
+            old_r = two(first ? x : 0.f, second ? y : 0.f);
+        }
+        const Two gg = two(g[2 * i], g[2 * i + 1]), new_m = mul_add(gg, two(k1, k1), old_m), more = mul(gg, two(k2, k2)), v = mul_add(more, more, mul(old_r, old_r));
+        float x, y;
+        split(v, x, y);
+        r[2 * i] = coarse_root(x);
+        r[2 * i + 1] = coarse_root(y);
+        split(mul_add(two(r[2 * i], r[2 * i + 1]), two(s.root_scale, s.root_scale), two(a.eps, a.eps)), x, y);
+        const Two ratio = mul(new_m, two(reciprocal(x), reciprocal(y)));
+        split(mul_add(two(p[2 * i], p[2 * i + 1]), two(s.decay, s.decay), mul(ratio, two(-s.rate, -s.rate))), p[2 * i], p[2 * i + 1]);
+        split(new_m, m[2 * i], m[2 * i + 1]);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        g[i] *= s.c;
-        m[i] = fmaf(a.b1, m[i], a.one_minus_b1 * g[i]);
-        r[i] = coarse_root(fmaf(a.b2, r[i] * r[i], a.one_minus_b2 * (g[i] * g[i])));
-        p[i] = fmaf(p[i], s.decay, -s.rate * (m[i] * reciprocal(fmaf(r[i], s.root_scale, a.eps))));
         ok &= fabsf(p[i]) < limit;
         m_top = larger(m_top, fabsf(m[i]));
         r_top = larger(r_top, r[i]);
@@ -190,27 +216,39 @@ __device__ __forceinline__ void step8(const StepArgs &a, const Scalars &s, float
     rc = make_uint2(top_bytes(rt), top_bytes(rt + 4));
 }
 
-// What a thread loads for eight elements, so that it can be fetched early.
-template <typename P, typename G> struct Raw8 {
-    Pack8<P> p;
-    Pack8<G> g;
-    uint2 mc, rc;
-    float m_scale, r_scale;
-    __device__ __forceinline__ void load(const Entry &t, long long e0) {
-        p.load(static_cast<const P *>(t.param) + e0);
-        g.load(static_cast<const G *>(t.grad) + e0);
-        mc = *reinterpret_cast<const uint2 *>(static_cast<const char *>(t.exp_avg) + e0);
-        rc = *reinterpret_cast<const uint2 *>(static_cast<const char *>(t.exp_avg_sq) + e0);
-        m_scale = t.exp_avg_scale[e0 / kBlock];
-        r_scale = t.exp_avg_sq_scale[e0 / kBlock];
+template <int BYTES> __device__ __forceinline__ void copy_async(void *to, const void *from) {
+    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+
+// Eight elements of each thread on their way to it, in shared memory; nobody reads another thread's.
+template <typename P, typename G> struct Stage {
+    uint4 p[sizeof(P) / 2][kThreads8], g[sizeof(G) / 2][kThreads8];
+    uint2 mc[kThreads8], rc[kThreads8];
+    __device__ __forceinline__ void fetch(const Entry &t, long long e0) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(P) / 2; ++i) copy_async<16>(&p[i][threadIdx.x], reinterpret_cast<const uint4 *>(static_cast<const P *>(t.param) + e0) + i);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(G) / 2; ++i) copy_async<16>(&g[i][threadIdx.x], reinterpret_cast<const uint4 *>(static_cast<const G *>(t.grad) + e0) + i);
+        copy_async<8>(&mc[threadIdx.x], static_cast<const char *>(t.exp_avg) + e0);
+        copy_async<8>(&rc[threadIdx.x], static_cast<const char *>(t.exp_avg_sq) + e0);
+    }
+    template <typename T> __device__ __forceinline__ static void take(const uint4 (*from)[kThreads8], float (&v)[8]) {
+        Pack8<T> pack;
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(&pack)[i] = from[i][threadIdx.x];
+        pack.get(v);
     }
 };
 
+// A chunk on 16-byte boundaries is fetched three steps ahead through shared memory (2.5 KB a warp and step for fp32 gradients and parameters): one step
+// ahead in registers left the kernel waiting for DRAM, as 62 to 72 registers a thread allow 24 to 28 warps an SM.
 template <typename P, typename G, typename C, class L>
-__global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant__ L list, const __grid_constant__ StepArgs a) {
+__global__ void __launch_bounds__(kThreads8) adamw8_kernel(const __grid_constant__ L list, const __grid_constant__ StepArgs a) {
+    __shared__ Stage<P, G> stage[kStages];
     const Scalars s = scalars(a);
     if (s.skip) return;
-    const int index = entry_of(list, blockIdx.x);
+    const int index = entry_of(list, blockIdx.x), lane = threadIdx.x % 32;
     const Entry &t = list.entry[index];
     const long long n = t.size_shift >> 4, first = (long long)(blockIdx.x - list.first[index]) * kChunk8;
     P *const param = static_cast<P *>(t.param);
@@ -218,23 +256,35 @@ __global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant_
     const float limit = fminf(Limit<P>::value, Limit<C>::value);
     bool ok = true;
     float m_scale, r_scale;
-    if ((t.size_shift & 1) && first + kChunk8 <= n) {    // a whole chunk on 16-byte boundaries: the next elements are fetched early
-        long long e0 = first + threadIdx.x * 8;
-        Raw8<P, G> raw;
-        raw.load(t, e0);
+    long long e0 = first + threadIdx.x * 8;
+    if ((t.size_shift & 1) && first + kChunk8 <= n) {
+#pragma unroll
+        for (int step = 0; step < kStages - 1; ++step) {
+            stage[step].fetch(t, e0 + step * kThreads8 * 8);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+        static_assert(kSteps8 <= 16, "");
+        // the steps' scales: a lane each, m's in the lower half of the warp
+        const float *const scale_of = lane < 16 ? t.exp_avg_scale : t.exp_avg_sq_scale;
+        const long long block = e0 / kBlock;
+        const float scales = lane % 16 < kSteps8 ? scale_of[block + lane % 16 * (kThreads8 * 8 / kBlock)] : 0.f;
 #pragma unroll 1
-        for (int step = 0; step < kSteps8; ++step, e0 += kThreads * 8) {
-            Raw8<P, G> now = raw;
-            if (step + 1 < kSteps8) raw.load(t, e0 + kThreads * 8);
+        for (int step = 0; step < kSteps8; ++step, e0 += kThreads8 * 8) {
+            if (step + kStages - 1 < kSteps8) stage[(step + kStages - 1) % kStages].fetch(t, e0 + (kStages - 1) * kThreads8 * 8);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+            Stage<P, G> &now = stage[step % kStages];
             float p[8], g[8];
-            now.p.get(p);
-            now.g.get(g);
-            step8(a, s, limit, e0, now.m_scale, now.r_scale, p, g, now.mc, now.rc, n, true, &m_scale, &r_scale, ok);
-            now.p.set(p);
-            now.p.store(param + e0);
-            *reinterpret_cast<uint2 *>(m_codes + e0) = now.mc;
-            *reinterpret_cast<uint2 *>(r_codes + e0) = now.rc;
-            if (threadIdx.x % 32 == 0) {
+            now.template take<P>(now.p, p);
+            now.template take<G>(now.g, g);
+            uint2 mc = now.mc[threadIdx.x], rc = now.rc[threadIdx.x];
+            step8(a, s, limit, e0, __shfl_sync(0xffffffffu, scales, step), __shfl_sync(0xffffffffu, scales, 16 + step), p, g, mc, rc, n, true, &m_scale, &r_scale, ok);
+            Pack8<P> pack;
+            pack.set(p);
+            pack.store(param + e0);
+            *reinterpret_cast<uint2 *>(m_codes + e0) = mc;
+            *reinterpret_cast<uint2 *>(r_codes + e0) = rc;
+            if (lane == 0) {
                 t.exp_avg_scale[e0 / kBlock] = m_scale;
                 t.exp_avg_sq_scale[e0 / kBlock] = r_scale;
             }
@@ -245,17 +295,21 @@ __global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant_
             }
         }
     } else {
-        long long e0 = first + threadIdx.x * 8;
 #pragma unroll 1
-        for (int step = 0; step < kSteps8; ++step, e0 += kThreads * 8) {
-            if (e0 - (int)(threadIdx.x % 32) * 8 >= n) break;      // (whole warps: a block's lanes meet)
+        for (int step = 0; step < kSteps8; ++step, e0 += kThreads8 * 8) {
+            if (e0 - lane * 8 >= n) break;               // (whole warps: a block's lanes meet)
             const bool whole = (t.size_shift & 1) && e0 + 8 <= n;
-            Raw8<P, G> raw = {};
             float p[8], g[8];
+            uint2 mc, rc;
             if (whole) {
-                raw.load(t, e0);
-                raw.p.get(p);
-                raw.g.get(g);
+                Pack8<P> pack;
+                Pack8<G> grads;
+                pack.load(param + e0);
+                grads.load(static_cast<const G *>(t.grad) + e0);
+                mc = *reinterpret_cast<const uint2 *>(m_codes + e0);
+                rc = *reinterpret_cast<const uint2 *>(r_codes + e0);
+                pack.get(p);
+                grads.get(g);
             } else {
                 load_some(param, e0, n, p);
                 load_some(static_cast<const G *>(t.grad), e0, n, g);
@@ -266,24 +320,30 @@ __global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant_
                         c[i / 4] |= (uint32_t)(unsigned char)m_codes[e0 + i] << (i % 4 * 8);
                         c[2 + i / 4] |= (uint32_t)(unsigned char)r_codes[e0 + i] << (i % 4 * 8);
                     }
-                raw.mc = make_uint2(c[0], c[1]);
-                raw.rc = make_uint2(c[2], c[3]);
-                const long long block = min(e0, n - 1) / kBlock;
-                raw.m_scale = t.exp_avg_scale[block];
-                raw.r_scale = t.exp_avg_sq_scale[block];
+                mc = make_uint2(c[0], c[1]);
+                rc = make_uint2(c[2], c[3]);
             }
-            step8(a, s, limit, e0, raw.m_scale, raw.r_scale, p, g, raw.mc, raw.rc, n, whole, &m_scale, &r_scale, ok);
-            if (threadIdx.x % 32 == 0) {
-                t.exp_avg_scale[e0 / kBlock] = m_scale;
-                t.exp_avg_sq_scale[e0 / kBlock] = r_scale;
+            const long long block = min(e0, n - 1) / kBlock;
+            step8(a, s, limit, e0, t.exp_avg_scale[block], t.exp_avg_sq_scale[block], p, g, mc, rc, n, whole, &m_scale, &r_scale, ok);
+            if (lane == 0) {
+                t.exp_avg_scale[block] = m_scale;
+                t.exp_avg_sq_scale[block] = r_scale;
             }
-            store_some(param, e0, n, p);
+            if (whole) {
+                Pack8<P> pack;
+                pack.set(p);
+                pack.store(param + e0);
+                *reinterpret_cast<uint2 *>(m_codes + e0) = mc;
+                *reinterpret_cast<uint2 *>(r_codes + e0) = rc;
+            } else {
+                store_some(param, e0, n, p);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (e0 + i < n) {
-                    m_codes[e0 + i] = (char)((i < 4 ? raw.mc.x : raw.mc.y) >> (i % 4 * 8));
-                    r_codes[e0 + i] = (char)((i < 4 ? raw.rc.x : raw.rc.y) >> (i % 4 * 8));
-                }
+                for (int i = 0; i < 8; ++i)
+                    if (e0 + i < n) {
+                        m_codes[e0 + i] = (char)((i < 4 ? mc.x : mc.y) >> (i % 4 * 8));
+                        r_codes[e0 + i] = (char)((i < 4 ? rc.x : rc.y) >> (i % 4 * 8));
+                    }
+            }
             if constexpr (!std::is_same<C, NoCopy>::value) store_some(static_cast<C *>(t.copy), e0, n, p);
         }
     }
@@ -291,7 +351,7 @@ __global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant_
 }
 
 template <typename P, typename G, typename C, class L>
-__global__ void __launch_bounds__(kThreads) adamw32_kernel(const __grid_constant__ L list, const __grid_constant__ StepArgs a) {
+__global__ void __launch_bounds__(kThreads32) adamw32_kernel(const __grid_constant__ L list, const __grid_constant__ StepArgs a) {
     const Scalars s = scalars(a);
     if (s.skip) return;
     const int index = entry_of(list, blockIdx.x);
@@ -305,7 +365,7 @@ __global__ void __launch_bounds__(kThreads) adamw32_kernel(const __grid_constant
     const float limit = fminf(Limit<P>::value, Limit<C>::value);
     bool ok = true;
     long long e0 = (long long)(blockIdx.x - list.first[index]) * kChunk32 + threadIdx.x * 8 - shift;
-    for (int step = 0; step < kSteps32; ++step, e0 += kThreads * 8) {
+    for (int step = 0; step < kSteps32; ++step, e0 += kThreads32 * 8) {
         if (e0 >= n) break;
         const bool whole = aligned && e0 >= 0 && e0 + 8 <= n;
         float p[8], g[8], m[8], v[8];
@@ -394,8 +454,8 @@ class Addresses {
 };
 
 template <typename P, typename G, typename C, int BITS, class L> int launch_list(const L &list, const StepArgs &a, unsigned chunks, cudaStream_t stream) {
-    if constexpr (BITS == 8) adamw8_kernel<P, G, C, L><<<chunks, kThreads, 0, stream>>>(list, a);
-    else adamw32_kernel<P, G, C, L><<<chunks, kThreads, 0, stream>>>(list, a);
+    if constexpr (BITS == 8) adamw8_kernel<P, G, C, L><<<chunks, kThreads8, 0, stream>>>(list, a);
+    else adamw32_kernel<P, G, C, L><<<chunks, kThreads32, 0, stream>>>(list, a);
     return launch_status();
 }
 
@@ -479,6 +539,7 @@ extern "C" int parle_adamw(const parle_adamw_tensor *tensors, int count, int par
     StepArgs a = {};
     a.b1 = (float)h.beta1; a.one_minus_b1 = (float)(1.0 - h.beta1);
     a.b2 = (float)h.beta2; a.one_minus_b2 = (float)(1.0 - h.beta2);
+    a.root_b2 = (float)sqrt(h.beta2); a.root_one_minus_b2 = (float)sqrt(1.0 - h.beta2);
     a.eps = (float)h.eps;
     a.log_b1 = log(h.beta1); a.log_b2 = log(h.beta2);    // (-inf for 0: b^t = 0)
     a.lr = h.lr; a.weight_decay = h.weight_decay; a.step = h.step;

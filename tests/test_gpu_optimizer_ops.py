@@ -141,9 +141,10 @@ class Case:
             m, v = oo.moments(g, m0, v0, f32(b1), f32(b2))
             m = m + (f32(1 - b1) - (1 - f32(b1))) * g       # (the complements are rounded from 1 - b)
             v = v + (f32(1 - b2) - (1 - f32(b2))) * g * g
-            # roundings: of the coefficient 4 u, of its product with g u, then of a product and a fused sum; the old 8-bit values have one more
+            # roundings: of the coefficient 4 u, of its product with 1 - b or its root and of that with g, doubled by the square; of the old 8-bit
+            # values: of sqrt(b2), of its product with the scale, of that with the code, doubled, and of the square; then of the sum
             m_off = (b1 * np.abs(m0) * 2 + (1 - b1) * np.abs(g) * 8) * U + np.abs(m) * U
-            v_off = (b2 * v0 * 4 + (1 - b2) * g * g * 14) * U + v * U
+            v_off = (b2 * v0 * (4 if self.bits == 32 else 8) + (1 - b2) * g * g * 15) * U + v * U
             den = np.sqrt(v / (1 - b2 ** step)) + eps
             rate = lr / (1 - b1 ** step)
             want = oo.param(p0, m, v, step, lr, b1, b2, eps, wd)
