@@ -30,9 +30,9 @@ constexpr int kBlock = 256;                              // elements that share 
 constexpr float kLargest = 448.f;                        // of e4m3
 constexpr float kNothing = 0x1p-100f;                    // a block whose values all lie below this holds zeros
 constexpr uint32_t kWeylI = 12664745, kWeylT = 9560335;  // 2^24 / p and 2^24 / p^2, p the plastic number; odd: all 2^24 thresholds occur
-constexpr int kSteps32 = 2, kSteps8 = 8;                 // groups of a thread in a chunk
+constexpr int kSteps32 = 2, kSteps8 = 4;                 // groups of a thread in a chunk
 constexpr int kChunk32 = kThreads32 * 8 * kSteps32, kChunk8 = kThreads8 * 8 * kSteps8;
-constexpr int kStages = 4;                               // of them in shared memory, 8-bit moments
+constexpr int kStages = 2;                               // of them in shared memory, 8-bit moments
 
 struct Entry {
     void *param, *exp_avg, *exp_avg_sq, *copy;
@@ -221,28 +221,36 @@ template <int BYTES> __device__ __forceinline__ void copy_async(void *to, const 
     else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
 }
 
-// Eight elements of each thread on their way to it, in shared memory; nobody reads another thread's.
+// Eight elements of each thread on their way, in shared memory.  Of 32-bit types a warp's 1024 bytes are fetched in two runs of 512: fetched as each
+// thread's own 32 bytes, every sector comes from L2 twice, as these copies pass L1 by (60 M fp32 parameters 191 us, so 144).  Threads of a warp read what
+// others fetched.
 template <typename P, typename G> struct Stage {
-    uint4 p[sizeof(P) / 2][kThreads8], g[sizeof(G) / 2][kThreads8];
+    static constexpr int kWarps = kThreads8 / 32;
+    uint4 p[kWarps][sizeof(P) / 2 * 32], g[kWarps][sizeof(G) / 2 * 32];
     uint2 mc[kThreads8], rc[kThreads8];
+    template <typename T> __device__ __forceinline__ static void fetch(uint4 *to, const T *from) {      // from: the thread's elements
+        const int lane = threadIdx.x % 32;
+        const uint4 *const first = reinterpret_cast<const uint4 *>(from - lane * 8);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) copy_async<16>(to + i * 32 + lane, first + i * 32 + lane);
+    }
     __device__ __forceinline__ void fetch(const Entry &t, long long e0) {
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(P) / 2; ++i) copy_async<16>(&p[i][threadIdx.x], reinterpret_cast<const uint4 *>(static_cast<const P *>(t.param) + e0) + i);
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(G) / 2; ++i) copy_async<16>(&g[i][threadIdx.x], reinterpret_cast<const uint4 *>(static_cast<const G *>(t.grad) + e0) + i);
+        fetch(p[threadIdx.x / 32], static_cast<const P *>(t.param) + e0);
+        fetch(g[threadIdx.x / 32], static_cast<const G *>(t.grad) + e0);
         copy_async<8>(&mc[threadIdx.x], static_cast<const char *>(t.exp_avg) + e0);
         copy_async<8>(&rc[threadIdx.x], static_cast<const char *>(t.exp_avg_sq) + e0);
     }
-    template <typename T> __device__ __forceinline__ static void take(const uint4 (*from)[kThreads8], float (&v)[8]) {
+    template <typename T> __device__ __forceinline__ static void take(const uint4 *from, float (&v)[8]) {
         Pack8<T> pack;
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(&pack)[i] = from[i][threadIdx.x];
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(&pack)[i] = from[threadIdx.x % 32 * (sizeof(T) / 2) + i];
         pack.get(v);
     }
 };
 
-// A chunk on 16-byte boundaries is fetched three steps ahead through shared memory (2.5 KB a warp and step for fp32 gradients and parameters): one step
-// ahead in registers left the kernel waiting for DRAM, as 62 to 72 registers a thread allow 24 to 28 warps an SM.
+// A chunk on 16-byte boundaries is fetched a step ahead through shared memory (one step ahead in registers, 62 to 72 of them a thread, it waited for DRAM:
+// 102 M bf16 parameters 282 us; without 347).  Measured in us, with 2 / 3 / 4 stages and chunks of four steps: 102 M bf16 176, 179, 187 (floor 159);
+// 60 M fp32 144, 144, 148 (149); 15 M fp32 40, 40, 45 (37); chunks of eight steps 15 M 55, of sixteen 67, as few blocks fill the SMs unevenly.
 template <typename P, typename G, typename C, class L>
 __global__ void __launch_bounds__(kThreads8) adamw8_kernel(const __grid_constant__ L list, const __grid_constant__ StepArgs a) {
     __shared__ Stage<P, G> stage[kStages];
@@ -273,11 +281,13 @@ __global__ void __launch_bounds__(kThreads8) adamw8_kernel(const __grid_constant
             if (step + kStages - 1 < kSteps8) stage[(step + kStages - 1) % kStages].fetch(t, e0 + (kStages - 1) * kThreads8 * 8);
             asm volatile("cp.async.commit_group;" ::: "memory");
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+            __syncwarp();                                // (what the others fetched is there)
             Stage<P, G> &now = stage[step % kStages];
             float p[8], g[8];
-            now.template take<P>(now.p, p);
-            now.template take<G>(now.g, g);
+            now.template take<P>(now.p[threadIdx.x / 32], p);
+            now.template take<G>(now.g[threadIdx.x / 32], g);
             uint2 mc = now.mc[threadIdx.x], rc = now.rc[threadIdx.x];
+            __syncwarp();                                // (it is read, before the next step fetches into this place)
             step8(a, s, limit, e0, __shfl_sync(0xffffffffu, scales, step), __shfl_sync(0xffffffffu, scales, 16 + step), p, g, mc, rc, n, true, &m_scale, &r_scale, ok);
             Pack8<P> pack;
             pack.set(p);
