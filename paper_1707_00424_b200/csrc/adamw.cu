@@ -431,7 +431,7 @@ __global__ void __launch_bounds__(kThreads32) adamw32_kernel(const __grid_consta
 
 // Whether an address occurs twice among those given to see().  Room for the addresses is on the stack for a list of one launch's size.
 class Addresses {
-    static constexpr int kSmall = 4096;
+    static constexpr int kSmall = 4096;                  // (of which a short list uses less)
     uintptr_t small_[kSmall];
     uintptr_t *slot_ = small_;
     size_t mask_ = kSmall - 1;
@@ -441,7 +441,7 @@ class Addresses {
         if (slot_ != small_) free(slot_);
     }
     bool prepare(size_t addresses) {
-        size_t slots = kSmall;
+        size_t slots = 64;
         while (slots < 2 * addresses) slots *= 2;
         if (slots > kSmall && !(slot_ = static_cast<uintptr_t *>(malloc(slots * sizeof(uintptr_t))))) {
             slot_ = small_;
@@ -524,25 +524,24 @@ extern "C" int parle_adamw(const parle_adamw_tensor *tensors, int count, int par
     if (reinterpret_cast<uintptr_t>(h.norm) % 4 || reinterpret_cast<uintptr_t>(h.lr_dev) % 4 || reinterpret_cast<uintptr_t>(h.step_dev) % 8 ||
         reinterpret_cast<uintptr_t>(flags) % 4) return PARLE_EALIGN;
     const bool copies = copy_dtype != PARLE_NO_COPY;
+    // The same array twice would be stepped by two blocks at once.
+    Addresses seen;
+    if (count > (1 << 26) || !seen.prepare((size_t)count * (3 + copies + (state_bits == 8 ? 2 : 0)))) return PARLE_ETOOBIG;
+    const uintptr_t param_mask = dtype_bytes(param_dtype) - 1, grad_mask = dtype_bytes(grad_dtype) - 1;
     for (int i = 0; i < count; ++i) {
         const parle_adamw_tensor &t = tensors[i];
-        if (t.size < 0) return PARLE_EINVAL;
-        if (t.size == 0) continue;
+        if (t.size <= 0) {
+            if (t.size < 0) return PARLE_EINVAL;
+            continue;
+        }
         if (t.size > PARLE_TOKEN_MAX_ELEMENTS) return PARLE_ETOOBIG;
         if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq || (copies && !t.copy)) return PARLE_EINVAL;
         if (state_bits == 8 && (!t.exp_avg_scale || !t.exp_avg_sq_scale)) return PARLE_EINVAL;
-        uintptr_t off = reinterpret_cast<uintptr_t>(t.param) % dtype_bytes(param_dtype) | reinterpret_cast<uintptr_t>(t.grad) % dtype_bytes(grad_dtype);
-        if (copies) off |= reinterpret_cast<uintptr_t>(t.copy) % 2;
-        if (state_bits == 32) off |= (reinterpret_cast<uintptr_t>(t.exp_avg) | reinterpret_cast<uintptr_t>(t.exp_avg_sq)) % 4;
-        else off |= (reinterpret_cast<uintptr_t>(t.exp_avg_scale) | reinterpret_cast<uintptr_t>(t.exp_avg_sq_scale)) % 4;
+        uintptr_t off = (reinterpret_cast<uintptr_t>(t.param) & param_mask) | (reinterpret_cast<uintptr_t>(t.grad) & grad_mask);
+        if (copies) off |= reinterpret_cast<uintptr_t>(t.copy) & 1;
+        if (state_bits == 32) off |= (reinterpret_cast<uintptr_t>(t.exp_avg) | reinterpret_cast<uintptr_t>(t.exp_avg_sq)) & 3;
+        else off |= (reinterpret_cast<uintptr_t>(t.exp_avg_scale) | reinterpret_cast<uintptr_t>(t.exp_avg_sq_scale)) & 3;
         if (off) return PARLE_EALIGN;
-    }
-    // The same array twice would be stepped by two blocks at once.
-    Addresses seen;
-    if (count > (1 << 26) || !seen.prepare((size_t)count * 6)) return PARLE_ETOOBIG;
-    for (int i = 0; i < count; ++i) {
-        const parle_adamw_tensor &t = tensors[i];
-        if (t.size == 0) continue;
         if (seen.see(t.param) || seen.see(t.exp_avg) || seen.see(t.exp_avg_sq) || (copies && seen.see(t.copy))) return PARLE_EINVAL;
         if (state_bits == 8 && (seen.see(t.exp_avg_scale) || seen.see(t.exp_avg_sq_scale))) return PARLE_EINVAL;
     }

@@ -29,7 +29,7 @@ template <int CAP> struct List {
     uint32_t first[CAP];
     Entry entry[CAP];
 };
-constexpr int kFew = 96, kMany = 1600;                   // a launch takes 32764 bytes of arguments at most
+constexpr int kFew = 96, kSome = 400, kMany = 1600;      // a launch takes 32764 bytes of arguments at most, and 2 us more with that many
 
 // The sum of a block's numbers, in thread 0; the same order always.
 template <int THREADS> __device__ __forceinline__ double block_sum(double v) {
@@ -153,7 +153,8 @@ extern "C" int parle_grad_norm(const parle_grad_tensor *tensors, int count, int 
     long long written = 0;
     const int rc = with_dtype(grad_dtype, [&](auto *g) {
         using G = std::remove_pointer_t<decltype(g)>;
-        return count <= kFew ? launch_all<kFew, G>(tensors, count, partial, &written, stream) : launch_all<kMany, G>(tensors, count, partial, &written, stream);
+        return count <= kFew ? launch_all<kFew, G>(tensors, count, partial, &written, stream)
+             : count <= kSome ? launch_all<kSome, G>(tensors, count, partial, &written, stream) : launch_all<kMany, G>(tensors, count, partial, &written, stream);
     });
     if (rc != PARLE_OK) return rc;
     norm_finish_kernel<<<1, kFinish, 0, stream>>>(partial, written, norm);

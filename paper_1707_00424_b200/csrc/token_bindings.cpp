@@ -485,11 +485,12 @@ struct Tensors {
     PyObject *object(Py_ssize_t i) const { return items[i]; }
 };
 
-// The tensors of a list, checked: all of this type, contiguous, on the call's device, of the shapes of `like`'s if that is given; their
-// addresses go to place(i, tensor, address).  A list of some hundreds is checked faster than its kernel runs only if its objects, which lie
+// The tensors of a list, checked: all of this type, contiguous, on the call's device, of the shapes of `like`'s if that is given; each
+// goes to place(i, number of elements, tensor).  A list of some hundreds is checked faster than its kernel runs only if its objects, which lie
 // anywhere, are fetched ahead.
 template <class F> void members(const Call &c, const char *what, const Tensors &list, at::ScalarType type, const Tensors *like, F place) {
     const caffe2::TypeMeta meta = c10::scalarTypeToTypeMeta(type);
+    const c10::Device device(at::kCUDA, (c10::DeviceIndex)c.index);
     constexpr Py_ssize_t kAhead = 4;
     for (Py_ssize_t i = 0; i < list.n; ++i) {
         if (i + 2 * kAhead < list.n) __builtin_prefetch(list.items[i + 2 * kAhead]);
@@ -500,12 +501,12 @@ template <class F> void members(const Call &c, const char *what, const Tensors &
         const at::Tensor &t = c.tensor(what, list.items[i]);
         const at::TensorImpl *const impl = t.unsafeGetTensorImpl();
         const at::Tensor *const same = like ? &THPVariable_Unpack(like->items[i]) : nullptr;
-        if (t.dtype() != meta || !t.is_contiguous() || !t.is_cuda() || t.get_device() != c.index || (same && impl->sizes() != same->sizes())) {
+        if (impl->dtype() != meta || !impl->is_contiguous() || impl->device() != device || (same && impl->sizes() != same->sizes())) {
             const std::string name = std::string(what) + "[" + std::to_string(i) + "]";
             c.here(name.c_str(), t);
             c.refuse(name + " is " + Call::describe(t) + ": a contiguous " + c10::toString(type) + " tensor" + (same ? " like " + Call::describe(*same) : "") + " is needed");
         }
-        place(i, (long long)t.numel(), t.data_ptr());
+        place(i, (long long)impl->numel(), t);
     }
 }
 
@@ -529,7 +530,7 @@ PyObject *grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     const at::ScalarType type = first.scalar_type();
     const int dtype = c.dtype("grads[0]", first);
     std::vector<parle_grad_tensor> list((size_t)grads.n);
-    members(c, "grads", grads, type, nullptr, [&](Py_ssize_t i, long long size, void *p) { list[i] = {p, size}; });
+    members(c, "grads", grads, type, nullptr, [&](Py_ssize_t i, long long size, const at::Tensor &g) { list[i] = {g.const_data_ptr(), size}; });
     Result out(a[1]);
     if (!out.given) out.made = c.make({}, at::kFloat);
     float *const norm = (float *)c.word("out", out.given ? out.given : Py_None, at::kFloat, at::kFloat);
@@ -589,18 +590,20 @@ PyObject *adamw(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
         if (copy_dtype == PARLE_F32 || param_dtype != PARLE_F32) c.refuse("copies are 16-bit ones of fp32 params");
     }
     std::vector<parle_adamw_tensor> list((size_t)params.n);
-    members(c, names[0], params, types[0], nullptr, [&](Py_ssize_t i, long long size, void *p) { list[i] = {p, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, size}; });
-    members(c, names[1], lists[1], types[1], &params, [&](Py_ssize_t i, long long, void *p) { list[i].grad = p; });
-    members(c, names[2], lists[2], types[2], &params, [&](Py_ssize_t i, long long, void *p) { list[i].exp_avg = p; });
-    members(c, names[3], lists[3], types[3], &params, [&](Py_ssize_t i, long long, void *p) { list[i].exp_avg_sq = p; });
+    members(c, names[0], params, types[0], nullptr, [&](Py_ssize_t i, long long size, const at::Tensor &p) {
+        list[i] = {p.data_ptr(), nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, size};
+    });
+    members(c, names[1], lists[1], types[1], &params, [&](Py_ssize_t i, long long, const at::Tensor &g) { list[i].grad = g.const_data_ptr(); });
+    members(c, names[2], lists[2], types[2], &params, [&](Py_ssize_t i, long long, const at::Tensor &m) { list[i].exp_avg = m.data_ptr(); });
+    members(c, names[3], lists[3], types[3], &params, [&](Py_ssize_t i, long long, const at::Tensor &v) { list[i].exp_avg_sq = v.data_ptr(); });
     for (int k = 4; k < 6; ++k)
-        members(c, names[k], lists[k], types[k], nullptr, [&](Py_ssize_t i, long long scales, void *p) {
+        members(c, names[k], lists[k], types[k], nullptr, [&](Py_ssize_t i, long long scales, const at::Tensor &s) {
             if (scales != (list[i].size + PARLE_ADAMW_BLOCK - 1) / PARLE_ADAMW_BLOCK)
                 c.refuse(std::string(names[k]) + "[" + std::to_string(i) + "] has " + std::to_string(scales) + " numbers: one for each " + std::to_string(PARLE_ADAMW_BLOCK) + " of " +
                          std::to_string(list[i].size) + " elements is needed");
-            (k == 4 ? list[i].exp_avg_scale : list[i].exp_avg_sq_scale) = (float *)p;
+            (k == 4 ? list[i].exp_avg_scale : list[i].exp_avg_sq_scale) = (float *)s.data_ptr();
         });
-    members(c, names[6], lists[6], lists[6] ? types[6] : at::kFloat, &params, [&](Py_ssize_t i, long long, void *p) { list[i].copy = p; });
+    members(c, names[6], lists[6], lists[6] ? types[6] : at::kFloat, &params, [&](Py_ssize_t i, long long, const at::Tensor &copy) { list[i].copy = copy.data_ptr(); });
     parle_adamw_step h;
     h.step = c.integer("step", a[7], 0, LLONG_MAX);
     h.lr = c.number("lr", a[8]);
