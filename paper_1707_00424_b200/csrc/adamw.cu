@@ -4,8 +4,8 @@
 //   g = c grad,  m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p = (1 - lr wd) p - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
 //
 // Every element is read once and written once: bound by DRAM, 28 bytes an fp32 element with 32-bit moments, 10 to 16 with 8-bit ones.
-// All arithmetic is fp32; the root and the reciprocal are the hardware's (2^-22 of the step, which moves p by far less than p's own
-// rounding).
+// All arithmetic is fp32; in the step of p the root (of 32-bit moments) and the reciprocal are the hardware's (2^-22 of the step, which moves p by
+// far less than p's own rounding).
 //
 // 8-bit moments.  256 elements, a warp's eight a lane, share an fp32 scale; codes are e4m3 (range 2^-9 .. 448) of m and of r = sqrt(v),
 // whose range is half of v's in powers of two.  A code's neighbours are 6 to 12 % away, but b2 = 0.999 moves v by 0.1 % a step: rounded to
@@ -48,8 +48,7 @@ template <int CAP> struct List {
 constexpr int kFew = 24, kMany = 440;                    // a launch takes 32764 bytes of arguments at most
 
 struct StepArgs {
-    float b1, one_minus_b1, b2, one_minus_b2, eps;
-    float root_b2, root_one_minus_b2;
+    float b1, one_minus_b1, b2, one_minus_b2, eps, minus_zero;
     float rate, root_scale, decay;                       // lr / (1 - b1^t), 1 / sqrt(1 - b2^t), 1 - lr wd, where neither step_dev nor lr_dev is given
     float grad_scale, max_norm;
     double lr, weight_decay, log_b1, log_b2;
@@ -77,9 +76,9 @@ __device__ __forceinline__ float root(float v) {
     asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-__device__ __forceinline__ float coarse_root(float v) { // 0 below 2^-126
+__device__ __forceinline__ float inverse_root(float v) {
     float r;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
 __device__ __forceinline__ float larger(float v, float w) {      // NaN if either is
@@ -112,7 +111,7 @@ __device__ __forceinline__ Scalars scalars(const StepArgs &a) {
     if (a.norm) {
         const float norm = *a.norm;
         s.skip = !(fabsf(norm) < INFINITY);
-        s.c *= fminf(1.f, __fdiv_rn(a.max_norm, norm * a.grad_scale));
+        s.c *= fminf(1.f, __fmul_rn(__frcp_rn(norm * a.grad_scale), a.max_norm));
         if (s.skip && a.flags && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.flags, PARLE_FLAG_NONFINITE);
     }
     return s;
@@ -131,18 +130,18 @@ __device__ __forceinline__ uint32_t top_bytes(const uint32_t *t) {
     return __byte_perm(__byte_perm(t[0], t[1], 0x0073), __byte_perm(t[2], t[3], 0x0073), 0x5410);
 }
 
-// The scale of a block of a warp from the largest magnitude of each lane (NaN if one is); factor: what values are multiplied by to lie in
-// [0, 448] 2^-120 (rounded down: no product is above).  Values from 2^14 on are scaled first, so that the factor is no subnormal number.
+// The scale of a block of a warp from the largest magnitude of each lane (NaN if one is); factor: 448 (1 / largest) 2^-120, by which values come to
+// lie in [0, 448] 2^-120 or a rounding above.  Values from 2^14 on are scaled first, so that the factor is no subnormal number.
 __device__ __forceinline__ float block_scale(float largest, float (&x)[8], float *factor) {
     float top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(largest)));      // (as bits, what is no number is largest)
     const bool none = top < kNothing, finite = top < INFINITY;
-    const float scale = none ? 0.f : finite ? __fdiv_rn(top, kLargest) : NAN;
+    const float scale = none ? 0.f : finite ? __fmul_rn(top, 1.f / kLargest) : NAN;
     if (top >= 0x1p14f) {
-        top *= 0x1p-120f;
+        top = __fmul_rn(top, 0x1p-120f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] *= 0x1p-120f;
-        *factor = finite ? __fdiv_rd(kLargest * 0x1p-120f, top) : 0.f;
-    } else *factor = none ? 0.f : __fdiv_rd(kLargest * 0x1p-120f, top);
+        for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(x[i], 0x1p-120f);
+    }
+    *factor = none || !finite ? 0.f : __fmul_rn(__fmul_rn(__frcp_rn(top), kLargest), 0x1p-120f);
     return scale;
 }
 
@@ -159,36 +158,47 @@ __device__ __forceinline__ Two mul(Two a, Two b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(t) : "l"(a), "l"(b));
     return t;
 }
+__device__ __forceinline__ Two add(Two a, Two b) {
+    Two t;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(t) : "l"(a), "l"(b));
+    return t;
+}
 __device__ __forceinline__ Two mul_add(Two a, Two b, Two c) {
     Two t;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(t) : "l"(a), "l"(b), "l"(c));
     return t;
 }
 
-// One step of eight elements with moments in 8 bits, a whole warp's block: mc and rc come as the old codes and go as the new ones.  The old
-// moments' factors b1 and sqrt(b2) go into their scales, c and the roots of the new ones' into what g is multiplied by.
+// One step of eight elements with moments in 8 bits, a whole warp's block: mc and rc come as the old codes and go as the new ones.
+// The moments, their root and what the codes are taken from are rounded after every operation, to nearest: a value next to the border
+// between two codes falls to one side in any implementation of these operations, so that codes can be compared.  (Fused and with the hardware's
+// root: 102 M bf16 parameters 174 us.)
 __device__ __forceinline__ void step8(const StepArgs &a, const Scalars &s, float limit, long long e0, float m_scale, float r_scale, float (&p)[8], const float (&g)[8], uint2 &mc, uint2 &rc,
                                       long long n, bool whole, float *new_m_scale, float *new_r_scale, bool &ok) {
     float m[8], r[8], m_top = 0.f, r_top = 0.f;
-    const float ms = m_scale * a.b1, rs = r_scale * a.root_b2, k1 = s.c * a.one_minus_b1, k2 = s.c * a.root_one_minus_b2;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 cm = decode2((i < 2 ? mc.x : mc.y) >> (i % 2 * 16)), cr = decode2((i < 2 ? rc.x : rc.y) >> (i % 2 * 16));
-        Two old_m = mul(two(cm.x, cm.y), two(ms, ms)), old_r = mul(two(cr.x, cr.y), two(rs, rs));
+        Two old_m = mul(two(cm.x, cm.y), two(m_scale, m_scale)), old_r = mul(two(cr.x, cr.y), two(r_scale, r_scale));
+        float x, y;
         if (!whole) {                                    // (a scale may be NaN: behind the end there are zeros all the same)
-            float x, y;
             const bool first = e0 + 2 * i < n, second = e0 + 2 * i + 1 < n;
             split(old_m, x, y);
             old_m = two(first ? x : 0.f, second ? y : 0.f);
             split(old_r, x, y);
             old_r = two(first ? x : 0.f, second ? y : 0.f);
         }
-        const Two gg = two(g[2 * i], g[2 * i + 1]), new_m = mul_add(gg, two(k1, k1), old_m), more = mul(gg, two(k2, k2)), v = mul_add(more, more, mul(old_r, old_r));
-        float x, y;
+        const Two gg = mul(two(g[2 * i], g[2 * i + 1]), two(s.c, s.c));
+        const Two zero = two(a.minus_zero, a.minus_zero);      // (products to be added: the assembler makes one operation of mul.rn.f32x2 and add.rn.f32x2)
+        const Two new_m = add(mul_add(old_m, two(a.b1, a.b1), zero), mul_add(gg, two(a.one_minus_b1, a.one_minus_b1), zero));
+        const Two v = add(mul_add(mul(old_r, old_r), two(a.b2, a.b2), zero), mul_add(mul(gg, gg), two(a.one_minus_b2, a.one_minus_b2), zero));
+        // The root by one of Newton's steps with the exact remainder (Markstein, "Computation of elementary functions on the IBM RISC System/6000
+        // processor", 1990): to nearest but for one number in millions.
         split(v, x, y);
-        r[2 * i] = coarse_root(x);
-        r[2 * i + 1] = coarse_root(y);
-        split(mul_add(two(r[2 * i], r[2 * i + 1]), two(s.root_scale, s.root_scale), two(a.eps, a.eps)), x, y);
+        const Two inverse = two(inverse_root(fmaxf(x, 0x1p-126f)), inverse_root(fmaxf(y, 0x1p-126f))), guess = mul(v, inverse);
+        const Two rest = mul_add(mul(guess, two(-1.f, -1.f)), guess, v), root = mul_add(rest, mul(inverse, two(0.5f, 0.5f)), guess);
+        split(root, r[2 * i], r[2 * i + 1]);
+        split(mul_add(root, two(s.root_scale, s.root_scale), two(a.eps, a.eps)), x, y);
         const Two ratio = mul(new_m, two(reciprocal(x), reciprocal(y)));
         split(mul_add(two(p[2 * i], p[2 * i + 1]), two(s.decay, s.decay), mul(ratio, two(-s.rate, -s.rate))), p[2 * i], p[2 * i + 1]);
         split(new_m, m[2 * i], m[2 * i + 1]);
@@ -208,8 +218,8 @@ __device__ __forceinline__ void step8(const StepArgs &a, const Scalars &s, float
     for (int i = 0; i < 8; ++i) {
         const uint32_t u = (first + i * kWeylI) & 0xffffffu;
         // (__fmul_rn: products written with * came out as zeros from CUDA 12.9's assembler at its default level)
-        mt[i] = code_above(__fmul_rn(fabsf(m[i]), m_factor), u) | (__float_as_uint(m[i]) & 0x80000000u);
-        rt[i] = code_above(__fmul_rn(r[i], r_factor), u ^ 0xffffffu);
+        mt[i] = code_above(fminf(__fmul_rn(fabsf(m[i]), m_factor), kLargest * 0x1p-120f), u) | (__float_as_uint(m[i]) & 0x80000000u);
+        rt[i] = code_above(fminf(__fmul_rn(r[i], r_factor), kLargest * 0x1p-120f), u ^ 0xffffffu);
         if (r[i] > 0.f) rt[i] = max(rt[i], 1u << 24);    // else m would be divided by eps alone one day
     }
     mc = make_uint2(top_bytes(mt), top_bytes(mt + 4));
@@ -548,8 +558,8 @@ extern "C" int parle_adamw(const parle_adamw_tensor *tensors, int count, int par
     StepArgs a = {};
     a.b1 = (float)h.beta1; a.one_minus_b1 = (float)(1.0 - h.beta1);
     a.b2 = (float)h.beta2; a.one_minus_b2 = (float)(1.0 - h.beta2);
-    a.root_b2 = (float)sqrt(h.beta2); a.root_one_minus_b2 = (float)sqrt(1.0 - h.beta2);
     a.eps = (float)h.eps;
+    a.minus_zero = -0.f;
     a.log_b1 = log(h.beta1); a.log_b2 = log(h.beta2);    // (-inf for 0: b^t = 0)
     a.lr = h.lr; a.weight_decay = h.weight_decay; a.step = h.step;
     if (!h.step_dev) {

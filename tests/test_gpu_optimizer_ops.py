@@ -235,6 +235,40 @@ def test_a_second_moment_in_8_bits_that_moves_slowly_arrives():
     assert abs(r.mean() - exact) < 0.03 and np.abs(r - exact).max() < 0.25
 
 
+def test_moments_in_8_bits_are_those_of_single_operations_bit_for_bit():
+    """Each operation rounded to nearest in fp32 by numpy: the same codes and scales, over steps in which one difference would grow."""
+    f = np.float32
+    g = torch.Generator().manual_seed(21)
+    n, (b1, b2) = 70000, (0.9, 0.999)
+    p = [torch.zeros(n, device=DEV)]
+    m, v, ms, vs = pb.adamw_state(p, 8)
+    mc, rc, m_scale, r_scale = np.zeros(n, f), np.zeros(n, f), np.zeros(-(-n // 256), f), np.zeros(-(-n // 256), f)
+    wide = lambda s: np.repeat(s, 256)[:n]                  # noqa: E731
+    for t in range(1, 6):
+        grad = (torch.randn(n, generator=g) * torch.exp(2 * torch.randn(n, generator=g))).to(DEV)
+        grad[1000:1400] = 0.0
+        pb.adamw(p, [grad], m, v, step=t, lr=1e-3, betas=(b1, b2), exp_avg_scales=ms, exp_avg_sq_scales=vs)
+        x = grad.cpu().numpy()
+        old, root = mc * wide(m_scale), rc * wide(r_scale)
+        first = old * f(b1) + x * f(1 - b1)
+        second = np.sqrt(root * root * f(b2) + x * x * f(1 - b2))
+        u = oo.thresholds(n, t).astype(np.float64)
+        for what, value, threshold, codes, scales in (("m", first, u, m, ms), ("r", second, (1 << 24) - 1 - u, v, vs)):
+            top = np.array([np.abs(b).max() for b in oo.blocks(value)], f)
+            with np.errstate(divide="ignore"):
+                y = np.minimum(np.abs(value) * wide(np.where(top < f(2.0 ** -100), f(0), f(448) * (f(1) / top))), f(448)).astype(np.float64)
+            apart = np.exp2(np.maximum(np.floor(np.log2(np.maximum(y, 2.0 ** -20))), -6) - 3)
+            code = (np.floor(y / apart + threshold / (1 << 24)) * apart * np.sign(value)).astype(f)
+            if what == "r":
+                code = np.where(value > 0, np.maximum(code, f(2.0 ** -9)), f(0))
+            scale = np.where(top < f(2.0 ** -100), f(0), top * f(1 / f(448)))
+            assert np.array_equal(codes[0].float().cpu().numpy(), code) and np.array_equal(scales[0].cpu().numpy(), scale), (t, what)
+            if what == "m":
+                mc, m_scale = code, scale
+            else:
+                rc, r_scale = code, scale
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_clipped_and_scaled_gradients(bits):
     case = Case((3000, 17), torch.float32, torch.float16, bits, seed=6)
