@@ -5,13 +5,22 @@
 // at which the sum of kept weights exceeds u times their total.
 //
 // A token is right or wrong, and with 10^5 tokens u lies within 10^-6 of one of the sums' steps in every tenth row: sums of fp32
-// exponentials would give another token there than the definition.  So weights are formed in fp64, 2^(k/32) from a table times a
-// polynomial of degree 5 (Taylor's, to 3 10^-15), and kept as whole numbers of 2^-44: their sums are exact and the same in any order, whichever
-// threads and atomics form them.  u times the total is formed exactly, too (128 bits).
+// exponentials would give another token there than the definition.  So weights are formed in fp64 (nine operations) and kept as whole
+// numbers of 2^-44: their sums are exact and the same in any order, whichever threads and atomics form them.  u times the total is formed exactly,
+// too (128 bits).  fp32 sums serve where their error, which is bounded, does not matter.
 //
-// T is found by histograms: first of scale (m - x) in steps of 1/32, then of the logits' bits within the step that holds the border, 11
-// bits at a time.  A bin's 64-bit sum is two 32-bit words in shared memory, the carry passed on by the adding thread.  A row is read by
-// one block, or by a cluster of up to eight where there are few rows.
+// A row is read by one block of 512 threads, or by a cluster of up to eight where there are few rows (of 128 threads up to 4096 tokens), two
+// blocks an SM (one, with twice the registers, took 1.2 to 1.3 times as long).  By what is asked for:
+//   top_k up to 256, min_p, top_p that is reached by as many: one pass over the row finds its largest logit and lists the logits from a
+//     bound on, which the largest logits of the threads' first granules give; the list is sorted and decides everything.  512 rows of 131072 bf16
+//     logits with all three 73 us: DRAM, then sorting while DRAM rests (the floor is 21 us).  One row 13 us: latency of a cluster's eight joins.
+//   nothing: one pass that forms all weights, relative to the guess that the first granules give, and their sums by segments of 256 logits; the
+//     segment and the token by sums of sums.  256 rows of 131072 bf16 logits 76 us: issue slots (fp64 takes 20 us of its pipe).
+//   top_p of an undecided model, larger top_k: logits are counted by steps of scale (m - x), 1/128 wide, which tells nearly where the border lies;
+//     one more pass forms the weights, their exact total and segments' sums, and lists the logits around the border.  256 rows with top_p = 0.95,
+//     25000 tokens kept, 202 us: a fifth the counts, two fifths the weights.
+//   what escapes these (thousands of equal logits at the border, a wrong guess): exact histograms of 64-bit sums, of which two 32-bit words lie
+//     in shared memory and the adding thread passes on the carry, of steps of scale (m - x) and then of the logits' bits, 11 at a time.
 #include <math.h>
 
 #include <type_traits>
@@ -1229,21 +1238,23 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
         const u64 one = (u64)__double_as_longlong(s.weigh.one);
         if (unlimited) {
             // All logits are kept.  Where the largest one is not known yet, weights are relative to the guess, and the largest logit is found beside
-            // them; the sums stand if they fit (below 2^62), else they are formed again.
+            // them.  The sums stand if eight weights fit into 64 bits (w < e^11) and so do all (their fp64 sum is below 2^62), else they are formed again.
             for (;;) {
                 sum = 0.0;
                 s.each_segment(a.seg_steps, [&](int g, const Pack8<T> &p, const float (&v)[8], u64 &m) {
                     const float most = g >= end ? -INFINITY : row.flat ? best : row.most(p, g);
                     mine = largest(mine, most);
+                    u64 part = 0;
                     if (most > s.weigh.most) {
 #pragma unroll 1
-                        for (int k = 0; k < 8; ++k) m += s.weigh(row.at(row.first(g) + k));
+                        for (int k = 0; k < 8; ++k) part += s.weigh(row.at(row.first(g) + k));
                     } else {
-                        u64 part = 0;
 #pragma unroll
                         for (int k = 0; k < 8; ++k) part += s.weigh.raw(fmaxf(v[k], s.weigh.least));
-                        m += part - 8 * one;
+                        part -= 8 * one;
                     }
+                    m += part;
+                    sum += (double)part;
 #pragma unroll
                     for (int k = 0; k < 8; ++k) count += v[k] > -INFINITY;
                 }, [&](int g, u64 m) {
@@ -1251,10 +1262,11 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
                         sh.seg.mass[g] = m;
                         sh.seg.ties[g] = 0;
                         mass += m;
-                        sum += (double)m;
                     }
                 });
                 if (!rest || blind) break;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
                 if (lane == 0) sh.scan_f[warp] = sum;
                 const float top = s.all_largest(mine);   // (a barrier between)
                 if (!(fabsf(top) < INFINITY)) {
@@ -1271,7 +1283,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
                 sum = 0.0;
                 s.of_blocks([](const Shared<THREADS> &b) { return b.part.sum; }, [&](int, double p) { sum += p; });
                 all_meet(blocks);
-                if (((double)top - best) * scale < 12.0 && sum < 0x1p62) break;
+                if (((double)top - best) * scale < 11.0 && sum < 0x1p62) break;
                 s.best = best = top;
                 s.weigh.set(best, scale, a.frac_bits, sh.table);
                 mass = 0;

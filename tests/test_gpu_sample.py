@@ -140,6 +140,23 @@ def test_random_numbers_at_the_ends():
             check(x.expand(len(tiny), vocab), u, **limits)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("apart", [0.5, 3.0, 6.0, 10.0, 10.9, 11.1, 14.0, 60.0, 1000.0])
+def test_rows_whose_beginning_says_little_about_the_rest(dtype, apart):
+    """The first logits are lower, or higher, than all others by some nats: what is guessed from them is wrong."""
+    g = torch.Generator().manual_seed(30)
+    for vocab in (20000, 131072, 300007):
+        x = torch.randn(4, vocab, generator=g) * 0.3
+        x[0, vocab // 3:] += apart
+        x[1, :vocab // 3] += apart
+        x[2, vocab - 5000:] += apart
+        x[3, -1] += apart
+        x = x.to(dtype).to(DEV)
+        u = torch.rand(4, generator=g).to(DEV)
+        for limits in ({}, dict(top_k=40), dict(top_p=0.9), dict(min_p=0.3), dict(top_k=200, top_p=0.8, min_p=0.01)):
+            check(x, u, **limits, most_near=0.25)
+
+
 def test_logits_of_any_size_and_extreme_temperatures():
     g = torch.Generator().manual_seed(10)
     u = torch.rand(6, generator=g).to(DEV)
