@@ -31,7 +31,12 @@ using namespace parle;
 
 namespace {
 
-constexpr int kBins = 2048, kSegments = 1024, kList = 1024;
+// Entries of the list, bins of a histogram and segments of a block's part, for blocks of long and of short rows (of which fewer logits fall into
+// a coarser bin, and 128 threads sort a long list slowly).
+template <int THREADS> struct Sizes {
+    static constexpr int kList = THREADS == 512 ? 1024 : 256;
+    static constexpr int kLogBins = THREADS == 512 ? 11 : 9, kBins = 1 << kLogBins, kSegments = THREADS == 512 ? 1024 : 128;
+};
 constexpr uint32_t kNegInf = 0x007fffffu;                // key of -inf
 
 struct SampleArgs {
@@ -206,12 +211,13 @@ enum Outcome { kDone, kNeedTotal, kNeedAll };            // of a list of the lar
 enum Settled { kNot, kSums, kCutOnly };                  // a border was not found; with the segments' sums; without them
 
 template <int THREADS> struct Shared {
+    static constexpr int kBins = Sizes<THREADS>::kBins, kSegments = Sizes<THREADS>::kSegments, kList = Sizes<THREADS>::kList;
     double table[32];
     union alignas(16) {
         uint32_t hist[2][kBins];
         struct {
             u64 mass[kSegments];
-            uint32_t ties[kSegments];
+            uint32_t ties[kList];                        // (of segments; or the keys of list entries)
         } seg;
     };
     alignas(16) u64 list[kList];                                     // ~key << 32 | token
@@ -280,14 +286,14 @@ template <int THREADS> __device__ __forceinline__ u64 block_scan(u64 v, u64 (&sc
 }
 
 template <typename T, int THREADS> struct Sampler {
-    static constexpr int kPer = kBins / THREADS;
+    static constexpr int kList = Sizes<THREADS>::kList, kLogBins = Sizes<THREADS>::kLogBins, kBins = Sizes<THREADS>::kBins, kPer = kBins / THREADS;
     Shared<THREADS> &sh;
     Row<T> row;
     int blocks, rank, begin, end;                        // the row's blocks; this one's granules
     float scale, best;
     Weigher weigh;
 
-    __device__ __forceinline__ int step_of(float x) const { return min(kBins - 1, (int)((best - x) * scale * 32.f)); }
+    __device__ __forceinline__ int step_of(float x) const { return min(kBins - 1, (int)((best - x) * scale * (kBins / 64.f))); }
 
     __device__ __forceinline__ Shared<THREADS> *block(int o) const { return blocks == 1 ? &sh : at_rank(&sh, o); }
     // f(o, value(block o)) for the row's blocks: a word of another block's shared memory takes some 200 ns, so all are fetched first.
@@ -529,7 +535,7 @@ template <typename T, int THREADS> struct Sampler {
         uint32_t low = sh.found.low, high = sh.found.high;
         for (;;) {
             const uint32_t range = high - low;
-            const int shift = max(0, 32 - __clz(range) - 11);      // (range >> shift) < 2048
+            const int shift = max(0, 32 - __clz(range) - kLogBins);      // (range >> shift) < kBins
             clear();
             each([&](float x) {
                 const uint32_t key = key_of(x);
@@ -724,9 +730,10 @@ template <typename T, int THREADS> struct Sampler {
         return kDone;
     }
 
-    // Steps of 1/128 for counts.
+    // Steps for counts: of 1/128, or 1/32 for short rows.
     static constexpr int kCounts = 2 * kBins;
-    __device__ __forceinline__ float count_place_of(float x) const { return fminf((best - x) * scale * 128.f, kCounts - 1); }
+    static constexpr float kPerNat = kCounts / 32.f;
+    __device__ __forceinline__ float count_place_of(float x) const { return fminf((best - x) * scale * kPerNat, kCounts - 1); }
     __device__ __forceinline__ int count_step_of(float x) const { return (int)count_place_of(x); }
     // The smallest key above `floor` of a step up to `step`.
     __device__ __forceinline__ uint32_t first_key(uint32_t floor, int step) const {
@@ -796,13 +803,13 @@ template <typename T, int THREADS> struct Sampler {
         }
         const u64 before = known + block_scan<THREADS>(sum, sh.scan, &count);
         if (top_p < 1.f) {
-            const auto weight = [&](float step) { return exp2f(step * (-1.44269504f / 128)) * 0x1p30f; };
+            const auto weight = [&](float step) { return exp2f(step * (-1.44269504f / kPerNat)) * 0x1p30f; };
             u64 part[2 * kPer], sum = 0, all;
 #pragma unroll
             for (int i = 0; i < 2 * kPer; ++i) sum += part[i] = (u64)(n[i] * weight(threadIdx.x * 2 * kPer + i + place[i]));
             u64 at = known_sum + block_scan<THREADS>(sum, sh.scan, &all);
             all += known_sum;
-            const u64 tied = ties * (u64)weight((best - floor_value) * scale * 128.f);
+            const u64 tied = ties * (u64)weight((best - floor_value) * scale * kPerNat);
             const u64 goal = part_of(known_total ? known_total : all + tied, top_p, true), low = max((u64)1, goal - (goal >> 13)), high = max((u64)1, min(goal + (goal >> 13), all));
 #pragma unroll
             for (int i = 0; i < 2 * kPer; ++i) {
@@ -984,8 +991,9 @@ template <typename T, int THREADS> struct Sampler {
     }
 };
 
-template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 2 : 4) sample_kernel(const __grid_constant__ SampleArgs a, int blocks) {
+template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 2 : 6) sample_kernel(const __grid_constant__ SampleArgs a, int blocks) {
     __shared__ Shared<THREADS> sh;
+    constexpr int kList = Sizes<THREADS>::kList;
     const int rank = blocks == 1 ? 0 : cluster_rank();
     const long long r = blockIdx.x / blocks;
     const T *const x = static_cast<const T *>(a.logits) + r * a.ld;
@@ -1343,7 +1351,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
     if (summed) kept = sh.choice.kept;
     const u64 target = min(part_of(total, u, false), total - 1);
     if (target >= mass_before && target - mass_before < own) {      // the token lies in this block's part
-        constexpr int kPer = kSegments / THREADS;
+        constexpr int kPer = Sizes<THREADS>::kSegments / THREADS;
         u64 t[kPer], m[kPer], sum = 0, any;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
@@ -1430,7 +1438,7 @@ template <typename T, int THREADS> int launch_sample(SampleArgs a, int blocks, c
     for (;;) {
         const int each = 32 * a.seg_steps;
         a.granules = ((granules + blocks - 1) / blocks + each - 1) / each * each;
-        if (a.granules / each <= kSegments) break;
+        if (a.granules / each <= Sizes<THREADS>::kSegments) break;
         a.seg_steps *= 2;
     }
     cudaLaunchAttribute attr;
