@@ -1,4 +1,5 @@
-// parle_grad_norm: the norm of all elements of a list of tensors, sqrt(sum g^2).  One read of every element: bound by DRAM.
+// parle_grad_norm: the norm of all elements of a list of tensors, sqrt(sum g^2).  One read of every element: bound by DRAM (243 M fp32 136 us, the
+// copy rate and 10 % more; 60 M bf16 23 us, 0.8 of it; two launches, 4 to 5 us, where there is little).
 //
 // Eight squares are added in fp32, which is exact enough (8 u) and fast; these sums are added in fp64 (a conversion and an addition for
 // eight elements).  Where eight squares leave fp32's range, above or below, they are formed again in fp64: the result is that of 64-bit

@@ -13,7 +13,8 @@
 // blocks an SM (one, with twice the registers, took 1.2 to 1.3 times as long).  By what is asked for:
 //   top_k up to 256, min_p, top_p that is reached by as many: one pass over the row finds its largest logit and lists the logits from a
 //     bound on, which the largest logits of the threads' first granules give; the list is sorted and decides everything.  512 rows of 131072 bf16
-//     logits with all three 73 us: DRAM, then sorting while DRAM rests (the floor is 21 us).  One row 13 us: latency of a cluster's eight joins.
+//     logits with all three 73 us: DRAM, then sorting while DRAM rests (the floor is 21 us).  One row 14 us: latency of a
+//     cluster's joins.
 //   nothing: one pass that forms all weights, relative to the guess that the first granules give, and their sums by segments of 256 logits; the
 //     segment and the token by sums of sums.  256 rows of 131072 bf16 logits 76 us: issue slots (fp64 takes 20 us of its pipe).
 //   top_p of an undecided model, larger top_k: logits are counted by steps of scale (m - x), 1/128 wide, which tells nearly where the border lies;

@@ -1,5 +1,6 @@
 // Kernels over a list of tensors (AdamW, gradient norm): the list travels in the launch's own arguments, so that a call needs no table in
-// device memory, no copy to fill it and nothing that two calls could share.  A block takes one chunk of one tensor.
+// device memory, no copy to fill it and nothing that two calls could share.  (A launch with 32 KB of arguments takes 2 us more of the host's time
+// than one with 2 KB, so there are kernels for short lists.)  A block takes one chunk of one tensor.
 #pragma once
 
 #include "token_types.cuh"
