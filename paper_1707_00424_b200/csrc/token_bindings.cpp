@@ -471,11 +471,12 @@ PyObject *dropout(PyObject *, PyObject *const *a, Py_ssize_t n) {
 
 // A list or tuple of tensors; None: none.
 struct Tensors {
-    PyObject **items = nullptr;
+    PyObject *source = nullptr, **items = nullptr;
     Py_ssize_t n = 0;
     Tensors(const Call &c, const char *what, PyObject *o, Py_ssize_t want = -1) {
         if (o == Py_None) return;
         if (!PyList_Check(o) && !PyTuple_Check(o)) c.refuse(std::string(what) + " has to be a list or tuple of tensors, not " + Py_TYPE(o)->tp_name);
+        source = o;
         n = PySequence_Fast_GET_SIZE(o);
         static PyObject *none[1] = {nullptr};
         items = n ? PySequence_Fast_ITEMS(o) : none;
@@ -510,10 +511,13 @@ template <class F> void members(const Call &c, const char *what, const Tensors &
     }
 }
 
-// As Call::written(), for a list.
+// As Call::written(), for a list.  (Behind the call, during which another thread may have changed it: it is looked at anew.)
 void written(const Tensors &list) {
-    for (Py_ssize_t i = 0; i < list.n; ++i) {
-        const at::Tensor &t = THPVariable_Unpack(list.items[i]);
+    const Py_ssize_t n = list ? PySequence_Fast_GET_SIZE(list.source) : 0;
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        PyObject *const o = PySequence_Fast_GET_ITEM(list.source, i);
+        if (!THPVariable_Check(o)) continue;
+        const at::Tensor &t = THPVariable_Unpack(o);
         if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
     }
 }

@@ -439,3 +439,47 @@ def test_refused_arguments(call):
     with pytest.raises(pb.ParleError) as e:
         call(c)
     assert e.value.code == -1
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_past_32_bit_offsets(bits):
+    """Elements from 2^32 on are stepped as those of a tensor of their own are (2^32 is a multiple of the thresholds' period and of a block)."""
+    n, last = (1 << 32) + 5003, 5003
+    big = [torch.zeros(n, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    g = torch.Generator().manual_seed(40)
+    p, grad = (torch.randn(last, generator=g).bfloat16().to(DEV) for _ in range(2))
+    big[0][-last:], big[1][-last:] = p, grad
+    state, small = pb.adamw_state([big[0]], bits), pb.adamw_state([p], bits)
+    assert float(pb.grad_norm([big[1]])) == float(pb.grad_norm([grad]))
+    for t in (1, 2):
+        pb.adamw([big[0]], [big[1]], state[0], state[1], step=t, lr=0.01, exp_avg_scales=state[2], exp_avg_sq_scales=state[3])
+        pb.adamw([p], [grad], small[0], small[1], step=t, lr=0.01, exp_avg_scales=small[2], exp_avg_sq_scales=small[3])
+    assert torch.equal(big[0][-last:], p) and not bool(big[0][:1 << 20].any()) and not bool(big[0][(1 << 32) - (1 << 20):1 << 32].any())
+    for a, b in zip(state[:2], small[:2]):
+        assert torch.equal(a[0][-last:].view(torch.uint8), b[0].view(torch.uint8))
+    if bits == 8:
+        assert all(torch.equal(a[0][-20:], b[0]) for a, b in zip(state[2:], small[2:]))
+
+
+def test_calls_from_several_threads_and_streams():
+    import threading
+    cases = [Case((3000, 17, 40000), torch.float32, torch.bfloat16, 8, seed=50 + i) for i in range(4)]
+    twins = [Case((3000, 17, 40000), torch.float32, torch.bfloat16, 8, seed=50 + i) for i in range(4)]
+    torch.cuda.synchronize()
+
+    def work(case):
+        s = torch.cuda.Stream()
+        for t in range(1, 20):
+            case.step(t, norm=pb.grad_norm(case.grads, stream=s), max_norm=1.0, stream=s)
+        s.synchronize()
+
+    threads = [threading.Thread(target=work, args=(c,)) for c in cases]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    for case, twin in zip(cases, twins):
+        for t in range(1, 20):
+            twin.step(t, norm=pb.grad_norm(twin.grads), max_norm=1.0)
+        for a, b in ((case.params, twin.params), (case.m, twin.m), (case.v, twin.v), (case.ms, twin.ms), (case.vs, twin.vs)):
+            assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a, b))

@@ -287,3 +287,37 @@ def test_a_model_of_tokens_takes_a_step_and_answers(bits):
         full, _, _, _ = pb.token_logprobs(answers, token, scale=1 / 0.8)
         assert bool((logprob >= full - 1e-5).all()) and bool((kept <= 20).all())
         prev = token
+
+
+def test_calls_from_several_threads_and_streams():
+    import threading
+    x, u = logits(40, 60000, torch.bfloat16, 33)
+    y, v = logits(500, 300, torch.float16, 34)
+    limits = [{}, dict(top_k=30), dict(top_p=0.9), dict(min_p=0.01), dict(top_k=5000, top_p=0.95)]
+    want = [[pb.sample_tokens(a, b, **k) for k in limits] for a, b in ((x, u), (y, v))]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work():
+        s = torch.cuda.Stream()
+        for _ in range(10):
+            got = [[pb.sample_tokens(a, b, **k, stream=s) for k in limits] for a, b in ((x, u), (y, v))]
+        s.synchronize()
+        if not all(torch.equal(p, q) for a, b in zip(got, want) for c, d in zip(a, b) for p, q in zip(c, d)):
+            wrong.append(1)
+
+    threads = [threading.Thread(target=work) for _ in range(4)]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert not wrong
+
+
+def test_short_and_long_rows_around_the_borders_between_kernels():
+    """Around 4096 tokens (blocks of 128 or 512 threads), lists' lengths and blocks' parts."""
+    for rows, vocab in ((3, 255), (3, 256), (3, 257), (2, 1023), (2, 1025), (2, 4095), (2, 4096), (2, 4097), (2, 16383), (1, 16384), (2, 32767), (3, 32768), (2, 131071)):
+        for dtype in TYPES:
+            x, u = logits(rows, vocab, dtype, vocab, spread=1.0)
+            for k in (dict(top_k=64), dict(top_k=65), dict(top_k=256), dict(top_k=257), dict(top_k=vocab - 1), dict(top_k=vocab), dict(top_p=0.97), dict(min_p=0.05), dict(top_k=vocab // 2, top_p=0.5, min_p=0.2)):
+                check(x, u, **k, most_near=1 / rows)
