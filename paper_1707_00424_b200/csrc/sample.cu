@@ -668,6 +668,15 @@ template <typename T, int THREADS> struct Sampler {
     // (0: none) is at most n, or the list complete.  total_low, total_high: bounds of the weights' total where no top_k gives it, equal where it
     // is known.
     __device__ __forceinline__ Outcome from_list(const SampleArgs &a, long long r, int n, bool complete, int top_k, float top_p, u64 total_low, u64 total_high, uint32_t least_key, float u) {
+        if (top_p < 1.f && top_k == 0 && !complete) {    // far from enough, as of an undecided model: no need to sort
+            u64 sum = 0, all;
+            for (int i = threadIdx.x; i < n; i += THREADS) sum += weigh(value_of(~(uint32_t)(sh.list[i] >> 32)));
+            block_scan<THREADS>(sum, sh.scan, &all);
+            if (part_of(total_low, top_p, true) > all) {
+                if (threadIdx.x == 0) sh.sums[n - 1] = all;
+                return kNeedAll;
+            }
+        }
         sort(n);
         for (int i = threadIdx.x; i < n; i += THREADS) sh.weight[i] = weigh(value_of(~(uint32_t)(sh.list[i] >> 32)));
         running(n, [&](int i) { return sh.weight[i]; });
@@ -869,7 +878,7 @@ template <typename T, int THREADS> struct Sampler {
         __syncthreads();
         u64 above_count = sh.bracket.before, upto = sh.bracket.upto;
         if (from >= 0 && upto - above_count < kList && top_p < 1.f) {      // some more, as sums of few logits are less exact
-            const u64 more = (kList - (upto - above_count)) / 4;
+            const u64 more = (kList - (upto - above_count)) / 8;
             __syncthreads();
             bounds(above_count - min(above_count - known, more), min(upto + more, known + count));
             __syncthreads();
@@ -892,31 +901,46 @@ template <typename T, int THREADS> struct Sampler {
         const u64 one = (u64)__double_as_longlong(weigh.one);
         const float weightless = fmaxf(top_p < 1.f ? floor_value : high, weigh.least);
         u64 total = 0, above = 0;
-        each_segment(seg_steps, [&](int at, const Pack8<T> &, const float (&v)[8], u64 &m) {
-            bool some = false, any = top_p < 1.f;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                some |= v[k] >= low && v[k] <= high;
-                any |= v[k] > high;
-            }
-            if (__any_sync(0xffffffffu, any)) {
-                u64 all = 0, most = 0;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const u64 w = weigh.raw(v[k] > weightless ? v[k] : weigh.least);
-                    all += w;
-                    most += v[k] > high ? w : one;
-                }
-                total += all - 8 * one;
-                m += most - 8 * one;
-            }
-            if (some) note(at, v, low, high);
-        }, [&](int g, u64 m) {
+        const auto summed = [&](int g, u64 m) {
             if (lane == 0) {
                 sh.seg.mass[g] = m;
                 above += m;
             }
-        });
+        };
+        if (top_p < 1.f) {
+            each_segment(seg_steps, [&](int at, const Pack8<T> &, const float (&v)[8], u64 &m) {
+                bool some = false;
+                u64 all = 0, most = 0;
+                uint32_t many = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const u64 w = weigh.raw(v[k] > weightless ? v[k] : weigh.least);
+                    all += w;
+                    if (v[k] > high) {
+                        most += w;
+                        ++many;
+                    } else some |= v[k] >= low;
+                }
+                total += all - 8 * one;
+                m += most - many * one;
+                if (some) note(at, v, low, high);
+            }, summed);
+        } else {
+            each_segment(seg_steps, [&](int at, const Pack8<T> &, const float (&v)[8], u64 &m) {
+                bool some = false, any = false;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    if (v[k] > high) any = true; else some |= v[k] >= low;
+                }
+                if (__any_sync(0xffffffffu, any)) {
+                    u64 most = 0;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) most += weigh.raw(v[k] > weightless ? v[k] : weigh.least);
+                    m += most - 8 * one;
+                }
+                if (some) note(at, v, low, high);
+            }, summed);
+        }
         u64 all_total, all_above;
         block_scan<THREADS>(total, sh.scan, &all_total);
         block_scan<THREADS>(above, sh.scan, &all_above);
