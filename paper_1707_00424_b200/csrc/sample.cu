@@ -15,11 +15,11 @@
 //     bound on, which the largest logits of the threads' first granules give; the list is sorted and decides everything.  512 rows of 131072 bf16
 //     logits with all three 73 us: DRAM, then sorting while DRAM rests (the floor is 21 us).  One row 14 us: latency of a
 //     cluster's joins.
-//   nothing: one pass that forms all weights, relative to the guess that the first granules give, and their sums by segments of 256 logits; the
-//     segment and the token by sums of sums.  256 rows of 131072 bf16 logits 76 us: issue slots (fp64 takes 20 us of its pipe).
+//   nothing: one pass that forms all weights, relative to the guess that the first granules give, and their sums by segments of 256 or 1024 logits; the
+//     segment and the token by sums of sums.  256 rows of 131072 bf16 logits 66 us: issue slots (fp64 takes 20 us of its pipe).
 //   top_p of an undecided model, larger top_k: logits are counted by steps of scale (m - x), 1/128 wide, which tells nearly where the border lies;
 //     one more pass forms the weights, their exact total and segments' sums, and lists the logits around the border.  256 rows with top_p = 0.95,
-//     25000 tokens kept, 202 us: a fifth the counts, two fifths the weights.
+//     25000 tokens kept, 174 us: a fifth the counts, two fifths the weights.
 //   what escapes these (thousands of equal logits at the border, a wrong guess): exact histograms of 64-bit sums, of which two 32-bit words lie
 //     in shared memory and the adding thread passes on the carry, of steps of scale (m - x) and then of the logits' bits, 11 at a time.
 #include <math.h>
@@ -123,8 +123,9 @@ template <typename T> struct Row {
     const T *x;
     int vocab, skew;                                     // logits of the first granule before the row
     bool flat;
+    int whole_from, whole_to;                            // granules that lie in the row altogether
     __device__ __forceinline__ long long first(int granule) const { return (long long)granule * 8 - skew; }
-    __device__ __forceinline__ bool whole(int granule) const { return first(granule) >= 0 && first(granule) + 8 <= vocab; }
+    __device__ __forceinline__ bool whole(int granule) const { return granule >= whole_from && granule < whole_to; }
     __device__ __forceinline__ float at(long long token) const {
         const float v = token >= 0 && token < vocab ? to_float(x[token]) : -INFINITY;
         return flat && v > -INFINITY ? 0.f : v;
@@ -261,6 +262,11 @@ __device__ __forceinline__ void all_meet(int blocks) {
     }
 }
 
+__device__ __forceinline__ u64 of_warp(u64 v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
 __device__ __forceinline__ u64 shfl_up64(u64 v, int by) { return __shfl_up_sync(0xffffffffu, v, by); }
 
 // Exclusive sum over the block's threads; *total: of all.
@@ -433,7 +439,7 @@ template <typename T, int THREADS> struct Sampler {
     }
 
     // f(granule, raw form, logits, sum) for the granules of each segment, a warp's granules side by side and the whole warp in each call (behind the
-    // part's end with logits of -inf); then done(segment, sum of the lanes' sums).
+    // part's end with logits of -inf); then done(segment, the lane's sum).
     template <class F, class G> __device__ __forceinline__ void each_segment(int seg_steps, F f, G done) const {
         const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, segments = (end - begin + 32 * seg_steps - 1) / (32 * seg_steps);
         int at = begin + warp * seg_steps * 32 + lane;
@@ -453,8 +459,6 @@ template <typename T, int THREADS> struct Sampler {
                 }
                 f(now, p, v, m);
             }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) m += __shfl_xor_sync(0xffffffffu, m, o);
             done(g, m);
         }
     }
@@ -902,6 +906,7 @@ template <typename T, int THREADS> struct Sampler {
         const float weightless = fmaxf(top_p < 1.f ? floor_value : high, weigh.least);
         u64 total = 0, above = 0;
         const auto summed = [&](int g, u64 m) {
+            m = of_warp(m);
             if (lane == 0) {
                 sh.seg.mass[g] = m;
                 above += m;
@@ -1022,7 +1027,8 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
     const int rank = blocks == 1 ? 0 : cluster_rank();
     const long long r = blockIdx.x / blocks;
     const T *const x = static_cast<const T *>(a.logits) + r * a.ld;
-    Row<T> row{x, a.vocab, (int)(reinterpret_cast<uintptr_t>(x) % 16 / sizeof(T)), false};
+    const int skew = (int)(reinterpret_cast<uintptr_t>(x) % 16 / sizeof(T));
+    Row<T> row{x, a.vocab, skew, false, skew > 0, (a.vocab + skew) / 8};
     const int all = (a.vocab + row.skew + 7) / 8, begin = min(all, rank * a.granules), end = min(all, begin + a.granules);
     const float scale = a.scales ? a.scales[r] : a.scale, top_p = a.top_ps ? a.top_ps[r] : a.top_p, min_p = a.min_ps ? a.min_ps[r] : a.min_p, u = a.u[r];
     int top_k = a.top_ks ? a.top_ks[r] : a.top_k;
@@ -1271,11 +1277,12 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
         const u64 one = (u64)__double_as_longlong(s.weigh.one);
         if (unlimited) {
             // All logits are kept.  Where the largest one is not known yet, weights are relative to the guess, and the largest logit is found beside
-            // them.  The sums stand if eight weights fit into 64 bits (w < e^11) and so do all (their fp64 sum is below 2^62), else they are formed again.
+            // them.  The sums stand if a thread's of a segment fit into 64 bits (w < e^10, at most
+            // vocab / 2^15 or 32 of them) and so do all (their fp64 sum is below 2^62), else they are formed again.
             for (;;) {
                 sum = 0.0;
-                s.each_segment(a.seg_steps, [&](int g, const Pack8<T> &p, const float (&v)[8], u64 &m) {
-                    const float most = g >= end ? -INFINITY : row.flat ? best : row.most(p, g);
+                s.each_segment(a.seg_steps, [&](int g, const Pack8<T> &, const float (&v)[8], u64 &m) {
+                    const float most = largest(largest(largest(v[0], v[1]), largest(v[2], v[3])), largest(largest(v[4], v[5]), largest(v[6], v[7])));
                     mine = largest(mine, most);
                     u64 part = 0;
                     if (most > s.weigh.most) {
@@ -1287,10 +1294,14 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
                         part -= 8 * one;
                     }
                     m += part;
-                    sum += (double)part;
+                    if (fminf(fminf(fminf(v[0], v[1]), fminf(v[2], v[3])), fminf(fminf(v[4], v[5]), fminf(v[6], v[7]))) > -INFINITY) count += 8;
+                    else {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) count += v[k] > -INFINITY;
+                        for (int k = 0; k < 8; ++k) count += v[k] > -INFINITY;
+                    }
                 }, [&](int g, u64 m) {
+                    sum += (double)m;
+                    m = of_warp(m);
                     if (lane == 0) {
                         sh.seg.mass[g] = m;
                         sh.seg.ties[g] = 0;
@@ -1316,7 +1327,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
                 sum = 0.0;
                 s.of_blocks([](const Shared<THREADS> &b) { return b.part.sum; }, [&](int, double p) { sum += p; });
                 all_meet(blocks);
-                if (((double)top - best) * scale < 11.0 && sum < 0x1p62) break;
+                if (((double)top - best) * scale < 10.0 && sum < 0x1p62) break;
                 s.best = best = top;
                 s.weigh.set(best, scale, a.frac_bits, sh.table);
                 mass = 0;
@@ -1342,6 +1353,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
                 for (int k = 0; k < 8; ++k) part += s.weigh.raw(v[k] > weightless ? v[k] : s.weigh.least);
                 m += part - 8 * one;
             }, [&](int g, u64 m) {
+                m = of_warp(m);
                 const uint32_t equal = cut.ties ? __reduce_add_sync(0xffffffffu, t) : 0;
                 t = 0;
                 if (lane == 0) {
@@ -1459,7 +1471,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
 
 template <typename T, int THREADS> int launch_sample(SampleArgs a, int blocks, cudaStream_t stream) {
     const int granules = a.vocab / 8 + 2;                // wherever a row begins
-    a.seg_steps = 1;
+    a.seg_steps = blocks == 1 && granules >= 128 * (THREADS / 32) ? 4 : 1;      // (adding up a segment over a warp takes as long as half a step)
     for (;;) {
         const int each = 32 * a.seg_steps;
         a.granules = ((granules + blocks - 1) / blocks + each - 1) / each * each;
