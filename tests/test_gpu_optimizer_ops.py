@@ -56,10 +56,12 @@ def test_norm(dtype, shift):
         assert torch.equal(pb.grad_norm(grads), got)
 
 
-def test_norm_of_many_tensors_takes_several_launches():
+@pytest.mark.parametrize("count", [96, 97, 400, 401, 1600, 1601, 4000])
+def test_norm_of_lists_of_any_length(count):
+    """Around the lengths of one launch's list, and several launches."""
     g = torch.Generator().manual_seed(4)
-    flat = torch.randn(40000, generator=g).to(DEV)
-    grads = list(flat.view(4000, 10).unbind())
+    flat = torch.randn(10 * count, generator=g).to(DEV)
+    grads = list(flat.view(count, 10).unbind())
     want = oo.grad_norm([f64(flat)])
     assert abs(float(pb.grad_norm(grads)) - want) <= want * 6 * U
 
