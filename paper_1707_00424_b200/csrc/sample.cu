@@ -668,8 +668,8 @@ template <typename T, int THREADS> struct Sampler {
         return count;
     }
 
-    // Samples from the n largest logits, in list[], if these hold all that is kept.  complete: whatever is not in the list is below min_p.  top_k
-    // (0: none) is at most n, or the list complete.  total_low, total_high: bounds of the weights' total where no top_k gives it, equal where it
+    // Samples from the n largest logits, in list[], if these hold all that is kept.  complete: whatever is not in the list is below min_p (-inf where
+    // both top_k and top_p limit).  top_k (0: none) is at most n, or the list complete.  total_low, total_high: bounds of the weights' total where no top_k gives it, equal where it
     // is known.
     __device__ __forceinline__ Outcome from_list(const SampleArgs &a, long long r, int n, bool complete, int top_k, float top_p, u64 total_low, u64 total_high, uint32_t least_key, float u) {
         if (top_p < 1.f && top_k == 0 && !complete) {    // far from enough, as of an undecided model: no need to sort
@@ -1170,7 +1170,8 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
             sh.part.sum = sum;
         }
         all_meet(blocks);
-        const bool complete = from <= max(least_key, kNegInf + 1);
+        // (`lower`: what min_p leaves may be listed, but top_k's other weights are missing in top_p's total)
+        const bool complete = from <= (lower ? kNegInf + 1 : max(least_key, kNegInf + 1));
         int n = 0;
         s.of_blocks([](const Shared<THREADS> &b) { return b.listed; }, [&](int, uint32_t k) { n += (int)min(2u * kList + 1, k); });
         u64 low = 0, high = 0;

@@ -1,0 +1,63 @@
+"""Sampling where a border is hard to place: rows whose large logits have low numbers under all three limits, borders at a logit of zero,
+logits so large that their distances are coarse.  Against the fp64 oracle; comparisons of sums as near as the whole numbers' roundings reach
+(vocab of 2^-45 against sums of at least 1, 2^-47 for the exponentials) are left out."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_1707_00424_b200 as pb
+from oracle import token_oracle as to
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+TYPES = (torch.float32, torch.bfloat16, torch.float16)
+
+
+def check(x, u, scale=1.0, most_near=0.02, **limits):
+    token, logprob, kept = (t.cpu().numpy() for t in pb.sample_tokens(x, u, scale=scale, **limits))
+    host, z, left = x.double().cpu().numpy(), u.cpu().numpy(), 0
+    for r in range(len(host)):
+        want = to.sample(host[r], z[r], scale, limits.get("top_k", 0), limits.get("top_p", 1.0), limits.get("min_p", 0.0))
+        if want[3] <= host.shape[1] * 2.0 ** -45 + 2.0 ** -47:
+            left += 1
+            continue
+        assert (token[r], kept[r]) == (want[0], want[2]), (r, token[r], kept[r], want)
+        assert abs(logprob[r] - want[1]) <= U * abs(want[1]) + 1e-9, (r, logprob[r], want)
+    assert left <= most_near * len(host)
+    return token, logprob, kept
+
+
+# ---- top-k, top-p and min-p together: all of top-k's weights count towards top-p's total ---------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_list_that_holds_fewer_than_top_k_is_no_basis_for_top_p(dtype):
+    """The first logits tell of a bound that min_p reaches, but fewer than top_k logits are from it on."""
+    rows, vocab = 160, 131072
+    x = torch.full((rows, vocab), -30.0, dtype=dtype, device=DEV)
+    x[:, 0], x[:, 1], x[:, 8:488:8], x[:, 20000:21000] = 0.0, -3.5, -7.0, -7.5
+    u = (torch.arange(rows, device=DEV) + 0.5) / rows
+    _, _, kept = check(x, u, top_k=200, top_p=0.9, min_p=0.02, most_near=0)
+    assert (kept == 2).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("top_k, min_p", [(50, 0.05), (200, 0.02), (256, 0.001)])
+def test_rows_whose_large_logits_have_low_numbers(dtype, top_k, min_p):
+    """As real vocabularies are ordered: frequent tokens first."""
+    for rows, vocab in ((160, 131072), (160, 40000), (20, 131072), (400, 20001)):
+        g = torch.Generator(device=DEV).manual_seed(rows + vocab)
+        x = torch.randn(rows, vocab, generator=g, device=DEV) * 2.5
+        x = (x - 1.5 * torch.log1p(torch.arange(vocab, device=DEV) / 100)).to(dtype)
+        some = slice(None) if dtype == torch.bfloat16 and vocab > 100000 else slice(0, None, 5)
+        u = torch.rand(rows, generator=g, device=DEV)
+        got = pb.sample_tokens(x, u, top_k=top_k, top_p=0.9, min_p=min_p)
+        host, z = x[some].double().cpu().numpy(), u[some].cpu().numpy()
+        for r in range(len(host)):
+            # (nothing below the 1024 largest matters to top_k; in their order by number)
+            first = np.sort(np.argpartition(-host[r], 1024)[:1024])
+            want = to.sample(host[r][first], z[r], 1.0, top_k, 0.9, min_p)
+            if want[3] > vocab * 2.0 ** -45 + 2.0 ** -47:
+                assert (int(got[0][some][r]), int(got[2][some][r])) == (first[want[0]], want[2]), (rows, vocab, r)
