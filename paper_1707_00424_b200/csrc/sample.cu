@@ -63,6 +63,8 @@ __device__ __forceinline__ uint32_t key_of(float x) {
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
+// The number that logits of keys above `key` are above, and no others.  (The key below 0's is that of -0, which no logit has, and 0 > -0 is false.)
+__device__ __forceinline__ float below(uint32_t key) { return value_of(key - (key == 0x7fffffffu ? 1 : 0)); }
 
 // f total, f in [0, 1), exactly: rounded down or up to a whole number.
 __device__ __forceinline__ u64 part_of(u64 total, float f, bool up) {
@@ -900,7 +902,7 @@ template <typename T, int THREADS> struct Sampler {
             if (threadIdx.x == 0) sh.found.low = key; else sh.found.high = known ? min(key, known_key) - 1 : key - 1;
         }
         __syncthreads();
-        const float low = value_of(sh.found.low), high = value_of(sh.found.high);
+        const float low = value_of(sh.found.low), high = below(sh.found.high);
         const int lane = threadIdx.x % 32;
         const u64 one = (u64)__double_as_longlong(weigh.one);
         const float weightless = fmaxf(top_p < 1.f ? floor_value : high, weigh.least);
@@ -1335,7 +1337,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
                 count = 0;
             }
         } else {
-            const float border = value_of(cut.key), weightless = fmaxf(border, s.weigh.least);
+            const float border = below(cut.key), weightless = fmaxf(border, s.weigh.least);      // (the key of ties is a logit's)
             uint32_t t = 0;
             s.each_segment(a.seg_steps, [&](int, const Pack8<T> &, const float (&v)[8], u64 &m) {
                 bool some = false;

@@ -61,3 +61,41 @@ def test_rows_whose_large_logits_have_low_numbers(dtype, top_k, min_p):
             want = to.sample(host[r][first], z[r], 1.0, top_k, 0.9, min_p)
             if want[3] > vocab * 2.0 ** -45 + 2.0 ** -47:
                 assert (int(got[0][some][r]), int(got[2][some][r])) == (first[want[0]], want[2]), (rows, vocab, r)
+
+
+# ---- borders at a logit of zero --------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [256, 257, 4096, 4097, 20001, 131072])
+def test_min_p_of_one_keeps_all_zeros(dtype, vocab):
+    """More of them than a list holds; a row that is masked altogether counts as zeros, and so does min_p above 1 of a row."""
+    x = torch.zeros(5, vocab, dtype=dtype, device=DEV)
+    x[1] = torch.finfo(dtype).min
+    x[2, ::2] = -1.0
+    x[3, ::2] = -0.0
+    x[4, vocab // 2:] = -math.inf
+    u = (torch.arange(5, device=DEV) + 0.25) / 5
+    for _ in range(2):
+        check(x, u, min_p=1.0, most_near=1)
+        few = torch.tensor([vocab, vocab, vocab // 2, vocab, vocab // 2], device=DEV)
+        marked = [torch.full((5,), -7, device=DEV, dtype=t) for t in (torch.int32, torch.float32, torch.int32)]
+        token, logprob, kept = pb.sample_tokens(x, u, min_p=torch.full((5,), 2.0, device=DEV), token=marked[0], logprob=marked[1], kept=marked[2])
+        assert torch.equal(kept, few.int())
+        want = (u.double() * few).floor().long()
+        want[2] = 2 * want[2] + 1
+        assert torch.equal(token.long(), want)
+        assert bool(((logprob.double() + few.double().log()).abs() <= U * few.double().log() + 1e-9).all())
+        u = u.flip(0)
+
+
+def test_zeros_that_are_listed_already_are_kept_once():
+    """top_p's border lies just below the zeros that the first pass has listed."""
+    rows, vocab = 4, 20000
+    x = torch.full((rows, vocab), -20.0, dtype=torch.bfloat16, device=DEV)
+    x[:, :1200:8] = 0.0                                     # in the first granules of one or two blocks, one a thread
+    x[:, 10000:11200:8] = 0.0
+    x[:, 8500:8800], x[:, 18500:18800] = -0.003, -0.004
+    u = torch.rand(rows, generator=torch.Generator().manual_seed(3)).to(DEV)
+    for k in (1, 40):
+        for top_p in (0.2, 0.35, 0.4, 0.52, 0.75, 0.95):
+            check(x.repeat(k, 1), u.repeat(k), top_p=top_p, most_near=1)
