@@ -83,7 +83,7 @@ __device__ __forceinline__ u64 part_of(u64 total, float f, bool up) {
 struct Weigher {                                         // w(x) = exp(scale (x - best)) as a whole number of 2^-frac_bits
     double best, c, one;                                 // c: 32 scale log2 e; one: whose last bit is 2^-frac_bits
     float least;                                         // it and all logits below weigh nothing
-    float most;                                          // logits above `best` that raw() may be used for (where best is a guess): w < 2^7
+    float most;                                          // logits above `best` that raw() may be used for (where best is a guess): w < e^4.8 < 2^7
     const double *table;                                 // 2^(i / 32), in shared memory; less i 2^15 in the upper word, which n 2^15 adds
     __device__ __forceinline__ void set(float best_, float scale, int frac_bits, const double *table_) {
         best = best_;
@@ -92,7 +92,7 @@ struct Weigher {                                         // w(x) = exp(scale (x 
         // e^-45 < 2^-64.  Where best - 45 / scale is best again, the next number below weighs nothing, and is taken for as little as fits.
         least = fminf(best_ - 45.f / scale, value_of(key_of(best_) - 1));
         c = fmin(32.0 * 1.44269504088896340736 * scale, 4096.0 / (best - (double)least));
-        most = best_ + 4.8f / scale;
+        most = __fadd_rd(best_, 4.8f / scale);           // (rounded down: the next logit above `best` may lie farther away)
     }
     // 2^(n / 32) from the table and its exponent, e^y of the rest, |y| <= ln 2 / 64 = h, by Taylor's polynomial of degree 5 whose last term is spread over y and y^3
     // (Chebyshev's economisation: 16 z^5 - 20 z^3 + 5 z is at most 1): off by h^5 / 1920 = 8 10^-14.  Nine operations in fp64.

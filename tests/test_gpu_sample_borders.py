@@ -25,7 +25,8 @@ def check(x, u, scale=1.0, most_near=0.02, **limits):
             left += 1
             continue
         assert (token[r], kept[r]) == (want[0], want[2]), (r, token[r], kept[r], want)
-        assert abs(logprob[r] - want[1]) <= U * abs(want[1]) + 1e-9, (r, logprob[r], want)
+        # the result's rounding; the sum is at least 1 and each weight in it off by 2^-45 (equal ones by the same)
+        assert abs(float(logprob[r]) - want[1]) <= U * abs(want[1]) + host.shape[1] * 2.0 ** -45 + 1e-9, (r, logprob[r], want)
     assert left <= most_near * len(host)
     return token, logprob, kept
 
@@ -99,3 +100,17 @@ def test_zeros_that_are_listed_already_are_kept_once():
     for k in (1, 40):
         for top_p in (0.2, 0.35, 0.4, 0.52, 0.75, 0.95):
             check(x.repeat(k, 1), u.repeat(k), top_p=top_p, most_near=1)
+
+
+# ---- logits whose distances are coarse -----------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("vocab", [20000, 131072, 300007])
+@pytest.mark.parametrize("size, apart, scale", [(1e8, 8, 1.0), (1e8, 8, 0.7), (1e8, 8, 1.2), (5e7, 4, 2.0), (5e7, 8, 0.7), (3e7, 4, 1 / 0.7), (100.0, 2.0 ** -17, 1e6), (-1e8, 8, 1.1), (6e5, 2.0 ** -4, 100.0)])
+def test_the_largest_logits_are_one_step_above_all_others(vocab, size, apart, scale):
+    """The first logits do not show them; few, so that sums relative to the first logits would stand."""
+    for rows in (3, 170) if vocab == 131072 else (3,):
+        x = torch.full((rows, vocab), size, device=DEV)
+        x[:, -100:-60] += apart
+        x[0, vocab - 3000::100] += apart
+        u = (torch.arange(rows, device=DEV) + 0.3) / rows
+        check(x, u, scale=scale, most_near=1)
