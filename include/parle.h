@@ -475,7 +475,7 @@ typedef struct {
  * u / 2^24 is at least 1: u = (12664745 i + 9560335 t) mod 2^24 for m, 2^24 - 1 - u for r, i the element's number in its tensor; a root above 0
  * is held as at least the smallest code.  Over the steps this rounds to neither side: moments that move by less than a code's distance a
  * step move all the same.  Each of these operations (the moments' above, code times scale, r^2, sqrt, 1 / largest, the products) is
- * rounded to nearest in fp32 by itself: codes and scales are the same bits wherever they are formed so (v below 2^-126 aside).
+ * rounded to nearest in fp32 by itself: codes and scales are the same bits wherever they are formed so.
  * All zeros are the state of no steps, in both forms.  Arrays may not overlap; an array that begins where another begins is EINVAL.
  * copy_dtype: PARLE_BF16 or PARLE_F16 beside fp32 parameters, else PARLE_NO_COPY.  step_dev and lr_dev are read when the kernel runs: a
  * captured step that is replayed moves on when the caller advances them. */

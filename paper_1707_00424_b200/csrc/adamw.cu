@@ -69,6 +69,7 @@ struct Scalars {                                         // what a block needs b
     float c, rate, root_scale, decay;
     uint32_t weyl;                                       // t's part of the threshold
     bool skip;
+    bool tiny_eps;                                       // it does not hide small errors of small roots
 };
 
 __device__ __forceinline__ float root(float v) {
@@ -94,7 +95,7 @@ __device__ __forceinline__ float reciprocal(float v) {
 
 __device__ __forceinline__ Scalars scalars(const StepArgs &a) {
     __shared__ Scalars shared;
-    Scalars s{a.grad_scale, a.rate, a.root_scale, a.decay, (uint32_t)a.step * kWeylT, false};
+    Scalars s{a.grad_scale, a.rate, a.root_scale, a.decay, (uint32_t)a.step * kWeylT, false, false};
     if (a.step_dev || a.lr_dev) {                        // (the same for all blocks)
         if (threadIdx.x == 0) {
             const long long t = a.step + (a.step_dev ? *a.step_dev : 0);
@@ -108,6 +109,7 @@ __device__ __forceinline__ Scalars scalars(const StepArgs &a) {
         __syncthreads();
         s = shared;
     }
+    s.tiny_eps = a.eps < s.root_scale * 0x1p-39f;
     if (a.norm) {
         const float norm = *a.norm;
         s.skip = !(fabsf(norm) < INFINITY);
@@ -130,10 +132,12 @@ __device__ __forceinline__ uint32_t top_bytes(const uint32_t *t) {
     return __byte_perm(__byte_perm(t[0], t[1], 0x0073), __byte_perm(t[2], t[3], 0x0073), 0x5410);
 }
 
-// The scale of a block of a warp from the largest magnitude of each lane (NaN if one is); factor: 448 (1 / largest) 2^-120, by which values come to
+// The largest of a warp's magnitudes, NaN if one is.  (As bits, what is no number is largest.)
+__device__ __forceinline__ float warp_largest(float v) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v))); }
+
+// The scale of a block from its largest magnitude (NaN if that is); factor: 448 (1 / largest) 2^-120, by which values come to
 // lie in [0, 448] 2^-120 or a rounding above.  Values from 2^14 on are scaled first, so that the factor is no subnormal number.
-__device__ __forceinline__ float block_scale(float largest, float (&x)[8], float *factor) {
-    float top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(largest)));      // (as bits, what is no number is largest)
+__device__ __forceinline__ float block_scale(float top, float (&x)[8], float *factor) {
     const bool none = top < kNothing, finite = top < INFINITY;
     const float scale = none ? 0.f : finite ? __fmul_rn(top, 1.f / kLargest) : NAN;
     if (top >= 0x1p14f) {
@@ -169,13 +173,23 @@ __device__ __forceinline__ Two mul_add(Two a, Two b, Two c) {
     return t;
 }
 
-// One step of eight elements with moments in 8 bits, a whole warp's block: mc and rc come as the old codes and go as the new ones.
+// The root of a number from 2^-102 on or of 0, to nearest: one of Newton's steps with the exact remainder (Markstein, "Computation of elementary functions on
+// the IBM RISC System/6000 processor", 1990).  (All numbers were compared with the library's root: that of some below 2^-102 is wrong, where the remainder is
+// subnormal, and that of infinity is NaN.)
+__device__ __forceinline__ float root_of(float v) {
+    const float inverse = inverse_root(fmaxf(v, 0x1p-126f)), guess = __fmul_rn(v, inverse);
+    return fmaf(fmaf(-guess, guess, v), __fmul_rn(inverse, 0.5f), guess);
+}
+
+// One step of eight elements with moments in 8 bits, a whole warp's block: mc and rc come as the old codes and go as the new ones.  (param: the elements'
+// old values, for those whose roots are formed in another way.)
 // The moments, their root and what the codes are taken from are rounded after every operation, to nearest: a value next to the border
 // between two codes falls to one side in any implementation of these operations, so that codes can be compared.  (Fused and with the hardware's
 // root: 102 M bf16 parameters 174 us.)
-__device__ __forceinline__ void step8(const StepArgs &a, const Scalars &s, float limit, long long e0, float m_scale, float r_scale, float (&p)[8], const float (&g)[8], uint2 &mc, uint2 &rc,
+template <typename P>
+__device__ __forceinline__ void step8(const StepArgs &a, const Scalars &s, float limit, const P *param, long long e0, float m_scale, float r_scale, float (&p)[8], const float (&g)[8], uint2 &mc, uint2 &rc,
                                       long long n, bool whole, float *new_m_scale, float *new_r_scale, bool &ok) {
-    float m[8], r[8], m_top = 0.f, r_top = 0.f;
+    float m[8], r[8], m_top = 0.f, v_top = 0.f;          // r: first of v, then of its root
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 cm = decode2((i < 2 ? mc.x : mc.y) >> (i % 2 * 16)), cr = decode2((i < 2 ? rc.x : rc.y) >> (i % 2 * 16));
@@ -190,24 +204,68 @@ __device__ __forceinline__ void step8(const StepArgs &a, const Scalars &s, float
         }
         const Two gg = mul(two(g[2 * i], g[2 * i + 1]), two(s.c, s.c));
         const Two zero = two(a.minus_zero, a.minus_zero);      // (products to be added: the assembler makes one operation of mul.rn.f32x2 and add.rn.f32x2)
-        const Two new_m = add(mul_add(old_m, two(a.b1, a.b1), zero), mul_add(gg, two(a.one_minus_b1, a.one_minus_b1), zero));
-        const Two v = add(mul_add(mul(old_r, old_r), two(a.b2, a.b2), zero), mul_add(mul(gg, gg), two(a.one_minus_b2, a.one_minus_b2), zero));
-        // The root by one of Newton's steps with the exact remainder (Markstein, "Computation of elementary functions on the IBM RISC System/6000
-        // processor", 1990): to nearest but for one number in millions.
-        split(v, x, y);
-        const Two inverse = two(inverse_root(fmaxf(x, 0x1p-126f)), inverse_root(fmaxf(y, 0x1p-126f))), guess = mul(v, inverse);
-        const Two rest = mul_add(mul(guess, two(-1.f, -1.f)), guess, v), root = mul_add(rest, mul(inverse, two(0.5f, 0.5f)), guess);
-        split(root, r[2 * i], r[2 * i + 1]);
-        split(mul_add(root, two(s.root_scale, s.root_scale), two(a.eps, a.eps)), x, y);
-        const Two ratio = mul(new_m, two(reciprocal(x), reciprocal(y)));
-        split(mul_add(two(p[2 * i], p[2 * i + 1]), two(s.decay, s.decay), mul(ratio, two(-s.rate, -s.rate))), p[2 * i], p[2 * i + 1]);
-        split(new_m, m[2 * i], m[2 * i + 1]);
+        split(add(mul_add(old_m, two(a.b1, a.b1), zero), mul_add(gg, two(a.one_minus_b1, a.one_minus_b1), zero)), m[2 * i], m[2 * i + 1]);
+        split(add(mul_add(mul(old_r, old_r), two(a.b2, a.b2), zero), mul_add(mul(gg, gg), two(a.one_minus_b2, a.one_minus_b2), zero)), r[2 * i], r[2 * i + 1]);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        ok &= fabsf(p[i]) < limit;
         m_top = larger(m_top, fabsf(m[i]));
-        r_top = larger(r_top, r[i]);
+        v_top = larger(v_top, r[i]);
+    }
+    m_top = warp_largest(m_top);
+    v_top = warp_largest(v_top);
+    // root_of() is not for v below 2^-102.  In a block of small ones the roots are formed of 2^64 v.  Beside a largest v of 2^-66 or more, such a root's code is
+    // the smallest one in any case, and beside eps >= 2^-39 root_scale it moves the step of p by less than 2^-24; beside a smaller eps it is formed so, too.
+    const bool small = v_top < 0x1p-66f && v_top > 0.f;
+    float root_scale = s.root_scale;
+    uint32_t apart = 0;                                  // elements whose root is formed in another way than the block's
+    bool mixed = !(v_top < INFINITY);
+    if (s.tiny_eps && !small) {
+        bool low = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) low |= r[i] > 0.f && r[i] < 0x1p-102f;
+        mixed |= __any_sync(0xffffffffu, low);
+    }
+    if (small) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] = __fmul_rn(r[i], 0x1p64f);
+        v_top = __fmul_rn(v_top, 0x1p64f);
+        root_scale = __fmul_rn(root_scale, 0x1p-32f);
+    }
+    if (mixed) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool low = r[i] > 0.f && r[i] < 0x1p-102f;
+            if (low) r[i] = __fmul_rn(r[i], 0x1p64f);
+            apart |= low || r[i] == INFINITY ? 1u << i : 0u;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        // (as root_of)
+        float x = r[2 * i], y = r[2 * i + 1];
+        const Two v = two(x, y), inverse = two(inverse_root(fmaxf(x, 0x1p-126f)), inverse_root(fmaxf(y, 0x1p-126f))), guess = mul(v, inverse);
+        const Two rest = mul_add(mul(guess, two(-1.f, -1.f)), guess, v), root = mul_add(rest, mul(inverse, two(0.5f, 0.5f)), guess);
+        split(root, r[2 * i], r[2 * i + 1]);
+        split(mul_add(root, two(root_scale, root_scale), two(a.eps, a.eps)), x, y);
+        const Two ratio = mul(two(m[2 * i], m[2 * i + 1]), two(reciprocal(x), reciprocal(y)));
+        split(mul_add(two(p[2 * i], p[2 * i + 1]), two(s.decay, s.decay), mul(ratio, two(-s.rate, -s.rate))), p[2 * i], p[2 * i + 1]);
+    }
+    if (mixed) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (apart >> i & 1) {
+                r[i] = r[i] < INFINITY ? __fmul_rn(r[i], 0x1p-32f) : INFINITY;
+                p[i] = fmaf(to_float(param[i]), s.decay, -s.rate * (m[i] * reciprocal(fmaf(r[i], s.root_scale, a.eps))));
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ok &= fabsf(p[i]) < limit;
+    float r_top = root_of(v_top);
+    if (small) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] = __fmul_rn(r[i], 0x1p-32f);
+        r_top = __fmul_rn(r_top, 0x1p-32f);
     }
     float m_factor, r_factor;
     *new_m_scale = block_scale(m_top, m, &m_factor);
@@ -298,7 +356,7 @@ __global__ void __launch_bounds__(kThreads8) adamw8_kernel(const __grid_constant
             now.template take<G>(now.g[threadIdx.x / 32], g);
             uint2 mc = now.mc[threadIdx.x], rc = now.rc[threadIdx.x];
             __syncwarp();                                // (it is read, before the next step fetches into this place)
-            step8(a, s, limit, e0, __shfl_sync(0xffffffffu, scales, step), __shfl_sync(0xffffffffu, scales, 16 + step), p, g, mc, rc, n, true, &m_scale, &r_scale, ok);
+            step8(a, s, limit, param + e0, e0, __shfl_sync(0xffffffffu, scales, step), __shfl_sync(0xffffffffu, scales, 16 + step), p, g, mc, rc, n, true, &m_scale, &r_scale, ok);
             Pack8<P> pack;
             pack.set(p);
             pack.store(param + e0);
@@ -344,7 +402,7 @@ __global__ void __launch_bounds__(kThreads8) adamw8_kernel(const __grid_constant
                 rc = make_uint2(c[2], c[3]);
             }
             const long long block = min(e0, n - 1) / kBlock;
-            step8(a, s, limit, e0, t.exp_avg_scale[block], t.exp_avg_sq_scale[block], p, g, mc, rc, n, whole, &m_scale, &r_scale, ok);
+            step8(a, s, limit, param + e0, e0, t.exp_avg_scale[block], t.exp_avg_sq_scale[block], p, g, mc, rc, n, whole, &m_scale, &r_scale, ok);
             if (lane == 0) {
                 t.exp_avg_scale[block] = m_scale;
                 t.exp_avg_sq_scale[block] = r_scale;
