@@ -136,16 +136,19 @@ __device__ __forceinline__ uint32_t top_bytes(const uint32_t *t) {
 __device__ __forceinline__ float warp_largest(float v) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v))); }
 
 // The scale of a block from its largest magnitude (NaN if that is); factor: 448 (1 / largest) 2^-120, by which values come to
-// lie in [0, 448] 2^-120 or a rounding above.  Values from 2^14 on are scaled first, so that the factor is no subnormal number.
+// lie in [0, 448] 2^-120 or a rounding above.  Blocks with values from 2^14 on are scaled by a part of 2^-120 first, so that the factor is no subnormal number;
+// what becomes one so is 0 as a code all the same (but not 0 itself: a root above 0 stays above it).
 __device__ __forceinline__ float block_scale(float top, float (&x)[8], float *factor) {
     const bool none = top < kNothing, finite = top < INFINITY;
     const float scale = none ? 0.f : finite ? __fmul_rn(top, 1.f / kLargest) : NAN;
+    float rest = 0x1p-120f;
     if (top >= 0x1p14f) {
-        top = __fmul_rn(top, 0x1p-120f);
+        const float part = top < 0x1p74f ? 0x1p-60f : 0x1p-120f;
+        rest = top < 0x1p74f ? 0x1p-60f : 1.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(x[i], 0x1p-120f);
+        for (int i = 0; i < 8; ++i) x[i] = x[i] > 0.f ? fmaxf(__fmul_rn(x[i], part), 0x1p-149f) : __fmul_rn(x[i], part);
     }
-    *factor = none || !finite ? 0.f : __fmul_rn(__fmul_rn(__frcp_rn(top), kLargest), 0x1p-120f);
+    *factor = none || !finite ? 0.f : __fmul_rn(__fmul_rn(__frcp_rn(top), kLargest), rest);
     return scale;
 }
 

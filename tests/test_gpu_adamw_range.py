@@ -111,3 +111,29 @@ def test_a_square_that_overflows_leaves_a_finite_parameter(n):
     pb.adamw([p], [torch.from_numpy(grad).to(DEV)], state[0], state[1], step=1, lr=1e-3, weight_decay=0.1, exp_avg_scales=state[2], exp_avg_sq_scales=state[3], flags=flags)
     assert bool(torch.isfinite(p).all()) and int(flags) == 0
     assert p[[5, 100, n - 1]].tolist() == [float(F(0.5) * F(1 - 1e-4))] * 3
+
+
+# ---- blocks of large numbers ---------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n", [300, 5000])
+@pytest.mark.parametrize("size", [2.0 ** 19, 2.0 ** 26, 2.0 ** 50, 2.0 ** 60])
+def test_small_roots_in_blocks_of_large_ones(n, size):
+    """Every root above 0 has at least the smallest code, however small it is beside the block's largest."""
+    grad = normal(n, 8) * F(size)
+    for i in range(1, 9):
+        grad[i::16] = normal(len(grad[i::16]), i) * F(2.0 ** (13 * i - 70))
+    grad[9::16] = 0
+    compare(n, [grad, np.roll(grad, 3), np.roll(grad, 7)])
+    p = torch.zeros(n, device=DEV)
+    state = pb.adamw_state([p], 8)
+    pb.adamw([p], [torch.from_numpy(grad).to(DEV)], state[0], state[1], step=1, lr=1e-3, exp_avg_scales=state[2], exp_avg_sq_scales=state[3])
+    assert np.array_equal(state[1][0].float().cpu().numpy() > 0, grad * grad * F(1 - 0.999) > 0)
+
+
+@pytest.mark.parametrize("size", [2.0 ** 14, 2.0 ** 40, 2.0 ** 74, 2.0 ** 75, 2.0 ** 100, 2.0 ** 125, 2.0 ** 126])
+def test_first_moments_up_to_the_end_of_fp32(size):
+    """beta1 = 0: m is the gradient.  1 / largest is a subnormal number at the end; small numbers lie at the borders between codes."""
+    g = np.random.default_rng(11)
+    grad = (g.uniform(0.5, 1, 4000) * np.exp2(-g.integers(0, 30, 4000)) * size * np.where(g.random(4000) < 0.5, -1, 1)).astype(F)
+    grad[::256] = F(1.9 * size)
+    compare(4000, [grad, grad[::-1].copy()], betas=(0.0, 0.999))
