@@ -471,11 +471,11 @@ typedef struct {
  * is set in *flags (dev [1] int32 or NULL); it is set, too, where a new parameter is no finite number.  state_bits 32: moments are fp32.
  * state_bits 8: m and r = sqrt(v) are e4m3 codes times a scale for each PARLE_ADAMW_BLOCK consecutive elements: 1/448 times the largest
  * magnitude (0, with codes of 0, where all magnitudes are below 2^-100; NaN where one is no finite number).  A magnitude x stands at
- * y = min(x (448 (1 / largest)), 448); between two codes it goes to the upper one where its distance from the lower, in parts of theirs, plus
+ * y = min(x (448 (1 / largest)), 448), below 2^-6 a multiple of 2^-29; between two codes it goes to the upper one where its distance from the lower, in parts of theirs, plus
  * u / 2^24 is at least 1: u = (12664745 i + 9560335 t) mod 2^24 for m, 2^24 - 1 - u for r, i the element's number in its tensor; a root above 0
  * is held as at least the smallest code.  Over the steps this rounds to neither side: moments that move by less than a code's distance a
  * step move all the same.  Each of these operations (the moments' above, code times scale, r^2, sqrt, 1 / largest, the products) is
- * rounded to nearest in fp32 by itself: codes and scales are the same bits wherever they are formed so.
+ * rounded to nearest in fp32 by itself (y to that multiple where it is small): codes and scales are the same bits wherever they are formed so.
  * All zeros are the state of no steps, in both forms.  Arrays may not overlap; an array that begins where another begins is EINVAL.
  * copy_dtype: PARLE_BF16 or PARLE_F16 beside fp32 parameters, else PARLE_NO_COPY.  step_dev and lr_dev are read when the kernel runs: a
  * captured step that is replayed moves on when the caller advances them. */

@@ -126,7 +126,7 @@ __device__ __forceinline__ float2 decode2(uint32_t codes) {
     return __half22float2(*reinterpret_cast<const __half2 *>(&h));
 }
 // A code in the top byte.  y in [0, 448] 2^-120: its exponent is fp32's, subnormal where the code is: 20 bits lie below the code, 24 with the shift,
-// where the threshold is added.
+// where the threshold is added.  (A subnormal y is a multiple of 2^-149, which 2^-120 away is the definition's multiple of 2^-29: one rounding, of the product.)
 __device__ __forceinline__ uint32_t code_above(float y, uint32_t threshold) { return (__float_as_uint(y) << 4) + threshold; }
 __device__ __forceinline__ uint32_t top_bytes(const uint32_t *t) {
     return __byte_perm(__byte_perm(t[0], t[1], 0x0073), __byte_perm(t[2], t[3], 0x0073), 0x5410);

@@ -137,3 +137,18 @@ def test_first_moments_up_to_the_end_of_fp32(size):
     grad = (g.uniform(0.5, 1, 4000) * np.exp2(-g.integers(0, 30, 4000)) * size * np.where(g.random(4000) < 0.5, -1, 1)).astype(F)
     grad[::256] = F(1.9 * size)
     compare(4000, [grad, grad[::-1].copy()], betas=(0.0, 0.999))
+
+
+# ---- small numbers beside large ones: their place between two codes is a multiple of 2^-29 ----------------------------------------------
+
+def test_many_numbers_far_below_their_blocks_largest():
+    """Two of these codes would be others if the product were rounded to 24 bits there, too."""
+    n = 1 << 21
+    grad = normal(n, 1, 4.0)
+    x = np.abs(grad * F(1 - 0.9))
+    factor = np.repeat(F(448) * (F(1) / x.reshape(-1, 256).max(1)), 256)
+    exact, u = x.astype(np.float64) * factor.astype(np.float64), oo.thresholds(n, 1).astype(np.float64) / (1 << 24)
+    low = exact < 2.0 ** -6
+    codes = [np.floor(y * 2.0 ** 9 + u)[low] for y in ((x * factor).astype(np.float64), np.rint(exact * 2.0 ** 29) * 2.0 ** -29)]
+    assert (codes[0] != codes[1]).sum() == 2
+    compare(n, [grad])
