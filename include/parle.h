@@ -476,7 +476,8 @@ typedef struct {
  * is held as at least the smallest code.  Over the steps this rounds to neither side: moments that move by less than a code's distance a
  * step move all the same.  Each of these operations (the moments' above, code times scale, r^2, sqrt, 1 / largest, the products) is
  * rounded to nearest in fp32 by itself (y to that multiple where it is small): codes and scales are the same bits wherever they are formed so.
- * All zeros are the state of no steps, in both forms.  Arrays may not overlap; an array that begins where another begins is EINVAL.
+ * All zeros are the state of no steps, in both forms.  Written arrays may overlap nothing: one that begins where another written one, a gradient
+ * or a number on the device begins is EINVAL.  Tensors may share a gradient.
  * copy_dtype: PARLE_BF16 or PARLE_F16 beside fp32 parameters, else PARLE_NO_COPY.  step_dev and lr_dev are read when the kernel runs: a
  * captured step that is replayed moves on when the caller advances them. */
 int parle_adamw(const parle_adamw_tensor *tensors, int count, int param_dtype, int grad_dtype, int copy_dtype, int state_bits,

@@ -501,7 +501,7 @@ __global__ void __launch_bounds__(kThreads32) adamw32_kernel(const __grid_consta
     if (a.flags && !ok) atomicOr(a.flags, PARLE_FLAG_NONFINITE);
 }
 
-// Whether an address occurs twice among those given to see().  Room for the addresses is on the stack for a list of one launch's size.
+// Whether an address occurs twice among those given to see(), or is one of them.  Room for the addresses is on the stack for a list of one launch's size.
 class Addresses {
     static constexpr int kSmall = 4096;                  // (of which a short list uses less)
     uintptr_t small_[kSmall];
@@ -524,14 +524,19 @@ class Addresses {
         return true;
     }
     bool see(const void *p) {
+        uintptr_t &slot = place(p);
+        if (slot) return true;
+        slot = reinterpret_cast<uintptr_t>(p);
+        return false;
+    }
+    bool seen(const void *p) { return p && place(p) != 0; }
+
+  private:
+    uintptr_t &place(const void *p) {                    // where it is, or the empty one where it would be
         const uintptr_t key = reinterpret_cast<uintptr_t>(p);
-        for (size_t i = (size_t)((key * 0x9E3779B97F4A7C15ull) >> 20) & mask_;; i = (i + 1) & mask_) {
-            if (slot_[i] == key) return true;
-            if (slot_[i] == 0) {
-                slot_[i] = key;
-                return false;
-            }
-        }
+        size_t i = (size_t)((key * 0x9E3779B97F4A7C15ull) >> 20) & mask_;
+        while (slot_[i] != key && slot_[i] != 0) i = (i + 1) & mask_;
+        return slot_[i];
     }
 };
 
@@ -617,6 +622,10 @@ extern "C" int parle_adamw(const parle_adamw_tensor *tensors, int count, int par
         if (seen.see(t.param) || seen.see(t.exp_avg) || seen.see(t.exp_avg_sq) || (copies && seen.see(t.copy))) return PARLE_EINVAL;
         if (state_bits == 8 && (seen.see(t.exp_avg_scale) || seen.see(t.exp_avg_sq_scale))) return PARLE_EINVAL;
     }
+    // What is read may be shared, but not be written by another block meanwhile.
+    for (int i = 0; i < count; ++i)
+        if (tensors[i].size && seen.seen(tensors[i].grad)) return PARLE_EINVAL;
+    if (seen.seen(h.norm) || seen.seen(h.lr_dev) || seen.seen(h.step_dev) || seen.seen(flags)) return PARLE_EINVAL;
     StepArgs a = {};
     a.b1 = (float)h.beta1; a.one_minus_b1 = (float)(1.0 - h.beta1);
     a.b2 = (float)h.beta2; a.one_minus_b2 = (float)(1.0 - h.beta2);

@@ -1,0 +1,37 @@
+"""Calls of the operators over lists that their documentation allows: gradients that tensors share, clipping of scaled gradients at the ends of
+fp32, workspaces of the documented size."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_1707_00424_b200 as pb
+from oracle import optimizer_oracle as oo
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_tensors_may_share_a_gradient(bits):
+    """Three replicas take one gradient; each ends as it does with a gradient of its own."""
+    g = torch.Generator().manual_seed(1)
+    grad = torch.randn(3000, generator=g).to(DEV)
+    start = [torch.randn(3000, generator=g).to(DEV) for _ in range(3)]
+    ends = []
+    for grads in ([grad] * 3, [grad.clone() for _ in range(3)]):
+        params = [p.clone() for p in start]
+        state = pb.adamw_state(params, bits)
+        for t in (1, 2):
+            pb.adamw(params, grads, state[0], state[1], step=t, lr=0.1, exp_avg_scales=state[2], exp_avg_sq_scales=state[3])
+        ends.append(params)
+    assert all(torch.equal(a, b) for a, b in zip(*ends))
+    with pytest.raises(pb.ParleError) as e:
+        pb.adamw(params, [grad, params[0], grad], state[0], state[1], step=3, lr=0.1, exp_avg_scales=state[2], exp_avg_sq_scales=state[3])
+    assert e.value.code == -1
