@@ -1,10 +1,10 @@
 // parle_grad_norm: the norm of all elements of a list of tensors, sqrt(sum g^2).  One read of every element: bound by DRAM (243 M fp32 136 us, the
 // copy rate and 10 % more; 60 M bf16 23 us, 0.8 of it; two launches, 4 to 5 us, where there is little).
 //
-// Eight squares are added in fp32, which is exact enough (8 u) and fast; these sums are added in fp64 (a conversion and an addition for
-// eight elements).  Where eight squares leave fp32's range, above or below, they are formed again in fp64: the result is that of 64-bit
-// sums over the whole range of the types.  A chunk's sum depends on its elements alone, and chunks are added in one fixed order: the
-// same inputs give the same bits.
+// Squares and sums are fp64, over the whole range of the types, and the result is the correctly rounded norm but where a tie is as near
+// as the sums' roundings (a conversion and a fused operation an element, beside DRAM: squares and sums of eight in fp32 were up to 2 units of the
+// last place off where there is little to average, and no faster at 243 M fp32, 3 % at as many bf16).  A chunk's sum depends on its elements alone, and
+// chunks are added in one fixed order: the same inputs give the same bits.
 #include <math.h>
 
 #include <type_traits>
@@ -46,17 +46,6 @@ template <int THREADS> __device__ __forceinline__ double block_sum(double v) {
     return v;
 }
 
-__device__ __forceinline__ double sum_of_squares(const float (&v)[8]) {
-    float sum = v[0] * v[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) sum = fmaf(v[i], v[i], sum);
-    if (sum > 0x1p-80f && sum < INFINITY) return (double)sum;      // (squares lost below add at most 7 x 2^-149)
-    double exact = 0.0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) exact = fma((double)v[i], (double)v[i], exact);
-    return exact;
-}
-
 template <typename G, class L> __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ L list, double *partial) {
     const int index = entry_of(list, blockIdx.x);
     const Entry &t = list.entry[index];
@@ -79,7 +68,10 @@ template <typename G, class L> __global__ void __launch_bounds__(kThreads) norm_
             float v[8];
             if (e >= 0 && e + 8 <= n) x[u].get(v);
             else load_some(grad, e, n, v);
-            sum += sum_of_squares(v);
+            double group = 0.0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) group = fma((double)v[i], (double)v[i], group);
+            sum += group;
         }
         e0 += kFlight * kThreads * 8;
     }

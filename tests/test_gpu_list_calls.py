@@ -35,3 +35,17 @@ def test_tensors_may_share_a_gradient(bits):
     with pytest.raises(pb.ParleError) as e:
         pb.adamw(params, [grad, params[0], grad], state[0], state[1], step=3, lr=0.1, exp_avg_scales=state[2], exp_avg_sq_scales=state[3])
     assert e.value.code == -1
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_the_norm_of_few_elements_is_correctly_rounded(dtype):
+    """Of each list alone: the 64-bit norm rounded once, but where it lies as near to a tie as the sums' roundings of 2^-53 reach."""
+    g = torch.Generator().manual_seed(5)
+    for n in (1, 2, 3, 8, 9, 31, 64, 257, 5000):
+        x = torch.randn(300 if n < 300 else 20, n, generator=g).to(dtype).to(DEV)
+        out = torch.empty(len(x), device=DEV)
+        for i in range(len(x)):
+            pb.grad_norm([x[i].contiguous()], out=out[i:i + 1])
+        for got, row in zip(f64(out), f64(x)):
+            want = math.sqrt(math.fsum(v * v for v in row))
+            assert abs(got - want) <= 2.0 ** (math.floor(math.log2(want)) - 24) * (1 + 1e-12) + n * 2.0 ** -53 * want, (n, got, want)
