@@ -12,7 +12,7 @@ BLOCK = 256
 
 def grad_norm(grads, *, out=None, workspace=None, stream=None):
     """The norm of all elements of the tensors in `grads`, a tensor of one fp32 number (parle_grad_norm).  workspace: scratch, allocated
-    when not given; 8 bytes for each begun 16384 elements of each tensor, and 128 bytes more, are enough."""
+    when not given; 8 bytes for each begun 16376 elements of each tensor, and 128 bytes more, are enough wherever the tensors begin."""
     return (token_ops._MODULE or token_ops.load()).grad_norm(grads, out, workspace, stream)
 
 

@@ -49,3 +49,12 @@ def test_the_norm_of_few_elements_is_correctly_rounded(dtype):
         for got, row in zip(f64(out), f64(x)):
             want = math.sqrt(math.fsum(v * v for v in row))
             assert abs(got - want) <= 2.0 ** (math.floor(math.log2(want)) - 24) * (1 + 1e-12) + n * 2.0 ** -53 * want, (n, got, want)
+
+
+@pytest.mark.parametrize("size", [1, 16376, 16377, 16378, 16384, 16385, 2 * 16376, 32768, 10 * 16384])
+@pytest.mark.parametrize("shift", [0, 1, 7])
+def test_a_workspace_of_the_documented_size_is_enough(size, shift):
+    flat = torch.ones(40, size + 8, dtype=torch.bfloat16, device=DEV)
+    grads = [row[shift:shift + size] for row in flat.unbind()]
+    ws = torch.empty(8 * 40 * -(-size // 16376) + 128, dtype=torch.uint8, device=DEV)
+    assert abs(float(pb.grad_norm(grads, workspace=ws)) - math.sqrt(40 * size)) <= 2 * U * math.sqrt(40 * size)
