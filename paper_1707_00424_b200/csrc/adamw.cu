@@ -113,7 +113,8 @@ __device__ __forceinline__ Scalars scalars(const StepArgs &a) {
     if (a.norm) {
         const float norm = *a.norm;
         s.skip = !(fabsf(norm) < INFINITY);
-        s.c *= fminf(1.f, __fmul_rn(__frcp_rn(norm * a.grad_scale), a.max_norm));
+        const float scaled = norm * a.grad_scale;        // (may be beyond fp32 where what is left of it after clipping is not)
+        s.c = scaled < INFINITY ? s.c * fminf(1.f, __fmul_rn(__frcp_rn(scaled), a.max_norm)) : fminf(s.c, __fmul_rn(__frcp_rn(norm), a.max_norm));
         if (s.skip && a.flags && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.flags, PARLE_FLAG_NONFINITE);
     }
     return s;

@@ -58,3 +58,24 @@ def test_a_workspace_of_the_documented_size_is_enough(size, shift):
     grads = [row[shift:shift + size] for row in flat.unbind()]
     ws = torch.empty(8 * 40 * -(-size // 16376) + 128, dtype=torch.uint8, device=DEV)
     assert abs(float(pb.grad_norm(grads, workspace=ws)) - math.sqrt(40 * size)) <= 2 * U * math.sqrt(40 * size)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("size, scale, most", [(1e30, 1e10, 1.0), (1e37, 1e30, 1e3), (1e37, 64.0, 1e-3), (1e30, 2.0 ** 30, math.inf), (1e-30, 1e-12, 1.0), (1e-10, 1e20, 2.0)])
+def test_a_scaled_norm_beyond_fp32_is_clipped(bits, size, scale, most):
+    """max_norm / norm is an ordinary number where grad_scale norm is none."""
+    n = 700
+    grad = (torch.randn(n, generator=torch.Generator().manual_seed(2)) * size / 26).to(DEV)
+    p = torch.zeros(n, device=DEV)
+    state = pb.adamw_state([p], bits)
+    norm = pb.grad_norm([grad])
+    pb.adamw([p], [grad], state[0], state[1], step=1, lr=0.1, weight_decay=0.0, exp_avg_scales=state[2], exp_avg_sq_scales=state[3], norm=norm, max_norm=most, grad_scale=scale)
+    g = f64(grad) * oo.coefficient(scale, float(norm), most)
+    with np.errstate(over="ignore"):
+        v = np.where(0.001 * np.square(g) > 3.4e38, np.inf, 0.001 * np.square(g))
+    if not np.isfinite(0.1 * np.abs(g)).all() or np.abs(g).max() > 3.4e38:
+        return                                              # (the gradient itself is none then)
+    want = -0.1 * g / (np.sqrt(v / 0.001) + 1e-8)
+    # of steps of at most 0.1: root and reciprocal 2^-22 each, the coefficient 4 u (its reciprocal is a subnormal number from 2^126 on: 2^-21), 8 products;
+    # squares that are subnormal numbers are off by 2^-150 beside eps = 1e-8: nothing
+    assert np.abs(f64(p) - want).max() <= 0.1 * (2.0 ** -20 + 12 * U) + 1e-12
