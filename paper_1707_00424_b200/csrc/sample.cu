@@ -1188,7 +1188,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS, TH
                 // sum w |t|, t relative to the largest logit, is at most sum w log2(vocab / sum w), as no distribution's entropy is above log2 vocab.
                 sum *= exp2(-off_by);
                 const double off = sum * 0x1p-24 * (14.0 + 2.1 * (max(0.0, log2((double)a.vocab / sum)) + off_by)), unit = exp2((double)a.frac_bits);
-                low = (u64)((sum - off) * unit);
+                low = (u64)fmax((sum - off) * unit - a.vocab, 0.0);      // (whole numbers: each may be half of one less, or more)
                 high = (u64)((sum + off) * unit) + (u64)a.vocab;
                 known_total = (u64)(sum * 0x1p30);
             }

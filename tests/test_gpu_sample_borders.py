@@ -114,3 +114,20 @@ def test_the_largest_logits_are_one_step_above_all_others(vocab, size, apart, sc
         x[0, vocab - 3000::100] += apart
         u = (torch.arange(rows, device=DEV) + 0.3) / rows
         check(x, u, scale=scale, most_near=1)
+
+
+# ---- very long rows: whole numbers of less than 2^-44 ----------------------------------------------------------------------------------
+
+def test_weights_of_less_than_half_a_unit_count_nothing():
+    """Of 2^23 tokens' weights in units of 2^-39 all but some hundreds are rounded to 0.  Together they would be 7 10^-6 of the sum, enough to move
+    top_p's border."""
+    vocab = 1 << 23
+    x = torch.full((1, vocab), math.log(0.45 * 2.0 ** -39), device=DEV)
+    for at in range(0, vocab, 1 << 20):                     # some that the first pass lists, of 4 10^-11 each
+        x[0, at + 3:at + 24576:256] = -24.0
+    x[0, 5], x[0, 7000000] = 0.0, -14 * math.log(2)
+    for top_p, want in ((1 - 6.23e-5, 1), (1 - 5.9e-5, 2)):
+        total = (1 + 2.0 ** -14) * float(np.float32(top_p))
+        assert abs(total - 1) > 1e-6 and (total > 1) == (want == 2)
+        token, _, kept = pb.sample_tokens(x, torch.full((1,), 0.25, device=DEV), top_p=top_p)
+        assert (int(token), int(kept)) == (5, want)
