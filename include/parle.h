@@ -500,8 +500,8 @@ typedef struct {             /* of all rows, or of each: where an array (dev [ro
  *   token dev [rows] int32            the first kept token j, by number, with sum_{kept i <= j} w_i > u sum_kept w
  *   logprob dev [rows] fp32 or NULL   log of its weight over the sum of the kept ones'
  *   kept dev [rows] int32 or NULL     how many are kept
- * Weights are formed in fp64 and added exactly as whole numbers of 2^-44 (of less above 2^19 tokens): the same inputs give the same
- * tokens.  Tokens of a weight below 2^-45 can be kept, but are never sampled.  A row of -inf alone: PARLE_NO_TOKEN, -inf, 0.  A row with NaN or
+ * Weights are formed in fp64 and added exactly as whole numbers of 2^-44 (more coarsely above 2^19 tokens; down to 2^-58 where nothing limits a row): the
+ * same call gives the same tokens.  Tokens of a weight below half of that can be kept, but are never sampled.  A row of -inf alone: PARLE_NO_TOKEN, -inf, 0.  A row with NaN or
  * +inf: PARLE_NO_TOKEN, NaN, 0.  The same for an invalid row (NaN among its parameters, scale out of range, u not in [0, 1)), which also
  * sets PARLE_FLAG_BAD_SAMPLING in *flags (dev [1] int32 or NULL). */
 int parle_sample_tokens(const void *logits, int dtype, long long rows, int vocab, long long ld, const float *u,
