@@ -188,8 +188,8 @@ __device__ __forceinline__ float root_of(float v) {
 // One step of eight elements with moments in 8 bits, a whole warp's block: mc and rc come as the old codes and go as the new ones.  (param: the elements'
 // old values, for those whose roots are formed in another way.)
 // The moments, their root and what the codes are taken from are rounded after every operation, to nearest: a value next to the border
-// between two codes falls to one side in any implementation of these operations, so that codes can be compared.  (Fused and with the hardware's
-// root: 102 M bf16 parameters 174 us.)
+// between two codes falls to one side in any implementation of these operations, so that codes can be compared.  (102 M bf16 parameters 183 us; fused and with
+// the hardware's root 174.)
 template <typename P>
 __device__ __forceinline__ void step8(const StepArgs &a, const Scalars &s, float limit, const P *param, long long e0, float m_scale, float r_scale, float (&p)[8], const float (&g)[8], uint2 &mc, uint2 &rc,
                                       long long n, bool whole, float *new_m_scale, float *new_r_scale, bool &ok) {
@@ -279,7 +279,7 @@ __device__ __forceinline__ void step8(const StepArgs &a, const Scalars &s, float
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const uint32_t u = (first + i * kWeylI) & 0xffffffu;
-        // (__fmul_rn: products written with * came out as zeros from CUDA 12.9's assembler at its default level)
+        // (__fmul_rn: a product that ends in a subnormal number, by itself, whatever stands beside it)
         mt[i] = code_above(fminf(__fmul_rn(fabsf(m[i]), m_factor), kLargest * 0x1p-120f), u) | (__float_as_uint(m[i]) & 0x80000000u);
         rt[i] = code_above(fminf(__fmul_rn(r[i], r_factor), kLargest * 0x1p-120f), u ^ 0xffffffu);
         if (r[i] > 0.f) rt[i] = max(rt[i], 1u << 24);    // else m would be divided by eps alone one day
@@ -321,8 +321,9 @@ template <typename P, typename G> struct Stage {
 };
 
 // A chunk on 16-byte boundaries is fetched a step ahead through shared memory (one step ahead in registers, 62 to 72 of them a thread, it waited for DRAM:
-// 102 M bf16 parameters 282 us; without 347).  Measured in us, with 2 / 3 / 4 stages and chunks of four steps: 102 M bf16 176, 179, 187 (floor 159);
-// 60 M fp32 144, 144, 148 (149); 15 M fp32 40, 40, 45 (37); chunks of eight steps 15 M 55, of sixteen 67, as few blocks fill the SMs unevenly.
+// 102 M bf16 parameters 282 us; without 347).  Measured in us when the step had 3 instructions an element less, with 2 / 3 / 4 stages and chunks of four steps:
+// 102 M bf16 176, 179, 187 (floor 159; 183 with 2 now); 60 M fp32 144, 144, 148 (149); 15 M fp32 40, 40, 45 (37); chunks of eight steps 15 M 55, of
+// sixteen 67, as few blocks fill the SMs unevenly.
 template <typename P, typename G, typename C, class L>
 __global__ void __launch_bounds__(kThreads8) adamw8_kernel(const __grid_constant__ L list, const __grid_constant__ StepArgs a) {
     __shared__ Stage<P, G> stage[kStages];

@@ -1,5 +1,5 @@
-// parle_grad_norm: the norm of all elements of a list of tensors, sqrt(sum g^2).  One read of every element: bound by DRAM (243 M fp32 136 us, the
-// copy rate and 10 % more; 60 M bf16 23 us, 0.8 of it; two launches, 4 to 5 us, where there is little).
+// parle_grad_norm: the norm of all elements of a list of tensors, sqrt(sum g^2).  One read of every element: bound by DRAM (243 M fp32 137 us, the
+// copy rate and 10 % more; 60 M bf16 23 us, 0.8 of it; two launches, 4 to 6 us, where there is little).
 //
 // Squares and sums are fp64, over the whole range of the types, and the result is the correctly rounded norm but where a tie is as near
 // as the sums' roundings (a conversion and a fused operation an element, beside DRAM: squares and sums of eight in fp32 were up to 2 units of the

@@ -14,9 +14,11 @@
 //   top_k up to 256, min_p, top_p that is reached by as many: one pass over the row finds its largest logit and lists the logits from a
 //     bound on, which the largest logits of the threads' first granules give; the list is sorted and decides everything.  512 rows of 131072 bf16
 //     logits with all three 73 us: DRAM, then sorting while DRAM rests (the floor is 21 us).  One row 14 us: latency of a
-//     cluster's joins.
+//     cluster's joins.  Where the first granules hold more large logits than the rest, as where frequent tokens come first, a list is too short and a second
+//     pass looks at all logits for the bound: 256 rows with top_k = 50 37 us (26 without), 512 rows with top_k = 200 and the others 93 (91).
 //   nothing: one pass that forms all weights, relative to the guess that the first granules give, and their sums by segments of 256 or 1024 logits; the
-//     segment and the token by sums of sums.  256 rows of 131072 bf16 logits 66 us: issue slots (fp64 takes 20 us of its pipe).
+//     segment and the token by sums of sums.  256 rows of 131072 bf16 logits 66 us: latency at 25 warps an SM, beside fp64 (20 us of its pipe) and
+//     issue slots (62 %).
 //   top_p of an undecided model, larger top_k: logits are counted by steps of scale (m - x), 1/128 wide, which tells nearly where the border lies;
 //     one more pass forms the weights, their exact total and segments' sums, and lists the logits around the border.  256 rows with top_p = 0.95,
 //     25000 tokens kept, 174 us: a fifth the counts, two fifths the weights.
