@@ -64,10 +64,10 @@ def compare(n, gradients, betas=(0.9, 0.999), eps=1e-8, lr=1e-3, shift=0):
                 known = np.isfinite(single.wide(scales))
                 got = state[k][0].float().cpu().numpy()
                 assert np.array_equal(got[known], single.codes[k][known]), (t, k, np.argwhere(known & (got != single.codes[k]))[:5])
-            den = r.astype(np.float64) / np.sqrt(1 - F(betas[1]).astype(np.float64) ** t) + eps
+            den = r.astype(np.float64) / np.sqrt(1 - betas[1] ** t) + eps
             moved = lr / (1 - betas[0] ** t) * m.astype(np.float64) / den
             want = before * (1 - lr * 0.1) - moved
-            # reciprocal 2^-22, root and products around it 8 u; factor of the correction (1 - b^t of a rounded b) and decay, the sum
+            # reciprocal 2^-22, root and products around it 8 u; factor of the correction and decay, the sum
             off = np.abs(moved) * (2.0 ** -22 + 16 * U) + 3 * U * (np.abs(before) + np.abs(moved))
             got = p.double().cpu().numpy()
             known = np.isfinite(want) & (np.abs(moved) < 1e38)
